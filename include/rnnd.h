@@ -20,7 +20,8 @@
  *     to float, bit-identical for delta(u,v) and delta(v,u).
  *   - every call enqueues its work on `stream` (a hipStream_t, may be NULL for
  *     the default stream) and returns after that work has completed, so the
- *     status reflects kernel errors too.
+ *     status reflects kernel errors too.  (The calls that train rows, at the end of
+ *     this file, only enqueue.)
  *   - return value: RNND_OK (0) or a negative rnnd_status; outputs are
  *     unspecified after an error.  No call aborts or throws.
  *
@@ -59,7 +60,8 @@ typedef enum {
     RNND_ERR_OOM = -5,          /* workspace allocation failed (also: a workspace of more than 1 TiB, which no
                                    device holds, is refused before any device is touched) */
     RNND_ERR_HIP = -6,          /* a HIP call or kernel failed (no GPU, launch error, ...) */
-    RNND_ERR_SCRATCH = -7       /* rnnd_build_static: the workspace for these sizes exceeds RNND_STATIC_SCRATCH_BYTES */
+    RNND_ERR_SCRATCH = -7       /* rnnd_build_static: the workspace for these sizes exceeds RNND_STATIC_SCRATCH_BYTES; training calls: the
+                                   caller's workspace is smaller than the call needs */
 } rnnd_status;
 
 /* Counters of one build, filled on the host.  "algo" evaluations are the delta(v,w)
@@ -295,6 +297,85 @@ int rnnd_set_transpose_path(int path);
  * and profiling.  No effect on other inputs or where R <= 32 (short lists only); 3 is 1 where R <= 64 (one
  * longer class).  Process-wide, not thread-safe. */
 int rnnd_set_scan_launches(int mode);
+
+/* ------------------------------------------------------------------ training the rows of an index
+ * What a program needs to learn the rows it indexes in the distance that the graph searches by: rows looked up in a table,
+ * a loss on queries and keys with its gradients, the gradient of the table, and the step.  Rows are RNND_F32, RNND_F16 or
+ * RNND_BF16 here (uint8 rows are not learnt: RNND_ERR_UNSUPPORTED), row-major and contiguous.
+ *
+ * These calls differ from the others in how they wait: they only enqueue their work on `stream` and return; they allocate
+ * nothing, keep nothing and never wait for the device, so they can be captured into a HIP graph.  A status other than RNND_OK
+ * means that nothing or not everything was enqueued; an error inside a kernel shows up where the caller next waits.
+ * Memory they work in is the caller's `workspace` (device, 16-byte aligned, as many bytes as the call's _workspace query
+ * says, else RNND_ERR_SCRATCH; contents arbitrary; free for other use when the call's work on `stream` is done).
+ * Pointers must be aligned to their elements (else RNND_ERR_BAD_PARAM); rows whose address and length allow 16-byte
+ * accesses are faster.  Inputs and outputs must not overlap unless stated.  All sums are float32 and in an order that the
+ * sizes alone decide: the same call gives the same bits. */
+#define RNND_MAX_ROW 65536          /* coordinates of a row */
+#define RNND_MAX_CONTRAST 1048576   /* queries and keys of rnnd_contrast */
+
+/* out[t] = scale * table[ids[t]], computed in float32 and rounded once; a row of zeros where ids[t] is not in [0, V)
+ * (rnnd_search pads its results with -1).
+ *   table  device, V x d; ids device int32 [n]; out device, n x d of out_dtype.  n = 0 is allowed. */
+int rnnd_embed(const void *table, int64_t V, int32_t d, int dtype, const int32_t *ids, int64_t n, float scale,
+               void *out, int out_dtype, void *stream);
+
+/* The gradient of the table for rnnd_embed: grad[v] = scale * sum of dout[t] over the t with ids[t] = v, in ascending t
+ * (ids outside [0, V) are left out), summed in float32 and rounded once.
+ *   dout        device, n x d of dtype; grad device, V x d of grad_dtype
+ *   accumulate  0: every row of grad is written, those that no id names with zeros; 1: the sums are added to what grad
+ *               holds, and rows that no id names are not touched */
+int rnnd_embed_grad(const void *dout, int dtype, const int32_t *ids, int64_t n, int32_t d, float scale, int64_t V,
+                    void *grad, int grad_dtype, int accumulate, void *workspace, size_t workspace_bytes, void *stream);
+int rnnd_embed_grad_workspace(int64_t n, int32_t d, int64_t V, size_t *bytes);
+
+/* Softmax loss over squared distances (the index's delta), with gradients.  Logit of key j for query i:
+ *   s_ij = key_bias[j] - scale * delta(q_i, k_j);   loss[i] = log(sum_j exp s_ij) - s_it,  t = target[i]
+ *   dQ, dK: gradients of sum_i row_weight[i] * loss[i]
+ * Left out of the sums: keys with key_ids[j] < 0 or key_bias[j] = -infinity, whatever their rows hold (their dK is
+ * zero); and for query i the keys j != t with key_ids[j] = key_ids[t] (the positive again) or key_ids[j] = query_ids[i]
+ * (the query itself).  Where target[i] is outside [0, M) or names a key that is left out, the query does not count: loss 0,
+ * gradient 0, whatever its row holds.
+ *   Q, K        device, B x d and M x d of dtype (K: all keys, positives and negatives; shared by all queries)
+ *   target      device int32 [B]
+ *   query_ids   device int32 [B] or NULL; key_ids device int32 [M] or NULL (query_ids needs key_ids)
+ *   key_bias    device float [M] or NULL (0): for instance minus the log of how often a key is drawn
+ *   row_weight  device float [B] or NULL (1): 1 / B for the mean; a loss scale for float16 gradients
+ *   loss        device float [B], not weighted
+ *   dQ, dK      device, as Q and K; both NULL: only the loss
+ * 0 <= B <= RNND_MAX_CONTRAST, 1 <= M <= RNND_MAX_CONTRAST; the workspace holds two (float32 rows: six) 16-bit values per
+ * pair for the gradients. */
+int rnnd_contrast(const void *Q, int64_t B, const void *K, int64_t M, int32_t d, int dtype, int metric,
+                  const int32_t *target, const int32_t *query_ids, const int32_t *key_ids, const float *key_bias,
+                  const float *row_weight, float scale, float *loss, void *dQ, void *dK, void *workspace,
+                  size_t workspace_bytes, void *stream);
+int rnnd_contrast_workspace(int64_t B, int64_t M, int32_t d, int dtype, int want_grad, size_t *bytes);
+
+/* One tensor of an AdamW step: n elements each.  state_bits 32: m, v are float arrays.  state_bits 8: m, v are n bytes of
+ * codes of the OCP 8-bit float with 4 bits of exponent and 3 of fraction, m_scale, v_scale one byte b per 128 elements, and the moment
+ * is m = code * 2^(b - 127) and v = (code * 2^(b - 127))^2; b = 255 says that the block held a value that is not finite.
+ * All zero bytes are zero moments. */
+typedef struct {
+    float *param;           /* in place */
+    const void *grad;       /* of grad_dtype */
+    void *m, *v;            /* in place */
+    uint8_t *m_scale, *v_scale;
+    void *copy;             /* NULL, or copy_dtype (RNND_F16 or RNND_BF16): receives the new parameters, rounded */
+    int64_t n;
+    uint64_t counter;       /* 8 bits: number of this tensor's first element in the step's random sequence, even */
+    int32_t grad_dtype, copy_dtype, state_bits, reserved;
+} rnnd_adamw_tensor;
+
+/* One AdamW step over `count` tensors:
+ *   g = grad_scale * grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   param = param (1 - lr weight_decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * in float32, with the moments as they are before they are rounded to 8 bits.  Moments in 8 bits are rounded up
+ * with a probability equal to their distance from the code below: element i of a tensor takes the 32 bits of half
+ * (counter + i) % 2 of word mix64(mix64(seed + G * (step + 1)) + G * ((counter + i) / 2 + 1)) (see rnnd_random_graph), the low 16
+ * for m and the high 16 for the root of v.  A root above zero never becomes zero.
+ *   tensors  host array, read before the call returns; tensors must not overlap.  step >= 1. */
+int rnnd_adamw(const rnnd_adamw_tensor *tensors, int32_t count, int64_t step, double lr, double beta1, double beta2,
+               double eps, double weight_decay, double grad_scale, uint64_t seed, void *stream);
 
 const char *rnnd_strerror(int status);
 int rnnd_version(void);

@@ -56,6 +56,17 @@ class Stats(ctypes.Structure):
         }
 
 
+class AdamwTensor(ctypes.Structure):
+    """rnnd_adamw_tensor."""
+    _fields_ = [
+        ("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("copy", ctypes.c_void_p),
+        ("n", ctypes.c_int64), ("counter", ctypes.c_uint64),
+        ("grad_dtype", ctypes.c_int32), ("copy_dtype", ctypes.c_int32), ("state_bits", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
 def lib_path() -> str:
     return _LIB
 
@@ -110,6 +121,13 @@ def load_library():
         L.rnnd_set_transpose_path.argtypes = [c.c_int]
         L.rnnd_set_scan_launches.argtypes = [c.c_int]
         L.rnnd_set_event_timing.argtypes = [c.c_int]
+        sz, f32, f64 = c.c_size_t, c.c_float, c.c_double
+        L.rnnd_embed.argtypes = [vp, i64, i32, c.c_int, vp, i64, f32, vp, c.c_int, vp]
+        L.rnnd_embed_grad.argtypes = [vp, c.c_int, vp, i64, i32, f32, i64, vp, c.c_int, c.c_int, vp, sz, vp]
+        L.rnnd_embed_grad_workspace.argtypes = [i64, i32, i64, c.POINTER(sz)]
+        L.rnnd_contrast.argtypes = [vp, i64, vp, i64, i32, c.c_int, c.c_int, vp, vp, vp, vp, vp, f32, vp, vp, vp, vp, sz, vp]
+        L.rnnd_contrast_workspace.argtypes = [i64, i64, i32, c.c_int, c.c_int, c.POINTER(sz)]
+        L.rnnd_adamw.argtypes = [c.POINTER(AdamwTensor), i32, i64, f64, f64, f64, f64, f64, f64, u64, vp]
         L.rnnd_strerror.argtypes = [c.c_int]
         L.rnnd_strerror.restype = c.c_char_p
         L.rnnd_version.restype = c.c_int
@@ -118,7 +136,9 @@ def load_library():
                      "rnnd_set_kernel_variant", "rnnd_build_blocks", "rnnd_update_neighbors_blocks",
                      "rnnd_probe_gather", "rnnd_build_wide", "rnnd_build_static", "rnnd_release_workspace",
                      "rnnd_set_workspace_poison", "rnnd_add_reverse_edges_wide", "rnnd_set_transpose_path",
-                     "rnnd_set_event_timing", "rnnd_probe_gather_map", "rnnd_set_scan_launches"):
+                     "rnnd_set_event_timing", "rnnd_probe_gather_map", "rnnd_set_scan_launches",
+                     "rnnd_embed", "rnnd_embed_grad", "rnnd_embed_grad_workspace", "rnnd_contrast",
+                     "rnnd_contrast_workspace", "rnnd_adamw"):
             getattr(L, name).restype = c.c_int
         _lib = L
     return _lib
@@ -358,6 +378,205 @@ def rnnd_set_scan_launches(mode: int):
 
 def rnnd_set_kernel_variant(variant: int):
     _check(load_library().rnnd_set_kernel_variant(variant))
+
+
+# ---- training the rows of an index.  These calls only enqueue their work.  Outputs and workspaces are allocated on the stream
+# the call runs on; inputs are marked as in use there if it is not the current one.
+_FLOAT_TYPES = {}
+
+
+def _row_type(t, what):
+    if not _FLOAT_TYPES:
+        torch = _torch()
+        _FLOAT_TYPES.update({torch.float32: RNND_F32, torch.float16: RNND_F16, torch.bfloat16: RNND_BF16})
+    try:
+        return _FLOAT_TYPES[t]
+    except KeyError:
+        raise ValueError("%s must be float32, float16 or bfloat16, not %s" % (what, t)) from None
+
+
+def _need(ok, message):
+    if not ok:
+        raise ValueError(message)
+
+
+def _rows(x, what, d=None):
+    _need(x.is_cuda and x.dim() == 2 and x.is_contiguous(), "%s must be a contiguous 2-D tensor in device memory" % what)
+    _need(d is None or x.shape[1] == d, "%s must have rows of %s coordinates" % (what, d))
+    return _row_type(x.dtype, what)
+
+
+def _vector(x, what, n, dtype, device):
+    if x is None:
+        return None
+    _need(x.is_cuda and x.device == device and x.dim() == 1 and x.is_contiguous() and x.dtype == dtype and (n is None or x.shape[0] == n),
+          "%s must be a contiguous %s vector%s on the same device" % (what, dtype, "" if n is None else " of %d" % n))
+    return x.data_ptr()
+
+
+class _On:
+    """The device and stream of a call, current while it allocates and enqueues."""
+
+    def __init__(self, device, stream, used):
+        torch = _torch()
+        self.stream = stream
+        if stream is None:
+            self.handle = torch.cuda.current_stream(device).cuda_stream
+            self.context = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+        else:
+            _need(stream.device == device, "the stream is of another device than the tensors")
+            self.handle = stream.cuda_stream
+            self.context = torch.cuda.stream(stream)
+            if stream != torch.cuda.current_stream(device):
+                for x in used:
+                    if x is not None:
+                        x.record_stream(stream)
+
+    def __enter__(self):
+        if self.context is not None:
+            self.context.__enter__()
+        return self.handle
+
+    def __exit__(self, *error):
+        if self.context is not None:
+            return self.context.__exit__(*error)
+        return False
+
+
+def _work(workspace, need, device):
+    torch = _torch()
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    _need(workspace.is_cuda and workspace.device == device and workspace.is_contiguous(),
+          "workspace must be a contiguous tensor on the same device")
+    return workspace
+
+
+def rnnd_embed(table, ids, scale: float = 1.0, out_dtype=None, out=None, stream=None):
+    """rnnd_embed: returns scale * table[ids] ([n, d], of table's type or out_dtype); rows of zeros for ids outside the table."""
+    torch = _torch()
+    dt, device = _rows(table, "table"), table.device
+    n, (V, d) = ids.shape[0] if ids.dim() == 1 else -1, table.shape
+    pi = _vector(ids, "ids", None, torch.int32, device)
+    if out is not None:
+        _need(out_dtype is None or out_dtype == out.dtype, "out_dtype is not that of out")
+        _need(_rows(out, "out", d) is not None and out.shape[0] == n and out.device == device, "out must be [n, d] on the same device")
+    with _On(device, stream, (table, ids, out)) as st:
+        if out is None:
+            out = torch.empty((n, d), dtype=out_dtype or table.dtype, device=device)
+        _check(load_library().rnnd_embed(table.data_ptr(), V, d, dt, pi, n, scale, out.data_ptr(), _row_type(out.dtype, "out"), st))
+    return out
+
+
+def rnnd_embed_grad_workspace(n: int, d: int, V: int) -> int:
+    b = ctypes.c_size_t(0)
+    _check(load_library().rnnd_embed_grad_workspace(n, d, V, ctypes.byref(b)))
+    return b.value
+
+
+def rnnd_embed_grad(dout, ids, V: int, scale: float = 1.0, grad_dtype=None, grad=None, accumulate: bool = False,
+                    workspace=None, stream=None):
+    """rnnd_embed_grad: returns the gradient of the table ([V, d], float32 or grad_dtype).  grad: where to put it, or
+    (accumulate) what to add it to."""
+    torch = _torch()
+    dt, device = _rows(dout, "dout"), dout.device
+    n, d = dout.shape
+    pi = _vector(ids, "ids", n, torch.int32, device)
+    _need(grad is not None or not accumulate, "accumulate needs the gradient to add to")
+    if grad is not None:
+        _need(grad_dtype is None or grad_dtype == grad.dtype, "grad_dtype is not that of grad")
+        _need(_rows(grad, "grad", d) is not None and grad.shape[0] == V and grad.device == device, "grad must be [V, d] on the same device")
+    need = rnnd_embed_grad_workspace(n, d, V)
+    with _On(device, stream, (dout, ids, grad, workspace)) as st:
+        if grad is None:
+            grad = torch.empty((V, d), dtype=grad_dtype or torch.float32, device=device)
+        w = _work(workspace, need, device)
+        _check(load_library().rnnd_embed_grad(dout.data_ptr(), dt, pi, n, d, scale, V, grad.data_ptr(), _row_type(grad.dtype, "grad"),
+                                              1 if accumulate else 0, w.data_ptr(), w.numel() * w.element_size(), st))
+    return grad
+
+
+def rnnd_contrast_workspace(B: int, M: int, d: int, dtype: int, want_grad: bool = True) -> int:
+    b = ctypes.c_size_t(0)
+    _check(load_library().rnnd_contrast_workspace(B, M, d, dtype, 1 if want_grad else 0, ctypes.byref(b)))
+    return b.value
+
+
+def rnnd_contrast(Q, K, target, scale: float, query_ids=None, key_ids=None, key_bias=None, row_weight=None,
+                  want_grad: bool = True, metric: int = RNND_L2SQ, workspace=None, stream=None):
+    """rnnd_contrast: returns (loss [B] float32, dQ, dK), the gradients None without want_grad."""
+    torch = _torch()
+    dt, device = _rows(K, "K"), K.device
+    M, d = K.shape
+    _need(_rows(Q, "Q", d) == dt and Q.device == device, "Q and K must be of one type and on one device")
+    B = Q.shape[0]
+    pt = _vector(target, "target", B, torch.int32, device)
+    pq = _vector(query_ids, "query_ids", B, torch.int32, device)
+    pk = _vector(key_ids, "key_ids", M, torch.int32, device)
+    pb = _vector(key_bias, "key_bias", M, torch.float32, device)
+    pw = _vector(row_weight, "row_weight", B, torch.float32, device)
+    need = rnnd_contrast_workspace(B, M, d, dt, want_grad)
+    with _On(device, stream, (Q, K, target, query_ids, key_ids, key_bias, row_weight, workspace)) as st:
+        loss = torch.empty(B, dtype=torch.float32, device=device)
+        dQ, dK = (torch.empty_like(Q), torch.empty_like(K)) if want_grad else (None, None)
+        w = _work(workspace, need, device)
+        _check(load_library().rnnd_contrast(Q.data_ptr(), B, K.data_ptr(), M, d, dt, metric, pt, pq, pk, pb, pw, scale,
+                                            loss.data_ptr(), dQ.data_ptr() if want_grad else None,
+                                            dK.data_ptr() if want_grad else None, w.data_ptr(), w.numel() * w.element_size(), st))
+    return loss, dQ, dK
+
+
+class AdamwTensors:
+    """The tensors of an AdamW step, described once.  Each is a dict of 1-D views or whole contiguous tensors:
+    param (float32), grad, m, v (float32, or one byte an element for 8-bit states with m_scale and v_scale, one
+    byte per 128 elements), copy (float16 or bfloat16, optional) and counter (8 bits; by default the tensors' own elements,
+    counted through, each starting at a multiple of 128)."""
+
+    def __init__(self, tensors):
+        torch = _torch()
+        self.kept = [dict(t) for t in tensors]         # the descriptors hold addresses
+        self.array = (AdamwTensor * max(1, len(self.kept)))()
+        self.device, at = None, 0
+        for i, t in enumerate(self.kept):
+            unknown = set(t) - {"param", "grad", "m", "v", "m_scale", "v_scale", "copy", "counter"}
+            _need(not unknown, "tensor %d: unknown %s" % (i, sorted(unknown)))
+            p, g, m, v = (t[k] for k in ("param", "grad", "m", "v"))
+            n = p.numel()
+            self.device = self.device or p.device
+            eight = m.element_size() == 1
+            scales = [t.get("m_scale"), t.get("v_scale")]
+            _need(p.dtype == torch.float32, "tensor %d: param must be float32" % i)
+            _need(v.dtype == m.dtype and (eight or m.dtype == torch.float32), "tensor %d: m and v must both be float32 or both bytes" % i)
+            _need(eight == all(s is not None for s in scales) and eight == any(s is not None for s in scales),
+                  "tensor %d: 8-bit states need m_scale and v_scale, 32-bit states have none" % i)
+            for name, x, size, count in [("grad", g, None, n), ("m", m, None, n), ("v", v, None, n), ("copy", t.get("copy"), 2, n),
+                                         ("m_scale", scales[0], 1, -(-n // 128)), ("v_scale", scales[1], 1, -(-n // 128)), ("param", p, 4, n)]:
+                if x is None:
+                    continue
+                _need(x.is_cuda and x.device == self.device and x.is_contiguous() and x.numel() == count and size in (None, x.element_size()),
+                      "tensor %d: %s must be %d contiguous elements on one device" % (i, name, count))
+            a = self.array[i]
+            a.param, a.grad, a.m, a.v, a.n = p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), n
+            a.m_scale, a.v_scale = (s.data_ptr() if s is not None else None for s in scales)
+            a.grad_dtype, a.state_bits = _row_type(g.dtype, "grad"), 8 if eight else 32
+            if t.get("copy") is not None:
+                a.copy, a.copy_dtype = t["copy"].data_ptr(), _row_type(t["copy"].dtype, "copy")
+                _need(a.copy_dtype != RNND_F32, "tensor %d: copy must be float16 or bfloat16" % i)
+            a.counter = t.get("counter", at)
+            at += -(-n // 128) * 128
+
+
+def rnnd_adamw(tensors, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+               weight_decay: float = 0.0, grad_scale: float = 1.0, seed: int = 0, stream=None):
+    """rnnd_adamw on an AdamwTensors, in place."""
+    if not tensors.kept:
+        return
+    used = ()
+    if stream is not None:
+        used = [x for t in tensors.kept for x in t.values() if hasattr(x, "record_stream")]
+    with _On(tensors.device, stream, used) as st:
+        _check(load_library().rnnd_adamw(tensors.array, len(tensors.kept), step, lr, beta1, beta2, eps, weight_decay, grad_scale,
+                                         seed, st))
 
 
 # ---- snapshot format helpers (host side, numpy): layout conversion only

@@ -1,0 +1,302 @@
+// AdamW over many tensors at once, with states in 32 or in 8 bits.
+//
+//   g = grad_scale * grad;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2
+//   p = p (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+//
+// Every element is read and written once and nothing is shared between elements but the scale of a block of 8-bit states:
+// the step is bound by memory.  Bytes an element (float32 parameters and gradients, no copy): 32-bit states 16 read + 12
+// written, 8-bit states 10 + 6.  All arithmetic is float32; the constants of a step are formed on the host in double.
+//
+// 8-bit states: m and the root of v as e4m3 codes, with one power of two for each 128 elements.  The update of p uses the new
+// m and v before they are rounded.  A root changes by 0.05 % a step, far less than the distance of two codes: rounded to
+// nearest it would never move.  So a value is rounded up with a probability equal to its distance from the code below
+// (16 bits of a counter generator: the same call gives the same bits), and a root above zero never becomes zero, since
+// p moves by m / root.
+#include <cmath>
+
+#include "rows.h"
+
+#define ADAMW_TENSORS 48        // tensors a launch takes: their descriptors travel as its argument (a little under 4 KB)
+#define ADAMW_BLOCK 128         // elements that share a scale
+#define ADAMW_TILE 2048         // elements of one workgroup
+
+struct AdamwTensor {
+    float *param;
+    const void *grad;
+    void *m, *v;
+    unsigned char *m_scale, *v_scale;
+    void *copy;
+    u64 n, counter;
+    u32 first_tile;             // in this launch
+    unsigned char grad_type, copy_type, wide;       // wide: every array takes aligned accesses of 8 elements
+};
+struct AdamwPar {
+    AdamwTensor t[ADAMW_TENSORS];
+    u64 key;                    // of the step's random bits
+    u32 count;
+    float grad_scale, beta1, beta2, rest1, rest2, keep, rate, root_scale, eps;
+};
+static_assert(sizeof(AdamwPar) <= 4096, "kernel arguments");
+
+__device__ __forceinline__ void adamw_update(const AdamwPar &a, float g, float &p, float &m, float &v)
+{
+    g *= a.grad_scale;
+    m = fmaf(a.beta1, m, a.rest1 * g);
+    v = fmaf(a.beta2, v, a.rest2 * (g * g));
+    p = fmaf(p, a.keep, -a.rate * (m / fmaf(sqrtf(v), a.root_scale, a.eps)));
+}
+
+// the value of a code times a power of two (scale byte b: 2^(b - 127); 255: not a number)
+__device__ __forceinline__ float scale_of(u32 byte)
+{
+    if (byte == 255) return __uint_as_float(0x7FC00000u);
+    return byte ? __uint_as_float(byte << 23) : __uint_as_float(0x00400000u);
+}
+__device__ __forceinline__ void decode8(u64 codes, float scale, float (&x)[8])
+{
+    const u32 lo = (u32)codes, hi = (u32)(codes >> 32);
+    x[0] = __builtin_amdgcn_cvt_f32_fp8((int)lo, 0);
+    x[1] = __builtin_amdgcn_cvt_f32_fp8((int)lo, 1);
+    x[2] = __builtin_amdgcn_cvt_f32_fp8((int)lo, 2);
+    x[3] = __builtin_amdgcn_cvt_f32_fp8((int)lo, 3);
+    x[4] = __builtin_amdgcn_cvt_f32_fp8((int)hi, 0);
+    x[5] = __builtin_amdgcn_cvt_f32_fp8((int)hi, 1);
+    x[6] = __builtin_amdgcn_cvt_f32_fp8((int)hi, 2);
+    x[7] = __builtin_amdgcn_cvt_f32_fp8((int)hi, 3);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] *= scale;
+}
+
+// The scale byte for a block whose largest magnitude has these bits: brings it, times 1.01, into [128, 256).  (0.9 m + 0.1 g
+// of values of few bits is a power of two, but for its last bit, in one block of a thousand: without the 1.01 that bit
+// would choose the scale.)
+__device__ __forceinline__ u32 scale_byte(float top)
+{
+    if (!(__float_as_uint(top) < 0x7F800000u)) return 255;      // infinite or not a number
+    const u32 e = __float_as_uint(top * 1.01f) >> 23;
+    return e < 7 ? 0 : e - 7 > 254 ? 254 : e - 7;
+}
+// code of |x| * up, up = 2^(127 - byte): three bits of fraction from 2^-6 on, steps of 2^-9 below
+__device__ __forceinline__ u32 encode(float x, float up_a, float up_b, u32 random16)
+{
+    const float z = fabsf(x) * up_a * up_b;
+    const u32 big = ((__float_as_uint(z) + (random16 << 4)) >> 20) - (120u << 3);
+    const u32 small = (u32)fmaf(z, 512.0f, (float)random16 * (1.0f / 65536.0f));
+    return z >= 0.015625f ? big : small;
+}
+
+// The largest of a block's magnitudes over the 16 lanes that hold it, all of which receive it.  As bits, so that an infinity
+// or a NaN is the largest.
+__device__ __forceinline__ float lane16_max(u32 b)
+{
+    u32 o = xor_lane_u32<1>(b);
+    b = o > b ? o : b;
+    o = xor_lane_u32<2>(b);
+    b = o > b ? o : b;
+    o = xor_lane_u32<7>(b);
+    b = o > b ? o : b;
+    o = xor_lane_u32<8>(b);
+    b = o > b ? o : b;
+    return __uint_as_float(b);
+}
+
+template <int DT>
+__device__ __forceinline__ void load8(const void *base, u64 at, u32 have, bool wide, float (&x)[8])
+{
+    if (wide) {
+        unpack<DT, 8>(load_pack<DT, 8>(base, at), x);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = i < (int)have ? (float)((const typename RowType<DT>::T *)base)[at + i] : 0.0f;
+}
+template <int DT>
+__device__ __forceinline__ void store8(void *base, u64 at, u32 have, bool wide, const float (&x)[8])
+{
+    if (wide) {
+        store_pack<DT, 8>(base, at, x);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < (int)have) ((typename RowType<DT>::T *)base)[at + i] = (typename RowType<DT>::T)x[i];
+}
+__device__ __forceinline__ u64 load_codes(const void *base, u64 at, u32 have, bool wide)
+{
+    if (wide) return *(const u64 *)((const char *)base + at);
+    u64 c = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < (int)have) c |= (u64)((const unsigned char *)base)[at + i] << (8 * i);
+    return c;
+}
+__device__ __forceinline__ void store_codes(void *base, u64 at, u32 have, bool wide, u64 c)
+{
+    if (wide) {
+        *(u64 *)((char *)base + at) = c;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < (int)have) ((unsigned char *)base)[at + i] = (unsigned char)(c >> (8 * i));
+}
+
+// A thread takes 8 neighbouring elements (16 lanes a block of 128); have = how many of them there are.
+template <bool EIGHT>
+__global__ __launch_bounds__(256) void k_adamw(AdamwPar a)
+{
+    u32 lo = 0, hi = a.count - 1;       // the tensor whose tiles hold this block's
+    while (lo < hi) {
+        const u32 mid = (lo + hi + 1) / 2;
+        if (a.t[mid].first_tile <= blockIdx.x) lo = mid;
+        else hi = mid - 1;
+    }
+    const AdamwTensor &t = a.t[lo];
+    const u64 at = (u64)(blockIdx.x - t.first_tile) * ADAMW_TILE + threadIdx.x * 8;
+    const u32 have = at >= t.n ? 0 : t.n - at < 8 ? (u32)(t.n - at) : 8;
+    const bool wide = t.wide && have == 8;
+    float p[8], g[8], m[8], v[8];
+    if (have) {
+        load8<DT_F32>(t.param, at, have, wide, p);
+        if (t.grad_type == DT_F32) load8<DT_F32>(t.grad, at, have, wide, g);
+        else if (t.grad_type == DT_F16) load8<DT_F16>(t.grad, at, have, wide, g);
+        else load8<DT_BF16>(t.grad, at, have, wide, g);
+        if (EIGHT) {
+            const u64 cm = load_codes(t.m, at, have, wide), cv = load_codes(t.v, at, have, wide);
+            decode8(cm, scale_of(t.m_scale[at / ADAMW_BLOCK]), m);
+            decode8(cv, scale_of(t.v_scale[at / ADAMW_BLOCK]), v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= v[i];
+        } else {
+            load8<DT_F32>(t.m, at, have, wide, m);
+            load8<DT_F32>(t.v, at, have, wide, v);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) adamw_update(a, g[i], p[i], m[i], v[i]);
+        store8<DT_F32>(t.param, at, have, wide, p);
+        if (t.copy) {
+            if (t.copy_type == DT_F16) store8<DT_F16>(t.copy, at, have, wide, p);
+            else store8<DT_BF16>(t.copy, at, have, wide, p);
+        }
+        if (!EIGHT) {
+            store8<DT_F32>(t.m, at, have, wide, m);
+            store8<DT_F32>(t.v, at, have, wide, v);
+        }
+    }
+    if (!EIGHT) return;
+    u32 top_m = 0, top_v = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (i >= (int)have) m[i] = v[i] = 0.0f;
+        v[i] = sqrtf(v[i]);
+        const u32 bm = __float_as_uint(m[i]) & 0x7FFFFFFFu, bv = __float_as_uint(v[i]) & 0x7FFFFFFFu;
+        top_m = bm > top_m ? bm : top_m;
+        top_v = bv > top_v ? bv : top_v;
+    }
+    const u32 sm = scale_byte(lane16_max(top_m)), sv = scale_byte(lane16_max(top_v));
+    if (!have) return;
+    // 2^(127 - byte) in two factors (byte 254: 2^-127 is below the smallest normal number)
+    const int em = 127 - (sm == 255 ? 127 : (int)sm), ev = 127 - (sv == 255 ? 127 : (int)sv);
+    const float um_a = __uint_as_float((em / 2 + 127) << 23), um_b = __uint_as_float((em - em / 2 + 127) << 23);
+    const float uv_a = __uint_as_float((ev / 2 + 127) << 23), uv_b = __uint_as_float((ev - ev / 2 + 127) << 23);
+    u64 cm = 0, cv = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        const u64 r = row_mix64(a.key + ROW_MIX_G * ((t.counter + at + i) / 2 + 1));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const u32 half = (u32)(r >> (32 * h));
+            const u32 code_m = encode(m[i + h], um_a, um_b, half & 0xFFFFu) | (__float_as_uint(m[i + h]) >> 31 << 7);
+            u32 code_v = encode(v[i + h], uv_a, uv_b, half >> 16);
+            if (v[i + h] > 0.0f && code_v == 0) code_v = 1;
+            cm |= (u64)(code_m & 255u) << (8 * (i + h));
+            cv |= (u64)(code_v & 255u) << (8 * (i + h));
+        }
+    }
+    if (sm == 255) cm = 0;      // the scale says that the block's values are lost
+    if (sv == 255) cv = 0;
+    store_codes(t.m, at, have, wide, cm);
+    store_codes(t.v, at, have, wide, cv);
+    if ((threadIdx.x & 15) == 0) {
+        t.m_scale[at / ADAMW_BLOCK] = (unsigned char)sm;
+        t.v_scale[at / ADAMW_BLOCK] = (unsigned char)sv;
+    }
+}
+
+static int adamw_check(const rnnd_adamw_tensor &t)
+{
+    if (t.n < 0 || t.n > (int64_t)1 << 40) return RNND_ERR_BAD_SHAPE;
+    if (t.state_bits != 8 && t.state_bits != 32) return RNND_ERR_UNSUPPORTED;
+    if (!row_type(t.grad_dtype)) return RNND_ERR_UNSUPPORTED;
+    if (t.copy && t.copy_dtype != RNND_F16 && t.copy_dtype != RNND_BF16) return RNND_ERR_UNSUPPORTED;
+    if (!t.n) return RNND_OK;
+    if (!t.param || !t.grad || !t.m || !t.v) return RNND_ERR_NULL;
+    if (t.state_bits == 8 && (!t.m_scale || !t.v_scale)) return RNND_ERR_NULL;
+    if ((uintptr_t)t.param % 4 || (uintptr_t)t.grad % dt_size(t.grad_dtype) || (t.copy && (uintptr_t)t.copy % 2)) return RNND_ERR_BAD_PARAM;
+    if (t.state_bits == 32 && ((uintptr_t)t.m % 4 || (uintptr_t)t.v % 4)) return RNND_ERR_BAD_PARAM;
+    if (t.state_bits == 8 && t.counter % 2) return RNND_ERR_BAD_PARAM;
+    return RNND_OK;
+}
+
+extern "C" int rnnd_adamw(const rnnd_adamw_tensor *tensors, int32_t count, int64_t step, double lr, double beta1, double beta2,
+                          double eps, double weight_decay, double grad_scale, uint64_t seed, void *stream)
+{
+    if (count < 0) return RNND_ERR_BAD_SHAPE;
+    if (count && !tensors) return RNND_ERR_NULL;
+    // (written so that NaN is refused)
+    if (step < 1 || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0) || !std::isfinite(eps) ||
+        !std::isfinite(lr) || !std::isfinite(weight_decay) || !std::isfinite(grad_scale))
+        return RNND_ERR_BAD_PARAM;
+    bool any = false;
+    for (int32_t i = 0; i < count; ++i) {
+        const int rc = adamw_check(tensors[i]);
+        if (rc) return rc;
+        any = any || tensors[i].n;
+    }
+    if (!any) return RNND_OK;
+    AdamwPar a;
+    a.key = row_mix64(seed + ROW_MIX_G * ((u64)step + 1));
+    a.grad_scale = (float)grad_scale;
+    a.beta1 = (float)beta1;
+    a.beta2 = (float)beta2;
+    a.rest1 = (float)(1.0 - beta1);
+    a.rest2 = (float)(1.0 - beta2);
+    a.keep = (float)(1.0 - lr * weight_decay);
+    a.rate = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
+    a.root_scale = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
+    a.eps = (float)eps;
+    for (int bits = 8; bits <= 32; bits += 24) {
+        int32_t i = 0;
+        while (i < count) {
+            u64 tiles = 0;
+            a.count = 0;
+            for (; i < count && a.count < ADAMW_TENSORS; ++i) {
+                const rnnd_adamw_tensor &t = tensors[i];
+                if (t.state_bits != bits || !t.n) continue;
+                const u64 more = ((u64)t.n + ADAMW_TILE - 1) / ADAMW_TILE;
+                if (tiles + more > 0x7FFFFFFFull) break;
+                AdamwTensor &d = a.t[a.count++];
+                d.param = t.param;
+                d.grad = t.grad;
+                d.m = t.m;
+                d.v = t.v;
+                d.m_scale = t.m_scale;
+                d.v_scale = t.v_scale;
+                d.copy = t.copy;
+                d.n = (u64)t.n;
+                d.counter = t.counter;
+                d.first_tile = (u32)tiles;
+                d.grad_type = (unsigned char)t.grad_dtype;
+                d.copy_type = (unsigned char)t.copy_dtype;
+                uintptr_t low = (uintptr_t)t.param | (uintptr_t)t.grad | (uintptr_t)t.copy;     // 16 bytes an access
+                low |= bits == 32 ? (uintptr_t)t.m | (uintptr_t)t.v : ((uintptr_t)t.m | (uintptr_t)t.v) << 1;   // codes: 8
+                d.wide = low % 16 == 0;
+                tiles += more;
+            }
+            if (!a.count) break;
+            if (bits == 8) hipLaunchKernelGGL(k_adamw<true>, dim3((u32)tiles), dim3(256), 0, (hipStream_t)stream, a);
+            else hipLaunchKernelGGL(k_adamw<false>, dim3((u32)tiles), dim3(256), 0, (hipStream_t)stream, a);
+        }
+    }
+    return launched("rnnd_adamw");
+}

@@ -1473,6 +1473,12 @@ __global__ __launch_bounds__(256) void k_probe_gather_map(const uint4 *X, u32 n_
     } while (0)
 
 static char g_last_hip_error[512];
+
+int report_hip_error(const char *what, hipError_t e)
+{
+    snprintf(g_last_hip_error, sizeof g_last_hip_error, "%s: %s", what, hipGetErrorString(e));
+    return e == hipErrorOutOfMemory ? RNND_ERR_OOM : RNND_ERR_HIP;
+}
 static int g_kernel_variant = 0;
 static int g_event_timing = 0;    // 1: per-round times of the statistics from HIP events attached to the launches
 static int g_transpose_path = 0;   // AddReverseEdges' transposition: 0 by size, 1 atomics, 2 binned
@@ -2938,11 +2944,11 @@ extern "C" const char *rnnd_strerror(int status)
     switch (status) {
     case RNND_OK: return "ok";
     case RNND_ERR_NULL: return "a required pointer is NULL";
-    case RNND_ERR_BAD_SHAPE: return "bad shape (N < 2, N too large, d < 1, or uint8 d > 33025)";
-    case RNND_ERR_BAD_PARAM: return "bad parameter (S, R, T1 or T2 out of range)";
+    case RNND_ERR_BAD_SHAPE: return "bad shape (too few or too many rows, d < 1 or too large, or uint8 d > 33025)";
+    case RNND_ERR_BAD_PARAM: return "bad parameter (S, R, T1 or T2 out of range, a misaligned pointer, or a hyperparameter out of range)";
     case RNND_ERR_UNSUPPORTED: return "unsupported dtype or metric";
     case RNND_ERR_OOM: return "out of device memory";
-    case RNND_ERR_SCRATCH: return "the workspace for these sizes does not fit the static scratch array (rnnd_build_static)";
+    case RNND_ERR_SCRATCH: return "the workspace for these sizes does not fit the static scratch array (rnnd_build_static), or the caller's workspace is too small";
     case RNND_ERR_HIP: return g_last_hip_error[0] ? g_last_hip_error : "HIP error";
     default: return "unknown status";
     }
