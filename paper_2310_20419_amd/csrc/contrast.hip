@@ -2,7 +2,7 @@
 //
 //   s_ij   = bias_j - scale |q_i - k_j|^2                       logit of key j for query i
 //   loss_i = log( sum_j exp s_ij ) - s_it                       t = target[i]; the sum over the keys not left out
-//   g_ij   = w_i (p_ij - [j = t]),  p_ij = exp(s_ij - lse_i)
+//   g_ij   = w_i p_ij (j != t), g_it = -w_i (1 - p_it),  p_ij = exp(s_ij - lse_i)
 //   dq_i   = 2 scale sum_j g_ij (k_j - q_i)                     gradients of sum_i w_i loss_i
 //   dk_j   = 2 scale sum_i g_ij (q_i - k_j)
 //
@@ -15,25 +15,27 @@
 //   - 16-bit rows go to the matrix instructions as they are; float32 rows as three bfloat16 terms each (8 + 8 + 8 bits), of whose
 //     products the six largest are summed: what is left out is below 2^-24 of |a||b|.
 //   - all sums are float32.  The target is kept out of the row's sum: with x = lse over the others - s_t, loss = log(1 + e^x)
-//     and p_t - 1 = -(1 - e^-loss), neither of which cancels when the loss is small.
-//   - g is rounded to the type of the rows (float32 rows: three terms again).  The rounding leaves sum_j g_ij a little off
-//     zero, which rows far from the origin would turn into a large error: the gradients are formed from k_j - q_i, with the sums
-//     of the rounded g, as the formulas have it.  float16: g is scaled to below 2^15 first, so that it stays normal down to 2^-29
-//     of the largest weight.
+//     and 1 - p_t = 1 - e^-loss, neither of which cancels when the loss is small.
+//   - g of the other keys is rounded to the type of the rows (float32 rows: three terms again; float16: scaled to below 2^15 by
+//     a power of two for all weights, so that it is normal down to 2^-29 of the largest).  The term of the target, as a rule the
+//     largest, is added in float32 at the end.  Rounding leaves the sums of g a little off what they should be, which rows far from
+//     the origin would turn into a large error: the gradients are formed from k_j - q_i, with the sums of the rounded g, as
+//     the formulas have it.
 #include <cmath>
 #include <type_traits>
+#include <utility>
 
 #include "rows.h"
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned short us8 __attribute__((ext_vector_type(8)));
+typedef unsigned short half_t;      // float16 or bfloat16, as the rows are
 
-#define CT_TILE 128         // rows and columns of a workgroup's tile
+#define CT_PAD 256          // rows are padded to the largest tile
 #define CT_K 64             // summed per step: 128 bytes of a row
 #define CT_NEVER (-2)       // an id that no key has
-
-struct RowInfo { float lse, weight, own; int target, target_id, query_id; };    // lse in base 2; own = g at the target
 
 struct ContrastPar {
     const void *Q, *K;
@@ -41,21 +43,33 @@ struct ContrastPar {
     const float *bias, *row_weight;
     float scale, c1;                // c1 = 2 scale log2(e)
     int B, M, d;
-    int dp, Bp, Mp;                 // padded to CT_K
+    int dp, Bp, Mp, dr;             // padded to CT_K; dr: d padded to the tile of the gradient products
     size_t plane_q, plane_k, plane_qt, plane_kt, plane_g, plane_gt;     // elements
-    unsigned short *q, *k, *qt, *kt, *g, *gt;
-    float *key_base;                // [Mp128] (bias - scale |k|^2) log2(e), -inf where left out
-    int *key_id;                    // [Mp128]
-    float2 *part;                   // [B][tiles of M] largest and sum of a row's tile
+    half_t *q, *k, *qt, *kt, *g, *gt;
+    u32 *top;                       // largest weight, as bits (float16 rows)
+    int *first, *count;             // [M] the first query whose target the key is, and how many they are
+    float *key_base;                // [M padded] (bias - scale |k|^2) log2(e), -inf where left out
+    int *key_id;                    // [M padded]
+    int2 *row_id;                   // [B padded] ids that a query leaves out: the target's, its own
+    float2 *row_g;                  // [B padded] lse in base 2 (infinite: the query does not count), its weight (float16: scaled)
+    float *row_own;                 // [B] g at the target
     float *own_logit;               // [B]
-    RowInfo *row;                   // [Bp128]
-    u32 *weight_top;                // largest |w| as bits
-    float *sum_q, *sum_k;           // [B][tiles of M], [M][tiles of B]: sums of the rounded g
-    float *acc_q, *acc_k;           // [splits][rows][d]
+    float2 *part;                   // [B padded][parts_k] largest and sum of a row's part
+    float *sum_q, *sum_k;           // [B padded][parts_k], [M padded][parts_q]: sums of the rounded g
+    int parts_q, parts_k;           // one for half a tile
+    float *acc_q, *acc_k;           // [splits][rows padded][dr]
     int splits_q, splits_k;
     float *loss;
     void *dQ, *dK;
 };
+
+// float16 rows: the power of two that brings weights up to `top` below 2^15
+template <int DT> __device__ __forceinline__ int weight_exponent(const ContrastPar &c)
+{
+    if constexpr (DT != DT_F16) return 0;
+    const u32 top = *c.top;
+    return top >= 0x00800000u ? 14 + 127 - (int)(top >> 23) : 0;
+}
 
 // ------------------------------------------------------------------------------------------------ preparation
 __device__ __forceinline__ bool key_gone(const ContrastPar &c, int j)
@@ -68,122 +82,209 @@ __device__ __forceinline__ bool row_counts(const ContrastPar &c, int i)
     return (u32)t < (u32)c.M && !key_gone(c, t);
 }
 
-// a wavefront per key, then a thread per query
-template <int DT>
-__global__ __launch_bounds__(256) void k_contrast_rows(ContrastPar c, u32 key_blocks)
+__global__ __launch_bounds__(256) void k_contrast_clear(ContrastPar c)
 {
-    if (blockIdx.x >= key_blocks) {
-        const int i = (blockIdx.x - key_blocks) * 256 + threadIdx.x;
-        const int padded = (c.B + CT_TILE - 1) / CT_TILE * CT_TILE;
-        if (i >= padded) return;
-        RowInfo r = {0.0f, 0.0f, 0.0f, -1, CT_NEVER, CT_NEVER};
-        if (i < c.B && row_counts(c, i)) {
-            r.target = c.target[i];
-            r.weight = c.row_weight ? c.row_weight[i] : 1.0f;
-            if (c.key_ids) {
-                r.target_id = c.key_ids[r.target];
-                if (c.query_ids) r.query_id = c.query_ids[i];
-            }
-            if (DT == DT_F16) {
-                const u32 w = __float_as_uint(r.weight) & 0x7FFFFFFFu;
-                if (w < 0x7F800000u) atomicMax(c.weight_top, w);
-            }
-        }
-        c.row[i] = r;
-        return;
-    }
-    const int j = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int padded = (c.M + CT_TILE - 1) / CT_TILE * CT_TILE;
-    if (j >= padded) return;
-    if (j >= c.M || key_gone(c, j)) {
-        if (lane == 0) {
-            c.key_base[j] = -INFINITY;
-            c.key_id[j] = -1;
-        }
-        return;
-    }
-    const typename RowType<DT>::T *k = (const typename RowType<DT>::T *)c.K + (size_t)j * c.d;
-    float sum = 0.0f;
-    for (int e = lane; e < c.d; e += 64) {
-        const float x = (float)k[e];
-        sum = fmaf(x, x, sum);
-    }
-#pragma unroll
-    for (int s = 32; s; s >>= 1) sum += __shfl_xor(sum, s);
-    if (lane == 0) {
-        c.key_base[j] = ((c.bias ? c.bias[j] : 0.0f) - c.scale * sum) * 1.44269504f;
-        c.key_id[j] = c.key_ids ? c.key_ids[j] : -1;
+    const int j = blockIdx.x * 256 + threadIdx.x;
+    if (j == 0) *c.top = 0;
+    if (j < c.M) {
+        c.first[j] = 0x7FFFFFFF;
+        c.count[j] = 0;
     }
 }
 
-__device__ __forceinline__ unsigned short bits16(__bf16 x) { return __builtin_bit_cast(unsigned short, x); }
-__device__ __forceinline__ unsigned short bits16(_Float16 x) { return __builtin_bit_cast(unsigned short, x); }
+__device__ __forceinline__ float wave_sum(float v)
+{
+#pragma unroll
+    for (int s = 32; s; s >>= 1) v += __shfl_xor(v, s);
+    return v;
+}
+
+// Four coordinates of a row, zeros behind its end; WIDE: all rows allow it in one access.
+template <int DT, bool WIDE>
+__device__ __forceinline__ void load4(const void *rows, size_t row, int d, int e, float (&x)[4])
+{
+    if constexpr (WIDE) unpack<DT, 4>(load_pack<DT, 4>(rows, row * d + e), x);
+    else
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = e + k < d ? (float)((const typename RowType<DT>::T *)rows)[row * d + e + k] : 0.0f;
+}
+
+// A wavefront per row: keys first, then queries.  A key's own part of its logits, a query's logit of its target.
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(256) void k_contrast_rows(ContrastPar c, int key_blocks)
+{
+    __shared__ u32 most;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const bool keys = (int)blockIdx.x < key_blocks;
+    if (threadIdx.x == 0) most = 0;
+    __syncthreads();
+    const int blocks = keys ? key_blocks : gridDim.x - key_blocks;
+    const int padded = ((keys ? c.M : c.B) + CT_PAD - 1) / CT_PAD * CT_PAD;
+    for (int at = ((int)blockIdx.x - (keys ? 0 : key_blocks)) * 4 + wave; at < padded; at += blocks * 4) {
+        if (keys) {
+            const bool gone = at >= c.M || key_gone(c, at);
+            float sum = 0.0f;
+            if (!gone)
+                for (int e = lane * 4; e < c.d; e += 256) {
+                    float x[4];
+                    load4<DT, WIDE>(c.K, at, c.d, e, x);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) sum = fmaf(x[k], x[k], sum);
+                }
+            sum = wave_sum(sum);
+            if (lane == 0) {
+                c.key_base[at] = gone ? -INFINITY : ((c.bias ? c.bias[at] : 0.0f) - c.scale * sum) * 1.44269504f;
+                c.key_id[at] = gone ? -1 : c.key_ids ? c.key_ids[at] : at;
+            }
+        } else {
+            const bool on = at < c.B && row_counts(c, at);
+            float dot = 0.0f, norm = 0.0f;
+            int t = -1;
+            if (on) {
+                t = c.target[at];
+                for (int e = lane * 4; e < c.d; e += 256) {
+                    float x[4], y[4];
+                    load4<DT, WIDE>(c.Q, at, c.d, e, x);
+                    load4<DT, WIDE>(c.K, t, c.d, e, y);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        dot = fmaf(x[k], y[k], dot);
+                        norm = fmaf(y[k], y[k], norm);
+                    }
+                }
+            }
+            dot = wave_sum(dot);
+            norm = wave_sum(norm);
+            if (lane == 0) {
+                c.row_id[at] = make_int2(on ? c.key_ids ? c.key_ids[t] : t : CT_NEVER, on && c.query_ids ? c.query_ids[at] : CT_NEVER);
+                const float w = on ? c.row_weight ? c.row_weight[at] : 1.0f : 0.0f;
+                c.row_g[at] = make_float2(INFINITY, w);
+                if (at < c.B) {
+                    c.row_own[at] = w;
+                    c.own_logit[at] = fmaf(dot, c.c1, ((on && c.bias ? c.bias[t] : 0.0f) - c.scale * norm) * 1.44269504f);
+                }
+                if (on) {
+                    const u32 bits = __float_as_uint(w) & 0x7FFFFFFFu;
+                    if (DT == DT_F16 && bits < 0x7F800000u) atomicMax(&most, bits);
+                    atomicMin(&c.first[t], at);
+                    atomicAdd(&c.count[t], 1);
+                }
+            }
+        }
+    }
+    __syncthreads();
+    if (DT == DT_F16 && threadIdx.x == 0 && most) atomicMax(c.top, most);
+}
+
+__device__ __forceinline__ half_t bits16(__bf16 x) { return __builtin_bit_cast(half_t, x); }
+__device__ __forceinline__ half_t bits16(_Float16 x) { return __builtin_bit_cast(half_t, x); }
+template <int DT> __device__ __forceinline__ float value16(half_t x)
+{
+    if constexpr (DT == DT_F16) return (float)__builtin_bit_cast(_Float16, x);
+    else return __uint_as_float((u32)x << 16);
+}
 
 // The planes of a value: itself in 16 bits, or three bfloat16 terms.
-template <int DT, int PLANES>
-__device__ __forceinline__ void to_planes(float x, unsigned short (&o)[PLANES])
+template <int DT> constexpr int planes_of() { return DT == DT_F32 ? 3 : 1; }
+template <int DT> __device__ __forceinline__ void to_planes(float x, half_t (&o)[planes_of<DT>()])
 {
-    if constexpr (PLANES == 1) {
-        if constexpr (DT == DT_F16) o[0] = bits16((_Float16)x);
-        else o[0] = bits16((__bf16)x);
-    } else {
+    if constexpr (DT == DT_F16) o[0] = bits16((_Float16)x);
+    else
 #pragma unroll
-        for (int p = 0; p < PLANES; ++p) {
+        for (int p = 0; p < planes_of<DT>(); ++p) {
             const __bf16 h = (__bf16)x;
             o[p] = bits16(h);
             x -= (float)h;
         }
-    }
 }
 
-// Copies of the rows that the products read: padded with zeros, in planes, by rows and by columns; rows that do not count and
-// keys that are left out as zeros, whatever they hold.  One block per 64 x 64.
-template <int DT, int PLANES>
+// Copies of the rows that the products read: padded with zeros, in planes, by rows and by columns; rows that do not count
+// and keys that are left out as zeros, whatever they hold.  One block per 64 x 64.
+template <int DT>
 __global__ __launch_bounds__(256) void k_contrast_copy(ContrastPar c, u32 q_tiles, int columns)
 {
-    __shared__ unsigned short tile[64][66];
+    constexpr int PLANES = planes_of<DT>();
+    __shared__ half_t tile[64][66];
     const bool keys = blockIdx.x >= q_tiles;
     const int r0 = (int)(keys ? blockIdx.x - q_tiles : blockIdx.x) * 64, c0 = blockIdx.y * 64;
     const int rows = keys ? c.M : c.B;
     const typename RowType<DT>::T *x = (const typename RowType<DT>::T *)(keys ? c.K : c.Q);
-    unsigned short *by_row = keys ? c.k : c.q, *by_col = keys ? c.kt : c.qt;
+    half_t *by_row = keys ? c.k : c.q, *by_col = keys ? c.kt : c.qt;
     const size_t plane_r = keys ? c.plane_k : c.plane_q, plane_c = keys ? c.plane_kt : c.plane_qt;
     const int across = keys ? c.Mp : c.Bp;
     const int col = threadIdx.x & 63;
-    unsigned short o[16][PLANES];
+    half_t o[16][PLANES];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const int r = r0 + (threadIdx.x >> 6) + 4 * i;
         float v = 0.0f;
         if (r < rows && c0 + col < c.d && (keys ? !key_gone(c, r) : row_counts(c, r))) v = (float)x[(size_t)r * c.d + c0 + col];
-        to_planes<DT, PLANES>(v, o[i]);
+        to_planes<DT>(v, o[i]);
 #pragma unroll
         for (int p = 0; p < PLANES; ++p)
             if (c0 < c.dp) by_row[p * plane_r + (size_t)r * c.dp + c0 + col] = o[i][p];
     }
-    if (!columns) return;
+    if (!columns || r0 >= across) return;       // a whole block
 #pragma unroll
     for (int p = 0; p < PLANES; ++p) {
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 16; ++i) tile[(threadIdx.x >> 6) + 4 * i][col] = o[i][p];
         __syncthreads();
-        if (r0 < across)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int cc = (threadIdx.x >> 6) + 4 * i;
-                by_col[p * plane_c + (size_t)(c0 + cc) * across + r0 + col] = tile[col][cc];
-            }
+        for (int i = 0; i < 16; ++i) {
+            const int cc = (threadIdx.x >> 6) + 4 * i;
+            by_col[p * plane_c + (size_t)(c0 + cc) * across + r0 + col] = tile[col][cc];
+        }
     }
 }
 
 // ------------------------------------------------------------------------------------------------ the product
-// 128 x 128 results of A B' (both with the summed index along the row), 4 wavefronts of 64 x 64.  A step's 128 bytes of a
-// row lie in LDS as 8 pieces of 16 bytes, piece s of row r at place s ^ (r % 8): the loads go straight to LDS in its own order
-// (each lane fetches the piece that belongs at its place), and the 16 rows that a matrix instruction reads together
-// spread over the banks.
-template <int DT>
-__device__ __forceinline__ f32x4 mfma16(const uint4 &a, const uint4 &b, f32x4 c)
+// TILE x TILE results of A B' (both with the summed index along the row) by 4 wavefronts of TILE/2 x TILE/2.  A step's 128
+// bytes of a row lie in LDS as 8 pieces of 16 bytes, piece s of place p at s ^ (p % 8): the loads go straight to LDS in its
+// own order (each lane fetches the piece that belongs there), and the 16 rows that a matrix instruction reads together spread over
+// the banks.  LDS holds two steps.  While one half of a step is multiplied the other half's operands are read into registers, and
+// the loads of the step after next are under way: one barrier a step.  There has to be a step.
+//
+// Which row stands at which place is chosen for what comes after the product.  A lane of a wavefront gets the results of rows
+// (lane / 16) * 4 N + 4 m + r (m < N = TILE / 32, r < 4) and columns (lane % 16) * N + n (n < N): 4 N rows that lie
+// together, and N columns that lie together, so that results leave in accesses of 16 bytes both by rows and by columns.
+//
+// LDS traffic a step: each wavefront reads TILE rows, all write 2 TILE: (4 + 2) * TILE * 128 bytes at 128 a clock, against
+// TILE^2 * 128 / 4096 clocks of matrix work: 768 against 512 clocks with TILE = 128, 1,536 against 2,048 with TILE = 256.
+struct Operand { const half_t *p; size_t plane; int ld; };      // rows of ld elements, ld a multiple of CT_K
+
+template <int TILE> struct ProductLds { half_t a[2][TILE * CT_K], b[2][TILE * CT_K]; };
+
+template <int TILE> __device__ __forceinline__ int row_at(int p)      // row of A that stands at place p
+{
+    constexpr int N = TILE / 32, H = TILE / 2;
+    const int q = p % H, m = q >> 4, l = q & 15;
+    return p - q + (l >> 2) * (4 * N) + m * 4 + (l & 3);
+}
+template <int TILE> __device__ __forceinline__ int col_at(int p)      // row of B that stands at place p
+{
+    constexpr int N = TILE / 32, H = TILE / 2;
+    const int q = p % H;
+    return p - q + (q & 15) * N + (q >> 4);
+}
+
+// 16 bytes of every lane from base + v + at (bytes; `bytes` of them may be read) to 1 KB of LDS, in the lanes' order
+__device__ __forceinline__ void to_lds(const half_t *base, int bytes, half_t *lds, int v, int at)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)base, 0, bytes, 0x00027000),
+                                             (__attribute__((address_space(3))) void *)lds, 16, v, at, 0, 0);
+}
+
+// With tiles of 256 the results take all 256 accumulation registers.  Left to itself the compiler moves some of them to and fro (180
+// moves for 128 matrix instructions); as operands of the class "a" they stay.  It does not know what the instruction is, so product()
+// keeps the distances it asks for: before the first, and after the last.
+template <int DT> __device__ __forceinline__ void mfma_in_agprs(f32x4 &c, const us8 &a, const us8 &b)
+{
+    if constexpr (DT == DT_F16) asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+    else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+template <int DT> __device__ __forceinline__ f32x4 mfma(const us8 &a, const us8 &b, f32x4 c)
 {
     if constexpr (DT == DT_F16)
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -191,323 +292,410 @@ __device__ __forceinline__ f32x4 mfma16(const uint4 &a, const uint4 &b, f32x4 c)
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-struct Operand { const unsigned short *p; size_t plane; int ld; };      // rows of ld elements, ld a multiple of CT_K
+template <int N> struct Half { us8 a[N], b[N]; };      // what half a step multiplies
 
-__device__ __forceinline__ void lds_load16(const unsigned short *from, unsigned short *to)
-{
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
-                                     (__attribute__((address_space(3))) void *)to, 16, 0, 0);
-}
-
-struct ProductLds { unsigned short a[2][CT_TILE * CT_K], b[2][CT_TILE * CT_K]; };
-
-template <int PLANES> __device__ __forceinline__ void plane_pair(int i, int &a, int &b)
-{
-    a = b = 0;
-    if constexpr (PLANES == 3) {        // (0,0) (0,1) (1,0) (1,1) (0,2) (2,0)
-        a = i == 2 || i == 3 ? 1 : i == 5 ? 2 : 0;
-        b = i == 1 || i == 3 ? 1 : i == 4 ? 2 : 0;
-    }
-}
-
-template <int DT, int PLANES>
+template <int TILE, int DT>
 __device__ __forceinline__ void product(const Operand &A, const Operand &B, int row_a, int row_b, int k_begin, int k_end,
-                                        ProductLds &lds, f32x4 (&acc)[4][4])
+                                        ProductLds<TILE> &lds, f32x4 (&acc)[TILE / 32][TILE / 32])
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int N = TILE / 32;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int per = (k_end - k_begin) / CT_K;
-    const int steps = per * (PLANES == 3 ? 6 : 1);
-    const int piece = (lane & 7) ^ (lane >> 3);
+    const int steps = per * (DT == DT_F32 ? 6 : 1);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
-    // each wavefront brings 32 rows of A and of B, 8 at a time
+        for (int j = 0; j < N; ++j) acc[i][j] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+    // each wavefront brings a quarter of the places, 8 at a time
+    int va[N], vb[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int p = wave * (TILE / 4) + i * 8 + (lane >> 3), piece = (lane & 7) ^ (lane >> 3);
+        va[i] = (row_at<TILE>(p) * A.ld + piece * 8) * 2;
+        vb[i] = (col_at<TILE>(p) * B.ld + piece * 8) * 2;
+    }
+    const half_t *pa = A.p + (size_t)row_a * A.ld, *pb = B.p + (size_t)row_b * B.ld;
     auto fetch = [&](int s, int buf) {
-        int pa = 0, pb = 0, kk = s;
-        if (PLANES == 3) {
+        int kk = s;
+        const half_t *qa = pa, *qb = pb;
+        if (DT == DT_F32) {         // planes (0, 0) (0, 1) (1, 0) (1, 1) (0, 2) (2, 0)
             const int pair = s / per;
             kk = s - pair * per;
-            plane_pair<PLANES>(pair, pa, pb);
+            qa += (pair == 2 || pair == 3 ? 1 : pair == 5 ? 2 : 0) * A.plane;
+            qb += (pair == 1 || pair == 3 ? 1 : pair == 4 ? 2 : 0) * B.plane;
         }
-        const size_t k0 = (size_t)k_begin + (size_t)kk * CT_K + piece * 8;
+        const int at = (k_begin + kk * CT_K) * 2;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = wave * 32 + i * 8;
-            lds_load16(A.p + pa * A.plane + (size_t)(row_a + r + (lane >> 3)) * A.ld + k0, &lds.a[buf][r * CT_K]);
-            lds_load16(B.p + pb * B.plane + (size_t)(row_b + r + (lane >> 3)) * B.ld + k0, &lds.b[buf][r * CT_K]);
+        for (int i = 0; i < N; ++i) {
+            const int place = (wave * (TILE / 4) + i * 8) * CT_K;
+            to_lds(qa, TILE * A.ld * 2, &lds.a[buf][place], va[i], at);
+            to_lds(qb, TILE * B.ld * 2, &lds.b[buf][place], vb[i], at);
         }
     };
-    if (steps > 0) fetch(0, 0);
-    const int ra = (wave >> 1) * 64 + (lane & 15), rb = (wave & 1) * 64 + (lane & 15);
-    for (int s = 0; s < steps; ++s) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (s + 1 < steps) fetch(s + 1, (s + 1) & 1);
-        const unsigned short *la = lds.a[s & 1], *lb = lds.b[s & 1];
+    
+    const int ra0 = ((wave >> 1) * (TILE / 2) + (lane & 15)) * CT_K, rb0 = ((wave & 1) * (TILE / 2) + (lane & 15)) * CT_K;
+    auto read = [&](Half<N> &f, int buf, int h) {
+        const int at = ((h * 4 + (lane >> 4)) ^ (lane & 7)) * 8;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            uint4 fa[4], fb[4];
-            const int at = ((h * 4 + (lane >> 4)) ^ (lane & 7)) * 8;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                fa[i] = *(const uint4 *)&la[(ra + i * 16) * CT_K + at];
-                fb[i] = *(const uint4 *)&lb[(rb + i * 16) * CT_K + at];
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = mfma16<DT>(fa[i], fb[j], acc[i][j]);
+        for (int i = 0; i < N; ++i) {
+            f.a[i] = *(const us8 *)&lds.a[buf][ra0 + i * 16 * CT_K + at];
+            f.b[i] = *(const us8 *)&lds.b[buf][rb0 + i * 16 * CT_K + at];
         }
+    };
+    auto multiply = [&](const Half<N> &f) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                if constexpr (TILE == 256) mfma_in_agprs<DT>(acc[i][j], f.a[i], f.b[j]);
+                else acc[i][j] = mfma<DT>(f.a[i], f.b[j], acc[i][j]);
+            }
+    };
+    if constexpr (TILE == 256) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) asm volatile("" : "+a"(acc[i][j]));
+        asm volatile("s_nop 7" ::: "memory");
     }
+    Half<N> h0, h1;
+    fetch(0, 0);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
+    if (steps > 1) fetch(1, 1);
+    read(h0, 0, 0);
+    for (int s = 0; s + 1 < steps; ++s) {
+        read(h1, s & 1, 1);
+        multiply(h0);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // the next step is there
+        __syncthreads();                                        // ... for all, and all have read this one
+        fetch(s + 2 < steps ? s + 2 : s + 1, s & 1);            // (the last one is read by nobody)
+        read(h0, (s + 1) & 1, 0);
+        multiply(h1);
+    }
+    read(h1, (steps - 1) & 1, 1);
+    multiply(h0);
+    multiply(h1);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if constexpr (TILE == 256) {
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");       // a result may be read 18 clocks behind its instruction
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) asm volatile("" : "+a"(acc[i][j]));
+    }
 }
 
-// the logit of acc for row info r and column j, base 2; -inf where the pair is left out
-__device__ __forceinline__ float logit2(float acc, float c1, float base, int id, const RowInfo &r, int j)
+// Neighbouring tiles to the same XCD (workgroups go round the 8 of them), in blocks of 8 rows of tiles, so that what
+// its L2 holds serves several of them.
+__device__ __forceinline__ void tile_of(int id, int tiles_r, int tiles_c, int &r, int &c)
 {
-    const float s = fmaf(acc, c1, base);
-    return base == -INFINITY || ((id == r.target_id || id == r.query_id) && j != r.target) ? -INFINITY : s;
+    const int total = tiles_r * tiles_c, per = total / 8;
+    if (id < per * 8) id = (id & 7) * per + (id >> 3);
+    const int group = 8 * tiles_c, g = id / group, in = id - g * group;
+    const int high = tiles_r - g * 8 < 8 ? tiles_r - g * 8 : 8;
+    r = g * 8 + in % high;
+    c = in / high;
 }
+
+// over the 16 lanes that share a row
+__device__ __forceinline__ float row16_max(float v)
+{
+    v = fmaxf(v, __uint_as_float(xor_lane_u32<1>(__float_as_uint(v))));
+    v = fmaxf(v, __uint_as_float(xor_lane_u32<2>(__float_as_uint(v))));
+    v = fmaxf(v, __uint_as_float(xor_lane_u32<7>(__float_as_uint(v))));
+    return fmaxf(v, __uint_as_float(xor_lane_u32<15>(__float_as_uint(v))));
+}
+__device__ __forceinline__ float row16_sum(float v)
+{
+    v += __uint_as_float(xor_lane_u32<1>(__float_as_uint(v)));
+    v += __uint_as_float(xor_lane_u32<2>(__float_as_uint(v)));
+    v += __uint_as_float(xor_lane_u32<7>(__float_as_uint(v)));
+    return v + __uint_as_float(xor_lane_u32<15>(__float_as_uint(v)));
+}
+
+// What a lane's columns and rows are after product().
+template <int TILE> struct Place {
+    static constexpr int N = TILE / 32;
+    int row, col;       // first of 4 N rows, first of N columns
+    int half_r, half_c; // number of the half tile
+    __device__ __forceinline__ Place(int tile_r, int tile_c)
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        half_r = tile_r * 2 + (wave >> 1);
+        half_c = tile_c * 2 + (wave & 1);
+        row = half_r * (TILE / 2) + (lane >> 4) * (4 * N);
+        col = half_c * (TILE / 2) + (lane & 15) * N;
+    }
+};
 
 // ------------------------------------------------------------------------------------------------ first product: largest and sum of every row
-template <int DT, int PLANES>
-__global__ __launch_bounds__(256) void k_contrast_sums(ContrastPar c)
+template <int TILE, int DT>
+__global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_sums(ContrastPar c, int tiles_q, int tiles_k)
 {
-    __shared__ ProductLds lds;
-    f32x4 acc[4][4];
-    const int row0 = blockIdx.y * CT_TILE, col0 = blockIdx.x * CT_TILE;
-    product<DT, PLANES>({c.q, c.plane_q, c.dp}, {c.k, c.plane_k, c.dp}, row0, col0, 0, c.dp, lds, acc);
-    float2 (*half)[CT_TILE] = (float2 (*)[CT_TILE])&lds;        // [2 halves of the columns][row]
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int cb = (wave & 1) * 64 + (lane & 15);
-    float base[4];
-    int id[4];
+    constexpr int N = TILE / 32;
+    __shared__ ProductLds<TILE> lds;
+    f32x4 acc[N][N];
+    int tr, tc;
+    tile_of(blockIdx.x, tiles_q, tiles_k, tr, tc);
+    product<TILE, DT>({c.q, c.plane_q, c.dp}, {c.k, c.plane_k, c.dp}, tr * TILE, tc * TILE, 0, c.dp, lds, acc);
+    const Place<TILE> at(tr, tc);
+    float base[N];
+    int id[N];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        base[j] = c.key_base[col0 + cb + j * 16];
-        id[j] = c.key_id[col0 + cb + j * 16];
+    for (int n = 0; n < N; ++n) {
+        base[n] = c.key_base[at.col + n];
+        id[n] = c.key_id[at.col + n];
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int m = 0; m < N; ++m)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int local = (wave >> 1) * 64 + i * 16 + (lane >> 4) * 4 + r;
-            const RowInfo info = c.row[row0 + local];
-            float s[4], top = -INFINITY;
+            const int row = at.row + m * 4 + r;
+            const int2 out = c.row_id[row];
+            float s[N], top = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int col = col0 + cb + j * 16;
-                s[j] = logit2(acc[i][j][r], c.c1, base[j], id[j], info, col);
-                if (col == info.target) {
-                    c.own_logit[row0 + local] = s[j];
-                    s[j] = -INFINITY;
-                }
-                top = s[j] > top || s[j] != s[j] ? s[j] : top;
+            for (int n = 0; n < N; ++n) {
+                s[n] = id[n] == out.x || id[n] == out.y ? -INFINITY : fmaf(acc[m][n][r], c.c1, base[n]);
+                top = fmaxf(top, s[n]);
             }
-            // over the 16 lanes that share the row; a NaN stays
-#pragma unroll
-            for (int k = 1; k < 16; k <<= 1) {
-                const float o = __shfl_xor(top, k);
-                top = o > top || o != o ? o : top;
-            }
+            top = row16_max(top);
+            const float ref = top == -INFINITY ? 0.0f : top;
             float sum = 0.0f;
-            if (top != -INFINITY)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sum += __builtin_amdgcn_exp2f(s[j] - top);
-#pragma unroll
-            for (int k = 1; k < 16; k <<= 1) sum += __shfl_xor(sum, k);
-            if ((lane & 15) == 0) half[wave & 1][local] = make_float2(top, sum);
+            for (int n = 0; n < N; ++n) sum += __builtin_amdgcn_exp2f(s[n] - ref);
+            sum = row16_sum(sum);
+            if ((threadIdx.x & 15) == 0) c.part[(size_t)row * c.parts_k + at.half_c] = make_float2(top, sum);
         }
-    __syncthreads();
-    if (threadIdx.x < CT_TILE && row0 + (int)threadIdx.x < c.B) {
-        const float2 a = half[0][threadIdx.x], b = half[1][threadIdx.x];
-        const float top = a.x > b.x || a.x != a.x ? a.x : b.x;
-        const float sum = top == -INFINITY ? 0.0f : a.y * __builtin_amdgcn_exp2f(a.x - top) + b.y * __builtin_amdgcn_exp2f(b.x - top);
-        c.part[(size_t)(row0 + threadIdx.x) * gridDim.x + blockIdx.x] = make_float2(top, sum);
-    }
 }
 
-// A wavefront per query joins its tiles: the loss, and what the second product needs.
+// (largest, sum) of two parts; a NaN in either stays
+__device__ __forceinline__ void join_parts(float &top, float &sum, float ot, float os)
+{
+    const float m = fmaxf(top, ot), ref = m == -INFINITY ? 0.0f : m;
+    sum = sum * __builtin_amdgcn_exp2f(top - ref) + os * __builtin_amdgcn_exp2f(ot - ref);
+    top = m;
+}
+
+// A wavefront per query joins its parts: the loss, and what the second product needs.
 template <int DT>
-__global__ __launch_bounds__(256) void k_contrast_loss(ContrastPar c, int tiles)
+__global__ __launch_bounds__(256) void k_contrast_loss(ContrastPar c)
 {
     const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (i >= c.B) return;
-    RowInfo r = c.row[i];
     float top = -INFINITY, sum = 0.0f;
-    for (int t = lane; t < tiles; t += 64) {
-        const float2 p = c.part[(size_t)i * tiles + t];
-        if (p.x == -INFINITY) continue;
-        const float m = p.x > top || p.x != p.x ? p.x : top;
-        sum = (top == -INFINITY ? 0.0f : sum * __builtin_amdgcn_exp2f(top - m)) + p.y * __builtin_amdgcn_exp2f(p.x - m);
-        top = m;
+    for (int t = lane; t < c.parts_k; t += 64) {
+        const float2 p = c.part[(size_t)i * c.parts_k + t];
+        join_parts(top, sum, p.x, p.y);
     }
 #pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-        const float ot = __shfl_xor(top, s), os = __shfl_xor(sum, s);
-        const float m = ot > top || ot != ot ? ot : top;
-        sum = m == -INFINITY ? 0.0f : (top == -INFINITY ? 0.0f : sum * __builtin_amdgcn_exp2f(top - m)) +
-                                          (ot == -INFINITY ? 0.0f : os * __builtin_amdgcn_exp2f(ot - m));
-        top = m;
-    }
+    for (int s = 1; s < 64; s <<= 1) join_parts(top, sum, __shfl_xor(top, s), __shfl_xor(sum, s));
     if (lane) return;
-    if (r.target < 0) {
+    if (!row_counts(c, i)) {
         c.loss[i] = 0.0f;
+        c.row_own[i] = 0.0f;
         return;
     }
     // x = lse of the others - own logit; loss = log(1 + e^x)
-    const float own = c.own_logit[i], ln2 = 0.693147181f;
+    const float own = c.own_logit[i];
     float loss = 0.0f;
-    if (top != -INFINITY) {
-        const float x = (top - own + log2f(sum)) * ln2;
+    if (!(top == -INFINITY && sum == 0.0f)) {
+        const float x = (top - own + log2f(sum)) * 0.693147181f;
         loss = x > 0.0f ? x + log1pf(expf(-x)) : log1pf(expf(x));
     }
     c.loss[i] = loss;
-    float w = r.weight;
-    if (DT == DT_F16) {     // times a power of two that brings the largest weight into [2^14, 2^15)
-        const u32 t = *c.weight_top;
-        if (t >= 0x00800000u) w = ldexpf(w, 14 + 127 - (int)(t >> 23));
-    }
-    r.weight = w;
-    r.own = expm1f(-loss) * w;
-    r.lse = own + loss * 1.44269504f;
-    c.row[i] = r;
+    const float w = c.row_own[i];
+    c.row_own[i] = w * expm1f(-loss);
+    c.row_g[i] = make_float2(own + loss * 1.44269504f, ldexpf(w, weight_exponent<DT>(c)));
 }
 
 // ------------------------------------------------------------------------------------------------ second product: g
-template <int DT, int PLANES>
-__global__ __launch_bounds__(256) void k_contrast_g(ContrastPar c)
+template <int TILE, int DT>
+__global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_g(ContrastPar c, int tiles_q, int tiles_k)
 {
-    __shared__ ProductLds lds;
-    f32x4 acc[4][4];
-    const int row0 = blockIdx.y * CT_TILE, col0 = blockIdx.x * CT_TILE;
-    product<DT, PLANES>({c.q, c.plane_q, c.dp}, {c.k, c.plane_k, c.dp}, row0, col0, 0, c.dp, lds, acc);
-    float (*row_half)[CT_TILE] = (float (*)[CT_TILE])&lds, (*col_half)[CT_TILE] = row_half + 2;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int cb = (wave & 1) * 64 + (lane & 15), rb = (wave >> 1) * 64 + (lane >> 4) * 4;
-    float base[4], col_sum[4] = {};
-    int id[4];
+    constexpr int N = TILE / 32, PLANES = planes_of<DT>();
+    __shared__ ProductLds<TILE> lds;
+    f32x4 acc[N][N];
+    int tr, tc;
+    tile_of(blockIdx.x, tiles_q, tiles_k, tr, tc);
+    product<TILE, DT>({c.q, c.plane_q, c.dp}, {c.k, c.plane_k, c.dp}, tr * TILE, tc * TILE, 0, c.dp, lds, acc);
+    const Place<TILE> at(tr, tc);
+    float base[N], col_sum[N] = {};
+    int id[N];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        base[j] = c.key_base[col0 + cb + j * 16];
-        id[j] = c.key_id[col0 + cb + j * 16];
+    for (int n = 0; n < N; ++n) {
+        base[n] = c.key_base[at.col + n];
+        id[n] = c.key_id[at.col + n];
     }
+    // (both paddings are multiples of 64: a lane's columns, and 8 of its rows, lie inside or outside together)
+    const bool cols_in = at.col < c.Mp;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        unsigned short o[4][4][PLANES];     // [row][column]
+    for (int pair = 0; pair < N / 2; ++pair) {       // 8 rows at a time
+        half_t o[PLANES][N][8];
+        const int row0 = at.row + pair * 8;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int local = rb + i * 16 + r;
-            const RowInfo info = c.row[row0 + local];
+        for (int r8 = 0; r8 < 8; ++r8) {
+            const int row = row0 + r8;
+            const int2 out = c.row_id[row];
+            const float2 info = c.row_g[row];
             float row_sum = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int col = col0 + cb + j * 16;
-                const float s = logit2(acc[i][j][r], c.c1, base[j], id[j], info, col);
-                float g = s == -INFINITY || info.target < 0 ? 0.0f : __builtin_amdgcn_exp2f(s - info.lse) * info.weight;
-                if (col == info.target) g = info.own;
-                to_planes<DT, PLANES>(g, o[r][j]);
-                if constexpr (PLANES == 1) g = DT == DT_F16 ? (float)__builtin_bit_cast(_Float16, o[r][j][0]) : (float)__builtin_bit_cast(__bf16, o[r][j][0]);
-                row_sum += g;
-                col_sum[j] += g;
-            }
+            for (int n = 0; n < N; ++n) {
+                const float s = id[n] == out.x || id[n] == out.y ? -INFINITY : fmaf(acc[pair * 2 + r8 / 4][n][r8 % 4], c.c1, base[n]);
+                const float g = __builtin_amdgcn_exp2f(s - info.x) * info.y;
+                half_t x[PLANES];
+                to_planes<DT>(g, x);
+                float rounded = 0.0f;
 #pragma unroll
-            for (int k = 1; k < 16; k <<= 1) row_sum += __shfl_xor(row_sum, k);
-            if ((lane & 15) == 0) row_half[wave & 1][local] = row_sum;
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int col = col0 + cb + j * 16, row = row0 + rb + i * 16;
-#pragma unroll
-            for (int p = 0; p < PLANES; ++p) {
-                if (col < c.Mp)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) c.g[p * c.plane_g + (size_t)(row + r) * c.Mp + col] = o[r][j][p];
-                if (row < c.Bp) {
-                    const uint2 four = {o[0][j][p] | (u32)o[1][j][p] << 16, o[2][j][p] | (u32)o[3][j][p] << 16};
-                    *(uint2 *)&c.gt[p * c.plane_gt + (size_t)col * c.Bp + row] = four;
+                for (int p = PLANES - 1; p >= 0; --p) {
+                    o[p][n][r8] = x[p];
+                    rounded += value16<DT>(x[p]);
                 }
+                row_sum += rounded;
+                col_sum[n] += rounded;
             }
+            if (cols_in)
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p) {
+                    typedef half_t line_t __attribute__((ext_vector_type(N)));
+                    line_t l;
+#pragma unroll
+                    for (int n = 0; n < N; ++n) l[n] = o[p][n][r8];
+                    *(line_t *)&c.g[p * c.plane_g + (size_t)row * c.Mp + at.col] = l;
+                }
+            row_sum = row16_sum(row_sum);
+            if ((threadIdx.x & 15) == 0) c.sum_q[(size_t)row * c.parts_k + at.half_c] = row_sum;
         }
+        if (row0 < c.Bp)
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    us8 l;
+#pragma unroll
+                    for (int r8 = 0; r8 < 8; ++r8) l[r8] = o[p][n][r8];
+                    *(us8 *)&c.gt[p * c.plane_gt + (size_t)(at.col + n) * c.Bp + row0] = l;
+                }
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        col_sum[j] += __shfl_xor(col_sum[j], 16);
-        col_sum[j] += __shfl_xor(col_sum[j], 32);
-        if (lane < 16) col_half[wave >> 1][cb + j * 16] = col_sum[j];
+    for (int n = 0; n < N; ++n) {
+        col_sum[n] += __shfl_xor(col_sum[n], 16);
+        col_sum[n] += __shfl_xor(col_sum[n], 32);
+        if ((threadIdx.x & 63) < 16) c.sum_k[(size_t)(at.col + n) * c.parts_q + at.half_r] = col_sum[n];
     }
-    __syncthreads();
-    const int x = threadIdx.x & 127;
-    if (threadIdx.x < 128) {
-        if (row0 + x < c.B) c.sum_q[(size_t)(row0 + x) * gridDim.x + blockIdx.x] = row_half[0][x] + row_half[1][x];
-    } else if (col0 + x < c.M)
-        c.sum_k[(size_t)(col0 + x) * gridDim.y + blockIdx.y] = col_half[0][x] + col_half[1][x];
 }
 
 // ------------------------------------------------------------------------------------------------ third and fourth: g k and g' q
-template <int DT, int PLANES>
-__global__ __launch_bounds__(256) void k_contrast_grad(ContrastPar c, int keys)
+// One launch: the parts of dq's sums, then those of dk's.
+template <int TILE, int DT>
+__global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_grad(ContrastPar c, int tiles_q, int tiles_k, int tiles_d)
 {
-    __shared__ ProductLds lds;
-    f32x4 acc[4][4];
-    const int row0 = blockIdx.y * CT_TILE, col0 = blockIdx.x * CT_TILE;
-    const int rows = keys ? c.M : c.B, depth = keys ? c.Bp : c.Mp, splits = keys ? c.splits_k : c.splits_q;
-    const int steps = depth / CT_K, k0 = (int)((long long)steps * blockIdx.z / splits) * CT_K,
-              k1 = (int)((long long)steps * (blockIdx.z + 1) / splits) * CT_K;
-    if (keys) product<DT, PLANES>({c.gt, c.plane_gt, c.Bp}, {c.qt, c.plane_qt, c.Bp}, row0, col0, k0, k1, lds, acc);
-    else product<DT, PLANES>({c.g, c.plane_g, c.Mp}, {c.kt, c.plane_kt, c.Mp}, row0, col0, k0, k1, lds, acc);
-    float *out = (keys ? c.acc_k : c.acc_q) + (size_t)blockIdx.z * rows * c.d;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int N = TILE / 32;
+    __shared__ ProductLds<TILE> lds;
+    f32x4 acc[N][N];
+    const int of_q = tiles_q * tiles_d * c.splits_q;
+    const bool keys = (int)blockIdx.x >= of_q;
+    const int id = keys ? blockIdx.x - of_q : blockIdx.x, tiles = keys ? tiles_k : tiles_q, splits = keys ? c.splits_k : c.splits_q;
+    const int split = id / (tiles * tiles_d);
+    int tr, tc;
+    tile_of(id - split * tiles * tiles_d, tiles, tiles_d, tr, tc);
+    const int depth = keys ? c.Bp : c.Mp, steps = depth / CT_K;
+    const int k0 = (int)((long long)steps * split / splits) * CT_K, k1 = (int)((long long)steps * (split + 1) / splits) * CT_K;
+    const Operand a = keys ? Operand{c.gt, c.plane_gt, c.Bp} : Operand{c.g, c.plane_g, c.Mp};
+    const Operand b = keys ? Operand{c.qt, c.plane_qt, c.Bp} : Operand{c.kt, c.plane_kt, c.Mp};
+    product<TILE, DT>(a, b, tr * TILE, tc * TILE, k0, k1, lds, acc);
+    const Place<TILE> at(tr, tc);
+    const size_t rows = (size_t)((keys ? c.M : c.B) + CT_PAD - 1) / CT_PAD * CT_PAD;
+    float *out = (keys ? c.acc_k : c.acc_q) + (size_t)split * rows * c.dr;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int m = 0; m < N; ++m)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int r = 0; r < 4; ++r) {
+            float *to = out + (size_t)(at.row + m * 4 + r) * c.dr + at.col;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = row0 + (wave >> 1) * 64 + i * 16 + (lane >> 4) * 4 + r, col = col0 + (wave & 1) * 64 + j * 16 + (lane & 15);
-                if (row < rows && col < c.d) out[(size_t)row * c.d + col] = acc[i][j][r];
-            }
+            for (int n = 0; n < N; n += 4) *(f32x4 *)(to + n) = (f32x4){acc[m][n][r], acc[m][n + 1][r], acc[m][n + 2][r], acc[m][n + 3][r]};
+        }
 }
 
-// Joins the parts of a sum in order, takes off the row itself times the sum of its g, and rounds.  A wavefront per row.
-template <int DT>
-__global__ __launch_bounds__(256) void k_contrast_finish(ContrastPar c, int tiles_k, int tiles_q)
+template <int DT, bool WIDE>
+__device__ __forceinline__ void store4(void *rows, size_t row, int d, int e, const float (&x)[4])
+{
+    if constexpr (WIDE) store_pack<DT, 4>(rows, row * d + e, x);
+    else
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (e + k < d) ((typename RowType<DT>::T *)rows)[row * d + e + k] = (typename RowType<DT>::T)x[k];
+}
+
+// Joins the parts of a sum in order, takes off the row itself times the sum of its g, adds the target's term, and rounds.  A
+// wavefront per row, four coordinates a lane.
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(256) void k_contrast_finish(ContrastPar c)
 {
     const int at = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (at >= c.B + c.M) return;
     const bool keys = at >= c.B;
-    const int row = keys ? at - c.B : at, rows = keys ? c.M : c.B, tiles = keys ? tiles_q : tiles_k;
-    typedef typename RowType<DT>::T T;
-    T *out = (T *)(keys ? c.dK : c.dQ) + (size_t)row * c.d;
+    const int row = keys ? at - c.B : at, rows = keys ? c.M : c.B, parts = keys ? c.parts_q : c.parts_k;
+    void *out = keys ? c.dK : c.dQ;
+    const void *mine = keys ? c.K : c.Q, *theirs = keys ? c.Q : c.K;
     if (keys ? key_gone(c, row) : !row_counts(c, row)) {
-        for (int e = lane; e < c.d; e += 64) out[e] = (T)0.0f;
+        const float zero[4] = {};
+        for (int e = lane * 4; e < c.d; e += 256) store4<DT, WIDE>(out, row, c.d, e, zero);
         return;
     }
-    const float *sums = (keys ? c.sum_k : c.sum_q) + (size_t)row * tiles;
+    const float *sums = (keys ? c.sum_k : c.sum_q) + (size_t)row * parts;
     float sum = 0.0f;
-    for (int t = lane; t < tiles; t += 64) sum += sums[t];
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) sum += __shfl_xor(sum, s);
-    const T *x = (const T *)(keys ? c.K : c.Q) + (size_t)row * c.d;
-    const float *acc = (keys ? c.acc_k : c.acc_q) + (size_t)row * c.d;
+    for (int t = lane; t < parts; t += 64) sum += sums[t];
+    sum = wave_sum(sum);
+    const size_t plane = (size_t)((rows + CT_PAD - 1) / CT_PAD * CT_PAD) * c.dr;
+    const float *acc = (keys ? c.acc_k : c.acc_q) + (size_t)row * c.dr;
     const int splits = keys ? c.splits_k : c.splits_q;
-    float f = 2.0f * c.scale;
-    int down = 0;
-    if (DT == DT_F16) {
-        const u32 t = *c.weight_top;
-        if (t >= 0x00800000u) down = 14 + 127 - (int)(t >> 23);
-    }
-    for (int e = lane; e < c.d; e += 64) {
-        float a = 0.0f;
-        for (int s = 0; s < splits; ++s) a += acc[(size_t)s * rows * c.d + e];
-        a = fmaf(-sum, (float)x[e], a) * f;
-        if (DT == DT_F16) a = ldexpf(a, -down);
-        out[e] = (T)a;
+    const int down = -weight_exponent<DT>(c);       // of g
+    const int found = keys ? c.count[row] : 1, first = keys ? found ? c.first[row] : 0 : c.target[row];
+    const float f = 2.0f * c.scale;
+    for (int e0 = 0; e0 < c.d; e0 += 256) {        // all lanes stay: the search below needs them
+        const int e = e0 + lane * 4;
+        const bool in = e < c.d;
+        float a[4] = {}, x[4] = {};
+        if (in) {
+            for (int s = 0; s < splits; ++s) {
+                const f32x4 part = *(const f32x4 *)&acc[s * plane + e];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) a[k] += part[k];
+            }
+            load4<DT, WIDE>(mine, row, c.d, e, x);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                a[k] = fmaf(-sum, x[k], a[k]);
+                if (DT == DT_F16) a[k] = ldexpf(a[k], down);
+            }
+        }
+        // the target's term; a key that is the target of several queries takes them in their order
+        int i = first;
+        for (int left = found; left > 0; --left) {
+            if (in) {
+                const float own = c.row_own[keys ? i : row];
+                float y[4];
+                load4<DT, WIDE>(theirs, i, c.d, e, y);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) a[k] = fmaf(own, y[k] - x[k], a[k]);
+            }
+            if (left == 1) break;
+            int next = -1;
+            for (int b = i + 1; b < c.B && next < 0; b += 64) {
+                const u64 hit = __ballot(b + lane < c.B && c.target[b + lane < c.B ? b + lane : 0] == row);
+                if (hit) next = b + __builtin_ctzll(hit);
+            }
+            if (next < 0) break;
+            i = next;
+        }
+        if (!in) continue;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) a[k] *= f;
+        store4<DT, WIDE>(out, row, c.d, e, a);
     }
 }
 
-__global__ void k_contrast_clear(u32 *p) { *p = 0; }
 __global__ void k_contrast_zero(unsigned short *p, size_t n)
 {
     for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = 0;
@@ -516,48 +704,91 @@ __global__ void k_contrast_zero(unsigned short *p, size_t n)
 // ------------------------------------------------------------------------------------------------ host side
 static int ct_up(int x, int m) { return (x + m - 1) / m * m; }
 
-// Workgroups that a gradient product should have at least; the sum is split among them where its results are too few tiles.
-static int ct_splits(int rows, int d, int depth)
+// How long `slots` workgroups take for na units of length a and nb of length b, the long ones first.
+static double makespan(double a, long long na, double b, long long nb, int slots)
 {
-    const long long tiles = (long long)ct_up(rows, CT_TILE) / CT_TILE * (ct_up(d, CT_TILE) / CT_TILE);
-    int splits = (int)(512 / tiles);
-    const int most = depth / (4 * CT_K);        // at least four steps each
-    if (splits > most) splits = most;
-    return splits < 1 ? 1 : splits;
+    if (a < b) {
+        std::swap(a, b);
+        std::swap(na, nb);
+    }
+    const long long r = na / slots, rem = na % slots;
+    const double low = r * a, high = rem ? low + a : low;
+    double t = high;
+    for (int i = 0; i < 1000; ++i) {
+        const long long fits = (rem ? rem * (long long)((t - high) / b + 1e-6) : 0) + (slots - rem) * (long long)((t - low) / b + 1e-6);
+        if (fits >= nb) break;
+        t += (double)(nb - fits) / slots < 1.0 ? b / 4 : b * (double)((nb - fits) / slots);
+    }
+    return t;
 }
 
-static size_t contrast_layout(ContrastPar &c, int dtype, int want_grad, char *base)
+struct ContrastPlan { int tile, tile_g; };
+
+// Tiles of 256 keep the matrix cores busier (see product()), tiles of 128 spread small problems over more CUs.
+static ContrastPlan contrast_plan(ContrastPar &c, int planes)
 {
-    const int planes = dtype == RNND_F32 ? 3 : 1;
-    const size_t Br = ct_up(c.B, CT_TILE), Mr = ct_up(c.M, CT_TILE), dr = ct_up(c.d, CT_TILE);
-    const size_t tq = Br / CT_TILE, tk = Mr / CT_TILE;
+    ContrastPlan p;
+    auto tiles = [](int x, int t) { return (long long)(x + t - 1) / t; };
+    p.tile = planes == 1 && tiles(c.B, 256) * tiles(c.M, 256) >= 128 ? 256 : 128;
+    // the gradient products: also by how much of the last tile of d would be padding
+    const int d128 = ct_up(c.d, 128), d256 = ct_up(c.d, 256);
+    p.tile_g = (tiles(c.B, 256) + tiles(c.M, 256)) * (d256 / 256) >= 64 && d256 * 4 <= d128 * 5 ? 256 : 128;
     c.dp = ct_up(c.d, CT_K);
     c.Bp = ct_up(c.B, CT_K);
     c.Mp = ct_up(c.M, CT_K);
+    c.dr = ct_up(c.d, p.tile_g);
+    c.parts_k = 2 * (int)tiles(c.M, p.tile);
+    c.parts_q = 2 * (int)tiles(c.B, p.tile);
+    // parts of the gradients' sums: few tiles are split over the workgroups that run at a time; a part costs about 24 steps of the
+    // product, for what it starts with and for its results, written and read again
+    static const int choices[] = {1, 2, 3, 4, 6, 8, 12, 16};
+    const long long tq = tiles(c.B, p.tile_g) * (c.dr / p.tile_g), tk = tiles(c.M, p.tile_g) * (c.dr / p.tile_g);
+    const int steps_q = c.Mp / CT_K * (planes == 3 ? 6 : 1), steps_k = c.Bp / CT_K * (planes == 3 ? 6 : 1);
+    double best = 1e300;
+    for (int sq : choices)
+        for (int sk : choices) {
+            if ((sq > 1 && sq > c.Mp / CT_K) || (sk > 1 && sk > c.Bp / CT_K)) continue;
+            const double t = makespan((double)steps_q / sq + 24, tq * sq, (double)steps_k / sk + 24, tk * sk, p.tile_g == 256 ? 256 : 512);
+            if (t < best * 0.999) {
+                best = t;
+                c.splits_q = sq;
+                c.splits_k = sk;
+            }
+        }
+    return p;
+}
+
+static size_t contrast_layout(ContrastPar &c, ContrastPlan &plan, int dtype, int want_grad, char *base)
+{
+    const int planes = dtype == RNND_F32 ? 3 : 1;
+    plan = contrast_plan(c, planes);
+    const size_t Br = ct_up(c.B, CT_PAD), Mr = ct_up(c.M, CT_PAD);
     size_t off = 0;
     auto take = [&](auto *&p, size_t count) {
         p = (typename std::remove_reference<decltype(p)>::type)(base + off);
         off += ws_align(count * sizeof(*p));
     };
-    take(c.weight_top, 1);
+    take(c.top, 1);
+    take(c.first, c.M);
+    take(c.count, c.M);
     take(c.key_base, Mr);
     take(c.key_id, Mr);
-    take(c.row, Br);
+    take(c.row_id, Br);
+    take(c.row_g, Br);
+    take(c.row_own, Br);
     take(c.own_logit, Br);
-    take(c.part, (size_t)c.B * tk);
+    take(c.part, Br * c.parts_k);
     take(c.q, planes * (c.plane_q = Br * c.dp));
     take(c.k, planes * (c.plane_k = Mr * c.dp));
     if (want_grad) {
-        c.splits_q = ct_splits(c.B, c.d, c.Mp);
-        c.splits_k = ct_splits(c.M, c.d, c.Bp);
-        take(c.qt, planes * (c.plane_qt = dr * c.Bp));
-        take(c.kt, planes * (c.plane_kt = dr * c.Mp));
+        take(c.qt, planes * (c.plane_qt = (size_t)c.dr * c.Bp));
+        take(c.kt, planes * (c.plane_kt = (size_t)c.dr * c.Mp));
         take(c.g, planes * (c.plane_g = Br * c.Mp));
         take(c.gt, planes * (c.plane_gt = Mr * c.Bp));
-        take(c.sum_q, (size_t)c.B * tk);
-        take(c.sum_k, (size_t)c.M * tq);
-        take(c.acc_q, (size_t)c.splits_q * c.B * c.d);
-        take(c.acc_k, (size_t)c.splits_k * c.M * c.d);
+        take(c.sum_q, Br * c.parts_k);
+        take(c.sum_k, Mr * c.parts_q);
+        take(c.acc_q, (size_t)c.splits_q * Br * c.dr);
+        take(c.acc_k, (size_t)c.splits_k * Mr * c.dr);
     }
     return off;
 }
@@ -579,30 +810,48 @@ extern "C" int rnnd_contrast_workspace(int64_t B, int64_t M, int32_t d, int dtyp
         return RNND_OK;
     }
     ContrastPar c = {};
+    ContrastPlan plan;
     c.B = (int)B;
     c.M = (int)M;
     c.d = d;
-    *bytes = contrast_layout(c, dtype, want_grad, nullptr);
+    *bytes = contrast_layout(c, plan, dtype, want_grad, nullptr);
     return RNND_OK;
 }
 
-template <int DT>
-static void launch_contrast(ContrastPar &c, int want_grad, hipStream_t st)
+template <int DT, int TILE>
+static void launch_products(ContrastPar &c, int want_grad, hipStream_t st)
 {
-    constexpr int PLANES = DT == DT_F32 ? 3 : 1;
-    const u32 tq = ct_up(c.B, CT_TILE) / CT_TILE, tk = ct_up(c.M, CT_TILE) / CT_TILE, td = ct_up(c.d, CT_TILE) / CT_TILE;
-    if (DT == DT_F16) hipLaunchKernelGGL(k_contrast_clear, dim3(1), dim3(1), 0, st, c.weight_top);
-    const u32 key_blocks = tk * CT_TILE / 4;
-    hipLaunchKernelGGL(k_contrast_rows<DT>, dim3(key_blocks + (tq * CT_TILE + 255) / 256), dim3(256), 0, st, c, key_blocks);
+    static_assert(DT != DT_F32 || TILE == 128, "g of three planes takes more registers than tiles of 256 leave");
+    const int tq = ct_up(c.B, TILE) / TILE, tk = ct_up(c.M, TILE) / TILE;
+    hipLaunchKernelGGL((k_contrast_sums<TILE, DT>), dim3((u32)tq * tk), dim3(256), 0, st, c, tq, tk);
+    hipLaunchKernelGGL(k_contrast_loss<DT>, dim3((c.B + 3) / 4), dim3(256), 0, st, c);
+    if (want_grad) hipLaunchKernelGGL((k_contrast_g<TILE, DT>), dim3((u32)tq * tk), dim3(256), 0, st, c, tq, tk);
+}
+template <int DT, int TILE>
+static void launch_grads(ContrastPar &c, hipStream_t st)
+{
+    const int tq = ct_up(c.B, TILE) / TILE, tk = ct_up(c.M, TILE) / TILE, td = c.dr / TILE;
+    hipLaunchKernelGGL((k_contrast_grad<TILE, DT>), dim3((u32)td * (tq * c.splits_q + tk * c.splits_k)), dim3(256), 0, st, c, tq, tk, td);
+}
+
+template <int DT, bool WIDE>
+static void launch_contrast(ContrastPar &c, const ContrastPlan &plan, int want_grad, hipStream_t st)
+{
+    const int Br = ct_up(c.B, CT_PAD), Mr = ct_up(c.M, CT_PAD);
+    hipLaunchKernelGGL(k_contrast_clear, dim3((c.M + 255) / 256), dim3(256), 0, st, c);
+    const int key_blocks = Mr / 4 < 1024 ? Mr / 4 : 1024, row_blocks = Br / 4 < 1024 ? Br / 4 : 1024;
+    hipLaunchKernelGGL((k_contrast_rows<DT, WIDE>), dim3(key_blocks + row_blocks), dim3(256), 0, st, c, key_blocks);
     // (by columns the padding of d up to a whole tile is written too: the products read it)
-    hipLaunchKernelGGL((k_contrast_copy<DT, PLANES>), dim3(tq * 2 + tk * 2, want_grad ? td * 2 : c.dp / 64), dim3(256), 0, st, c, tq * 2, want_grad);
-    hipLaunchKernelGGL((k_contrast_sums<DT, PLANES>), dim3(tk, tq), dim3(256), 0, st, c);
-    hipLaunchKernelGGL(k_contrast_loss<DT>, dim3((c.B + 3) / 4), dim3(256), 0, st, c, (int)tk);
+    hipLaunchKernelGGL(k_contrast_copy<DT>, dim3((Br + Mr) / 64, (want_grad ? c.dr : c.dp) / 64), dim3(256), 0, st, c, Br / 64, want_grad);
+    if constexpr (DT != DT_F32) {
+        if (plan.tile == 256) launch_products<DT, 256>(c, want_grad, st);
+        else launch_products<DT, 128>(c, want_grad, st);
+    } else
+        launch_products<DT, 128>(c, want_grad, st);
     if (!want_grad) return;
-    hipLaunchKernelGGL((k_contrast_g<DT, PLANES>), dim3(tk, tq), dim3(256), 0, st, c);
-    hipLaunchKernelGGL((k_contrast_grad<DT, PLANES>), dim3(td, tq, c.splits_q), dim3(256), 0, st, c, 0);
-    hipLaunchKernelGGL((k_contrast_grad<DT, PLANES>), dim3(td, tk, c.splits_k), dim3(256), 0, st, c, 1);
-    hipLaunchKernelGGL(k_contrast_finish<DT>, dim3((c.B + c.M + 3) / 4), dim3(256), 0, st, c, (int)tk, (int)tq);
+    if (plan.tile_g == 256) launch_grads<DT, 256>(c, st);
+    else launch_grads<DT, 128>(c, st);
+    hipLaunchKernelGGL((k_contrast_finish<DT, WIDE>), dim3((c.B + c.M + 3) / 4), dim3(256), 0, st, c);
 }
 
 extern "C" int rnnd_contrast(const void *Q, int64_t B, const void *K, int64_t M, int32_t d, int dtype, int metric, const int32_t *target,
@@ -628,6 +877,7 @@ extern "C" int rnnd_contrast(const void *Q, int64_t B, const void *K, int64_t M,
         return launched("rnnd_contrast");
     }
     ContrastPar c = {};
+    ContrastPlan plan;
     c.Q = Q;
     c.K = K;
     c.target = target;
@@ -645,9 +895,19 @@ extern "C" int rnnd_contrast(const void *Q, int64_t B, const void *K, int64_t M,
     c.dK = dK;
     if (!workspace) return RNND_ERR_NULL;
     if ((uintptr_t)workspace % 16) return RNND_ERR_BAD_PARAM;
-    if (workspace_bytes < contrast_layout(c, dtype, want_grad, (char *)workspace)) return RNND_ERR_SCRATCH;
-    if (dtype == RNND_F32) launch_contrast<DT_F32>(c, want_grad, (hipStream_t)stream);
-    else if (dtype == RNND_F16) launch_contrast<DT_F16>(c, want_grad, (hipStream_t)stream);
-    else launch_contrast<DT_BF16>(c, want_grad, (hipStream_t)stream);
+    if (workspace_bytes < contrast_layout(c, plan, dtype, want_grad, (char *)workspace)) return RNND_ERR_SCRATCH;
+    hipStream_t st = (hipStream_t)stream;
+    int vec = row_vec(d, Q, (int)size, K, (int)size);
+    if (want_grad) {
+        const int vg = row_vec(d, dQ, (int)size, dK, (int)size);
+        vec = vg < vec ? vg : vec;
+    }
+#define RNND_CONTRAST(DT) \
+    if (vec >= 4) launch_contrast<DT, true>(c, plan, want_grad, st); \
+    else launch_contrast<DT, false>(c, plan, want_grad, st)
+    if (dtype == RNND_F32) { RNND_CONTRAST(DT_F32); }
+    else if (dtype == RNND_F16) { RNND_CONTRAST(DT_F16); }
+    else { RNND_CONTRAST(DT_BF16); }
+#undef RNND_CONTRAST
     return launched("rnnd_contrast");
 }
