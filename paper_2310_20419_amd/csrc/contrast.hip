@@ -419,15 +419,33 @@ template <int TILE> struct Place {
     static constexpr int N = TILE / 32;
     int row, col;       // first of 4 N rows, first of N columns
     int half_r, half_c; // number of the half tile
+    int in_row, in_col; // of the tile
     __device__ __forceinline__ Place(int tile_r, int tile_c)
     {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         half_r = tile_r * 2 + (wave >> 1);
         half_c = tile_c * 2 + (wave & 1);
-        row = half_r * (TILE / 2) + (lane >> 4) * (4 * N);
-        col = half_c * (TILE / 2) + (lane & 15) * N;
+        in_row = (wave >> 1) * (TILE / 2) + (lane >> 4) * (4 * N);
+        in_col = (wave & 1) * (TILE / 2) + (lane & 15) * N;
+        row = tile_r * TILE + in_row;
+        col = tile_c * TILE + in_col;
     }
 };
+
+// What the logits of a tile need besides the product, in LDS before it starts: behind it nothing else hides the latency of
+// loads from memory (one wavefront per SIMD; with loads in the middle of it g took 35 us for a tile of 256, of which its product
+// is 20).
+template <int TILE> struct SideLds { int2 row_id[TILE]; float2 row_g[TILE]; float base[TILE]; int id[TILE]; };
+template <int TILE> __device__ __forceinline__ void load_side(const ContrastPar &c, SideLds<TILE> &side, int row0, int col0)
+{
+    const int t = threadIdx.x;
+    if (t < TILE) {
+        side.row_id[t] = c.row_id[row0 + t];
+        side.row_g[t] = c.row_g[row0 + t];
+        side.base[t] = c.key_base[col0 + t];
+        side.id[t] = c.key_id[col0 + t];
+    }
+}
 
 // ------------------------------------------------------------------------------------------------ first product: largest and sum of every row
 template <int TILE, int DT>
@@ -435,24 +453,26 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_sums(Cont
 {
     constexpr int N = TILE / 32;
     __shared__ ProductLds<TILE> lds;
+    __shared__ SideLds<TILE> side;
     f32x4 acc[N][N];
     int tr, tc;
     tile_of(blockIdx.x, tiles_q, tiles_k, tr, tc);
+    load_side(c, side, tr * TILE, tc * TILE);
     product<TILE, DT>({c.q, c.plane_q, c.dp}, {c.k, c.plane_k, c.dp}, tr * TILE, tc * TILE, 0, c.dp, lds, acc);
     const Place<TILE> at(tr, tc);
     float base[N];
     int id[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        base[n] = c.key_base[at.col + n];
-        id[n] = c.key_id[at.col + n];
+        base[n] = side.base[at.in_col + n];
+        id[n] = side.id[at.in_col + n];
     }
 #pragma unroll
     for (int m = 0; m < N; ++m)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int row = at.row + m * 4 + r;
-            const int2 out = c.row_id[row];
+            const int2 out = side.row_id[at.in_row + m * 4 + r];
             float s[N], top = -INFINITY;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
@@ -515,18 +535,24 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_g(Contras
 {
     constexpr int N = TILE / 32, PLANES = planes_of<DT>();
     __shared__ ProductLds<TILE> lds;
+    __shared__ SideLds<TILE> side;
     f32x4 acc[N][N];
     int tr, tc;
     tile_of(blockIdx.x, tiles_q, tiles_k, tr, tc);
+    load_side(c, side, tr * TILE, tc * TILE);
     product<TILE, DT>({c.q, c.plane_q, c.dp}, {c.k, c.plane_k, c.dp}, tr * TILE, tc * TILE, 0, c.dp, lds, acc);
     const Place<TILE> at(tr, tc);
     float base[N], col_sum[N] = {};
     int id[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        base[n] = c.key_base[at.col + n];
-        id[n] = c.key_id[at.col + n];
+        base[n] = side.base[at.in_col + n];
+        id[n] = side.id[at.in_col + n];
     }
+    constexpr int H = TILE / 2;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    half_t *turn = (half_t *)&lds + wave * H * H;
+    __syncthreads();        // all have read their operands
     // (both paddings are multiples of 64: a lane's columns, and 8 of its rows, lie inside or outside together)
     const bool cols_in = at.col < c.Mp;
 #pragma unroll
@@ -536,8 +562,8 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_g(Contras
 #pragma unroll
         for (int r8 = 0; r8 < 8; ++r8) {
             const int row = row0 + r8;
-            const int2 out = c.row_id[row];
-            const float2 info = c.row_g[row];
+            const int2 out = side.row_id[at.in_row + pair * 8 + r8];
+            const float2 info = side.row_g[at.in_row + pair * 8 + r8];
             float row_sum = 0.0f;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
@@ -566,16 +592,27 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_g(Contras
             row_sum = row16_sum(row_sum);
             if ((threadIdx.x & 15) == 0) c.sum_q[(size_t)row * c.parts_k + at.half_c] = row_sum;
         }
+        // by columns: 8 rows of a column are 16 bytes.  One plane: first into the wavefront's own part of LDS, in which a
+        // column's rows lie together (piece k of column x at k ^ x / N % 8: both sides free of bank conflicts)
+#pragma unroll
+        for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                us8 l;
+#pragma unroll
+                for (int r8 = 0; r8 < 8; ++r8) l[r8] = o[p][n][r8];
+                if constexpr (PLANES == 1) *(us8 *)&turn[((lane & 15) * N + n) * H + (((lane >> 4) * (N / 2) + pair) ^ (lane & 7)) * 8] = l;
+                else if (row0 < c.Bp) *(us8 *)&c.gt[p * c.plane_gt + (size_t)(at.col + n) * c.Bp + row0] = l;
+            }
+    }
+    if constexpr (PLANES == 1) {
+        wave_sync();
+        constexpr int per = H / 8;          // lanes for a column
+        const int piece = lane % per, row0 = tr * TILE + (wave >> 1) * H + piece * 8, col0 = tc * TILE + (wave & 1) * H;
         if (row0 < c.Bp)
-#pragma unroll
-            for (int p = 0; p < PLANES; ++p)
-#pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    us8 l;
-#pragma unroll
-                    for (int r8 = 0; r8 < 8; ++r8) l[r8] = o[p][n][r8];
-                    *(us8 *)&c.gt[p * c.plane_gt + (size_t)(at.col + n) * c.Bp + row0] = l;
-                }
+#pragma unroll 4
+            for (int x = lane / per; x < H; x += 64 / per)
+                *(us8 *)&c.gt[(size_t)(col0 + x) * c.Bp + row0] = *(const us8 *)&turn[x * H + (piece ^ (x / N & 7)) * 8];
     }
 #pragma unroll
     for (int n = 0; n < N; ++n) {
@@ -682,9 +719,15 @@ __global__ __launch_bounds__(256) void k_contrast_finish(ContrastPar c)
             }
             if (left == 1) break;
             int next = -1;
-            for (int b = i + 1; b < c.B && next < 0; b += 64) {
-                const u64 hit = __ballot(b + lane < c.B && c.target[b + lane < c.B ? b + lane : 0] == row);
-                if (hit) next = b + __builtin_ctzll(hit);
+            for (int b = i + 1; b < c.B && next < 0; b += 256) {
+                int t[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) t[k] = b + k * 64 + lane < c.B ? c.target[b + k * 64 + lane] : -1;
+#pragma unroll
+                for (int k = 3; k >= 0; --k) {
+                    const u64 hit = __ballot(t[k] == row);
+                    if (hit) next = b + k * 64 + __builtin_ctzll(hit);
+                }
             }
             if (next < 0) break;
             i = next;
