@@ -315,7 +315,8 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int 
         vb[i] = (col_at<TILE>(p) * B.ld + piece * 8) * 2;
     }
     const half_t *pa = A.p + (size_t)row_a * A.ld, *pb = B.p + (size_t)row_b * B.ld;
-    auto fetch = [&](int s, int buf) {
+    // 1 / N of a step's loads
+    auto fetch = [&](int s, int buf, int i) {
         int kk = s;
         const half_t *qa = pa, *qb = pb;
         if (DT == DT_F32) {         // planes (0, 0) (0, 1) (1, 0) (1, 1) (0, 2) (2, 0)
@@ -324,32 +325,23 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int 
             qa += (pair == 2 || pair == 3 ? 1 : pair == 5 ? 2 : 0) * A.plane;
             qb += (pair == 1 || pair == 3 ? 1 : pair == 4 ? 2 : 0) * B.plane;
         }
-        const int at = (k_begin + kk * CT_K) * 2;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int place = (wave * (TILE / 4) + i * 8) * CT_K;
-            to_lds(qa, TILE * A.ld * 2, &lds.a[buf][place], va[i], at);
-            to_lds(qb, TILE * B.ld * 2, &lds.b[buf][place], vb[i], at);
-        }
+        const int at = (k_begin + kk * CT_K) * 2, place = (wave * (TILE / 4) + i * 8) * CT_K;
+        to_lds(qa, TILE * A.ld * 2, &lds.a[buf][place], va[i], at);
+        to_lds(qb, TILE * B.ld * 2, &lds.b[buf][place], vb[i], at);
     };
-    
     const int ra0 = ((wave >> 1) * (TILE / 2) + (lane & 15)) * CT_K, rb0 = ((wave & 1) * (TILE / 2) + (lane & 15)) * CT_K;
-    auto read = [&](Half<N> &f, int buf, int h) {
-        const int at = ((h * 4 + (lane >> 4)) ^ (lane & 7)) * 8;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            f.a[i] = *(const us8 *)&lds.a[buf][ra0 + i * 16 * CT_K + at];
-            f.b[i] = *(const us8 *)&lds.b[buf][rb0 + i * 16 * CT_K + at];
-        }
+    const int piece0 = ((lane >> 4) ^ (lane & 7)) * 8;
+    auto read = [&](Half<N> &f, int buf, int h, int i) {
+        const int at = piece0 ^ (h * 32);
+        f.a[i] = *(const us8 *)&lds.a[buf][ra0 + i * 16 * CT_K + at];
+        f.b[i] = *(const us8 *)&lds.b[buf][rb0 + i * 16 * CT_K + at];
     };
-    auto multiply = [&](const Half<N> &f) {
+    auto multiply = [&](const Half<N> &f, int i) {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                if constexpr (TILE == 256) mfma_in_agprs<DT>(acc[i][j], f.a[i], f.b[j]);
-                else acc[i][j] = mfma<DT>(f.a[i], f.b[j], acc[i][j]);
-            }
+        for (int j = 0; j < N; ++j) {
+            if constexpr (TILE == 256) mfma_in_agprs<DT>(acc[i][j], f.a[i], f.b[j]);
+            else acc[i][j] = mfma<DT>(f.a[i], f.b[j], acc[i][j]);
+        }
     };
     if constexpr (TILE == 256) {
 #pragma unroll
@@ -359,23 +351,49 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int 
         asm volatile("s_nop 7" ::: "memory");
     }
     Half<N> h0, h1;
-    fetch(0, 0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) fetch(0, 0, i);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (steps > 1) fetch(1, 1);
-    read(h0, 0, 0);
+    if (steps > 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) fetch(1, 1, i);
+#pragma unroll
+    for (int i = 0; i < N; ++i) read(h0, 0, 0, i);
+    // A wavefront issues in order: reads and loads in one lump would hold its matrix instructions back until they are accepted.  So
+    // a few of them go before each N matrix instructions, the reads early enough to be there for the next half.
     for (int s = 0; s + 1 < steps; ++s) {
-        read(h1, s & 1, 1);
-        multiply(h0);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (i < N / 2) {
+                read(h1, s & 1, 1, 2 * i);
+                read(h1, s & 1, 1, 2 * i + 1);
+            }
+            multiply(h0, i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // the next step is there
         __syncthreads();                                        // ... for all, and all have read this one
-        fetch(s + 2 < steps ? s + 2 : s + 1, s & 1);            // (the last one is read by nobody)
-        read(h0, (s + 1) & 1, 0);
-        multiply(h1);
+        const int next = s + 2 < steps ? s + 2 : s + 1;         // (the last one is read by nobody)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (i < N / 2) {
+                fetch(next, s & 1, 2 * i);
+                fetch(next, s & 1, 2 * i + 1);
+            } else {
+                read(h0, (s + 1) & 1, 0, 2 * i - N);
+                read(h0, (s + 1) & 1, 0, 2 * i - N + 1);
+            }
+            multiply(h1, i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
-    read(h1, (steps - 1) & 1, 1);
-    multiply(h0);
-    multiply(h1);
+#pragma unroll
+    for (int i = 0; i < N; ++i) read(h1, (steps - 1) & 1, 1, i);
+#pragma unroll
+    for (int i = 0; i < N; ++i) multiply(h0, i);
+#pragma unroll
+    for (int i = 0; i < N; ++i) multiply(h1, i);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if constexpr (TILE == 256) {
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");       // a result may be read 18 clocks behind its instruction
