@@ -44,6 +44,7 @@ struct ContrastPar {
     float scale, c1;                // c1 = 2 scale log2(e)
     int B, M, d;
     int dp, Bp, Mp, dr;             // padded to CT_K; dr: d padded to the tile of the gradient products
+    int ld_g, ld_gt;                // rows of g by rows and by columns: M and B padded to the largest tile
     size_t plane_q, plane_k, plane_qt, plane_kt, plane_g, plane_gt;     // elements
     half_t *q, *k, *qt, *kt, *g, *gt;
     u32 *top;                       // largest weight, as bits (float16 rows)
@@ -410,26 +411,40 @@ __device__ __forceinline__ void tile_of(int id, int tiles_r, int tiles_c, int &r
 {
     const int total = tiles_r * tiles_c, per = total / 8;
     if (id < per * 8) id = (id & 7) * per + (id >> 3);
+    if (tiles_c <= 4) {         // all columns of a row of tiles together
+        r = id / tiles_c;
+        c = id - r * tiles_c;
+        return;
+    }
     const int group = 8 * tiles_c, g = id / group, in = id - g * group;
     const int high = tiles_r - g * 8 < 8 ? tiles_r - g * 8 : 8;
     r = g * 8 + in % high;
     c = in / high;
 }
 
-// over the 16 lanes that share a row
-__device__ __forceinline__ float row16_max(float v)
+// over the 16 lanes that share a row, R rows at a time
+template <int S> __device__ __forceinline__ float xor_lane_f32(float v) { return __uint_as_float(xor_lane_u32<S>(__float_as_uint(v))); }
+template <int R> __device__ __forceinline__ void row16_max(float (&v)[R])
 {
-    v = fmaxf(v, __uint_as_float(xor_lane_u32<1>(__float_as_uint(v))));
-    v = fmaxf(v, __uint_as_float(xor_lane_u32<2>(__float_as_uint(v))));
-    v = fmaxf(v, __uint_as_float(xor_lane_u32<7>(__float_as_uint(v))));
-    return fmaxf(v, __uint_as_float(xor_lane_u32<15>(__float_as_uint(v))));
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = fmaxf(v[r], xor_lane_f32<1>(v[r]));
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = fmaxf(v[r], xor_lane_f32<2>(v[r]));
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = fmaxf(v[r], xor_lane_f32<7>(v[r]));
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = fmaxf(v[r], xor_lane_f32<15>(v[r]));
 }
-__device__ __forceinline__ float row16_sum(float v)
+template <int R> __device__ __forceinline__ void row16_sum(float (&v)[R])
 {
-    v += __uint_as_float(xor_lane_u32<1>(__float_as_uint(v)));
-    v += __uint_as_float(xor_lane_u32<2>(__float_as_uint(v)));
-    v += __uint_as_float(xor_lane_u32<7>(__float_as_uint(v)));
-    return v + __uint_as_float(xor_lane_u32<15>(__float_as_uint(v)));
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] += xor_lane_f32<1>(v[r]);
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] += xor_lane_f32<2>(v[r]);
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] += xor_lane_f32<7>(v[r]);
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] += xor_lane_f32<15>(v[r]);
 }
 
 // What a lane's columns and rows are after product().
@@ -485,26 +500,40 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_sums(Cont
         base[n] = side.base[at.in_col + n];
         id[n] = side.id[at.in_col + n];
     }
+    // four rows at a time without a branch, so that their chains of instructions overlap; lane l of 16 keeps the rows l, l + 16
+    float keep_top[N / 4], keep_sum[N / 4];
 #pragma unroll
-    for (int m = 0; m < N; ++m)
+    for (int m = 0; m < N; ++m) {
+        float s[4][N], top[4], sum[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int row = at.row + m * 4 + r;
             const int2 out = side.row_id[at.in_row + m * 4 + r];
-            float s[N], top = -INFINITY;
+            top[r] = -INFINITY;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                s[n] = id[n] == out.x || id[n] == out.y ? -INFINITY : fmaf(acc[m][n][r], c.c1, base[n]);
-                top = fmaxf(top, s[n]);
+                s[r][n] = id[n] == out.x || id[n] == out.y ? -INFINITY : fmaf(acc[m][n][r], c.c1, base[n]);
+                top[r] = fmaxf(top[r], s[r][n]);
             }
-            top = row16_max(top);
-            const float ref = top == -INFINITY ? 0.0f : top;
-            float sum = 0.0f;
-#pragma unroll
-            for (int n = 0; n < N; ++n) sum += __builtin_amdgcn_exp2f(s[n] - ref);
-            sum = row16_sum(sum);
-            if ((threadIdx.x & 15) == 0) c.part[(size_t)row * c.parts_k + at.half_c] = make_float2(top, sum);
         }
+        row16_max(top);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float ref = top[r] == -INFINITY ? 0.0f : top[r];
+            sum[r] = 0.0f;
+#pragma unroll
+            for (int n = 0; n < N; ++n) sum[r] += __builtin_amdgcn_exp2f(s[r][n] - ref);
+        }
+        row16_sum(sum);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const bool mine = (int)(threadIdx.x & 15) == m % 4 * 4 + r;
+            keep_top[m / 4] = mine ? top[r] : m % 4 || r ? keep_top[m / 4] : 0.0f;
+            keep_sum[m / 4] = mine ? sum[r] : m % 4 || r ? keep_sum[m / 4] : 0.0f;
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < N / 4; ++h)
+        c.part[(size_t)(at.row + h * 16 + (threadIdx.x & 15)) * c.parts_k + at.half_c] = make_float2(keep_top[h], keep_sum[h]);
 }
 
 // (largest, sum) of two parts; a NaN in either stays
@@ -571,18 +600,16 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_g(Contras
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     half_t *turn = (half_t *)&lds + wave * H * H;
     __syncthreads();        // all have read their operands
-    // (both paddings are multiples of 64: a lane's columns, and 8 of its rows, lie inside or outside together)
-    const bool cols_in = at.col < c.Mp;
+    float keep_sum[N / 4];
 #pragma unroll
     for (int pair = 0; pair < N / 2; ++pair) {       // 8 rows at a time
         half_t o[PLANES][N][8];
         const int row0 = at.row + pair * 8;
+        float row_sum[8] = {};
 #pragma unroll
         for (int r8 = 0; r8 < 8; ++r8) {
-            const int row = row0 + r8;
             const int2 out = side.row_id[at.in_row + pair * 8 + r8];
             const float2 info = side.row_g[at.in_row + pair * 8 + r8];
-            float row_sum = 0.0f;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 const float s = id[n] == out.x || id[n] == out.y ? -INFINITY : fmaf(acc[pair * 2 + r8 / 4][n][r8 % 4], c.c1, base[n]);
@@ -595,21 +622,22 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_g(Contras
                     o[p][n][r8] = x[p];
                     rounded += value16<DT>(x[p]);
                 }
-                row_sum += rounded;
+                row_sum[r8] += rounded;
                 col_sum[n] += rounded;
             }
-            if (cols_in)
 #pragma unroll
-                for (int p = 0; p < PLANES; ++p) {
-                    typedef half_t line_t __attribute__((ext_vector_type(N)));
-                    line_t l;
+            for (int p = 0; p < PLANES; ++p) {
+                typedef half_t line_t __attribute__((ext_vector_type(N)));
+                line_t l;
 #pragma unroll
-                    for (int n = 0; n < N; ++n) l[n] = o[p][n][r8];
-                    *(line_t *)&c.g[p * c.plane_g + (size_t)row * c.Mp + at.col] = l;
-                }
-            row_sum = row16_sum(row_sum);
-            if ((threadIdx.x & 15) == 0) c.sum_q[(size_t)row * c.parts_k + at.half_c] = row_sum;
+                for (int n = 0; n < N; ++n) l[n] = o[p][n][r8];
+                *(line_t *)&c.g[p * c.plane_g + (size_t)(row0 + r8) * c.ld_g + at.col] = l;
+            }
         }
+        row16_sum(row_sum);
+#pragma unroll
+        for (int r8 = 0; r8 < 8; ++r8)
+            keep_sum[pair / 2] = (int)(threadIdx.x & 15) == pair % 2 * 8 + r8 ? row_sum[r8] : pair % 2 || r8 ? keep_sum[pair / 2] : 0.0f;
         // by columns: 8 rows of a column are 16 bytes.  One plane: first into the wavefront's own part of LDS, in which a
         // column's rows lie together (piece k of column x at k ^ x / N % 8: both sides free of bank conflicts)
 #pragma unroll
@@ -620,18 +648,19 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_g(Contras
 #pragma unroll
                 for (int r8 = 0; r8 < 8; ++r8) l[r8] = o[p][n][r8];
                 if constexpr (PLANES == 1) *(us8 *)&turn[((lane & 15) * N + n) * H + (((lane >> 4) * (N / 2) + pair) ^ (lane & 7)) * 8] = l;
-                else if (row0 < c.Bp) *(us8 *)&c.gt[p * c.plane_gt + (size_t)(at.col + n) * c.Bp + row0] = l;
+                else *(us8 *)&c.gt[p * c.plane_gt + (size_t)(at.col + n) * c.ld_gt + row0] = l;
             }
     }
     if constexpr (PLANES == 1) {
         wave_sync();
         constexpr int per = H / 8;          // lanes for a column
         const int piece = lane % per, row0 = tr * TILE + (wave >> 1) * H + piece * 8, col0 = tc * TILE + (wave & 1) * H;
-        if (row0 < c.Bp)
-#pragma unroll 4
-            for (int x = lane / per; x < H; x += 64 / per)
-                *(us8 *)&c.gt[(size_t)(col0 + x) * c.Bp + row0] = *(const us8 *)&turn[x * H + (piece ^ (x / N & 7)) * 8];
+#pragma unroll 8
+        for (int x = lane / per; x < H; x += 64 / per)
+            *(us8 *)&c.gt[(size_t)(col0 + x) * c.ld_gt + row0] = *(const us8 *)&turn[x * H + (piece ^ (x / N & 7)) * 8];
     }
+#pragma unroll
+    for (int h = 0; h < N / 4; ++h) c.sum_q[(size_t)(at.row + h * 16 + (threadIdx.x & 15)) * c.parts_k + at.half_c] = keep_sum[h];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
         col_sum[n] += __shfl_xor(col_sum[n], 16);
@@ -656,7 +685,7 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_grad(Cont
     tile_of(id - split * tiles * tiles_d, tiles, tiles_d, tr, tc);
     const int depth = keys ? c.Bp : c.Mp, steps = depth / CT_K;
     const int k0 = (int)((long long)steps * split / splits) * CT_K, k1 = (int)((long long)steps * (split + 1) / splits) * CT_K;
-    const Operand a = keys ? Operand{c.gt, c.plane_gt, c.Bp} : Operand{c.g, c.plane_g, c.Mp};
+    const Operand a = keys ? Operand{c.gt, c.plane_gt, c.ld_gt} : Operand{c.g, c.plane_g, c.ld_g};
     const Operand b = keys ? Operand{c.qt, c.plane_qt, c.Bp} : Operand{c.kt, c.plane_kt, c.Mp};
     product<TILE, DT>(a, b, tr * TILE, tc * TILE, k0, k1, lds, acc);
     const Place<TILE> at(tr, tc);
@@ -844,8 +873,10 @@ static size_t contrast_layout(ContrastPar &c, ContrastPlan &plan, int dtype, int
     if (want_grad) {
         take(c.qt, planes * (c.plane_qt = (size_t)c.dr * c.Bp));
         take(c.kt, planes * (c.plane_kt = (size_t)c.dr * c.Mp));
-        take(c.g, planes * (c.plane_g = Br * c.Mp));
-        take(c.gt, planes * (c.plane_gt = Mr * c.Bp));
+        c.ld_g = (int)Mr;
+        c.ld_gt = (int)Br;
+        take(c.g, planes * (c.plane_g = Br * Mr));
+        take(c.gt, planes * (c.plane_gt = Mr * Br));
         take(c.sum_q, Br * c.parts_k);
         take(c.sum_k, Mr * c.parts_q);
         take(c.acc_q, (size_t)c.splits_q * Br * c.dr);
