@@ -819,7 +819,10 @@ static ContrastPlan contrast_plan(ContrastPar &c, int planes)
 {
     ContrastPlan p;
     auto tiles = [](int x, int t) { return (long long)(x + t - 1) / t; };
-    p.tile = planes == 1 && tiles(c.B, 256) * tiles(c.M, 256) >= 128 ? 256 : 128;
+    // logits: tiles of 128 come two to a CU, one's product beside the other's logits, which is the longer part of short rows.  Sums and g
+    // of 8,192 x 16,384, tiles of 128 / 256, us: d = 64 216 / 266, 256 349 / 357, 768 635 / 604, 1,536 1,035 / 944; of 1,000 x 11,000: d = 768
+    // 69 / 76 (172 tiles of 256 for 256 CUs), 1,536 117 / 119
+    p.tile = planes == 1 && c.d > 384 && tiles(c.B, 256) * tiles(c.M, 256) >= 512 ? 256 : 128;
     // the gradient products: also by how much of the last tile of d would be padding
     const int d128 = ct_up(c.d, 128), d256 = ct_up(c.d, 256);
     p.tile_g = (tiles(c.B, 256) + tiles(c.M, 256)) * (d256 / 256) >= 64 && d256 * 4 <= d128 * 5 ? 256 : 128;

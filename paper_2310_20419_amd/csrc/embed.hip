@@ -100,13 +100,13 @@ extern "C" int rnnd_embed(const void *table, int64_t V, int32_t d, int dtype, co
 }
 
 // ------------------------------------------------------------------------------------------------ tokens sorted by id
-// Least significant digit first, up to SORT_BITS bits a pass, three launches each: every block counts its digits, a
-// wavefront per digit makes the counts of the blocks offsets, every block places its tokens.  A block's order is kept
-// (stable) because its wavefronts number equal digits lane by lane, with a ballot per bit.
-// An id that is no row sorts as V, behind all rows.
+// Pairs (id, token), least significant digit first, up to SORT_BITS bits a pass, three launches each: every block counts its
+// digits, a wavefront per digit makes the counts of the blocks offsets, every block places its tokens.  A block's order
+// is kept (stable) because its wavefronts number equal digits lane by lane, with a ballot per bit.  An id that is no row
+// sorts as V, behind all rows.
 #define SORT_BITS 10
 #define SORT_DIGITS (1 << SORT_BITS)
-#define SORT_THREADS 1024
+#define SORT_THREADS 512
 #define SORT_WAVES (SORT_THREADS / 64)
 #define SORT_ITEMS 4
 #define SORT_TILE (SORT_THREADS * SORT_ITEMS)
@@ -114,20 +114,16 @@ extern "C" int rnnd_embed(const void *table, int64_t V, int32_t d, int dtype, co
 
 struct SortPass {
     const int *ids;             // first pass: the caller's ids; else null
-    const u32 *key_in, *pos_in;
-    u32 *key_out, *pos_out;
+    const uint2 *in;            // (key, token)
+    uint2 *out;
     u32 *hist;                  // [digits][blocks]
     u32 *totals;                // [digits]
+    unsigned char *named;       // first pass: set to 1 for every row that an id names (may be null)
     u32 n, V, blocks;
     int shift, bits;
 };
 
-__device__ __forceinline__ u32 sort_key(const SortPass &s, u32 t)
-{
-    if (!s.ids) return s.key_in[t];
-    const u32 id = (u32)s.ids[t];
-    return id < s.V ? id : s.V;
-}
+__device__ __forceinline__ u32 id_key(int id, u32 V) { return (u32)id < V ? (u32)id : V; }
 
 __global__ __launch_bounds__(SORT_THREADS) void k_sort_count(SortPass s)
 {
@@ -139,7 +135,10 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_count(SortPass s)
 #pragma unroll
     for (int i = 0; i < SORT_ITEMS; ++i) {
         const u32 t = base + i * SORT_THREADS + threadIdx.x;
-        if (t < s.n) atomicAdd(&count[(sort_key(s, t) >> s.shift) & (digits - 1)], 1u);
+        if (t >= s.n) continue;
+        const u32 key = s.ids ? id_key(s.ids[t], s.V) : s.in[t].x;
+        if (s.named && key < s.V) s.named[key] = 1;
+        atomicAdd(&count[(key >> s.shift) & (digits - 1)], 1u);
     }
     __syncthreads();
     for (u32 i = threadIdx.x; i < digits; i += SORT_THREADS) s.hist[(size_t)i * s.blocks + blockIdx.x] = count[i];
@@ -172,77 +171,91 @@ __global__ __launch_bounds__(64) void k_sort_offsets(SortPass s)
 
 __global__ __launch_bounds__(SORT_THREADS) void k_sort_place(SortPass s)
 {
+    constexpr int PER = SORT_DIGITS / SORT_THREADS;     // digits of a thread
     __shared__ u32 count[SORT_WAVES][SORT_DIGITS];
-    __shared__ u32 first[SORT_DIGITS], wave_sum[SORT_WAVES];
+    __shared__ u32 wave_total[SORT_WAVES];
     const u32 digits = 1u << s.bits;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (u32 i = threadIdx.x; i < SORT_WAVES * SORT_DIGITS; i += SORT_THREADS) (&count[0][0])[i] = 0;
-    // where each digit starts: exclusive sums of the totals (SORT_DIGITS = SORT_THREADS)
-    {
-        const u32 v = threadIdx.x < digits ? s.totals[threadIdx.x] : 0;
-        const u32 inc = wave_inclusive(v, lane);
-        if (lane == 63) wave_sum[wave] = inc;
-        __syncthreads();
-        u32 before = 0;
-        for (int w = 0; w < wave; ++w) before += wave_sum[w];
-        if (threadIdx.x < digits) first[threadIdx.x] = before + inc - v + s.hist[(size_t)threadIdx.x * s.blocks + blockIdx.x];
-    }
-    __syncthreads();
     // a wavefront owns SORT_ITEMS * 64 neighbouring tokens, so that its order is the order of the input
     const u32 base = blockIdx.x * SORT_TILE + wave * (64 * SORT_ITEMS);
-    u32 key[SORT_ITEMS], pos[SORT_ITEMS], rank[SORT_ITEMS];
+    uint2 item[SORT_ITEMS];
+    u32 rank[SORT_ITEMS];
 #pragma unroll
     for (int i = 0; i < SORT_ITEMS; ++i) {
         const u32 t = base + i * 64 + lane;
-        key[i] = t < s.n ? sort_key(s, t) : 0;
-        pos[i] = t < s.n ? (s.ids ? t : s.pos_in[t]) : 0;
+        item[i] = make_uint2(0, 0);
+        if (t < s.n) item[i] = s.ids ? make_uint2(id_key(s.ids[t], s.V), t) : s.in[t];
+    }
+    // where each digit starts: exclusive sums of the totals, and of this block's counts
+    u32 first[PER], mine = 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const u32 digit = threadIdx.x * PER + k;
+        first[k] = mine;
+        mine += digit < digits ? s.totals[digit] : 0;
+    }
+    const u32 inc = wave_inclusive(mine, lane);
+    if (lane == 63) wave_total[wave] = inc;
+    __syncthreads();
+    u32 before_waves = inc - mine;
+    for (int w = 0; w < wave; ++w) before_waves += wave_total[w];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const u32 digit = threadIdx.x * PER + k;
+        first[k] += before_waves + (digit < digits ? s.hist[(size_t)digit * s.blocks + blockIdx.x] : 0);
     }
 #pragma unroll
     for (int i = 0; i < SORT_ITEMS; ++i) {
         const bool on = base + i * 64 + lane < s.n;
-        const u32 digit = (key[i] >> s.shift) & (digits - 1);
+        const u32 digit = (item[i].x >> s.shift) & (digits - 1);
         u64 same = __ballot(on);
         for (int b = 0; b < s.bits; ++b) {
             const bool bit = digit >> b & 1;
             const u64 set = __ballot(bit);
             same &= bit ? set : ~set;
         }
-        const u32 mine = __popcll(same & lanes_below(lane));
+        const u32 ahead = __popcll(same & lanes_below(lane));
         u32 before = 0;
         if (on) before = count[wave][digit];
         wave_sync();
-        if (on && mine == 0) count[wave][digit] = before + __popcll(same);
+        if (on && ahead == 0) count[wave][digit] = before + __popcll(same);
         wave_sync();
-        rank[i] = before + mine;
+        rank[i] = before + ahead;
     }
     __syncthreads();
-    if (threadIdx.x < digits) {
-        u32 at = first[threadIdx.x];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        u32 at = first[k];
         for (int w = 0; w < SORT_WAVES; ++w) {
-            const u32 c = count[w][threadIdx.x];
-            count[w][threadIdx.x] = at;
-            at += c;
+            const u32 n = count[w][threadIdx.x * PER + k];
+            count[w][threadIdx.x * PER + k] = at;
+            at += n;
         }
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < SORT_ITEMS; ++i) {
-        if (base + i * 64 + lane >= s.n) continue;
-        const u32 at = count[wave][(key[i] >> s.shift) & (digits - 1)] + rank[i];
-        s.key_out[at] = key[i];
-        s.pos_out[at] = pos[i];
-    }
+    for (int i = 0; i < SORT_ITEMS; ++i)
+        if (base + i * 64 + lane < s.n) s.out[count[wave][(item[i].x >> s.shift) & (digits - 1)] + rank[i]] = item[i];
 }
 
-// Few tokens: 8 lanes per token count the tokens that sort before it -- those of a smaller key, and those before it of the same.
-__global__ __launch_bounds__(256) void k_sort_small(const int *__restrict__ ids, u32 n, u32 V, u32 *__restrict__ key_out,
-                                                    u32 *__restrict__ pos_out)
+// Few tokens, one launch: 8 lanes per token count the tokens that sort before it -- those of a smaller key, and those before it
+// of the same.  Blocks behind the first token_blocks clear the whole gradient meanwhile: its 16-byte words, and what lies before
+// and behind them.
+__global__ __launch_bounds__(256) void k_sort_small(const int *__restrict__ ids, u32 n, u32 V, uint2 *__restrict__ out, u32 *hot,
+                                                    u32 token_blocks, uint4 *words, size_t n_words, unsigned char *head, u32 head_bytes,
+                                                    unsigned char *tail, u32 tail_bytes)
 {
     __shared__ u32 keys[SORT_SMALL];
-    for (u32 t = threadIdx.x; t < n; t += 256) {
-        const u32 id = (u32)ids[t];
-        keys[t] = id < V ? id : V;
+    if (blockIdx.x >= token_blocks) {
+        const u32 b = blockIdx.x - token_blocks, blocks = gridDim.x - token_blocks;
+        for (size_t i = (size_t)b * 256 + threadIdx.x; i < n_words; i += (size_t)blocks * 256) words[i] = make_uint4(0, 0, 0, 0);
+        if (b == 0 && threadIdx.x < head_bytes) head[threadIdx.x] = 0;
+        if (b == 0 && threadIdx.x < tail_bytes) tail[threadIdx.x] = 0;
+        return;
     }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *hot = 0;
+    for (u32 t = threadIdx.x; t < n; t += 256) keys[t] = id_key(ids[t], V);
     __syncthreads();
     const u32 t = blockIdx.x * 32 + (threadIdx.x >> 3), sub = threadIdx.x & 7;
     if (t >= n) return;         // whole groups of 8
@@ -250,27 +263,25 @@ __global__ __launch_bounds__(256) void k_sort_small(const int *__restrict__ ids,
     u32 before = 0;
     for (u32 j = sub; j < n; j += 8) before += keys[j] < key + (j < t);
     before = (u32)group8_sum((int)before);
-    if (sub == 0) {
-        key_out[before] = key;
-        pos_out[before] = t;
-    }
+    if (sub == 0) out[before] = make_uint2(key, t);
 }
 
 // ------------------------------------------------------------------------------------------------ gradient
 // The sorted tokens are cut into chunks.  A group of G lanes takes a chunk and the G * VEC coordinates of a slab, and sums
 // the rows of one id after the other.  An id whose tokens end at most one chunk behind the chunk they start in is summed by
 // that chunk's group alone (it reads on, and the next group leaves them out).  A longer one -- words as frequent as "the" --
-// leaves one partial sum per chunk, which k_grad_join adds in order, a whole block for each such id.
+// leaves one partial sum per chunk, which k_grad_join adds in order, a whole block for each such id and slab.
 #define GRAD_UNROLL 8       // divides every chunk
 #define GRAD_SLOTS 2        // partial sums of a chunk: 0 = of an id that started before it, 1 = of the id that goes on after it
+#define JOIN_THREADS 512
 
 struct GradPar {
     const void *dout;
-    const u32 *key, *pos;       // sorted
+    const uint2 *item;          // sorted (key, token)
     void *grad;
     float *partial;             // [chunks][GRAD_SLOTS][d]
     u32 *hot;                   // [0] how many, [1 ..] chunks in which a long id starts
-    const unsigned char *named; // [V] whether a row is named (null: do not clear the others)
+    const unsigned char *named; // [V] whether a row is named (the others are cleared here)
     u32 n, V, chunk, pieces, slabs, reduce_blocks;
     int accumulate;
     float scale;
@@ -308,52 +319,44 @@ __global__ __launch_bounds__(256) void k_grad_reduce(GradPar g)
     const u64 begin64 = (u64)c * g.chunk;
     if (begin64 >= g.n || piece >= g.pieces) return;
     const u32 begin = (u32)begin64, end = g.n - begin < g.chunk ? g.n : begin + g.chunk, C = g.chunk;
-    u32 id = g.key[begin];
+    u32 id = g.item[begin].x;
     if (id >= g.V) return;
-    const bool incoming = begin > 0 && g.key[begin - 1] == id;
+    const bool incoming = begin > 0 && g.item[begin - 1].x == id;
     // (sorted: the tokens of `id` end at or before position x if x is the end or holds another key)
-    const bool skip = incoming && (begin - C == 0 || g.key[begin - C - 1] != id) && ((u64)begin + C >= g.n || g.key[begin + C] != id);
+    const bool skip = incoming && (begin - C == 0 || g.item[begin - C - 1].x != id) && ((u64)begin + C >= g.n || g.item[begin + C].x != id);
     bool first = incoming;          // still in the id that started before the chunk
-    const u32 last = g.key[end - 1];
-    const bool goes_on = end < g.n && g.key[end] == last && last < g.V && !(incoming && last == id);
-    const bool hot = goes_on && (u64)end + C < g.n && g.key[end + C] == last;
+    const u32 last = g.item[end - 1].x;
+    const bool goes_on = end < g.n && g.item[end].x == last && last < g.V && !(incoming && last == id);
+    const bool hot = goes_on && (u64)end + C < g.n && g.item[end + C].x == last;
     const u32 stop = goes_on && !hot ? (g.n - end < C ? g.n : end + C) : end;      // and no further than the key `last`
 
     float acc[VEC] = {};
     bool some = false;
     for (u32 t = begin; t < stop; t += GRAD_UNROLL) {
-        u32 key[GRAD_UNROLL];
+        uint2 it[GRAD_UNROLL];
         Pack<DT, VEC> row[GRAD_UNROLL];
-        u32 pos[GRAD_UNROLL];
 #pragma unroll
-        for (int i = 0; i < GRAD_UNROLL; ++i) {
-            const u32 at = t + i < stop ? t + i : stop - 1;
-            key[i] = g.key[at];
-            pos[i] = g.pos[at];
-        }
+        for (int i = 0; i < GRAD_UNROLL; ++i) it[i] = g.item[t + i < stop ? t + i : stop - 1];
 #pragma unroll
         for (int i = 0; i < GRAD_UNROLL; ++i) {
             const u32 at = t + i;
-            if (at >= stop || (at >= end && key[i] != last)) key[i] = 0xFFFFFFFFu;      // nothing there for this group
-            if (key[i] < g.V && !(skip && first && key[i] == id)) row[i] = load_pack<DT, VEC>(g.dout, ((u64)pos[i] * g.pieces + piece) * VEC);
+            if (at >= stop || (at >= end && it[i].x != last)) it[i].x = 0xFFFFFFFFu;      // nothing there for this group
+            if (it[i].x < g.V && !(skip && first && it[i].x == id)) row[i] = load_pack<DT, VEC>(g.dout, ((u64)it[i].y * g.pieces + piece) * VEC);
         }
         bool done = false;
 #pragma unroll
         for (int i = 0; i < GRAD_UNROLL; ++i) {
             if (done) break;
-            if (key[i] != id) {
+            if (it[i].x != id) {
                 if (some) {
-                    if (first) {
-#pragma unroll
-                        for (int k = 0; k < VEC; ++k) g.partial[((u64)c * GRAD_SLOTS * g.pieces + piece) * VEC + k] = acc[k];
-                    } else
-                        grad_write<GT, VEC>(g, id, piece, acc);
+                    if (first) store_pack<DT_F32, VEC>(g.partial, ((u64)c * GRAD_SLOTS * g.pieces + piece) * VEC, acc);
+                    else grad_write<GT, VEC>(g, id, piece, acc);
                 }
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) acc[k] = 0.0f;
                 some = false;
                 first = false;
-                id = key[i];
+                id = it[i].x;
                 if (id >= g.V) { done = true; break; }
             }
             if (skip && first) continue;
@@ -367,51 +370,57 @@ __global__ __launch_bounds__(256) void k_grad_reduce(GradPar g)
     }
     if (!some) return;
     if (first || hot) {
-        const u64 slot = (u64)c * GRAD_SLOTS + (first ? 0 : 1);
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) g.partial[(slot * g.pieces + piece) * VEC + k] = acc[k];
+        store_pack<DT_F32, VEC>(g.partial, (((u64)c * GRAD_SLOTS + (first ? 0 : 1)) * g.pieces + piece) * VEC, acc);
         if (!first && piece == 0) g.hot[1 + atomicAdd(&g.hot[0], 1u)] = c;
     } else
         grad_write<GT, VEC>(g, id, piece, acc);
 }
 
-// One block per long id: its groups take every (256 / G)-th partial sum, and their sums are added in the groups' order.
+// One block per long id and slab: its groups take every (JOIN_THREADS / G)-th partial sum, four at a time, and their sums are added
+// in the groups' order.
 template <int GT, int VEC, int G>
-__global__ __launch_bounds__(256) void k_grad_join(GradPar g)
+__global__ __launch_bounds__(JOIN_THREADS) void k_grad_join(GradPar g)
 {
-    constexpr u32 groups = 256 / G;
+    constexpr u32 groups = JOIN_THREADS / G;
     __shared__ float part[groups][G * VEC];
     const u32 lane = threadIdx.x % G, group = threadIdx.x / G;
-    for (u32 item = blockIdx.x; item < g.hot[0]; item += gridDim.x) {
-        const u32 c = g.hot[1 + item];
-        const u32 id = g.key[(u64)(c + 1) * g.chunk - 1];
-        u32 lo = (c + 1) * g.chunk, hi = g.n;         // the first position behind `id`
+    const u32 work = g.hot[0] * g.slabs;
+    for (u32 at = blockIdx.x; at < work; at += gridDim.x) {
+        const u32 c = g.hot[1 + at / g.slabs], piece = at % g.slabs * G + lane;
+        const u32 id = g.item[(u64)(c + 1) * g.chunk - 1].x;
+        u32 lo = c + 1, hi = (g.n - 1) / g.chunk;      // the last chunk whose first token is of `id`: a long id fills c + 1
         while (lo < hi) {
-            const u32 mid = lo + (hi - lo) / 2;
-            if (g.key[mid] == id) lo = mid + 1;
-            else hi = mid;
+            const u32 mid = lo + (hi - lo + 1) / 2;
+            if (g.item[(u64)mid * g.chunk].x == id) lo = mid;
+            else hi = mid - 1;
         }
-        const u32 chunks = (lo - 1) / g.chunk - c + 1;
-        for (u32 slab = 0; slab < g.slabs; ++slab) {
-            const u32 piece = slab * G + lane;
-            float acc[VEC] = {};
-            if (piece < g.pieces)
-                for (u32 j = group; j < chunks; j += groups) {
-                    const u64 slot = (u64)(c + j) * GRAD_SLOTS + (j == 0 ? 1 : 0);
+        const u32 chunks = lo - c + 1;
+        float acc[VEC] = {};
+        if (piece < g.pieces)
+            for (u32 j0 = group; j0 < chunks; j0 += 4 * groups) {
+                Pack<DT_F32, VEC> p[4];
 #pragma unroll
-                    for (int k = 0; k < VEC; ++k) acc[k] += g.partial[(slot * g.pieces + piece) * VEC + k];
+                for (int u = 0; u < 4; ++u) {
+                    const u32 j = j0 + u * groups;
+                    if (j < chunks) p[u] = load_pack<DT_F32, VEC>(g.partial, (((u64)(c + j) * GRAD_SLOTS + (j == 0 ? 1 : 0)) * g.pieces + piece) * VEC);
                 }
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) part[group][lane * VEC + k] = acc[k];
-            __syncthreads();
-            if (group == 0 && piece < g.pieces) {
-                for (u32 j = 1; j < groups; ++j)
+                for (int u = 0; u < 4; ++u)
+                    if (j0 + u * groups < chunks)
 #pragma unroll
-                    for (int k = 0; k < VEC; ++k) acc[k] += part[j][lane * VEC + k];
-                grad_write<GT, VEC>(g, id, piece, acc);
+                        for (int k = 0; k < VEC; ++k) acc[k] += p[u].v[k];
             }
-            __syncthreads();
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) part[group][lane * VEC + k] = acc[k];
+        __syncthreads();
+        if (group == 0 && piece < g.pieces) {
+            const u32 most = groups < chunks ? groups : chunks;
+            for (u32 j = 1; j < most; ++j)
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) acc[k] += part[j][lane * VEC + k];
+            grad_write<GT, VEC>(g, id, piece, acc);
         }
+        __syncthreads();
     }
 }
 
@@ -419,24 +428,20 @@ __global__ void k_grad_clear(u32 *p, size_t words)
 {
     for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < words; i += (size_t)gridDim.x * blockDim.x) p[i] = 0;
 }
-__global__ void k_grad_name(const int *__restrict__ ids, u32 n, u32 V, unsigned char *named)
-{
-    const u32 t = blockIdx.x * 256 + threadIdx.x;
-    if (t < n && (u32)ids[t] < V) named[(u32)ids[t]] = 1;
-}
 
 struct GradPlan {
     u32 chunk, chunks, blocks;
     int passes, bits;
-    size_t o_key[2], o_pos[2], o_hist, o_totals, o_partial, o_hot, o_named, bytes;
+    size_t o_item[2], o_hist, o_totals, o_partial, o_hot, o_named, bytes;
 };
 
 static GradPlan grad_plan(int64_t n, int d, int64_t V)
 {
     GradPlan p = {};
-    // Long chunks leave fewer partial sums; short calls need chunks short enough to occupy the GPU.
+    // Long chunks leave fewer partial sums; short calls need chunks short enough to occupy the GPU: two wavefronts per SIMD, of about
+    // 256 coordinates each.
     p.chunk = 128;
-    while (p.chunk > 16 && n / p.chunk < 4096) p.chunk >>= 1;
+    while (p.chunk > 16 && n / p.chunk * ((d + 255) / 256) < 4096) p.chunk >>= 1;
     p.chunks = (u32)((n + p.chunk - 1) / p.chunk);
     p.blocks = (u32)((n + SORT_TILE - 1) / SORT_TILE);
     int bits = 1;
@@ -445,15 +450,12 @@ static GradPlan grad_plan(int64_t n, int d, int64_t V)
     p.bits = p.passes ? (bits + p.passes - 1) / p.passes : 0;
     size_t off = 0;
     auto take = [&](size_t b) { const size_t o = off; off += ws_align(b); return o; };
-    for (int i = 0; i < 2; ++i) {
-        p.o_key[i] = take((size_t)n * 4);
-        p.o_pos[i] = take((size_t)n * 4);
-    }
+    for (int i = 0; i < 2; ++i) p.o_item[i] = take(i && !p.passes ? 0 : (size_t)n * 8);
     p.o_hist = take(p.passes ? (size_t)SORT_DIGITS * p.blocks * 4 : 0);
-    p.o_totals = take(SORT_DIGITS * 4);
+    p.o_totals = take(p.passes ? SORT_DIGITS * 4 : 0);
     p.o_partial = take((size_t)p.chunks * GRAD_SLOTS * d * 4);
-    p.o_hot = take((size_t)(p.chunks + 1) * 4);
-    p.o_named = take((size_t)V);
+    p.o_named = take(p.passes ? (size_t)V : 0);
+    p.o_hot = take((size_t)(p.chunks + 1) * 4);       // (right behind `named`: its first word is cleared with it)
     p.bytes = off;
     return p;
 }
@@ -475,7 +477,7 @@ static void launch_grad_group(GradPar &g, u32 clear_blocks, u32 chunks, hipStrea
     g.reduce_blocks = (u32)((units + 256 / G - 1) / (256 / G));
     hipLaunchKernelGGL((k_grad_reduce<DT, GT, VEC, G>), dim3(g.reduce_blocks + clear_blocks), dim3(256), 0, st, g);
     if (chunks > 2)     // an id of more than two chunks' tokens
-        hipLaunchKernelGGL((k_grad_join<GT, VEC, G>), dim3(chunks < 1024 ? chunks : 1024), dim3(256), 0, st, g);
+        hipLaunchKernelGGL((k_grad_join<GT, VEC, G>), dim3((u32)(units < 1024 ? units : 1024)), dim3(JOIN_THREADS), 0, st, g);
 }
 template <int DT, int GT, int VEC>
 static void launch_grad_vec(GradPar &g, int d, u32 clear_blocks, u32 chunks, hipStream_t st)
@@ -512,31 +514,34 @@ extern "C" int rnnd_embed_grad(const void *dout, int dtype, const int32_t *ids, 
     if (workspace_bytes < p.bytes) return RNND_ERR_SCRATCH;
     hipStream_t st = (hipStream_t)stream;
     char *w = (char *)workspace;
-    u32 *key[2] = {(u32 *)(w + p.o_key[0]), (u32 *)(w + p.o_key[1])}, *pos[2] = {(u32 *)(w + p.o_pos[0]), (u32 *)(w + p.o_pos[1])};
+    uint2 *item[2] = {(uint2 *)(w + p.o_item[0]), (uint2 *)(w + p.o_item[1])};
     u32 *hot = (u32 *)(w + p.o_hot);
     unsigned char *named = (unsigned char *)(w + p.o_named);
-    // the number of long ids, and (all rows written) which rows are named
-    {
-        const size_t words = ((accumulate ? p.o_hot + 4 : p.bytes) - p.o_hot) / 4;
-        const size_t blocks = (words + 1023) / 1024;
-        hipLaunchKernelGGL(k_grad_clear, dim3((u32)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, st, hot, words);
-    }
-    if (!accumulate && n) hipLaunchKernelGGL(k_grad_name, dim3((u32)((n + 255) / 256)), dim3(256), 0, st, ids, (u32)n, (u32)V, named);
     int at = 0;
     if (!p.passes) {
-        if (n) hipLaunchKernelGGL(k_sort_small, dim3((u32)((n + 31) / 32)), dim3(256), 0, st, ids, (u32)n, (u32)V, key[0], pos[0]);
+        const size_t bytes = accumulate ? 0 : (size_t)V * d * dt_size(grad_dtype);
+        size_t head = (16 - (uintptr_t)grad % 16) % 16;
+        if (head > bytes) head = bytes;
+        const size_t words = (bytes - head) / 16;
+        const u32 tail = (u32)(bytes - head - words * 16);
+        const u32 token_blocks = (u32)((n + 31) / 32) + (n ? 0 : 1), clear_blocks = accumulate ? 0 : (u32)(words / 1024 < 2048 ? words / 1024 + 1 : 2048);
+        hipLaunchKernelGGL(k_sort_small, dim3(token_blocks + clear_blocks), dim3(256), 0, st, ids, (u32)n, (u32)V, item[0], hot, token_blocks,
+                           (uint4 *)((char *)grad + head), words, (unsigned char *)grad, (u32)head, (unsigned char *)grad + head + words * 16, tail);
     } else {
+        // the number of long ids, and (all rows written) which rows are named
+        const size_t from = accumulate ? p.o_hot : p.o_named, words = (p.o_hot + 4 - from) / 4;
+        const size_t blocks = (words + 1023) / 1024;
+        hipLaunchKernelGGL(k_grad_clear, dim3((u32)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, st, (u32 *)(w + from), words);
         at = 1;
         for (int i = 0; i < p.passes; ++i) {
             SortPass s;
             s.ids = i ? nullptr : ids;
-            s.key_in = key[at];
-            s.pos_in = pos[at];
+            s.in = item[at];
             at ^= 1;
-            s.key_out = key[at];
-            s.pos_out = pos[at];
+            s.out = item[at];
             s.hist = (u32 *)(w + p.o_hist);
             s.totals = (u32 *)(w + p.o_totals);
+            s.named = i || accumulate ? nullptr : named;
             s.n = (u32)n;
             s.V = (u32)V;
             s.blocks = p.blocks;
@@ -547,10 +552,10 @@ extern "C" int rnnd_embed_grad(const void *dout, int dtype, const int32_t *ids, 
             hipLaunchKernelGGL(k_sort_place, dim3(p.blocks), dim3(SORT_THREADS), 0, st, s);
         }
     }
+    if (!n) return launched("rnnd_embed_grad");
     GradPar g = {};
     g.dout = dout;
-    g.key = key[at];
-    g.pos = pos[at];
+    g.item = item[at];
     g.grad = grad;
     g.partial = (float *)(w + p.o_partial);
     g.hot = hot;
@@ -560,7 +565,7 @@ extern "C" int rnnd_embed_grad(const void *dout, int dtype, const int32_t *ids, 
     g.chunk = p.chunk;
     g.accumulate = accumulate;
     g.scale = scale;
-    const u32 clear_blocks = accumulate ? 0 : (u32)(V / 64 < 4096 ? V / 64 + 1 : 4096);
+    const u32 clear_blocks = accumulate || !p.passes ? 0 : (u32)(V / 64 < 4096 ? V / 64 + 1 : 4096);
 #define RNND_F(A, B) launch_grad<A, B>(g, d, clear_blocks, p.chunks, st)
     RNND_FOR_TYPES(dtype, grad_dtype, RNND_F)
 #undef RNND_F
