@@ -157,9 +157,15 @@ def _check(rc: int):
         raise RnndError(rc, rnnd_strerror(rc))
 
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _data_args(X):
@@ -419,10 +425,11 @@ class _On:
 
     def __init__(self, device, stream, used):
         torch = _torch()
-        self.stream = stream
+        self.context = None
         if stream is None:
-            self.handle = torch.cuda.current_stream(device).cuda_stream
-            self.context = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+            self.handle = _raw_stream(device.index)
+            if torch.cuda.current_device() != device.index:
+                self.context = torch.cuda.device(device)
         else:
             _need(stream.device == device, "the stream is of another device than the tensors")
             self.handle = stream.cuda_stream
@@ -441,6 +448,13 @@ class _On:
         if self.context is not None:
             return self.context.__exit__(*error)
         return False
+
+
+def _raw_stream(index):
+    """The current stream's handle, without an object around it where torch has that (2 us of a lookup's 10)."""
+    torch = _torch()
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(index) if raw is not None else torch.cuda.current_stream(index).cuda_stream
 
 
 def _work(workspace, need, device):

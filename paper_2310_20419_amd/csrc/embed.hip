@@ -239,7 +239,7 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_place(SortPass s)
         if (base + i * 64 + lane < s.n) s.out[count[wave][(item[i].x >> s.shift) & (digits - 1)] + rank[i]] = item[i];
 }
 
-// Few tokens, one launch: 8 lanes per token count the tokens that sort before it -- those of a smaller key, and those before it
+// Few tokens, one launch: 32 lanes per token count the tokens that sort before it -- those of a smaller key, and those before it
 // of the same.  Blocks behind the first token_blocks clear the whole gradient meanwhile: its 16-byte words, and what lies before
 // and behind them.
 __global__ __launch_bounds__(256) void k_sort_small(const int *__restrict__ ids, u32 n, u32 V, uint2 *__restrict__ out, u32 *hot,
@@ -257,19 +257,19 @@ __global__ __launch_bounds__(256) void k_sort_small(const int *__restrict__ ids,
     if (blockIdx.x == 0 && threadIdx.x == 0) *hot = 0;
     for (u32 t = threadIdx.x; t < n; t += 256) keys[t] = id_key(ids[t], V);
     __syncthreads();
-    const u32 t = blockIdx.x * 32 + (threadIdx.x >> 3), sub = threadIdx.x & 7;
-    if (t >= n) return;         // whole groups of 8
-    const u32 key = keys[t];
+    const u32 t = blockIdx.x * 8 + (threadIdx.x >> 5), sub = threadIdx.x & 31;
+    const u32 key = t < n ? keys[t] : 0;
     u32 before = 0;
-    for (u32 j = sub; j < n; j += 8) before += keys[j] < key + (j < t);
-    before = (u32)group8_sum((int)before);
-    if (sub == 0) out[before] = make_uint2(key, t);
+    for (u32 j = sub; j < n; j += 32) before += keys[j] < key + (j < t);
+#pragma unroll
+    for (int k = 16; k; k >>= 1) before += __shfl_xor(before, k);
+    if (t < n && sub == 0) out[before] = make_uint2(key, t);
 }
 
 // ------------------------------------------------------------------------------------------------ gradient
-// The sorted tokens are cut into chunks.  A group of G lanes takes a chunk and the G * VEC coordinates of a slab, and sums
-// the rows of one id after the other.  An id whose tokens end at most one chunk behind the chunk they start in is summed by
-// that chunk's group alone (it reads on, and the next group leaves them out).  A longer one -- words as frequent as "the" --
+// The sorted tokens are cut into chunks.  A lane takes VEC coordinates of a chunk (no lane needs another, so they are counted
+// through, whatever the length of a row), and sums the rows of one id after the other.  An id whose tokens end at most one chunk behind the chunk they start in is summed by
+// that chunk's lanes alone (they read on, and the next chunk's leave them out).  A longer one -- words as frequent as "the" --
 // leaves one partial sum per chunk, which k_grad_join adds in order, a whole block for each such id and slab.
 #define GRAD_UNROLL 8       // divides every chunk
 #define GRAD_SLOTS 2        // partial sums of a chunk: 0 = of an id that started before it, 1 = of the id that goes on after it
@@ -282,7 +282,7 @@ struct GradPar {
     float *partial;             // [chunks][GRAD_SLOTS][d]
     u32 *hot;                   // [0] how many, [1 ..] chunks in which a long id starts
     const unsigned char *named; // [V] whether a row is named (the others are cleared here)
-    u32 n, V, chunk, pieces, slabs, reduce_blocks;
+    u32 n, V, chunk, chunks, pieces, slabs, reduce_blocks, clear_rows;
     int accumulate;
     float scale;
 };
@@ -302,22 +302,23 @@ __device__ __forceinline__ void grad_write(const GradPar &g, u32 id, u32 piece, 
     store_pack<GT, VEC>(g.grad, at, acc);
 }
 
-template <int DT, int GT, int VEC, int G>
+template <int DT, int GT, int VEC>
 __global__ __launch_bounds__(256) void k_grad_reduce(GradPar g)
 {
-    if (blockIdx.x >= g.reduce_blocks) {        // the other blocks clear the rows that no token names
-        const u32 per = 256 / G, lane = threadIdx.x % G;
+    if (blockIdx.x >= g.reduce_blocks) {        // the other blocks clear the rows that no token names, clear_rows each
         const float zero[VEC] = {};
-        for (u64 v = (u64)(blockIdx.x - g.reduce_blocks) * per + threadIdx.x / G; v < g.V; v += (u64)(gridDim.x - g.reduce_blocks) * per) {
-            if (g.named[v]) continue;
-            for (u32 p = lane; p < g.pieces; p += G) store_pack<GT, VEC>(g.grad, (v * g.pieces + p) * VEC, zero);
+        const u64 v0 = (u64)(blockIdx.x - g.reduce_blocks) * g.clear_rows;
+        const u32 rows = (u32)(g.V - v0 < g.clear_rows ? g.V - v0 : g.clear_rows);
+        for (u32 i = threadIdx.x; i < rows * g.pieces; i += 256) {
+            const u32 r = i / g.pieces;
+            if (!g.named[v0 + r]) store_pack<GT, VEC>(g.grad, (v0 * g.pieces + i) * VEC, zero);
         }
         return;
     }
-    const u32 unit = blockIdx.x * (256 / G) + threadIdx.x / G;
-    const u32 c = unit / g.slabs, piece = (unit - c * g.slabs) * G + threadIdx.x % G;
+    const u64 flat = (u64)blockIdx.x * 256 + threadIdx.x;
+    const u32 c = (u32)(flat / g.pieces), piece = (u32)(flat - (u64)c * g.pieces);
+    if (c >= g.chunks) return;
     const u64 begin64 = (u64)c * g.chunk;
-    if (begin64 >= g.n || piece >= g.pieces) return;
     const u32 begin = (u32)begin64, end = g.n - begin < g.chunk ? g.n : begin + g.chunk, C = g.chunk;
     u32 id = g.item[begin].x;
     if (id >= g.V) return;
@@ -340,7 +341,7 @@ __global__ __launch_bounds__(256) void k_grad_reduce(GradPar g)
 #pragma unroll
         for (int i = 0; i < GRAD_UNROLL; ++i) {
             const u32 at = t + i;
-            if (at >= stop || (at >= end && it[i].x != last)) it[i].x = 0xFFFFFFFFu;      // nothing there for this group
+            if (at >= stop || (at >= end && it[i].x != last)) it[i].x = 0xFFFFFFFFu;      // nothing there for this chunk
             if (it[i].x < g.V && !(skip && first && it[i].x == id)) row[i] = load_pack<DT, VEC>(g.dout, ((u64)it[i].y * g.pieces + piece) * VEC);
         }
         bool done = false;
@@ -441,7 +442,7 @@ static GradPlan grad_plan(int64_t n, int d, int64_t V)
     // Long chunks leave fewer partial sums; short calls need chunks short enough to occupy the GPU: two wavefronts per SIMD, of about
     // 256 coordinates each.
     p.chunk = 128;
-    while (p.chunk > 16 && n / p.chunk * ((d + 255) / 256) < 4096) p.chunk >>= 1;
+    while (p.chunk > 8 && n / p.chunk * ((d + 255) / 256) < 4096) p.chunk >>= 1;
     p.chunks = (u32)((n + p.chunk - 1) / p.chunk);
     p.blocks = (u32)((n + SORT_TILE - 1) / SORT_TILE);
     int bits = 1;
@@ -469,34 +470,37 @@ extern "C" int rnnd_embed_grad_workspace(int64_t n, int32_t d, int64_t V, size_t
     return RNND_OK;
 }
 
-template <int DT, int GT, int VEC, int G>
-static void launch_grad_group(GradPar &g, u32 clear_blocks, u32 chunks, hipStream_t st)
+template <int GT, int VEC, int G>
+static void launch_join(GradPar &g, hipStream_t st)
 {
     g.slabs = (g.pieces + G - 1) / G;
-    const u64 units = (u64)chunks * g.slabs;
-    g.reduce_blocks = (u32)((units + 256 / G - 1) / (256 / G));
-    hipLaunchKernelGGL((k_grad_reduce<DT, GT, VEC, G>), dim3(g.reduce_blocks + clear_blocks), dim3(256), 0, st, g);
-    if (chunks > 2)     // an id of more than two chunks' tokens
-        hipLaunchKernelGGL((k_grad_join<GT, VEC, G>), dim3((u32)(units < 1024 ? units : 1024)), dim3(JOIN_THREADS), 0, st, g);
+    const u64 units = (u64)g.chunks * g.slabs;
+    hipLaunchKernelGGL((k_grad_join<GT, VEC, G>), dim3((u32)(units < 1024 ? units : 1024)), dim3(JOIN_THREADS), 0, st, g);
 }
 template <int DT, int GT, int VEC>
-static void launch_grad_vec(GradPar &g, int d, u32 clear_blocks, u32 chunks, hipStream_t st)
+static void launch_grad_vec(GradPar &g, int d, bool clear, hipStream_t st)
 {
     g.pieces = d / VEC;
-    if (g.pieces <= 8) launch_grad_group<DT, GT, VEC, 8>(g, clear_blocks, chunks, st);
-    else if (g.pieces <= 16) launch_grad_group<DT, GT, VEC, 16>(g, clear_blocks, chunks, st);
-    else if (g.pieces <= 32) launch_grad_group<DT, GT, VEC, 32>(g, clear_blocks, chunks, st);
-    else launch_grad_group<DT, GT, VEC, 64>(g, clear_blocks, chunks, st);
+    g.reduce_blocks = (u32)(((u64)g.chunks * g.pieces + 255) / 256);
+    g.clear_rows = 2048 / g.pieces > 1 ? 2048 / g.pieces : 1;
+    while (clear && (u64)g.V > (u64)g.clear_rows << 30) g.clear_rows <<= 1;
+    const u32 clear_blocks = clear ? (g.V + g.clear_rows - 1) / g.clear_rows : 0;
+    hipLaunchKernelGGL((k_grad_reduce<DT, GT, VEC>), dim3(g.reduce_blocks + clear_blocks), dim3(256), 0, st, g);
+    if (g.chunks <= 2) return;      // no id of more than two chunks' tokens
+    if (g.pieces <= 8) launch_join<GT, VEC, 8>(g, st);
+    else if (g.pieces <= 16) launch_join<GT, VEC, 16>(g, st);
+    else if (g.pieces <= 32) launch_join<GT, VEC, 32>(g, st);
+    else launch_join<GT, VEC, 64>(g, st);
 }
 template <int DT, int GT>
-static void launch_grad(GradPar &g, int d, u32 clear_blocks, u32 chunks, hipStream_t st)
+static void launch_grad(GradPar &g, int d, bool clear, hipStream_t st)
 {
     const int vec = row_vec(d, g.dout, dt_size(DT), g.grad, dt_size(GT));
     if constexpr (DT != DT_F32)
-        if (vec == 8) return launch_grad_vec<DT, GT, 8>(g, d, clear_blocks, chunks, st);
-    if (vec >= 4) launch_grad_vec<DT, GT, 4>(g, d, clear_blocks, chunks, st);
-    else if (vec == 2) launch_grad_vec<DT, GT, 2>(g, d, clear_blocks, chunks, st);
-    else launch_grad_vec<DT, GT, 1>(g, d, clear_blocks, chunks, st);
+        if (vec == 8) return launch_grad_vec<DT, GT, 8>(g, d, clear, st);
+    if (vec >= 4) launch_grad_vec<DT, GT, 4>(g, d, clear, st);
+    else if (vec == 2) launch_grad_vec<DT, GT, 2>(g, d, clear, st);
+    else launch_grad_vec<DT, GT, 1>(g, d, clear, st);
 }
 
 extern "C" int rnnd_embed_grad(const void *dout, int dtype, const int32_t *ids, int64_t n, int32_t d, float scale, int64_t V,
@@ -524,7 +528,7 @@ extern "C" int rnnd_embed_grad(const void *dout, int dtype, const int32_t *ids, 
         if (head > bytes) head = bytes;
         const size_t words = (bytes - head) / 16;
         const u32 tail = (u32)(bytes - head - words * 16);
-        const u32 token_blocks = (u32)((n + 31) / 32) + (n ? 0 : 1), clear_blocks = accumulate ? 0 : (u32)(words / 1024 < 2048 ? words / 1024 + 1 : 2048);
+        const u32 token_blocks = (u32)((n + 7) / 8) + (n ? 0 : 1), clear_blocks = accumulate ? 0 : (u32)(words / 1024 < 2048 ? words / 1024 + 1 : 2048);
         hipLaunchKernelGGL(k_sort_small, dim3(token_blocks + clear_blocks), dim3(256), 0, st, ids, (u32)n, (u32)V, item[0], hot, token_blocks,
                            (uint4 *)((char *)grad + head), words, (unsigned char *)grad, (u32)head, (unsigned char *)grad + head + words * 16, tail);
     } else {
@@ -563,10 +567,10 @@ extern "C" int rnnd_embed_grad(const void *dout, int dtype, const int32_t *ids, 
     g.n = (u32)n;
     g.V = (u32)V;
     g.chunk = p.chunk;
+    g.chunks = p.chunks;
     g.accumulate = accumulate;
     g.scale = scale;
-    const u32 clear_blocks = accumulate || !p.passes ? 0 : (u32)(V / 64 < 4096 ? V / 64 + 1 : 4096);
-#define RNND_F(A, B) launch_grad<A, B>(g, d, clear_blocks, p.chunks, st)
+#define RNND_F(A, B) launch_grad<A, B>(g, d, !accumulate && p.passes, st)
     RNND_FOR_TYPES(dtype, grad_dtype, RNND_F)
 #undef RNND_F
     return launched("rnnd_embed_grad");
