@@ -295,9 +295,10 @@ template <int DT> __device__ __forceinline__ f32x4 mfma(const us8 &a, const us8 
 
 template <int N> struct Half { us8 a[N], b[N]; };      // what half a step multiplies
 
-template <int TILE, int DT>
+// `meanwhile` runs while the first loads are under way; what it leaves in LDS is there behind the product.
+template <int TILE, int DT, typename F>
 __device__ __forceinline__ void product(const Operand &A, const Operand &B, int row_a, int row_b, int k_begin, int k_end,
-                                        ProductLds<TILE> &lds, f32x4 (&acc)[TILE / 32][TILE / 32])
+                                        ProductLds<TILE> &lds, f32x4 (&acc)[TILE / 32][TILE / 32], F meanwhile)
 {
     constexpr int N = TILE / 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -354,6 +355,7 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int 
     Half<N> h0, h1;
 #pragma unroll
     for (int i = 0; i < N; ++i) fetch(0, 0, i);
+    meanwhile();
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (steps > 1)
@@ -465,18 +467,52 @@ template <int TILE> struct Place {
     }
 };
 
-// What the logits of a tile need besides the product, in LDS before it starts: behind it nothing else hides the latency of
-// loads from memory (one wavefront per SIMD; with loads in the middle of it g took 35 us for a tile of 256, of which its product
-// is 20).
-template <int TILE> struct SideLds { int2 row_id[TILE]; float2 row_g[TILE]; float base[TILE]; int id[TILE]; };
+// What the logits of a tile need besides the product, in LDS while its first loads are under way: behind it nothing else hides the
+// latency of loads from memory (one wavefront per SIMD).
+// A row leaves out few keys, so most rows leave out none of a tile's.  16,384 bits say which hashes the tile's keys have; a row
+// whose two ids are not among them needs no comparison (4 instructions of 14 for each logit).
+#define CT_HASH 14
+template <int TILE> struct SideLds {
+    int2 row_id[TILE];
+    float2 row_g[TILE];
+    float base[TILE];
+    int id[TILE];
+    u32 maybe[TILE];        // whether the row may leave out a key of the tile
+    u32 seen[(1 << CT_HASH) / 32];
+};
+__device__ __forceinline__ u32 id_hash(int id) { return (u32)id * 0x9E3779B1u >> (32 - CT_HASH); }
 template <int TILE> __device__ __forceinline__ void load_side(const ContrastPar &c, SideLds<TILE> &side, int row0, int col0)
 {
     const int t = threadIdx.x;
+    int id = -1;
+    int2 out = make_int2(CT_NEVER, CT_NEVER);
+#pragma unroll
+    for (int i = 0; i < (1 << CT_HASH) / 32 / 256; ++i) side.seen[i * 256 + t] = 0;
     if (t < TILE) {
-        side.row_id[t] = c.row_id[row0 + t];
+        side.row_id[t] = out = c.row_id[row0 + t];
         side.row_g[t] = c.row_g[row0 + t];
         side.base[t] = c.key_base[col0 + t];
-        side.id[t] = c.key_id[col0 + t];
+        side.id[t] = id = c.key_id[col0 + t];
+    }
+    __syncthreads();
+    if (t < TILE && id >= 0) atomicOr(&side.seen[id_hash(id) >> 5], 1u << (id_hash(id) & 31));
+    __syncthreads();
+    if (t < TILE) side.maybe[t] = (side.seen[id_hash(out.x) >> 5] >> (id_hash(out.x) & 31) | side.seen[id_hash(out.y) >> 5] >> (id_hash(out.y) & 31)) & 1;
+}
+
+// Logits of the keys that rows leave out become -infinity; nothing to do for most rows.
+template <int TILE, int R, int N>
+__device__ __forceinline__ void leave_out(const SideLds<TILE> &side, int row, const int (&id)[N], float (&s)[R][N])
+{
+    u32 maybe = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) maybe |= side.maybe[row + r];
+    if (!__any(maybe)) return;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int2 out = side.row_id[row + r];
+#pragma unroll
+        for (int n = 0; n < N; ++n) s[r][n] = id[n] == out.x || id[n] == out.y ? -INFINITY : s[r][n];
     }
 }
 
@@ -490,8 +526,8 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_sums(Cont
     f32x4 acc[N][N];
     int tr, tc;
     tile_of(blockIdx.x, tiles_q, tiles_k, tr, tc);
-    load_side(c, side, tr * TILE, tc * TILE);
-    product<TILE, DT>({c.q, c.plane_q, c.dp}, {c.k, c.plane_k, c.dp}, tr * TILE, tc * TILE, 0, c.dp, lds, acc);
+    product<TILE, DT>({c.q, c.plane_q, c.dp}, {c.k, c.plane_k, c.dp}, tr * TILE, tc * TILE, 0, c.dp, lds, acc,
+                      [&]() { load_side(c, side, tr * TILE, tc * TILE); });
     const Place<TILE> at(tr, tc);
     float base[N];
     int id[N];
@@ -506,14 +542,15 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_sums(Cont
     for (int m = 0; m < N; ++m) {
         float s[4][N], top[4], sum[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int2 out = side.row_id[at.in_row + m * 4 + r];
-            top[r] = -INFINITY;
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                s[r][n] = id[n] == out.x || id[n] == out.y ? -INFINITY : fmaf(acc[m][n][r], c.c1, base[n]);
-                top[r] = fmaxf(top[r], s[r][n]);
-            }
+            for (int n = 0; n < N; ++n) s[r][n] = fmaf(acc[m][n][r], c.c1, base[n]);
+        leave_out(side, at.in_row + m * 4, id, s);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            top[r] = s[r][0];
+#pragma unroll
+            for (int n = 1; n < N; ++n) top[r] = fmaxf(top[r], s[r][n]);
         }
         row16_max(top);
 #pragma unroll
@@ -586,8 +623,8 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_g(Contras
     f32x4 acc[N][N];
     int tr, tc;
     tile_of(blockIdx.x, tiles_q, tiles_k, tr, tc);
-    load_side(c, side, tr * TILE, tc * TILE);
-    product<TILE, DT>({c.q, c.plane_q, c.dp}, {c.k, c.plane_k, c.dp}, tr * TILE, tc * TILE, 0, c.dp, lds, acc);
+    product<TILE, DT>({c.q, c.plane_q, c.dp}, {c.k, c.plane_k, c.dp}, tr * TILE, tc * TILE, 0, c.dp, lds, acc,
+                      [&]() { load_side(c, side, tr * TILE, tc * TILE); });
     const Place<TILE> at(tr, tc);
     float base[N], col_sum[N] = {};
     int id[N];
@@ -605,15 +642,20 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_g(Contras
     for (int pair = 0; pair < N / 2; ++pair) {       // 8 rows at a time
         half_t o[PLANES][N][8];
         const int row0 = at.row + pair * 8;
-        float row_sum[8] = {};
+        float row_sum[8] = {}, logit[4][N];
 #pragma unroll
         for (int r8 = 0; r8 < 8; ++r8) {
-            const int2 out = side.row_id[at.in_row + pair * 8 + r8];
+            if (r8 % 4 == 0) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int n = 0; n < N; ++n) logit[r][n] = fmaf(acc[pair * 2 + r8 / 4][n][r], c.c1, base[n]);
+                leave_out(side, at.in_row + pair * 8 + r8, id, logit);
+            }
             const float2 info = side.row_g[at.in_row + pair * 8 + r8];
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                const float s = id[n] == out.x || id[n] == out.y ? -INFINITY : fmaf(acc[pair * 2 + r8 / 4][n][r8 % 4], c.c1, base[n]);
-                const float g = __builtin_amdgcn_exp2f(s - info.x) * info.y;
+                const float g = __builtin_amdgcn_exp2f(logit[r8 % 4][n] - info.x) * info.y;
                 half_t x[PLANES];
                 to_planes<DT>(g, x);
                 float rounded = 0.0f;
@@ -687,7 +729,7 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_grad(Cont
     const int k0 = (int)((long long)steps * split / splits) * CT_K, k1 = (int)((long long)steps * (split + 1) / splits) * CT_K;
     const Operand a = keys ? Operand{c.gt, c.plane_gt, c.ld_gt} : Operand{c.g, c.plane_g, c.ld_g};
     const Operand b = keys ? Operand{c.qt, c.plane_qt, c.Bp} : Operand{c.kt, c.plane_kt, c.Mp};
-    product<TILE, DT>(a, b, tr * TILE, tc * TILE, k0, k1, lds, acc);
+    product<TILE, DT>(a, b, tr * TILE, tc * TILE, k0, k1, lds, acc, []() {});
     const Place<TILE> at(tr, tc);
     const size_t rows = (size_t)((keys ? c.M : c.B) + CT_PAD - 1) / CT_PAD * CT_PAD;
     float *out = (keys ? c.acc_k : c.acc_q) + (size_t)split * rows * c.dr;
