@@ -199,44 +199,62 @@ template <int DT> __device__ __forceinline__ void to_planes(float x, half_t (&o)
         }
 }
 
-// Copies of the rows that the products read: padded with zeros, in planes, by rows and by columns; rows that do not count
-// and keys that are left out as zeros, whatever they hold.  One block per 64 x 64.
-template <int DT>
+// Copies of the rows that the products read: padded with zeros, in planes, by rows and by columns; rows that do not count and
+// keys that are left out as zeros, whatever they hold.  One block per 64 x 64: a thread reads 16 coordinates of a row, and writes 16
+// of a row and, through LDS, 16 of a column.
+template <int DT, bool WIDE>
 __global__ __launch_bounds__(256) void k_contrast_copy(ContrastPar c, u32 q_tiles, int columns)
 {
     constexpr int PLANES = planes_of<DT>();
-    __shared__ half_t tile[64][66];
+    __shared__ u32 tile[64][33];        // [column][two rows]
     const bool keys = blockIdx.x >= q_tiles;
     const int r0 = (int)(keys ? blockIdx.x - q_tiles : blockIdx.x) * 64, c0 = blockIdx.y * 64;
-    const int rows = keys ? c.M : c.B;
-    const typename RowType<DT>::T *x = (const typename RowType<DT>::T *)(keys ? c.K : c.Q);
+    const void *rows = keys ? c.K : c.Q;
     half_t *by_row = keys ? c.k : c.q, *by_col = keys ? c.kt : c.qt;
     const size_t plane_r = keys ? c.plane_k : c.plane_q, plane_c = keys ? c.plane_kt : c.plane_qt;
     const int across = keys ? c.Mp : c.Bp;
-    const int col = threadIdx.x & 63;
-    half_t o[16][PLANES];
+    const int x = threadIdx.x >> 2, y = (threadIdx.x & 3) * 16;
+    float v[16] = {};
+    if (keys ? c.key_id[r0 + x] >= 0 : c.row_id[r0 + x].x != CT_NEVER)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+            if (c0 + y + i < c.d) {
+                float four[4];
+                load4<DT, WIDE>(rows, r0 + x, c.d, c0 + y + i, four);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[i + k] = four[k];
+            }
+    half_t o[PLANES][16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        const int r = r0 + (threadIdx.x >> 6) + 4 * i;
-        float v = 0.0f;
-        if (r < rows && c0 + col < c.d && (keys ? !key_gone(c, r) : row_counts(c, r))) v = (float)x[(size_t)r * c.d + c0 + col];
-        to_planes<DT>(v, o[i]);
+        half_t one[PLANES];
+        to_planes<DT>(v[i], one);
+#pragma unroll
+        for (int p = 0; p < PLANES; ++p) o[p][i] = one[p];
+    }
+    if (c0 < c.dp)
 #pragma unroll
         for (int p = 0; p < PLANES; ++p)
-            if (c0 < c.dp) by_row[p * plane_r + (size_t)r * c.dp + c0 + col] = o[i][p];
-    }
+#pragma unroll
+            for (int h = 0; h < 16; h += 8) {
+                us8 l;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) l[i] = o[p][h + i];
+                *(us8 *)&by_row[p * plane_r + (size_t)(r0 + x) * c.dp + c0 + y + h] = l;
+            }
     if (!columns || r0 >= across) return;       // a whole block
 #pragma unroll
     for (int p = 0; p < PLANES; ++p) {
-        __syncthreads();
+        if (p) __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) tile[(threadIdx.x >> 6) + 4 * i][col] = o[i][p];
+        for (int i = 0; i < 16; ++i) ((half_t *)tile[y + i])[x] = o[p][i];
         __syncthreads();
+        u32 l[8];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int cc = (threadIdx.x >> 6) + 4 * i;
-            by_col[p * plane_c + (size_t)(c0 + cc) * across + r0 + col] = tile[col][cc];
-        }
+        for (int i = 0; i < 8; ++i) l[i] = tile[x][y / 2 + i];
+        uint4 *to = (uint4 *)&by_col[p * plane_c + (size_t)(c0 + x) * across + r0 + y];
+        to[0] = make_uint4(l[0], l[1], l[2], l[3]);
+        to[1] = make_uint4(l[4], l[5], l[6], l[7]);
     }
 }
 
@@ -979,7 +997,7 @@ static void launch_contrast(ContrastPar &c, const ContrastPlan &plan, int want_g
     const int key_blocks = Mr / 4 < 1024 ? Mr / 4 : 1024, row_blocks = Br / 4 < 1024 ? Br / 4 : 1024;
     hipLaunchKernelGGL((k_contrast_rows<DT, WIDE>), dim3(key_blocks + row_blocks), dim3(256), 0, st, c, key_blocks);
     // (by columns the padding of d up to a whole tile is written too: the products read it)
-    hipLaunchKernelGGL(k_contrast_copy<DT>, dim3((Br + Mr) / 64, (want_grad ? c.dr : c.dp) / 64), dim3(256), 0, st, c, Br / 64, want_grad);
+    hipLaunchKernelGGL((k_contrast_copy<DT, WIDE>), dim3((Br + Mr) / 64, (want_grad ? c.dr : c.dp) / 64), dim3(256), 0, st, c, Br / 64, want_grad);
     if constexpr (DT != DT_F32) {
         if (plan.tile == 256) launch_products<DT, 256>(c, want_grad, st);
         else launch_products<DT, 128>(c, want_grad, st);
