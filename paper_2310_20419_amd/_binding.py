@@ -540,6 +540,9 @@ def rnnd_contrast(Q, K, target, scale: float, query_ids=None, key_ids=None, key_
     return loss, dQ, dK
 
 
+_ADAMW_KEYS = {"param", "grad", "m", "v", "m_scale", "v_scale", "copy", "counter"}
+
+
 class AdamwTensors:
     """The tensors of an AdamW step, described once.  Each is a dict of 1-D views or whole contiguous tensors:
     param (float32), grad, m, v (float32, or one byte an element for 8-bit states with m_scale and v_scale, one
@@ -551,31 +554,36 @@ class AdamwTensors:
         self.kept = [dict(t) for t in tensors]         # the descriptors hold addresses
         self.array = (AdamwTensor * max(1, len(self.kept)))()
         self.device, at = None, 0
+        names = ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")
         for i, t in enumerate(self.kept):
-            unknown = set(t) - {"param", "grad", "m", "v", "m_scale", "v_scale", "copy", "counter"}
-            _need(not unknown, "tensor %d: unknown %s" % (i, sorted(unknown)))
-            p, g, m, v = (t[k] for k in ("param", "grad", "m", "v"))
-            n = p.numel()
-            self.device = self.device or p.device
-            eight = m.element_size() == 1
-            scales = [t.get("m_scale"), t.get("v_scale")]
-            _need(p.dtype == torch.float32, "tensor %d: param must be float32" % i)
-            _need(v.dtype == m.dtype and (eight or m.dtype == torch.float32), "tensor %d: m and v must both be float32 or both bytes" % i)
-            _need(eight == all(s is not None for s in scales) and eight == any(s is not None for s in scales),
-                  "tensor %d: 8-bit states need m_scale and v_scale, 32-bit states have none" % i)
-            for name, x, size, count in [("grad", g, None, n), ("m", m, None, n), ("v", v, None, n), ("copy", t.get("copy"), 2, n),
-                                         ("m_scale", scales[0], 1, -(-n // 128)), ("v_scale", scales[1], 1, -(-n // 128)), ("param", p, 4, n)]:
+            if not t.keys() <= _ADAMW_KEYS:
+                raise ValueError("tensor %d: unknown %s" % (i, sorted(t.keys() - _ADAMW_KEYS)))
+            p, g, m, v = given = [t[k] for k in names[:4]]
+            ms, vs, copy = rest = [t.get(k) for k in names[4:]]
+            n, eight = p.numel(), m.element_size() == 1
+            if self.device is None:
+                self.device = p.device
+            for name, x in zip(names, given + rest):
                 if x is None:
                     continue
-                _need(x.is_cuda and x.device == self.device and x.is_contiguous() and x.numel() == count and size in (None, x.element_size()),
-                      "tensor %d: %s must be %d contiguous elements on one device" % (i, name, count))
+                count = n if name in ("param", "grad", "m", "v", "copy") else -(-n // 128)
+                if not (x.is_cuda and x.device == self.device and x.is_contiguous() and x.numel() == count):
+                    raise ValueError("tensor %d: %s must be %d contiguous elements on one device" % (i, name, count))
+            if p.dtype != torch.float32:
+                raise ValueError("tensor %d: param must be float32" % i)
+            if v.dtype != m.dtype or not (eight or m.dtype == torch.float32):
+                raise ValueError("tensor %d: m and v must both be float32 or both bytes" % i)
+            if (ms is None) == eight or (vs is None) == eight or (eight and ms.element_size() + vs.element_size() != 2):
+                raise ValueError("tensor %d: 8-bit states need m_scale and v_scale of bytes, 32-bit states have none" % i)
             a = self.array[i]
             a.param, a.grad, a.m, a.v, a.n = p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), n
-            a.m_scale, a.v_scale = (s.data_ptr() if s is not None else None for s in scales)
+            if eight:
+                a.m_scale, a.v_scale = ms.data_ptr(), vs.data_ptr()
             a.grad_dtype, a.state_bits = _row_type(g.dtype, "grad"), 8 if eight else 32
-            if t.get("copy") is not None:
-                a.copy, a.copy_dtype = t["copy"].data_ptr(), _row_type(t["copy"].dtype, "copy")
-                _need(a.copy_dtype != RNND_F32, "tensor %d: copy must be float16 or bfloat16" % i)
+            if copy is not None:
+                a.copy, a.copy_dtype = copy.data_ptr(), _row_type(copy.dtype, "copy")
+                if a.copy_dtype == RNND_F32:
+                    raise ValueError("tensor %d: copy must be float16 or bfloat16" % i)
             a.counter = t.get("counter", at)
             at += -(-n // 128) * 128
 

@@ -13,32 +13,38 @@
 // (16 bits of a counter generator: the same call gives the same bits), and a root above zero never becomes zero, since
 // p moves by m / root.
 #include <cmath>
+#include <type_traits>
 
 #include "rows.h"
 
-#define ADAMW_TENSORS 48        // tensors a launch takes: their descriptors travel as its argument (a little under 4 KB)
+#define ADAMW_ARGUMENT 4000     // bytes of descriptors that travel as an argument of a launch: 80 bytes (50 tensors) with 8-bit
+                                // states, 56 bytes (71 tensors) with 32-bit states
 #define ADAMW_BLOCK 128         // elements that share a scale
 #define ADAMW_TILE 2048         // elements of one workgroup
 
-struct AdamwTensor {
+struct AdamwScales { unsigned char *m, *v; u64 counter; };
+struct AdamwNoScales {};
+template <bool EIGHT> struct AdamwTensor : std::conditional<EIGHT, AdamwScales, AdamwNoScales>::type {
     float *param;
     const void *grad;
-    void *m, *v;
-    unsigned char *m_scale, *v_scale;
-    void *copy;
-    u64 n, counter;
+    void *m_data, *v_data, *copy;
+    u64 n_types;                // n, and above it grad_type, copy_type (4 bits each) and wide: every array takes aligned accesses of 8
     u32 first_tile;             // in this launch
-    unsigned char grad_type, copy_type, wide;       // wide: every array takes aligned accesses of 8 elements
+    __device__ __forceinline__ u64 n() const { return n_types & ((1ull << 48) - 1); }
+    __device__ __forceinline__ int grad_type() const { return (int)(n_types >> 48) & 15; }
+    __device__ __forceinline__ int copy_type() const { return (int)(n_types >> 52) & 15; }
+    __device__ __forceinline__ bool wide() const { return n_types >> 56; }
 };
-struct AdamwPar {
-    AdamwTensor t[ADAMW_TENSORS];
+template <bool EIGHT> struct AdamwPar {
+    static constexpr int TENSORS = ADAMW_ARGUMENT / (int)sizeof(AdamwTensor<EIGHT>);
+    AdamwTensor<EIGHT> t[TENSORS];
     u64 key;                    // of the step's random bits
     u32 count;
     float grad_scale, beta1, beta2, rest1, rest2, keep, rate, root_scale, eps;
 };
-static_assert(sizeof(AdamwPar) <= 4096, "kernel arguments");
+static_assert(sizeof(AdamwPar<true>) <= 4096 && sizeof(AdamwPar<false>) <= 4096, "kernel arguments");
 
-__device__ __forceinline__ void adamw_update(const AdamwPar &a, float g, float &p, float &m, float &v)
+template <bool EIGHT> __device__ __forceinline__ void adamw_update(const AdamwPar<EIGHT> &a, float g, float &p, float &m, float &v)
 {
     g *= a.grad_scale;
     m = fmaf(a.beta1, m, a.rest1 * g);
@@ -143,7 +149,7 @@ __device__ __forceinline__ void store_codes(void *base, u64 at, u32 have, bool w
 
 // A thread takes 8 neighbouring elements (16 lanes a block of 128); have = how many of them there are.
 template <bool EIGHT>
-__global__ __launch_bounds__(256) void k_adamw(AdamwPar a)
+__global__ __launch_bounds__(256) void k_adamw(AdamwPar<EIGHT> a)
 {
     u32 lo = 0, hi = a.count - 1;       // the tensor whose tiles hold this block's
     while (lo < hi) {
@@ -151,75 +157,76 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwPar a)
         if (a.t[mid].first_tile <= blockIdx.x) lo = mid;
         else hi = mid - 1;
     }
-    const AdamwTensor &t = a.t[lo];
+    const AdamwTensor<EIGHT> &t = a.t[lo];
     const u64 at = (u64)(blockIdx.x - t.first_tile) * ADAMW_TILE + threadIdx.x * 8;
-    const u32 have = at >= t.n ? 0 : t.n - at < 8 ? (u32)(t.n - at) : 8;
-    const bool wide = t.wide && have == 8;
+    const u32 have = at >= t.n() ? 0 : t.n() - at < 8 ? (u32)(t.n() - at) : 8;
+    const bool wide = t.wide() && have == 8;
     float p[8], g[8], m[8], v[8];
     if (have) {
         load8<DT_F32>(t.param, at, have, wide, p);
-        if (t.grad_type == DT_F32) load8<DT_F32>(t.grad, at, have, wide, g);
-        else if (t.grad_type == DT_F16) load8<DT_F16>(t.grad, at, have, wide, g);
+        if (t.grad_type() == DT_F32) load8<DT_F32>(t.grad, at, have, wide, g);
+        else if (t.grad_type() == DT_F16) load8<DT_F16>(t.grad, at, have, wide, g);
         else load8<DT_BF16>(t.grad, at, have, wide, g);
-        if (EIGHT) {
-            const u64 cm = load_codes(t.m, at, have, wide), cv = load_codes(t.v, at, have, wide);
-            decode8(cm, scale_of(t.m_scale[at / ADAMW_BLOCK]), m);
-            decode8(cv, scale_of(t.v_scale[at / ADAMW_BLOCK]), v);
+        if constexpr (EIGHT) {
+            const u64 cm = load_codes(t.m_data, at, have, wide), cv = load_codes(t.v_data, at, have, wide);
+            decode8(cm, scale_of(t.AdamwScales::m[at / ADAMW_BLOCK]), m);
+            decode8(cv, scale_of(t.AdamwScales::v[at / ADAMW_BLOCK]), v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] *= v[i];
         } else {
-            load8<DT_F32>(t.m, at, have, wide, m);
-            load8<DT_F32>(t.v, at, have, wide, v);
+            load8<DT_F32>(t.m_data, at, have, wide, m);
+            load8<DT_F32>(t.v_data, at, have, wide, v);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) adamw_update(a, g[i], p[i], m[i], v[i]);
         store8<DT_F32>(t.param, at, have, wide, p);
         if (t.copy) {
-            if (t.copy_type == DT_F16) store8<DT_F16>(t.copy, at, have, wide, p);
+            if (t.copy_type() == DT_F16) store8<DT_F16>(t.copy, at, have, wide, p);
             else store8<DT_BF16>(t.copy, at, have, wide, p);
         }
         if (!EIGHT) {
-            store8<DT_F32>(t.m, at, have, wide, m);
-            store8<DT_F32>(t.v, at, have, wide, v);
+            store8<DT_F32>(t.m_data, at, have, wide, m);
+            store8<DT_F32>(t.v_data, at, have, wide, v);
         }
     }
-    if (!EIGHT) return;
-    u32 top_m = 0, top_v = 0;
+    if constexpr (EIGHT) {
+        u32 top_m = 0, top_v = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (i >= (int)have) m[i] = v[i] = 0.0f;
-        v[i] = sqrtf(v[i]);
-        const u32 bm = __float_as_uint(m[i]) & 0x7FFFFFFFu, bv = __float_as_uint(v[i]) & 0x7FFFFFFFu;
-        top_m = bm > top_m ? bm : top_m;
-        top_v = bv > top_v ? bv : top_v;
-    }
-    const u32 sm = scale_byte(lane16_max(top_m)), sv = scale_byte(lane16_max(top_v));
-    if (!have) return;
-    // 2^(127 - byte) in two factors (byte 254: 2^-127 is below the smallest normal number)
-    const int em = 127 - (sm == 255 ? 127 : (int)sm), ev = 127 - (sv == 255 ? 127 : (int)sv);
-    const float um_a = __uint_as_float((em / 2 + 127) << 23), um_b = __uint_as_float((em - em / 2 + 127) << 23);
-    const float uv_a = __uint_as_float((ev / 2 + 127) << 23), uv_b = __uint_as_float((ev - ev / 2 + 127) << 23);
-    u64 cm = 0, cv = 0;
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-        const u64 r = row_mix64(a.key + ROW_MIX_G * ((t.counter + at + i) / 2 + 1));
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const u32 half = (u32)(r >> (32 * h));
-            const u32 code_m = encode(m[i + h], um_a, um_b, half & 0xFFFFu) | (__float_as_uint(m[i + h]) >> 31 << 7);
-            u32 code_v = encode(v[i + h], uv_a, uv_b, half >> 16);
-            if (v[i + h] > 0.0f && code_v == 0) code_v = 1;
-            cm |= (u64)(code_m & 255u) << (8 * (i + h));
-            cv |= (u64)(code_v & 255u) << (8 * (i + h));
+        for (int i = 0; i < 8; ++i) {
+            if (i >= (int)have) m[i] = v[i] = 0.0f;
+            v[i] = sqrtf(v[i]);
+            const u32 bm = __float_as_uint(m[i]) & 0x7FFFFFFFu, bv = __float_as_uint(v[i]) & 0x7FFFFFFFu;
+            top_m = bm > top_m ? bm : top_m;
+            top_v = bv > top_v ? bv : top_v;
         }
-    }
-    if (sm == 255) cm = 0;      // the scale says that the block's values are lost
-    if (sv == 255) cv = 0;
-    store_codes(t.m, at, have, wide, cm);
-    store_codes(t.v, at, have, wide, cv);
-    if ((threadIdx.x & 15) == 0) {
-        t.m_scale[at / ADAMW_BLOCK] = (unsigned char)sm;
-        t.v_scale[at / ADAMW_BLOCK] = (unsigned char)sv;
+        const u32 sm = scale_byte(lane16_max(top_m)), sv = scale_byte(lane16_max(top_v));
+        if (!have) return;
+        // 2^(127 - byte) in two factors (byte 254: 2^-127 is below the smallest normal number)
+        const int em = 127 - (sm == 255 ? 127 : (int)sm), ev = 127 - (sv == 255 ? 127 : (int)sv);
+        const float um_a = __uint_as_float((em / 2 + 127) << 23), um_b = __uint_as_float((em - em / 2 + 127) << 23);
+        const float uv_a = __uint_as_float((ev / 2 + 127) << 23), uv_b = __uint_as_float((ev - ev / 2 + 127) << 23);
+        u64 cm = 0, cv = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            const u64 r = row_mix64(a.key + ROW_MIX_G * ((t.counter + at + i) / 2 + 1));
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const u32 half = (u32)(r >> (32 * h));
+                const u32 code_m = encode(m[i + h], um_a, um_b, half & 0xFFFFu) | (__float_as_uint(m[i + h]) >> 31 << 7);
+                u32 code_v = encode(v[i + h], uv_a, uv_b, half >> 16);
+                if (v[i + h] > 0.0f && code_v == 0) code_v = 1;
+                cm |= (u64)(code_m & 255u) << (8 * (i + h));
+                cv |= (u64)(code_v & 255u) << (8 * (i + h));
+            }
+        }
+        if (sm == 255) cm = 0;      // the scale says that the block's values are lost
+        if (sv == 255) cv = 0;
+        store_codes(t.m_data, at, have, wide, cm);
+        store_codes(t.v_data, at, have, wide, cv);
+        if ((threadIdx.x & 15) == 0) {
+            t.AdamwScales::m[at / ADAMW_BLOCK] = (unsigned char)sm;
+            t.AdamwScales::v[at / ADAMW_BLOCK] = (unsigned char)sv;
+        }
     }
 }
 
@@ -238,6 +245,54 @@ static int adamw_check(const rnnd_adamw_tensor &t)
     return RNND_OK;
 }
 
+struct AdamwStep {
+    u64 key;
+    float grad_scale, beta1, beta2, rest1, rest2, keep, rate, root_scale, eps;
+};
+
+template <bool EIGHT>
+static void launch_adamw(const rnnd_adamw_tensor *tensors, int32_t count, const AdamwStep &s, hipStream_t st)
+{
+    AdamwPar<EIGHT> a;
+    a.key = s.key;
+    a.grad_scale = s.grad_scale;
+    a.beta1 = s.beta1;
+    a.beta2 = s.beta2;
+    a.rest1 = s.rest1;
+    a.rest2 = s.rest2;
+    a.keep = s.keep;
+    a.rate = s.rate;
+    a.root_scale = s.root_scale;
+    a.eps = s.eps;
+    for (int32_t i = 0; i < count;) {
+        u64 tiles = 0;
+        a.count = 0;
+        for (; i < count && a.count < (u32)a.TENSORS; ++i) {
+            const rnnd_adamw_tensor &t = tensors[i];
+            if (t.state_bits != (EIGHT ? 8 : 32) || !t.n) continue;
+            const u64 more = ((u64)t.n + ADAMW_TILE - 1) / ADAMW_TILE;
+            if (tiles + more > 0x7FFFFFFFull) break;
+            AdamwTensor<EIGHT> &d = a.t[a.count++];
+            d.param = t.param;
+            d.grad = t.grad;
+            d.m_data = t.m;
+            d.v_data = t.v;
+            d.copy = t.copy;
+            if constexpr (EIGHT) {
+                d.m = t.m_scale;
+                d.v = t.v_scale;
+                d.counter = t.counter;
+            }
+            uintptr_t low = (uintptr_t)t.param | (uintptr_t)t.grad | (uintptr_t)t.copy;     // 16 bytes an access
+            low |= EIGHT ? ((uintptr_t)t.m | (uintptr_t)t.v) << 1 : (uintptr_t)t.m | (uintptr_t)t.v;    // codes: 8
+            d.n_types = (u64)t.n | (u64)t.grad_dtype << 48 | (u64)(t.copy ? t.copy_dtype : 0) << 52 | (u64)(low % 16 == 0) << 56;
+            d.first_tile = (u32)tiles;
+            tiles += more;
+        }
+        if (a.count) hipLaunchKernelGGL(k_adamw<EIGHT>, dim3((u32)tiles), dim3(256), 0, st, a);
+    }
+}
+
 extern "C" int rnnd_adamw(const rnnd_adamw_tensor *tensors, int32_t count, int64_t step, double lr, double beta1, double beta2,
                           double eps, double weight_decay, double grad_scale, uint64_t seed, void *stream)
 {
@@ -247,56 +302,25 @@ extern "C" int rnnd_adamw(const rnnd_adamw_tensor *tensors, int32_t count, int64
     if (step < 1 || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0) || !std::isfinite(eps) ||
         !std::isfinite(lr) || !std::isfinite(weight_decay) || !std::isfinite(grad_scale))
         return RNND_ERR_BAD_PARAM;
-    bool any = false;
+    bool any[2] = {false, false};       // tensors with 32-bit, with 8-bit states
     for (int32_t i = 0; i < count; ++i) {
         const int rc = adamw_check(tensors[i]);
         if (rc) return rc;
-        any = any || tensors[i].n;
+        if (tensors[i].n) any[tensors[i].state_bits == 8] = true;
     }
-    if (!any) return RNND_OK;
-    AdamwPar a;
-    a.key = row_mix64(seed + ROW_MIX_G * ((u64)step + 1));
-    a.grad_scale = (float)grad_scale;
-    a.beta1 = (float)beta1;
-    a.beta2 = (float)beta2;
-    a.rest1 = (float)(1.0 - beta1);
-    a.rest2 = (float)(1.0 - beta2);
-    a.keep = (float)(1.0 - lr * weight_decay);
-    a.rate = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
-    a.root_scale = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
-    a.eps = (float)eps;
-    for (int bits = 8; bits <= 32; bits += 24) {
-        int32_t i = 0;
-        while (i < count) {
-            u64 tiles = 0;
-            a.count = 0;
-            for (; i < count && a.count < ADAMW_TENSORS; ++i) {
-                const rnnd_adamw_tensor &t = tensors[i];
-                if (t.state_bits != bits || !t.n) continue;
-                const u64 more = ((u64)t.n + ADAMW_TILE - 1) / ADAMW_TILE;
-                if (tiles + more > 0x7FFFFFFFull) break;
-                AdamwTensor &d = a.t[a.count++];
-                d.param = t.param;
-                d.grad = t.grad;
-                d.m = t.m;
-                d.v = t.v;
-                d.m_scale = t.m_scale;
-                d.v_scale = t.v_scale;
-                d.copy = t.copy;
-                d.n = (u64)t.n;
-                d.counter = t.counter;
-                d.first_tile = (u32)tiles;
-                d.grad_type = (unsigned char)t.grad_dtype;
-                d.copy_type = (unsigned char)t.copy_dtype;
-                uintptr_t low = (uintptr_t)t.param | (uintptr_t)t.grad | (uintptr_t)t.copy;     // 16 bytes an access
-                low |= bits == 32 ? (uintptr_t)t.m | (uintptr_t)t.v : ((uintptr_t)t.m | (uintptr_t)t.v) << 1;   // codes: 8
-                d.wide = low % 16 == 0;
-                tiles += more;
-            }
-            if (!a.count) break;
-            if (bits == 8) hipLaunchKernelGGL(k_adamw<true>, dim3((u32)tiles), dim3(256), 0, (hipStream_t)stream, a);
-            else hipLaunchKernelGGL(k_adamw<false>, dim3((u32)tiles), dim3(256), 0, (hipStream_t)stream, a);
-        }
-    }
+    if (!any[0] && !any[1]) return RNND_OK;
+    AdamwStep s;
+    s.key = row_mix64(seed + ROW_MIX_G * ((u64)step + 1));
+    s.grad_scale = (float)grad_scale;
+    s.beta1 = (float)beta1;
+    s.beta2 = (float)beta2;
+    s.rest1 = (float)(1.0 - beta1);
+    s.rest2 = (float)(1.0 - beta2);
+    s.keep = (float)(1.0 - lr * weight_decay);
+    s.rate = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
+    s.root_scale = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
+    s.eps = (float)eps;
+    if (any[1]) launch_adamw<true>(tensors, count, s, (hipStream_t)stream);
+    if (any[0]) launch_adamw<false>(tensors, count, s, (hipStream_t)stream);
     return launched("rnnd_adamw");
 }
