@@ -653,7 +653,9 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_g(Contras
     }
     constexpr int H = TILE / 2;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    half_t *turn = (half_t *)&lds + wave * H * H;
+    half_t *turn = (half_t *)&lds + wave * H * H * (PLANES == 3 ? 2 : 1);
+    us8 third[PLANES == 3 ? N / 2 : 1][N];
+    auto turn_at = [&](int n, int pair) { return ((lane & 15) * N + n) * H + (((lane >> 4) * (N / 2) + pair) ^ (lane & 7)) * 8; };
     __syncthreads();        // all have read their operands
     float keep_sum[N / 4];
 #pragma unroll
@@ -698,8 +700,8 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_g(Contras
 #pragma unroll
         for (int r8 = 0; r8 < 8; ++r8)
             keep_sum[pair / 2] = (int)(threadIdx.x & 15) == pair % 2 * 8 + r8 ? row_sum[r8] : pair % 2 || r8 ? keep_sum[pair / 2] : 0.0f;
-        // by columns: 8 rows of a column are 16 bytes.  One plane: first into the wavefront's own part of LDS, in which a
-        // column's rows lie together (piece k of column x at k ^ x / N % 8: both sides free of bank conflicts)
+        // by columns: 8 rows of a column are 16 bytes.  First into the wavefront's own part of LDS, in which a column's rows lie
+        // together (piece k of column x at k ^ x / N % 8: both sides free of bank conflicts); a third plane waits for its turn
 #pragma unroll
         for (int p = 0; p < PLANES; ++p)
 #pragma unroll
@@ -707,17 +709,29 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_g(Contras
                 us8 l;
 #pragma unroll
                 for (int r8 = 0; r8 < 8; ++r8) l[r8] = o[p][n][r8];
-                if constexpr (PLANES == 1) *(us8 *)&turn[((lane & 15) * N + n) * H + (((lane >> 4) * (N / 2) + pair) ^ (lane & 7)) * 8] = l;
-                else *(us8 *)&c.gt[p * c.plane_gt + (size_t)(at.col + n) * c.ld_gt + row0] = l;
+                if (p < 2) *(us8 *)&turn[p * H * H + turn_at(n, pair)] = l;
+                else third[pair][n] = l;
             }
     }
-    if constexpr (PLANES == 1) {
-        wave_sync();
-        constexpr int per = H / 8;          // lanes for a column
-        const int piece = lane % per, row0 = tr * TILE + (wave >> 1) * H + piece * 8, col0 = tc * TILE + (wave & 1) * H;
+    constexpr int per = H / 8;          // lanes for a column
+    const int piece = lane % per;
+    half_t *const to = c.gt + (size_t)(tc * TILE + (wave & 1) * H) * c.ld_gt + tr * TILE + (wave >> 1) * H + piece * 8;
+    auto flush = [&](int p, const half_t *from) {
 #pragma unroll 8
         for (int x = lane / per; x < H; x += 64 / per)
-            *(us8 *)&c.gt[(size_t)(col0 + x) * c.ld_gt + row0] = *(const us8 *)&turn[x * H + (piece ^ (x / N & 7)) * 8];
+            *(us8 *)&to[p * c.plane_gt + (size_t)x * c.ld_gt] = *(const us8 *)&from[x * H + (piece ^ (x / N & 7)) * 8];
+    };
+    wave_sync();
+    flush(0, turn);
+    if constexpr (PLANES == 3) {
+        flush(1, turn + H * H);
+        wave_sync();
+#pragma unroll
+        for (int pair = 0; pair < N / 2; ++pair)
+#pragma unroll
+            for (int n = 0; n < N; ++n) *(us8 *)&turn[turn_at(n, pair)] = third[pair][n];
+        wave_sync();
+        flush(2, turn);
     }
 #pragma unroll
     for (int h = 0; h < N / 4; ++h) c.sum_q[(size_t)(at.row + h * 16 + (threadIdx.x & 15)) * c.parts_k + at.half_c] = keep_sum[h];
