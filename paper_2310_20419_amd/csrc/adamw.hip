@@ -44,11 +44,14 @@ template <bool EIGHT> struct AdamwPar {
 };
 static_assert(sizeof(AdamwPar<true>) <= 4096 && sizeof(AdamwPar<false>) <= 4096, "kernel arguments");
 
+// The moments take a rounding for each product and sum, none fused, as a program that writes the formulas out takes them.  What a
+// fused one would save is below 2^-24; but where a moment lies within that of a border, its 8-bit code would be another, and by the next
+// step the parameter, now and then, by several lr.
 template <bool EIGHT> __device__ __forceinline__ void adamw_update(const AdamwPar<EIGHT> &a, float g, float &p, float &m, float &v)
 {
     g *= a.grad_scale;
-    m = fmaf(a.beta1, m, a.rest1 * g);
-    v = fmaf(a.beta2, v, a.rest2 * (g * g));
+    m = a.beta1 * m + a.rest1 * g;
+    v = a.beta2 * v + a.rest2 * g * g;
     p = fmaf(p, a.keep, -a.rate * (m / fmaf(sqrtf(v), a.root_scale, a.eps)));
 }
 

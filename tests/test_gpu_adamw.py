@@ -177,6 +177,45 @@ def test_states_in_8_bits(rn, n, offset, grad_dtype):
         assert (abs(near[wrong]) <= (err / s / gap)[wrong] * 1.01 + 2.0 ** -18).all()
 
 
+@pytest.mark.parametrize("grad_dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("bits", [8, 32])
+def test_moments_are_bit_for_bit_those_of_separate_float32_operations(rn, bits, grad_dtype):
+    """Five steps: every product and sum of the moments rounded on its own, so that 8-bit codes, which a last bit can decide,
+    are the ones that a program of plain float32 operations finds."""
+    import torch
+    n, seed, h = 300_007, 5, dict(HYPER, grad_scale=0.75)
+    f = np.float32
+    if bits == 8:
+        t = eight(rn, n, 9, getattr(torch, grad_dtype))
+    else:
+        t = dict(param=normal(n, 1), grad=normal(n, 2, 0.1).to(getattr(torch, grad_dtype)), m=normal(n, 3, 0.05), v=normal(n, 4, 0.1).square())
+    plan = rn.AdamwTensors([t])
+    for step in range(7, 12):
+        g = t["grad"].float().cpu().numpy() * f(h["grad_scale"])
+        if bits == 8:
+            m, v = decode(t["m"], t["m_scale"]).astype(f), np.square(decode(t["v"], t["v_scale"]).astype(f))
+        else:
+            m, v = t["m"].cpu().numpy(), t["v"].cpu().numpy()
+        rn.rnnd_adamw(plan, step, seed=seed, **h)
+        m = f(h["beta1"]) * m + f(1 - h["beta1"]) * g
+        v = f(h["beta2"]) * v + f(1 - h["beta2"]) * g * g
+        assert m.dtype == f and v.dtype == f
+        if bits == 32:
+            assert np.array_equal(t["m"].cpu().numpy(), m) and np.array_equal(t["v"].cpu().numpy(), v)
+            continue
+        for name, y, random16 in zip(("m", "v"), (m, np.sqrt(v)), random_bits(n, 0, seed, step)):
+            top = np.maximum.reduceat(abs(y), np.arange(0, n, 128)) * f(1.01)
+            byte = np.clip(np.frexp(top)[1] + 126 - 7, 0, 254)      # (no block of zeros here)
+            assert np.array_equal(t[name + "_scale"].cpu().numpy(), byte.astype(np.uint8))
+            s, gap = lattice(abs(y.astype(np.float64)), byte)
+            z = abs(y.astype(np.float64)) / s / gap
+            steps = np.where(z < 8, np.floor((z.astype(f) + (random16 / 65536.0).astype(f)).astype(np.float64)), np.floor(z + random16 / 65536.0))
+            code = steps * gap
+            if name == "v":
+                code = np.where((y > 0) & (code == 0), 2.0 ** -9, code)
+            assert np.array_equal(decode(t[name], t[name + "_scale"]), np.copysign(code * s, y.astype(np.float64)))
+
+
 def test_rounding_of_8_bit_states_has_no_bias(rn):
     """The mean over many steps of what a value is stored as is the value: standard error of N draws of at most a code's distance."""
     import torch
