@@ -36,6 +36,7 @@ typedef unsigned short half_t;      // float16 or bfloat16, as the rows are
 #define CT_PAD 256          // rows are padded to the largest tile
 #define CT_K 64             // summed per step: 128 bytes of a row
 #define CT_NEVER (-2)       // an id that no key has
+#define CT_ROW_BLOCKS 1024  // at most, for the norms and targets of the rows of a side
 
 struct ContrastPar {
     const void *Q, *K;
@@ -47,7 +48,7 @@ struct ContrastPar {
     int ld_g, ld_gt;                // rows of g by rows and by columns: M and B padded to the largest tile
     size_t plane_q, plane_k, plane_qt, plane_kt, plane_g, plane_gt;     // elements
     half_t *q, *k, *qt, *kt, *g, *gt;
-    u32 *top;                       // largest weight, as bits (float16 rows)
+    u32 *tops, *top;                // float16 rows: largest weight of each block of queries, and of all, as bits
     int *first, *count;             // [M] the first query whose target the key is, and how many they are
     float *key_base;                // [M padded] (bias - scale |k|^2) log2(e), -inf where left out
     int *key_id;                    // [M padded]
@@ -65,12 +66,7 @@ struct ContrastPar {
 };
 
 // float16 rows: the power of two that brings weights up to `top` below 2^15
-template <int DT> __device__ __forceinline__ int weight_exponent(const ContrastPar &c)
-{
-    if constexpr (DT != DT_F16) return 0;
-    const u32 top = *c.top;
-    return top >= 0x00800000u ? 14 + 127 - (int)(top >> 23) : 0;
-}
+__device__ __forceinline__ int weight_exponent(u32 top) { return top >= 0x00800000u ? 14 + 127 - (int)(top >> 23) : 0; }
 
 // ------------------------------------------------------------------------------------------------ preparation
 __device__ __forceinline__ bool key_gone(const ContrastPar &c, int j)
@@ -81,16 +77,6 @@ __device__ __forceinline__ bool row_counts(const ContrastPar &c, int i)
 {
     const int t = c.target[i];
     return (u32)t < (u32)c.M && !key_gone(c, t);
-}
-
-__global__ __launch_bounds__(256) void k_contrast_clear(ContrastPar c)
-{
-    const int j = blockIdx.x * 256 + threadIdx.x;
-    if (j == 0) *c.top = 0;
-    if (j < c.M) {
-        c.first[j] = 0x7FFFFFFF;
-        c.count[j] = 0;
-    }
 }
 
 __device__ __forceinline__ float wave_sum(float v)
@@ -112,14 +98,16 @@ __device__ __forceinline__ void load4(const void *rows, size_t row, int d, int e
 
 // A wavefront per row: keys first, then queries.  A key's own part of its logits, a query's logit of its target.
 template <int DT, bool WIDE>
-__global__ __launch_bounds__(256) void k_contrast_rows(ContrastPar c, int key_blocks)
+__device__ __forceinline__ void contrast_rows(const ContrastPar &c, int key_blocks, int row_blocks)
 {
     __shared__ u32 most;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const bool keys = (int)blockIdx.x < key_blocks;
-    if (threadIdx.x == 0) most = 0;
-    __syncthreads();
-    const int blocks = keys ? key_blocks : gridDim.x - key_blocks;
+    if (DT == DT_F16 && !keys) {        // (a whole block)
+        if (threadIdx.x == 0) most = 0;
+        __syncthreads();
+    }
+    const int blocks = keys ? key_blocks : row_blocks;
     const int padded = ((keys ? c.M : c.B) + CT_PAD - 1) / CT_PAD * CT_PAD;
     for (int at = ((int)blockIdx.x - (keys ? 0 : key_blocks)) * 4 + wave; at < padded; at += blocks * 4) {
         if (keys) {
@@ -136,6 +124,10 @@ __global__ __launch_bounds__(256) void k_contrast_rows(ContrastPar c, int key_bl
             if (lane == 0) {
                 c.key_base[at] = gone ? -INFINITY : ((c.bias ? c.bias[at] : 0.0f) - c.scale * sum) * 1.44269504f;
                 c.key_id[at] = gone ? -1 : c.key_ids ? c.key_ids[at] : at;
+                if (at < c.M) {
+                    c.first[at] = 0x7FFFFFFF;
+                    c.count[at] = 0;
+                }
             }
         } else {
             const bool on = at < c.B && row_counts(c, at);
@@ -164,17 +156,15 @@ __global__ __launch_bounds__(256) void k_contrast_rows(ContrastPar c, int key_bl
                     c.row_own[at] = w;
                     c.own_logit[at] = fmaf(dot, c.c1, ((on && c.bias ? c.bias[t] : 0.0f) - c.scale * norm) * 1.44269504f);
                 }
-                if (on) {
-                    const u32 bits = __float_as_uint(w) & 0x7FFFFFFFu;
-                    if (DT == DT_F16 && bits < 0x7F800000u) atomicMax(&most, bits);
-                    atomicMin(&c.first[t], at);
-                    atomicAdd(&c.count[t], 1);
-                }
+                const u32 bits = __float_as_uint(w) & 0x7FFFFFFFu;
+                if (DT == DT_F16 && bits < 0x7F800000u) atomicMax(&most, bits);
             }
         }
     }
-    __syncthreads();
-    if (DT == DT_F16 && threadIdx.x == 0 && most) atomicMax(c.top, most);
+    if (DT == DT_F16 && !keys) {
+        __syncthreads();
+        if (threadIdx.x == 0) c.tops[(int)blockIdx.x - key_blocks] = most;
+    }
 }
 
 __device__ __forceinline__ half_t bits16(__bf16 x) { return __builtin_bit_cast(half_t, x); }
@@ -203,19 +193,19 @@ template <int DT> __device__ __forceinline__ void to_planes(float x, half_t (&o)
 // keys that are left out as zeros, whatever they hold.  One block per 64 x 64: a thread reads 16 coordinates of a row, and writes 16
 // of a row and, through LDS, 16 of a column.
 template <int DT, bool WIDE>
-__global__ __launch_bounds__(256) void k_contrast_copy(ContrastPar c, u32 q_tiles, int columns)
+__device__ __forceinline__ void contrast_copy(const ContrastPar &c, int tile_r, int c0, int q_tiles, int columns)
 {
     constexpr int PLANES = planes_of<DT>();
     __shared__ u32 tile[64][33];        // [column][two rows]
-    const bool keys = blockIdx.x >= q_tiles;
-    const int r0 = (int)(keys ? blockIdx.x - q_tiles : blockIdx.x) * 64, c0 = blockIdx.y * 64;
+    const bool keys = tile_r >= q_tiles;
+    const int r0 = (keys ? tile_r - q_tiles : tile_r) * 64;
     const void *rows = keys ? c.K : c.Q;
     half_t *by_row = keys ? c.k : c.q, *by_col = keys ? c.kt : c.qt;
     const size_t plane_r = keys ? c.plane_k : c.plane_q, plane_c = keys ? c.plane_kt : c.plane_qt;
     const int across = keys ? c.Mp : c.Bp;
     const int x = threadIdx.x >> 2, y = (threadIdx.x & 3) * 16;
     float v[16] = {};
-    if (keys ? c.key_id[r0 + x] >= 0 : c.row_id[r0 + x].x != CT_NEVER)
+    if (keys ? r0 + x < c.M && !key_gone(c, r0 + x) : r0 + x < c.B && row_counts(c, r0 + x))
 #pragma unroll
         for (int i = 0; i < 16; i += 4)
             if (c0 + y + i < c.d) {
@@ -256,6 +246,15 @@ __global__ __launch_bounds__(256) void k_contrast_copy(ContrastPar c, u32 q_tile
         to[0] = make_uint4(l[0], l[1], l[2], l[3]);
         to[1] = make_uint4(l[4], l[5], l[6], l[7]);
     }
+}
+
+// Both in one launch (neither reads what the other writes): small calls are bound by the number of dependent launches.
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(256) void k_contrast_prepare(ContrastPar c, int key_blocks, int row_blocks, int q_tiles, int across, int columns)
+{
+    const int id = (int)blockIdx.x - key_blocks - row_blocks;
+    if (id < 0) contrast_rows<DT, WIDE>(c, key_blocks, row_blocks);
+    else contrast_copy<DT, WIDE>(c, id / across, id % across * 64, q_tiles, columns);
 }
 
 // ------------------------------------------------------------------------------------------------ the product
@@ -601,9 +600,21 @@ __device__ __forceinline__ void join_parts(float &top, float &sum, float ot, flo
 
 // A wavefront per query joins its parts: the loss, and what the second product needs.
 template <int DT>
-__global__ __launch_bounds__(256) void k_contrast_loss(ContrastPar c)
+__global__ __launch_bounds__(256) void k_contrast_loss(ContrastPar c, int row_blocks)
 {
     const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    int up = 0;
+    if constexpr (DT == DT_F16) {
+        __shared__ u32 most;
+        if (threadIdx.x == 0) most = 0;
+        __syncthreads();
+        u32 top = 0;
+        for (int b = threadIdx.x; b < row_blocks; b += 256) top = c.tops[b] > top ? c.tops[b] : top;
+        atomicMax(&most, top);
+        __syncthreads();
+        up = weight_exponent(most);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *c.top = most;
+    }
     if (i >= c.B) return;
     float top = -INFINITY, sum = 0.0f;
     for (int t = lane; t < c.parts_k; t += 64) {
@@ -628,7 +639,10 @@ __global__ __launch_bounds__(256) void k_contrast_loss(ContrastPar c)
     c.loss[i] = loss;
     const float w = c.row_own[i];
     c.row_own[i] = w * expm1f(-loss);
-    c.row_g[i] = make_float2(own + loss * 1.44269504f, ldexpf(w, weight_exponent<DT>(c)));
+    c.row_g[i] = make_float2(own + loss * 1.44269504f, ldexpf(w, up));
+    const int t = c.target[i];
+    atomicMin(&c.first[t], i);
+    atomicAdd(&c.count[t], 1);
 }
 
 // ------------------------------------------------------------------------------------------------ second product: g
@@ -808,7 +822,7 @@ __global__ __launch_bounds__(256) void k_contrast_finish(ContrastPar c)
     const size_t plane = (size_t)((rows + CT_PAD - 1) / CT_PAD * CT_PAD) * c.dr;
     const float *acc = (keys ? c.acc_k : c.acc_q) + (size_t)row * c.dr;
     const int splits = keys ? c.splits_k : c.splits_q;
-    const int down = -weight_exponent<DT>(c);       // of g
+    const int down = DT == DT_F16 ? -weight_exponent(*c.top) : 0;       // of g
     const int found = keys ? c.count[row] : 1, first = keys ? found ? c.first[row] : 0 : c.target[row];
     const float f = 2.0f * c.scale;
     for (int e0 = 0; e0 < c.d; e0 += 256) {        // all lanes stay: the search below needs them
@@ -935,6 +949,7 @@ static size_t contrast_layout(ContrastPar &c, ContrastPlan &plan, int dtype, int
         p = (typename std::remove_reference<decltype(p)>::type)(base + off);
         off += ws_align(count * sizeof(*p));
     };
+    take(c.tops, CT_ROW_BLOCKS);
     take(c.top, 1);
     take(c.first, c.M);
     take(c.count, c.M);
@@ -988,12 +1003,12 @@ extern "C" int rnnd_contrast_workspace(int64_t B, int64_t M, int32_t d, int dtyp
 }
 
 template <int DT, int TILE>
-static void launch_products(ContrastPar &c, int want_grad, hipStream_t st)
+static void launch_products(ContrastPar &c, int want_grad, int row_blocks, hipStream_t st)
 {
     static_assert(DT != DT_F32 || TILE == 128, "g of three planes takes more registers than tiles of 256 leave");
     const int tq = ct_up(c.B, TILE) / TILE, tk = ct_up(c.M, TILE) / TILE;
     hipLaunchKernelGGL((k_contrast_sums<TILE, DT>), dim3((u32)tq * tk), dim3(256), 0, st, c, tq, tk);
-    hipLaunchKernelGGL(k_contrast_loss<DT>, dim3((c.B + 3) / 4), dim3(256), 0, st, c);
+    hipLaunchKernelGGL(k_contrast_loss<DT>, dim3((c.B + 3) / 4), dim3(256), 0, st, c, row_blocks);
     if (want_grad) hipLaunchKernelGGL((k_contrast_g<TILE, DT>), dim3((u32)tq * tk), dim3(256), 0, st, c, tq, tk);
 }
 template <int DT, int TILE>
@@ -1007,16 +1022,16 @@ template <int DT, bool WIDE>
 static void launch_contrast(ContrastPar &c, const ContrastPlan &plan, int want_grad, hipStream_t st)
 {
     const int Br = ct_up(c.B, CT_PAD), Mr = ct_up(c.M, CT_PAD);
-    hipLaunchKernelGGL(k_contrast_clear, dim3((c.M + 255) / 256), dim3(256), 0, st, c);
-    const int key_blocks = Mr / 4 < 1024 ? Mr / 4 : 1024, row_blocks = Br / 4 < 1024 ? Br / 4 : 1024;
-    hipLaunchKernelGGL((k_contrast_rows<DT, WIDE>), dim3(key_blocks + row_blocks), dim3(256), 0, st, c, key_blocks);
+    const int key_blocks = Mr / 4 < CT_ROW_BLOCKS ? Mr / 4 : CT_ROW_BLOCKS, row_blocks = Br / 4 < CT_ROW_BLOCKS ? Br / 4 : CT_ROW_BLOCKS;
     // (by columns the padding of d up to a whole tile is written too: the products read it)
-    hipLaunchKernelGGL((k_contrast_copy<DT, WIDE>), dim3((Br + Mr) / 64, (want_grad ? c.dr : c.dp) / 64), dim3(256), 0, st, c, Br / 64, want_grad);
+    const int across = (want_grad ? c.dr : c.dp) / 64;
+    hipLaunchKernelGGL((k_contrast_prepare<DT, WIDE>), dim3((u32)(key_blocks + row_blocks) + (u32)((Br + Mr) / 64) * across), dim3(256), 0, st, c,
+                       key_blocks, row_blocks, Br / 64, across, want_grad);
     if constexpr (DT != DT_F32) {
-        if (plan.tile == 256) launch_products<DT, 256>(c, want_grad, st);
-        else launch_products<DT, 128>(c, want_grad, st);
+        if (plan.tile == 256) launch_products<DT, 256>(c, want_grad, row_blocks, st);
+        else launch_products<DT, 128>(c, want_grad, row_blocks, st);
     } else
-        launch_products<DT, 128>(c, want_grad, st);
+        launch_products<DT, 128>(c, want_grad, row_blocks, st);
     if (!want_grad) return;
     if (plan.tile_g == 256) launch_grads<DT, 256>(c, st);
     else launch_grads<DT, 128>(c, st);

@@ -4,8 +4,9 @@
 //   grad[v] (+)= scale * sum of dout[t] over the t with ids[t] = v, in ascending t
 //
 // Both only move rows: a lookup reads and writes n of them, a gradient reads n and writes V (added to what is there:
-// reads and writes the rows that are named).  The gradient's sums are in float32 and in a fixed order, whatever
-// the launch: the tokens are sorted by id (stable), and every sum runs over neighbours in that order.
+// reads and writes the rows that are named).  The gradient's sums are in float32 and in an order that the sizes and ids alone decide:
+// up to SMALL_TOKENS tokens a block finds those of an id by itself, in one launch; more are sorted by id (stable), and every sum runs
+// over neighbours in that order.
 #include "rows.h"
 
 // ------------------------------------------------------------------------------------------------ lookup
@@ -110,7 +111,6 @@ extern "C" int rnnd_embed(const void *table, int64_t V, int32_t d, int dtype, co
 #define SORT_WAVES (SORT_THREADS / 64)
 #define SORT_ITEMS 4
 #define SORT_TILE (SORT_THREADS * SORT_ITEMS)
-#define SORT_SMALL 4096     // up to here every token counts the tokens before it: one launch
 
 struct SortPass {
     const int *ids;             // first pass: the caller's ids; else null
@@ -119,26 +119,52 @@ struct SortPass {
     u32 *hist;                  // [digits][blocks]
     u32 *totals;                // [digits]
     unsigned char *named;       // first pass: set to 1 for every row that an id names (may be null)
+    u32 *clear;                 // first pass: `clear_words` words that are set to zero beside the count, by the blocks behind it
+    u32 clear_words;
     u32 n, V, blocks;
     int shift, bits;
 };
 
 __device__ __forceinline__ u32 id_key(int id, u32 V) { return (u32)id < V ? (u32)id : V; }
 
+// the lanes of `on` that hold the same digit
+__device__ __forceinline__ u64 same_digit(u32 digit, int bits, bool on)
+{
+    u64 same = __ballot(on);
+    for (int b = 0; b < bits; ++b) {
+        const bool bit = digit >> b & 1;
+        const u64 set = __ballot(bit);
+        same &= bit ? set : ~set;
+    }
+    return same;
+}
+
+// One addition for the lanes of a digit: ids are popular or not, and of the high digits a few take most tokens; 64 additions to one
+// word one after the other took twice the time of the ballots.
 __global__ __launch_bounds__(SORT_THREADS) void k_sort_count(SortPass s)
 {
     __shared__ u32 count[SORT_DIGITS];
+    if (blockIdx.x >= s.blocks) {
+        for (size_t i = (size_t)(blockIdx.x - s.blocks) * SORT_THREADS + threadIdx.x; i < s.clear_words; i += (size_t)(gridDim.x - s.blocks) * SORT_THREADS)
+            s.clear[i] = 0;
+        return;
+    }
     const u32 digits = 1u << s.bits;
     for (u32 i = threadIdx.x; i < digits; i += SORT_THREADS) count[i] = 0;
     __syncthreads();
     const u32 base = blockIdx.x * SORT_TILE;
+    u32 key[SORT_ITEMS];
 #pragma unroll
     for (int i = 0; i < SORT_ITEMS; ++i) {
         const u32 t = base + i * SORT_THREADS + threadIdx.x;
-        if (t >= s.n) continue;
-        const u32 key = s.ids ? id_key(s.ids[t], s.V) : s.in[t].x;
-        if (s.named && key < s.V) s.named[key] = 1;
-        atomicAdd(&count[(key >> s.shift) & (digits - 1)], 1u);
+        key[i] = t < s.n ? s.ids ? id_key(s.ids[t], s.V) : s.in[t].x : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < SORT_ITEMS; ++i) {
+        const bool on = base + i * SORT_THREADS + threadIdx.x < s.n;
+        const u32 digit = (key[i] >> s.shift) & (digits - 1);
+        const u64 same = same_digit(digit, s.bits, on);
+        if (on && (same & lanes_below(threadIdx.x & 63)) == 0) atomicAdd(&count[digit], (u32)__popcll(same));
     }
     __syncthreads();
     for (u32 i = threadIdx.x; i < digits; i += SORT_THREADS) s.hist[(size_t)i * s.blocks + blockIdx.x] = count[i];
@@ -186,6 +212,7 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_place(SortPass s)
         const u32 t = base + i * 64 + lane;
         item[i] = make_uint2(0, 0);
         if (t < s.n) item[i] = s.ids ? make_uint2(id_key(s.ids[t], s.V), t) : s.in[t];
+        if (s.named && t < s.n && item[i].x < s.V) s.named[item[i].x] = 1;
     }
     // where each digit starts: exclusive sums of the totals, and of this block's counts
     u32 first[PER], mine = 0;
@@ -209,12 +236,7 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_place(SortPass s)
     for (int i = 0; i < SORT_ITEMS; ++i) {
         const bool on = base + i * 64 + lane < s.n;
         const u32 digit = (item[i].x >> s.shift) & (digits - 1);
-        u64 same = __ballot(on);
-        for (int b = 0; b < s.bits; ++b) {
-            const bool bit = digit >> b & 1;
-            const u64 set = __ballot(bit);
-            same &= bit ? set : ~set;
-        }
+        const u64 same = same_digit(digit, s.bits, on);
         const u32 ahead = __popcll(same & lanes_below(lane));
         u32 before = 0;
         if (on) before = count[wave][digit];
@@ -237,33 +259,6 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_place(SortPass s)
 #pragma unroll
     for (int i = 0; i < SORT_ITEMS; ++i)
         if (base + i * 64 + lane < s.n) s.out[count[wave][(item[i].x >> s.shift) & (digits - 1)] + rank[i]] = item[i];
-}
-
-// Few tokens, one launch: 32 lanes per token count the tokens that sort before it -- those of a smaller key, and those before it
-// of the same.  Blocks behind the first token_blocks clear the whole gradient meanwhile: its 16-byte words, and what lies before
-// and behind them.
-__global__ __launch_bounds__(256) void k_sort_small(const int *__restrict__ ids, u32 n, u32 V, uint2 *__restrict__ out, u32 *hot,
-                                                    u32 token_blocks, uint4 *words, size_t n_words, unsigned char *head, u32 head_bytes,
-                                                    unsigned char *tail, u32 tail_bytes)
-{
-    __shared__ u32 keys[SORT_SMALL];
-    if (blockIdx.x >= token_blocks) {
-        const u32 b = blockIdx.x - token_blocks, blocks = gridDim.x - token_blocks;
-        for (size_t i = (size_t)b * 256 + threadIdx.x; i < n_words; i += (size_t)blocks * 256) words[i] = make_uint4(0, 0, 0, 0);
-        if (b == 0 && threadIdx.x < head_bytes) head[threadIdx.x] = 0;
-        if (b == 0 && threadIdx.x < tail_bytes) tail[threadIdx.x] = 0;
-        return;
-    }
-    if (blockIdx.x == 0 && threadIdx.x == 0) *hot = 0;
-    for (u32 t = threadIdx.x; t < n; t += 256) keys[t] = id_key(ids[t], V);
-    __syncthreads();
-    const u32 t = blockIdx.x * 8 + (threadIdx.x >> 5), sub = threadIdx.x & 31;
-    const u32 key = t < n ? keys[t] : 0;
-    u32 before = 0;
-    for (u32 j = sub; j < n; j += 32) before += keys[j] < key + (j < t);
-#pragma unroll
-    for (int k = 16; k; k >>= 1) before += __shfl_xor(before, k);
-    if (t < n && sub == 0) out[before] = make_uint2(key, t);
 }
 
 // ------------------------------------------------------------------------------------------------ gradient
@@ -425,9 +420,106 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_grad_join(GradPar g)
     }
 }
 
-__global__ void k_grad_clear(u32 *p, size_t words)
+// Few tokens: one launch, without a sort.  A block for each token looks through all ids; if an earlier token has the same id that token's
+// block sums them, else this one does: it lists the tokens of its id in order, its groups of G lanes sum pieces of the list, and
+// their sums are added in the groups' order.  The ids are a few KB that every block finds in its L2 -- 4,096 blocks read 64 MB of
+// them, 2 us -- where a sort and its joins are five launches that wait for each other.  Blocks behind the first reduce_blocks clear
+// clear_rows rows each, but for those that an id names.
+#define SMALL_TOKENS 4096
+#define SMALL_SLABS 4           // blocks of a token, at most
+#define SMALL_CLEAR 8192        // rows of a block that clears, at most
+
+template <int DT, int GT, int VEC>
+__global__ __launch_bounds__(256) void k_grad_small(GradPar g, const int *__restrict__ ids, u32 log_lanes, u32 token_blocks)
 {
-    for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < words; i += (size_t)gridDim.x * blockDim.x) p[i] = 0;
+    constexpr int ITEMS = SMALL_TOKENS / 256;
+    __shared__ u64 mask[SMALL_TOKENS / 64];
+    __shared__ alignas(16) unsigned short list[SMALL_TOKENS];
+    __shared__ float part[256 * VEC];
+    const u32 tid = threadIdx.x, lane = tid & 63;
+    int id[ITEMS];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) id[i] = i * 256 + tid < g.n ? ids[i * 256 + tid] : -1;
+    if (blockIdx.x >= g.reduce_blocks) {
+        u32 *const named = (u32 *)list;         // a bit for each row: SMALL_CLEAR bits
+        static_assert(SMALL_CLEAR / 8 <= sizeof list, "bits");
+        const u64 v0 = (u64)(blockIdx.x - g.reduce_blocks) * g.clear_rows;
+        const u32 rows = (u32)(g.V - v0 < g.clear_rows ? g.V - v0 : g.clear_rows);
+        for (u32 i = tid; i < SMALL_CLEAR / 32; i += 256) named[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const u64 r = (u64)(u32)id[i] - v0;
+            if ((u32)id[i] < g.V && r < rows) atomicOr(&named[r >> 5], 1u << (r & 31));
+        }
+        __syncthreads();
+        const float zero[VEC] = {};
+        for (u32 i = tid; i < rows * g.pieces; i += 256) {
+            const u32 r = i / g.pieces;
+            if (!(named[r >> 5] >> (r & 31) & 1)) store_pack<GT, VEC>(g.grad, (v0 * g.pieces + i) * VEC, zero);
+        }
+        return;
+    }
+    const u32 t = blockIdx.x / token_blocks, lanes = 1u << log_lanes, groups = 256 >> log_lanes;
+    const int key = ids[t];
+    if ((u32)key >= g.V) return;        // a whole block
+    bool earlier = false;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const bool same = id[i] == key;     // (no token: -1, which is no key)
+        const u64 all = __ballot(same);
+        if (lane == 0) mask[i * 4 + (tid >> 6)] = all;
+        earlier |= same && i * 256 + tid < t;
+    }
+    if (__syncthreads_or(earlier)) return;
+    u32 count = 0;
+    for (u32 w = t >> 6; w < (g.n + 63) / 64; ++w) count += __popcll(mask[w]);
+    if (count > 1) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+            if (id[i] == key) {
+                const u32 word = i * 4 + (tid >> 6);
+                u32 rank = __popcll(mask[word] & lanes_below(lane));
+                for (u32 w = t >> 6; w < word; ++w) rank += __popcll(mask[w]);
+                list[rank] = (unsigned short)(i * 256 + tid);
+            }
+        __syncthreads();
+    }
+    const u32 group = tid >> log_lanes, at = tid & (lanes - 1);
+    u32 each = (count + groups - 1) / groups;
+    if (each < GRAD_UNROLL) each = GRAD_UNROLL;
+    const u32 begin = group * each < count ? group * each : count, end = begin + each < count ? begin + each : count;
+    const u32 used = (count + each - 1) / each;
+    for (u32 slab = blockIdx.x % token_blocks; slab < g.slabs; slab += token_blocks) {
+        const u32 piece = slab * lanes + at;
+        float acc[VEC] = {};
+        if (piece < g.pieces)
+            for (u32 j = begin; j < end; j += GRAD_UNROLL) {
+                Pack<DT, VEC> row[GRAD_UNROLL];
+#pragma unroll
+                for (int i = 0; i < GRAD_UNROLL; ++i)
+                    if (j + i < end) row[i] = load_pack<DT, VEC>(g.dout, ((u64)(count > 1 ? list[j + i] : t) * g.pieces + piece) * VEC);
+#pragma unroll
+                for (int i = 0; i < GRAD_UNROLL; ++i)
+                    if (j + i < end) {
+                        float x[VEC];
+                        unpack<DT, VEC>(row[i], x);
+#pragma unroll
+                        for (int k = 0; k < VEC; ++k) acc[k] += x[k];
+                    }
+            }
+        if (used > 1) {
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) part[(group * lanes + at) * VEC + k] = acc[k];
+            __syncthreads();
+            if (group == 0)
+                for (u32 o = 1; o < used; ++o)
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) acc[k] += part[(o * lanes + at) * VEC + k];
+            __syncthreads();
+        }
+        if (group == 0 && piece < g.pieces) grad_write<GT, VEC>(g, (u32)key, piece, acc);
+    }
 }
 
 struct GradPlan {
@@ -439,6 +531,10 @@ struct GradPlan {
 static GradPlan grad_plan(int64_t n, int d, int64_t V)
 {
     GradPlan p = {};
+    if (n <= SMALL_TOKENS) {
+        p.bytes = 256;          // (none of it is used)
+        return p;
+    }
     // Long chunks leave fewer partial sums; short calls need chunks short enough to occupy the GPU: two wavefronts per SIMD, of about
     // 256 coordinates each.
     p.chunk = 128;
@@ -447,15 +543,15 @@ static GradPlan grad_plan(int64_t n, int d, int64_t V)
     p.blocks = (u32)((n + SORT_TILE - 1) / SORT_TILE);
     int bits = 1;
     while ((V >> bits) != 0) ++bits;          // keys 0 .. V
-    p.passes = n <= SORT_SMALL ? 0 : (bits + SORT_BITS - 1) / SORT_BITS;
-    p.bits = p.passes ? (bits + p.passes - 1) / p.passes : 0;
+    p.passes = (bits + SORT_BITS - 1) / SORT_BITS;
+    p.bits = (bits + p.passes - 1) / p.passes;
     size_t off = 0;
     auto take = [&](size_t b) { const size_t o = off; off += ws_align(b); return o; };
-    for (int i = 0; i < 2; ++i) p.o_item[i] = take(i && !p.passes ? 0 : (size_t)n * 8);
-    p.o_hist = take(p.passes ? (size_t)SORT_DIGITS * p.blocks * 4 : 0);
-    p.o_totals = take(p.passes ? SORT_DIGITS * 4 : 0);
+    for (int i = 0; i < 2; ++i) p.o_item[i] = take((size_t)n * 8);
+    p.o_hist = take((size_t)SORT_DIGITS * p.blocks * 4);
+    p.o_totals = take(SORT_DIGITS * 4);
     p.o_partial = take((size_t)p.chunks * GRAD_SLOTS * d * 4);
-    p.o_named = take(p.passes ? (size_t)V : 0);
+    p.o_named = take((size_t)V);
     p.o_hot = take((size_t)(p.chunks + 1) * 4);       // (right behind `named`: its first word is cleared with it)
     p.bytes = off;
     return p;
@@ -478,29 +574,43 @@ static void launch_join(GradPar &g, hipStream_t st)
     hipLaunchKernelGGL((k_grad_join<GT, VEC, G>), dim3((u32)(units < 1024 ? units : 1024)), dim3(JOIN_THREADS), 0, st, g);
 }
 template <int DT, int GT, int VEC>
-static void launch_grad_vec(GradPar &g, int d, bool clear, hipStream_t st)
+static void launch_grad_vec(GradPar &g, int d, const int32_t *small_ids, hipStream_t st)
 {
     g.pieces = d / VEC;
+    const bool clear = !g.accumulate;
+    if (small_ids || !g.n) {
+        u32 log_lanes = 3;
+        while (log_lanes < 6 && (1u << log_lanes) < g.pieces) ++log_lanes;
+        g.slabs = (g.pieces + (1u << log_lanes) - 1) >> log_lanes;
+        const u32 token_blocks = g.slabs < SMALL_SLABS ? g.slabs : SMALL_SLABS;
+        g.reduce_blocks = g.n * token_blocks;
+        // 512 to 8,192 pieces for a block that clears: enough blocks, and each writes more than it reads of ids
+        u32 pieces = 512;
+        while (pieces < 8192 && (u64)g.V * g.pieces / pieces > 1024) pieces <<= 1;
+        g.clear_rows = pieces / g.pieces > 1 ? pieces / g.pieces : 1;
+        const u32 clear_blocks = clear ? (g.V + g.clear_rows - 1) / g.clear_rows : 0;
+        hipLaunchKernelGGL((k_grad_small<DT, GT, VEC>), dim3(g.reduce_blocks + clear_blocks), dim3(256), 0, st, g, small_ids, log_lanes, token_blocks);
+        return;
+    }
     g.reduce_blocks = (u32)(((u64)g.chunks * g.pieces + 255) / 256);
     g.clear_rows = 2048 / g.pieces > 1 ? 2048 / g.pieces : 1;
     while (clear && (u64)g.V > (u64)g.clear_rows << 30) g.clear_rows <<= 1;
     const u32 clear_blocks = clear ? (g.V + g.clear_rows - 1) / g.clear_rows : 0;
     hipLaunchKernelGGL((k_grad_reduce<DT, GT, VEC>), dim3(g.reduce_blocks + clear_blocks), dim3(256), 0, st, g);
-    if (g.chunks <= 2) return;      // no id of more than two chunks' tokens
     if (g.pieces <= 8) launch_join<GT, VEC, 8>(g, st);
     else if (g.pieces <= 16) launch_join<GT, VEC, 16>(g, st);
     else if (g.pieces <= 32) launch_join<GT, VEC, 32>(g, st);
     else launch_join<GT, VEC, 64>(g, st);
 }
 template <int DT, int GT>
-static void launch_grad(GradPar &g, int d, bool clear, hipStream_t st)
+static void launch_grad(GradPar &g, int d, const int32_t *small_ids, hipStream_t st)
 {
     const int vec = row_vec(d, g.dout, dt_size(DT), g.grad, dt_size(GT));
     if constexpr (DT != DT_F32)
-        if (vec == 8) return launch_grad_vec<DT, GT, 8>(g, d, clear, st);
-    if (vec >= 4) launch_grad_vec<DT, GT, 4>(g, d, clear, st);
-    else if (vec == 2) launch_grad_vec<DT, GT, 2>(g, d, clear, st);
-    else launch_grad_vec<DT, GT, 1>(g, d, clear, st);
+        if (vec == 8) return launch_grad_vec<DT, GT, 8>(g, d, small_ids, st);
+    if (vec >= 4) launch_grad_vec<DT, GT, 4>(g, d, small_ids, st);
+    else if (vec == 2) launch_grad_vec<DT, GT, 2>(g, d, small_ids, st);
+    else launch_grad_vec<DT, GT, 1>(g, d, small_ids, st);
 }
 
 extern "C" int rnnd_embed_grad(const void *dout, int dtype, const int32_t *ids, int64_t n, int32_t d, float scale, int64_t V,
@@ -517,28 +627,22 @@ extern "C" int rnnd_embed_grad(const void *dout, int dtype, const int32_t *ids, 
     if ((uintptr_t)workspace % 16) return RNND_ERR_BAD_PARAM;
     if (workspace_bytes < p.bytes) return RNND_ERR_SCRATCH;
     hipStream_t st = (hipStream_t)stream;
-    char *w = (char *)workspace;
-    uint2 *item[2] = {(uint2 *)(w + p.o_item[0]), (uint2 *)(w + p.o_item[1])};
-    u32 *hot = (u32 *)(w + p.o_hot);
-    unsigned char *named = (unsigned char *)(w + p.o_named);
-    int at = 0;
-    if (!p.passes) {
-        const size_t bytes = accumulate ? 0 : (size_t)V * d * dt_size(grad_dtype);
-        size_t head = (16 - (uintptr_t)grad % 16) % 16;
-        if (head > bytes) head = bytes;
-        const size_t words = (bytes - head) / 16;
-        const u32 tail = (u32)(bytes - head - words * 16);
-        const u32 token_blocks = (u32)((n + 7) / 8) + (n ? 0 : 1), clear_blocks = accumulate ? 0 : (u32)(words / 1024 < 2048 ? words / 1024 + 1 : 2048);
-        hipLaunchKernelGGL(k_sort_small, dim3(token_blocks + clear_blocks), dim3(256), 0, st, ids, (u32)n, (u32)V, item[0], hot, token_blocks,
-                           (uint4 *)((char *)grad + head), words, (unsigned char *)grad, (u32)head, (unsigned char *)grad + head + words * 16, tail);
-    } else {
+    GradPar g = {};
+    g.dout = dout;
+    g.grad = grad;
+    g.n = (u32)n;
+    g.V = (u32)V;
+    g.accumulate = accumulate;
+    g.scale = scale;
+    if (p.passes) {
+        char *w = (char *)workspace;
+        uint2 *item[2] = {(uint2 *)(w + p.o_item[0]), (uint2 *)(w + p.o_item[1])};
+        unsigned char *named = (unsigned char *)(w + p.o_named);
         // the number of long ids, and (all rows written) which rows are named
         const size_t from = accumulate ? p.o_hot : p.o_named, words = (p.o_hot + 4 - from) / 4;
-        const size_t blocks = (words + 1023) / 1024;
-        hipLaunchKernelGGL(k_grad_clear, dim3((u32)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, st, (u32 *)(w + from), words);
-        at = 1;
+        int at = 0;
         for (int i = 0; i < p.passes; ++i) {
-            SortPass s;
+            SortPass s = {};
             s.ids = i ? nullptr : ids;
             s.in = item[at];
             at ^= 1;
@@ -546,31 +650,26 @@ extern "C" int rnnd_embed_grad(const void *dout, int dtype, const int32_t *ids, 
             s.hist = (u32 *)(w + p.o_hist);
             s.totals = (u32 *)(w + p.o_totals);
             s.named = i || accumulate ? nullptr : named;
+            s.clear = (u32 *)(w + from);
+            s.clear_words = i ? 0 : (u32)words;
             s.n = (u32)n;
             s.V = (u32)V;
             s.blocks = p.blocks;
             s.shift = i * p.bits;
             s.bits = p.bits;
-            hipLaunchKernelGGL(k_sort_count, dim3(p.blocks), dim3(SORT_THREADS), 0, st, s);
+            const u32 clear_blocks = (s.clear_words + 2047) / 2048;
+            hipLaunchKernelGGL(k_sort_count, dim3(p.blocks + (clear_blocks < 1024 ? clear_blocks : 1024)), dim3(SORT_THREADS), 0, st, s);
             hipLaunchKernelGGL(k_sort_offsets, dim3(1u << p.bits), dim3(64), 0, st, s);
             hipLaunchKernelGGL(k_sort_place, dim3(p.blocks), dim3(SORT_THREADS), 0, st, s);
         }
+        g.item = item[at];
+        g.partial = (float *)(w + p.o_partial);
+        g.hot = (u32 *)(w + p.o_hot);
+        g.named = named;
+        g.chunk = p.chunk;
+        g.chunks = p.chunks;
     }
-    if (!n) return launched("rnnd_embed_grad");
-    GradPar g = {};
-    g.dout = dout;
-    g.item = item[at];
-    g.grad = grad;
-    g.partial = (float *)(w + p.o_partial);
-    g.hot = hot;
-    g.named = named;
-    g.n = (u32)n;
-    g.V = (u32)V;
-    g.chunk = p.chunk;
-    g.chunks = p.chunks;
-    g.accumulate = accumulate;
-    g.scale = scale;
-#define RNND_F(A, B) launch_grad<A, B>(g, d, !accumulate && p.passes, st)
+#define RNND_F(A, B) launch_grad<A, B>(g, d, p.passes ? nullptr : ids, st)
     RNND_FOR_TYPES(dtype, grad_dtype, RNND_F)
 #undef RNND_F
     return launched("rnnd_embed_grad");

@@ -167,6 +167,29 @@ def test_gradient_of_ids_that_end_around_the_pieces_of_the_sum(rn, first, d):
     check_gradient(rn, rows(len(ids), d, torch.bfloat16, d), ids, 200, 1.0, torch.float32, True, rows(200, d, torch.float32, 1))
 
 
+@pytest.mark.parametrize("dtype,grad_dtype", [("float32", "float32"), ("bfloat16", "float16")])
+@pytest.mark.parametrize("n,d,V", [(4096, 2050, 7), (4096, 33, 1), (3001, 1100, 3), (4095, 8, 20_000), (9, 768, 9_001), (300, 5, 70_000), (4096, 24, 4096)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradient_of_few_tokens(rn, dtype, grad_dtype, n, d, V, accumulate):
+    """Ids that many tokens share, rows of more pieces than blocks take at once, and borders of the blocks that clear."""
+    import torch
+    dout = rows(n, d, getattr(torch, dtype), 5)
+    grad = rows(V, d, getattr(torch, grad_dtype), 6) if accumulate else None
+    for ids in (zipf(n, V, 3), np.full(n, V - 1, np.int32), np.arange(n, dtype=np.int32)[::-1].copy() * 5 - 3):
+        check_gradient(rn, dout, ids.astype(np.int32), V, 1.5, getattr(torch, grad_dtype), accumulate, None if grad is None else grad.clone())
+
+
+@pytest.mark.parametrize("first", range(0, 9, 2))
+@pytest.mark.parametrize("d", [5, 96, 600])
+def test_gradient_of_sorted_ids_that_end_around_the_pieces_of_the_sum(rn, first, d):
+    """The same runs among enough other ids that the tokens are sorted: just before, at and behind chunks of 8 and 16."""
+    import torch
+    lengths = [first + 1] + [k for c in (8, 16, 24, 32, 48) for k in (c - 1, c, c + 1)] + [1, 2, 3, 8, 8, 16, 32, 17, 33, 100, 64, 5, 400] + [1] * 4_200
+    ids = runs(lengths, 5_000, first)
+    check_gradient(rn, rows(len(ids), d, torch.float32, d), ids, 5_000, 1.0, torch.float32, False)
+    check_gradient(rn, rows(len(ids), d, torch.bfloat16, d), ids, 5_000, 1.0, torch.float32, True, rows(5_000, d, torch.float32, 1))
+
+
 def test_gradient_of_long_calls(rn):
     """More tokens than the chunks of 128 need; a few ids hold most of them."""
     import torch
