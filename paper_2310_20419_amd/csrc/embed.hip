@@ -102,7 +102,7 @@ extern "C" int rnnd_embed(const void *table, int64_t V, int32_t d, int dtype, co
 
 // ------------------------------------------------------------------------------------------------ tokens sorted by id
 // Pairs (id, token), least significant digit first, up to SORT_BITS bits a pass, three launches each: every block counts its
-// digits, a wavefront per digit makes the counts of the blocks offsets, every block places its tokens.  A block's order
+// digits, the counts become sums over the blocks before, every block places its tokens.  A block's order
 // is kept (stable) because its wavefronts number equal digits lane by lane, with a ballot per bit.  An id that is no row
 // sorts as V, behind all rows.
 #define SORT_BITS 10
@@ -116,7 +116,7 @@ struct SortPass {
     const int *ids;             // first pass: the caller's ids; else null
     const uint2 *in;            // (key, token)
     uint2 *out;
-    u32 *hist;                  // [digits][blocks]
+    u32 *hist;                  // [blocks][digits]: a block's own lie together, so that it writes and reads whole lines
     u32 *totals;                // [digits]
     unsigned char *named;       // first pass: set to 1 for every row that an id names (may be null)
     u32 *clear;                 // first pass: `clear_words` words that are set to zero beside the count, by the blocks behind it
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_count(SortPass s)
         if (on && (same & lanes_below(threadIdx.x & 63)) == 0) atomicAdd(&count[digit], (u32)__popcll(same));
     }
     __syncthreads();
-    for (u32 i = threadIdx.x; i < digits; i += SORT_THREADS) s.hist[(size_t)i * s.blocks + blockIdx.x] = count[i];
+    for (u32 i = threadIdx.x; i < digits; i += SORT_THREADS) s.hist[((size_t)blockIdx.x << s.bits) + i] = count[i];
 }
 
 __device__ __forceinline__ u32 wave_inclusive(u32 v, int lane)
@@ -180,19 +180,41 @@ __device__ __forceinline__ u32 wave_inclusive(u32 v, int lane)
     return v;
 }
 
-// one wavefront per digit: exclusive sums of its counts over the blocks
-__global__ __launch_bounds__(64) void k_sort_offsets(SortPass s)
+// Exclusive sums of every digit's counts over the blocks: 64 digits (two lines of each block's counts) for a workgroup,
+// whose wavefronts take a run of blocks each.
+#define OFFSET_WAVES 16
+__global__ __launch_bounds__(64 * OFFSET_WAVES) void k_sort_offsets(SortPass s)
 {
-    const int lane = threadIdx.x;
-    u32 *h = s.hist + (size_t)blockIdx.x * s.blocks;
+    __shared__ u32 sums[OFFSET_WAVES][64];
+    const u32 lane = threadIdx.x & 63, wave = threadIdx.x >> 6, digit = blockIdx.x * 64 + lane;
+    const bool on = digit < 1u << s.bits;
+    const u32 each = (s.blocks + OFFSET_WAVES - 1) / OFFSET_WAVES;
+    const u32 begin = wave * each < s.blocks ? wave * each : s.blocks, end = s.blocks - begin < each ? s.blocks : begin + each;
+    u32 *const h = s.hist + digit;
     u32 sum = 0;
-    for (u32 b = 0; b < s.blocks; b += 64) {
-        const u32 v = b + lane < s.blocks ? h[b + lane] : 0;
-        const u32 inc = wave_inclusive(v, lane);
-        if (b + lane < s.blocks) h[b + lane] = sum + inc - v;
-        sum += __shfl(inc, 63);
+    if (on)
+#pragma unroll 8
+        for (u32 b = begin; b < end; ++b) sum += h[(size_t)b << s.bits];
+    sums[wave][lane] = sum;
+    __syncthreads();
+    u32 at = 0, all = 0;
+#pragma unroll
+    for (u32 w = 0; w < OFFSET_WAVES; ++w) {
+        if (w == wave) at = all;
+        all += sums[w][lane];
     }
-    if (lane == 0) s.totals[blockIdx.x] = sum;
+    if (!on) return;
+    if (wave == 0) s.totals[digit] = all;
+    for (u32 b = begin; b < end; b += 8) {
+        u32 v[8];
+#pragma unroll
+        for (u32 i = 0; i < 8; ++i) v[i] = b + i < end ? h[(size_t)(b + i) << s.bits] : 0;
+#pragma unroll
+        for (u32 i = 0; i < 8; ++i) {
+            if (b + i < end) h[(size_t)(b + i) << s.bits] = at;
+            at += v[i];
+        }
+    }
 }
 
 __global__ __launch_bounds__(SORT_THREADS) void k_sort_place(SortPass s)
@@ -230,7 +252,7 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_place(SortPass s)
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         const u32 digit = threadIdx.x * PER + k;
-        first[k] += before_waves + (digit < digits ? s.hist[(size_t)digit * s.blocks + blockIdx.x] : 0);
+        first[k] += before_waves + (digit < digits ? s.hist[((size_t)blockIdx.x << s.bits) + digit] : 0);
     }
 #pragma unroll
     for (int i = 0; i < SORT_ITEMS; ++i) {
@@ -385,10 +407,12 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_grad_join(GradPar g)
         const u32 c = g.hot[1 + at / g.slabs], piece = at % g.slabs * G + lane;
         const u32 id = g.item[(u64)(c + 1) * g.chunk - 1].x;
         u32 lo = c + 1, hi = (g.n - 1) / g.chunk;      // the last chunk whose first token is of `id`: a long id fills c + 1
-        while (lo < hi) {
-            const u32 mid = lo + (hi - lo + 1) / 2;
-            if (g.item[(u64)mid * g.chunk].x == id) lo = mid;
-            else hi = mid - 1;
+        while (lo < hi) {       // 64 places at a time: a wait for memory each
+            const u32 step = (hi - lo + 63) / 64, left = (hi - lo) / step, ahead = (threadIdx.x & 63) + 1;
+            const bool same = ahead <= left && g.item[(u64)(lo + ahead * step) * g.chunk].x == id;
+            const u32 found = __popcll(__ballot(same));
+            lo += found * step;
+            if (found < left) hi = lo + step - 1;
         }
         const u32 chunks = lo - c + 1;
         float acc[VEC] = {};
@@ -659,7 +683,7 @@ extern "C" int rnnd_embed_grad(const void *dout, int dtype, const int32_t *ids, 
             s.bits = p.bits;
             const u32 clear_blocks = (s.clear_words + 2047) / 2048;
             hipLaunchKernelGGL(k_sort_count, dim3(p.blocks + (clear_blocks < 1024 ? clear_blocks : 1024)), dim3(SORT_THREADS), 0, st, s);
-            hipLaunchKernelGGL(k_sort_offsets, dim3(1u << p.bits), dim3(64), 0, st, s);
+            hipLaunchKernelGGL(k_sort_offsets, dim3(((1u << p.bits) + 63) / 64), dim3(64 * OFFSET_WAVES), 0, st, s);
             hipLaunchKernelGGL(k_sort_place, dim3(p.blocks), dim3(SORT_THREADS), 0, st, s);
         }
         g.item = item[at];
