@@ -111,6 +111,7 @@ extern "C" int rnnd_embed(const void *table, int64_t V, int32_t d, int dtype, co
 #define SORT_WAVES (SORT_THREADS / 64)
 #define SORT_ITEMS 4
 #define SORT_TILE (SORT_THREADS * SORT_ITEMS)
+#define SORT_DIRECT 64          // blocks up to which each sums the counts of all by itself, instead of a launch that does it once
 
 struct SortPass {
     const int *ids;             // first pass: the caller's ids; else null
@@ -122,7 +123,7 @@ struct SortPass {
     u32 *clear;                 // first pass: `clear_words` words that are set to zero beside the count, by the blocks behind it
     u32 clear_words;
     u32 n, V, blocks;
-    int shift, bits;
+    int shift, bits, direct;    // direct: k_sort_place sums the counts itself
 };
 
 __device__ __forceinline__ u32 id_key(int id, u32 V) { return (u32)id < V ? (u32)id : V; }
@@ -237,12 +238,36 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_place(SortPass s)
         if (s.named && t < s.n && item[i].x < s.V) s.named[item[i].x] = 1;
     }
     // where each digit starts: exclusive sums of the totals, and of this block's counts
-    u32 first[PER], mine = 0;
+    u32 first[PER], ahead_of[PER] = {}, total[PER] = {}, mine = 0;
+    if (s.direct) {     // (2^bits counts of a block, bits > 0: a thread's digits are all there or none)
+        typedef u32 Counts __attribute__((ext_vector_type(PER)));
+        const u32 digit = threadIdx.x * PER;
+        for (u32 b0 = 0; b0 < s.blocks; b0 += 16) {
+            Counts v[16];
+#pragma unroll
+            for (u32 i = 0; i < 16; ++i)
+                if (b0 + i < s.blocks && digit < digits) v[i] = *(const Counts *)&s.hist[((size_t)(b0 + i) << s.bits) + digit];
+                else v[i] = Counts{};
+#pragma unroll
+            for (u32 i = 0; i < 16; ++i)
+#pragma unroll
+                for (int k = 0; k < PER; ++k) {
+                    total[k] += v[i][k];
+                    ahead_of[k] += b0 + i < blockIdx.x ? v[i][k] : 0;
+                }
+        }
+    } else
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const u32 digit = threadIdx.x * PER + k;
+            if (digit >= digits) continue;
+            total[k] = s.totals[digit];
+            ahead_of[k] = s.hist[((size_t)blockIdx.x << s.bits) + digit];
+        }
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-        const u32 digit = threadIdx.x * PER + k;
         first[k] = mine;
-        mine += digit < digits ? s.totals[digit] : 0;
+        mine += total[k];
     }
     const u32 inc = wave_inclusive(mine, lane);
     if (lane == 63) wave_total[wave] = inc;
@@ -250,10 +275,7 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_place(SortPass s)
     u32 before_waves = inc - mine;
     for (int w = 0; w < wave; ++w) before_waves += wave_total[w];
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        const u32 digit = threadIdx.x * PER + k;
-        first[k] += before_waves + (digit < digits ? s.hist[((size_t)blockIdx.x << s.bits) + digit] : 0);
-    }
+    for (int k = 0; k < PER; ++k) first[k] += before_waves + ahead_of[k];
 #pragma unroll
     for (int i = 0; i < SORT_ITEMS; ++i) {
         const bool on = base + i * 64 + lane < s.n;
@@ -559,10 +581,10 @@ static GradPlan grad_plan(int64_t n, int d, int64_t V)
         p.bytes = 256;          // (none of it is used)
         return p;
     }
-    // Long chunks leave fewer partial sums; short calls need chunks short enough to occupy the GPU: two wavefronts per SIMD, of about
+    // Long chunks leave fewer partial sums; short calls need chunks short enough to occupy the GPU: three wavefronts per SIMD, of about
     // 256 coordinates each.
     p.chunk = 128;
-    while (p.chunk > 8 && n / p.chunk * ((d + 255) / 256) < 4096) p.chunk >>= 1;
+    while (p.chunk > 8 && n / p.chunk * ((d + 255) / 256) < 6144) p.chunk >>= 1;
     p.chunks = (u32)((n + p.chunk - 1) / p.chunk);
     p.blocks = (u32)((n + SORT_TILE - 1) / SORT_TILE);
     int bits = 1;
@@ -681,9 +703,10 @@ extern "C" int rnnd_embed_grad(const void *dout, int dtype, const int32_t *ids, 
             s.blocks = p.blocks;
             s.shift = i * p.bits;
             s.bits = p.bits;
+            s.direct = p.blocks <= SORT_DIRECT;
             const u32 clear_blocks = (s.clear_words + 2047) / 2048;
             hipLaunchKernelGGL(k_sort_count, dim3(p.blocks + (clear_blocks < 1024 ? clear_blocks : 1024)), dim3(SORT_THREADS), 0, st, s);
-            hipLaunchKernelGGL(k_sort_offsets, dim3(((1u << p.bits) + 63) / 64), dim3(64 * OFFSET_WAVES), 0, st, s);
+            if (!s.direct) hipLaunchKernelGGL(k_sort_offsets, dim3(((1u << p.bits) + 63) / 64), dim3(64 * OFFSET_WAVES), 0, st, s);
             hipLaunchKernelGGL(k_sort_place, dim3(p.blocks), dim3(SORT_THREADS), 0, st, s);
         }
         g.item = item[at];
