@@ -424,6 +424,97 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int 
     }
 }
 
+// The product of float32 rows, for tiles of 128: the three terms of both operands stand in LDS together, so that six products are
+// made of each step of 32 that is loaded and read once -- with product() each of the six would load and read its two again: 64 operations
+// for a byte instead of 128, and both L2 and LDS were what it waited for.  LDS holds three steps, of which two are under way.
+// The next step's operands are read into registers between the matrix instructions of this one.
+#define CT_K3 32
+struct TermsLds { half_t a[3][3][128 * CT_K3], b[3][3][128 * CT_K3]; };       // [step % 3][term]
+
+template <typename F>
+__device__ __forceinline__ void product_of_terms(const Operand &A, const Operand &B, int row_a, int row_b, int k_begin, int k_end,
+                                                 TermsLds &lds, f32x4 (&acc)[4][4], F meanwhile)
+{
+    struct Step { us8 a[3][4], b[3][4]; };
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int steps = (k_end - k_begin) / CT_K3;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+    // a row's 64 bytes are 4 pieces, piece s of place p at s ^ (p / 2 % 4); each wavefront brings a quarter of the places, 16 at a time
+    int va[2], vb[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int p = (wave * 2 + i) * 16 + (lane >> 2), piece = (lane & 3) ^ (lane >> 3 & 3);
+        va[i] = (row_at<128>(p) * A.ld + piece * 8) * 2;
+        vb[i] = (col_at<128>(p) * B.ld + piece * 8) * 2;
+    }
+    const half_t *pa = A.p + (size_t)row_a * A.ld, *pb = B.p + (size_t)row_b * B.ld;
+    auto fetch = [&](int s, int slot) {         // 12 loads
+        const int at = (k_begin + s * CT_K3) * 2;
+#pragma unroll
+        for (int t = 0; t < 3; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int place = (wave * 2 + i) * 16 * CT_K3;
+                to_lds(pa + t * A.plane, 128 * A.ld * 2, &lds.a[slot][t][place], va[i], at);
+                to_lds(pb + t * B.plane, 128 * B.ld * 2, &lds.b[slot][t][place], vb[i], at);
+            }
+    };
+    const int piece = (lane >> 4 ^ (lane >> 1 & 3)) * 8;
+    const int ra = ((wave >> 1) * 64 + (lane & 15)) * CT_K3 + piece, rb = ((wave & 1) * 64 + (lane & 15)) * CT_K3 + piece;
+    auto read = [&](Step &f, int slot, int i) {
+#pragma unroll
+        for (int t = 0; t < 3; ++t) {
+            f.a[t][i] = *(const us8 *)&lds.a[slot][t][ra + i * 16 * CT_K3];
+            f.b[t][i] = *(const us8 *)&lds.b[slot][t][rb + i * 16 * CT_K3];
+        }
+    };
+    // all wavefronts have read what they held before, and the step that all but the last `left` loads brought is there
+    auto meet = [&](int left) {
+        if (left == 24) asm volatile("s_waitcnt vmcnt(24) lgkmcnt(0)" ::: "memory");
+        else if (left == 12) asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    int slot = 0;
+    auto step = [&](const Step &now, Step &next, int s) {
+        const int ahead = slot == 2 ? 0 : slot + 1;
+        if (s + 1 < steps) {
+            meet(s + 2 < steps ? 12 : 0);
+            if (s + 3 < steps) fetch(s + 3, slot);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            read(next, ahead, i);       // (behind the last step: what nobody uses)
+#pragma unroll
+            for (int pair = 0; pair < 6; ++pair) {      // (0, 0) (0, 1) (1, 0) (1, 1) (0, 2) (2, 0)
+                const int ta = pair == 2 || pair == 3 ? 1 : pair == 5 ? 2 : 0, tb = pair == 1 || pair == 3 ? 1 : pair == 4 ? 2 : 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = mfma<DT_BF16>(now.a[ta][i], now.b[tb][j], acc[i][j]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        slot = ahead;
+    };
+    fetch(0, 0);
+    if (steps > 1) fetch(1, 1);
+    if (steps > 2) fetch(2, 2);
+    meanwhile();
+    meet(steps > 2 ? 24 : steps > 1 ? 12 : 0);
+    Step even, odd;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) read(even, 0, i);
+    for (int s = 0;;) {
+        step(even, odd, s);
+        if (++s == steps) break;
+        step(odd, even, s);
+        if (++s == steps) break;
+    }
+}
+
 // Neighbouring tiles to the same XCD (workgroups go round the 8 of them), in blocks of 8 rows of tiles, so that what
 // its L2 holds serves several of them.
 __device__ __forceinline__ void tile_of(int id, int tiles_r, int tiles_c, int &r, int &c)
@@ -517,6 +608,16 @@ template <int TILE> __device__ __forceinline__ void load_side(const ContrastPar 
     if (t < TILE) side.maybe[t] = (side.seen[id_hash(out.x) >> 5] >> (id_hash(out.x) & 31) | side.seen[id_hash(out.y) >> 5] >> (id_hash(out.y) & 31)) & 1;
 }
 
+// q k' of a tile, its side tables read meanwhile
+template <int TILE, int DT, bool TERMS, typename LDS>
+__device__ __forceinline__ void logit_product(const ContrastPar &c, int tr, int tc, LDS &lds, SideLds<TILE> &side, f32x4 (&acc)[TILE / 32][TILE / 32])
+{
+    const Operand q = {c.q, c.plane_q, c.dp}, k = {c.k, c.plane_k, c.dp};
+    const auto tables = [&]() { load_side(c, side, tr * TILE, tc * TILE); };
+    if constexpr (TERMS) product_of_terms(q, k, tr * TILE, tc * TILE, 0, c.dp, lds, acc, tables);
+    else product<TILE, DT>(q, k, tr * TILE, tc * TILE, 0, c.dp, lds, acc, tables);
+}
+
 // Logits of the keys that rows leave out become -infinity; nothing to do for most rows.
 template <int TILE, int R, int N>
 __device__ __forceinline__ void leave_out(const SideLds<TILE> &side, int row, const int (&id)[N], float (&s)[R][N])
@@ -534,17 +635,16 @@ __device__ __forceinline__ void leave_out(const SideLds<TILE> &side, int row, co
 }
 
 // ------------------------------------------------------------------------------------------------ first product: largest and sum of every row
-template <int TILE, int DT>
-__global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_sums(ContrastPar c, int tiles_q, int tiles_k)
+template <int TILE, int DT, bool TERMS>
+__global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_contrast_sums(ContrastPar c, int tiles_q, int tiles_k)
 {
     constexpr int N = TILE / 32;
-    __shared__ ProductLds<TILE> lds;
+    __shared__ typename std::conditional<TERMS, TermsLds, ProductLds<TILE>>::type lds;
     __shared__ SideLds<TILE> side;
     f32x4 acc[N][N];
     int tr, tc;
     tile_of(blockIdx.x, tiles_q, tiles_k, tr, tc);
-    product<TILE, DT>({c.q, c.plane_q, c.dp}, {c.k, c.plane_k, c.dp}, tr * TILE, tc * TILE, 0, c.dp, lds, acc,
-                      [&]() { load_side(c, side, tr * TILE, tc * TILE); });
+    logit_product<TILE, DT, TERMS>(c, tr, tc, lds, side, acc);
     const Place<TILE> at(tr, tc);
     float base[N];
     int id[N];
@@ -646,17 +746,16 @@ __global__ __launch_bounds__(256) void k_contrast_loss(ContrastPar c, int row_bl
 }
 
 // ------------------------------------------------------------------------------------------------ second product: g
-template <int TILE, int DT>
-__global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_g(ContrastPar c, int tiles_q, int tiles_k)
+template <int TILE, int DT, bool TERMS>
+__global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_contrast_g(ContrastPar c, int tiles_q, int tiles_k)
 {
     constexpr int N = TILE / 32, PLANES = planes_of<DT>();
-    __shared__ ProductLds<TILE> lds;
+    __shared__ typename std::conditional<TERMS, TermsLds, ProductLds<TILE>>::type lds;
     __shared__ SideLds<TILE> side;
     f32x4 acc[N][N];
     int tr, tc;
     tile_of(blockIdx.x, tiles_q, tiles_k, tr, tc);
-    product<TILE, DT>({c.q, c.plane_q, c.dp}, {c.k, c.plane_k, c.dp}, tr * TILE, tc * TILE, 0, c.dp, lds, acc,
-                      [&]() { load_side(c, side, tr * TILE, tc * TILE); });
+    logit_product<TILE, DT, TERMS>(c, tr, tc, lds, side, acc);
     const Place<TILE> at(tr, tc);
     float base[N], col_sum[N] = {};
     int id[N];
@@ -760,10 +859,10 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_g(Contras
 // ------------------------------------------------------------------------------------------------ third and fourth: g k and g' q
 // One launch: the parts of dq's sums, then those of dk's.
 template <int TILE, int DT>
-__global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_grad(ContrastPar c, int tiles_q, int tiles_k, int tiles_d)
+__global__ __launch_bounds__(256, TILE == 256 || DT == DT_F32 ? 1 : 2) void k_contrast_grad(ContrastPar c, int tiles_q, int tiles_k, int tiles_d)
 {
     constexpr int N = TILE / 32;
-    __shared__ ProductLds<TILE> lds;
+    __shared__ typename std::conditional<DT == DT_F32, TermsLds, ProductLds<TILE>>::type lds;
     f32x4 acc[N][N];
     const int of_q = tiles_q * tiles_d * c.splits_q;
     const bool keys = (int)blockIdx.x >= of_q;
@@ -775,7 +874,8 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void k_contrast_grad(Cont
     const int k0 = (int)((long long)steps * split / splits) * CT_K, k1 = (int)((long long)steps * (split + 1) / splits) * CT_K;
     const Operand a = keys ? Operand{c.gt, c.plane_gt, c.ld_gt} : Operand{c.g, c.plane_g, c.ld_g};
     const Operand b = keys ? Operand{c.qt, c.plane_qt, c.Bp} : Operand{c.kt, c.plane_kt, c.Mp};
-    product<TILE, DT>(a, b, tr * TILE, tc * TILE, k0, k1, lds, acc, []() {});
+    if constexpr (DT == DT_F32) product_of_terms(a, b, tr * TILE, tc * TILE, k0, k1, lds, acc, []() {});
+    else product<TILE, DT>(a, b, tr * TILE, tc * TILE, k0, k1, lds, acc, []() {});
     const Place<TILE> at(tr, tc);
     const size_t rows = (size_t)((keys ? c.M : c.B) + CT_PAD - 1) / CT_PAD * CT_PAD;
     float *out = (keys ? c.acc_k : c.acc_q) + (size_t)split * rows * c.dr;
@@ -900,7 +1000,10 @@ static double makespan(double a, long long na, double b, long long nb, int slots
     return t;
 }
 
-struct ContrastPlan { int tile, tile_g; };
+struct ContrastPlan {
+    int tile, tile_g;
+    bool terms;     // float32 rows: logits by product_of_terms()
+};
 
 // Tiles of 256 keep the matrix cores busier (see product()), tiles of 128 spread small problems over more CUs.
 static ContrastPlan contrast_plan(ContrastPar &c, int planes)
@@ -911,9 +1014,14 @@ static ContrastPlan contrast_plan(ContrastPar &c, int planes)
     // of 8,192 x 16,384, tiles of 128 / 256, us: d = 64 216 / 266, 256 349 / 357, 768 635 / 604, 1,536 1,035 / 944; of 1,000 x 11,000: d = 768
     // 69 / 76 (172 tiles of 256 for 256 CUs), 1,536 117 / 119
     p.tile = planes == 1 && c.d > 384 && tiles(c.B, 256) * tiles(c.M, 256) >= 512 ? 256 : 128;
+    // float32 rows: product_of_terms() takes the LDS of a CU, so a second workgroup no longer works on its logits meanwhile.  It is ahead
+    // where rows are long or every workgroup has a CU of its own.  The whole call with two workgroups / with the terms together, us:
+    // 3,000 x 12,000, d = 32 332 / 361, 128 381 / 415, 256 586 / 599, 384 807 / 799, 768 1,501 / 1,412; 2,200 x 2,200 x 128 (324 tiles)
+    // 83 / 94, 700 x 4,000 x 300 (192 tiles) 119 / 101, 100 x 1,100 x 32 49.0 / 45.6
+    p.terms = planes == 3 && (c.d > 320 || tiles(c.B, 128) * tiles(c.M, 128) <= 256);
     // the gradient products: also by how much of the last tile of d would be padding
     const int d128 = ct_up(c.d, 128), d256 = ct_up(c.d, 256);
-    p.tile_g = (tiles(c.B, 256) + tiles(c.M, 256)) * (d256 / 256) >= 64 && d256 * 4 <= d128 * 5 ? 256 : 128;
+    p.tile_g = planes == 1 && (tiles(c.B, 256) + tiles(c.M, 256)) * (d256 / 256) >= 64 && d256 * 4 <= d128 * 5 ? 256 : 128;
     c.dp = ct_up(c.d, CT_K);
     c.Bp = ct_up(c.B, CT_K);
     c.Mp = ct_up(c.M, CT_K);
@@ -929,7 +1037,7 @@ static ContrastPlan contrast_plan(ContrastPar &c, int planes)
     for (int sq : choices)
         for (int sk : choices) {
             if ((sq > 1 && sq > c.Mp / CT_K) || (sk > 1 && sk > c.Bp / CT_K)) continue;
-            const double t = makespan((double)steps_q / sq + 24, tq * sq, (double)steps_k / sk + 24, tk * sk, p.tile_g == 256 ? 256 : 512);
+            const double t = makespan((double)steps_q / sq + 24, tq * sq, (double)steps_k / sk + 24, tk * sk, p.tile_g == 256 || planes == 3 ? 256 : 512);
             if (t < best * 0.999) {
                 best = t;
                 c.splits_q = sq;
@@ -1002,14 +1110,14 @@ extern "C" int rnnd_contrast_workspace(int64_t B, int64_t M, int32_t d, int dtyp
     return RNND_OK;
 }
 
-template <int DT, int TILE>
+template <int DT, int TILE, bool TERMS>
 static void launch_products(ContrastPar &c, int want_grad, int row_blocks, hipStream_t st)
 {
     static_assert(DT != DT_F32 || TILE == 128, "g of three planes takes more registers than tiles of 256 leave");
     const int tq = ct_up(c.B, TILE) / TILE, tk = ct_up(c.M, TILE) / TILE;
-    hipLaunchKernelGGL((k_contrast_sums<TILE, DT>), dim3((u32)tq * tk), dim3(256), 0, st, c, tq, tk);
+    hipLaunchKernelGGL((k_contrast_sums<TILE, DT, TERMS>), dim3((u32)tq * tk), dim3(256), 0, st, c, tq, tk);
     hipLaunchKernelGGL(k_contrast_loss<DT>, dim3((c.B + 3) / 4), dim3(256), 0, st, c, row_blocks);
-    if (want_grad) hipLaunchKernelGGL((k_contrast_g<TILE, DT>), dim3((u32)tq * tk), dim3(256), 0, st, c, tq, tk);
+    if (want_grad) hipLaunchKernelGGL((k_contrast_g<TILE, DT, TERMS>), dim3((u32)tq * tk), dim3(256), 0, st, c, tq, tk);
 }
 template <int DT, int TILE>
 static void launch_grads(ContrastPar &c, hipStream_t st)
@@ -1028,13 +1136,16 @@ static void launch_contrast(ContrastPar &c, const ContrastPlan &plan, int want_g
     hipLaunchKernelGGL((k_contrast_prepare<DT, WIDE>), dim3((u32)(key_blocks + row_blocks) + (u32)((Br + Mr) / 64) * across), dim3(256), 0, st, c,
                        key_blocks, row_blocks, Br / 64, across, want_grad);
     if constexpr (DT != DT_F32) {
-        if (plan.tile == 256) launch_products<DT, 256>(c, want_grad, row_blocks, st);
-        else launch_products<DT, 128>(c, want_grad, row_blocks, st);
-    } else
-        launch_products<DT, 128>(c, want_grad, row_blocks, st);
+        if (plan.tile == 256) launch_products<DT, 256, false>(c, want_grad, row_blocks, st);
+        else launch_products<DT, 128, false>(c, want_grad, row_blocks, st);
+    } else if (plan.terms) launch_products<DT, 128, true>(c, want_grad, row_blocks, st);
+    else launch_products<DT, 128, false>(c, want_grad, row_blocks, st);
     if (!want_grad) return;
-    if (plan.tile_g == 256) launch_grads<DT, 256>(c, st);
-    else launch_grads<DT, 128>(c, st);
+    if constexpr (DT != DT_F32) {
+        if (plan.tile_g == 256) launch_grads<DT, 256>(c, st);
+        else launch_grads<DT, 128>(c, st);
+    } else
+        launch_grads<DT, 128>(c, st);
     hipLaunchKernelGGL((k_contrast_finish<DT, WIDE>), dim3((c.B + c.M + 3) / 4), dim3(256), 0, st, c);
 }
 

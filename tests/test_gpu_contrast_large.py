@@ -75,3 +75,9 @@ def test_wide_tiles(rn, dtype, B, M, d):
         # and as a whole: roundings do not all point the same way
         assert off.norm() <= 1.5 * max(h, 1e-6) * exact.norm() + floor
     assert (loss[~counts] == 0).all() and (dq[~counts] == 0).all() and (dk[gone] == 0).all()
+
+
+@pytest.mark.parametrize("B,M,d", [(2050, 4200, 72), (1100, 8300, 320), (2050, 4200, 321), (4300, 2100, 5)])
+def test_float32_rows_by_either_product(rn, B, M, d):
+    """More than 256 tiles of 128: rows of up to 320 coordinates take two workgroups a CU, longer ones all terms of a step at once."""
+    test_wide_tiles(rn, "float32", B, M, d)
