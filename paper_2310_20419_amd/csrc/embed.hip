@@ -518,17 +518,18 @@ __global__ __launch_bounds__(256) void k_grad_small(GradPar g, const int *__rest
         earlier |= same && i * 256 + tid < t;
     }
     if (__syncthreads_or(earlier)) return;
-    u32 count = 0;
-    for (u32 w = t >> 6; w < (g.n + 63) / 64; ++w) count += __popcll(mask[w]);
+    // a word's tokens follow those of the words before it: sums over the lanes, a word each
+    static_assert(SMALL_TOKENS <= 64 * 64, "a word for each lane");
+    const u32 mine = lane < (g.n + 63) / 64 ? __popcll(mask[lane]) : 0, upto = wave_inclusive(mine, lane);
+    const u32 count = __builtin_amdgcn_readlane(upto, 63);
     if (count > 1) {
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i)
-            if (id[i] == key) {
-                const u32 word = i * 4 + (tid >> 6);
-                u32 rank = __popcll(mask[word] & lanes_below(lane));
-                for (u32 w = t >> 6; w < word; ++w) rank += __popcll(mask[w]);
-                list[rank] = (unsigned short)(i * 256 + tid);
-            }
+        for (int i = 0; i < ITEMS; ++i) {
+            const u32 word = i * 4 + (tid >> 6);
+            const u64 all = __ballot(id[i] == key);
+            const u32 before = __builtin_amdgcn_readlane(upto - mine, __builtin_amdgcn_readfirstlane(word));
+            if (id[i] == key) list[before + __popcll(all & lanes_below(lane))] = (unsigned short)(i * 256 + tid);
+        }
         __syncthreads();
     }
     const u32 group = tid >> log_lanes, at = tid & (lanes - 1);
