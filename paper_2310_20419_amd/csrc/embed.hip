@@ -469,10 +469,11 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_grad_join(GradPar g)
 // Few tokens: one launch, without a sort.  A block for each token looks through all ids; if an earlier token has the same id that token's
 // block sums them, else this one does: it lists the tokens of its id in order, its groups of G lanes sum pieces of the list, and
 // their sums are added in the groups' order.  The ids are a few KB that every block finds in its L2 -- 4,096 blocks read 64 MB of
-// them, 2 us -- where a sort and its joins are five launches that wait for each other.  Blocks behind the first reduce_blocks clear
-// clear_rows rows each, but for those that an id names.
+// them -- where a sort and its joins are four launches at least that wait for each other: 1,000 x 32 10.5 us (18 sorted), 4,096 x 32 10.4
+// (36), 4,096 x 768 f32 into 30,000 rows 32 (44).  The looking grows with the square of the tokens: 8,192 x 32 took 30 us, 8,192 x 768
+// 94, sorted 32 and 44.  Blocks behind the first reduce_blocks clear clear_rows rows each, but for those that an id names.
 #define SMALL_TOKENS 4096
-#define SMALL_SLABS 4           // blocks of a token, at most
+#define SMALL_SLABS 4           // blocks of a token, at most (more than 1,024 tokens fill the GPU with one each)
 #define SMALL_CLEAR 8192        // rows of a block that clears, at most
 
 template <int DT, int GT, int VEC>
@@ -629,7 +630,7 @@ static void launch_grad_vec(GradPar &g, int d, const int32_t *small_ids, hipStre
         u32 log_lanes = 3;
         while (log_lanes < 6 && (1u << log_lanes) < g.pieces) ++log_lanes;
         g.slabs = (g.pieces + (1u << log_lanes) - 1) >> log_lanes;
-        const u32 token_blocks = g.slabs < SMALL_SLABS ? g.slabs : SMALL_SLABS;
+        const u32 token_blocks = g.n > 1024 ? 1 : g.slabs < SMALL_SLABS ? g.slabs : SMALL_SLABS;
         g.reduce_blocks = g.n * token_blocks;
         // 512 to 8,192 pieces for a block that clears: enough blocks, and each writes more than it reads of ids
         u32 pieces = 512;
