@@ -401,22 +401,22 @@ def _row_type(t, what):
         raise ValueError("%s must be float32, float16 or bfloat16, not %s" % (what, t)) from None
 
 
-def _need(ok, message):
+def _need(ok, message, *values):
     if not ok:
-        raise ValueError(message)
+        raise ValueError(message % values)
 
 
 def _rows(x, what, d=None):
-    _need(x.is_cuda and x.dim() == 2 and x.is_contiguous(), "%s must be a contiguous 2-D tensor in device memory" % what)
-    _need(d is None or x.shape[1] == d, "%s must have rows of %s coordinates" % (what, d))
+    _need(x.is_cuda and x.dim() == 2 and x.is_contiguous(), "%s must be a contiguous 2-D tensor in device memory", what)
+    _need(d is None or x.shape[1] == d, "%s must have rows of %s coordinates", what, d)
     return _row_type(x.dtype, what)
 
 
 def _vector(x, what, n, dtype, device):
     if x is None:
         return None
-    _need(x.is_cuda and x.device == device and x.dim() == 1 and x.is_contiguous() and x.dtype == dtype and (n is None or x.shape[0] == n),
-          "%s must be a contiguous %s vector%s on the same device" % (what, dtype, "" if n is None else " of %d" % n))
+    if not (x.is_cuda and x.device == device and x.dim() == 1 and x.is_contiguous() and x.dtype == dtype and (n is None or x.shape[0] == n)):
+        raise ValueError("%s must be a contiguous %s vector%s on the same device" % (what, dtype, "" if n is None else " of %d" % n))
     return x.data_ptr()
 
 
@@ -558,16 +558,14 @@ class AdamwTensors:
         for i, t in enumerate(self.kept):
             if not t.keys() <= _ADAMW_KEYS:
                 raise ValueError("tensor %d: unknown %s" % (i, sorted(t.keys() - _ADAMW_KEYS)))
-            p, g, m, v = given = [t[k] for k in names[:4]]
-            ms, vs, copy = rest = [t.get(k) for k in names[4:]]
+            p, g, m, v = t["param"], t["grad"], t["m"], t["v"]
+            ms, vs, copy = t.get("m_scale"), t.get("v_scale"), t.get("copy")
             n, eight = p.numel(), m.element_size() == 1
             if self.device is None:
-                self.device = p.device
-            for name, x in zip(names, given + rest):
-                if x is None:
-                    continue
-                count = n if name in ("param", "grad", "m", "v", "copy") else -(-n // 128)
-                if not (x.is_cuda and x.device == self.device and x.is_contiguous() and x.numel() == count):
+                self.device, index = p.device, p.get_device()
+            blocks = -(-n // 128)
+            for name, x, count in zip(names, (p, g, m, v, ms, vs, copy), (n, n, n, n, blocks, blocks, n)):
+                if x is not None and not (x.get_device() == index >= 0 and x.numel() == count and x.is_contiguous()):
                     raise ValueError("tensor %d: %s must be %d contiguous elements on one device" % (i, name, count))
             if p.dtype != torch.float32:
                 raise ValueError("tensor %d: param must be float32" % i)

@@ -5,7 +5,10 @@
 //
 // Every element is read and written once and nothing is shared between elements but the scale of a block of 8-bit states:
 // the step is bound by memory.  Bytes an element (float32 parameters and gradients, no copy): 32-bit states 16 read + 12
-// written, 8-bit states 10 + 6.  All arithmetic is float32; the constants of a step are formed on the host in double.
+// written, 8-bit states 10 + 6.  All arithmetic is float32; the constants of a step are formed on the host in double.  300,000 x 768
+// elements with 8-bit states, bfloat16 gradients and copy: 3.7 GB in 0.74-0.79 ms (4.7-5.0 TB/s; a large copy makes 5.2); 61 tensors of 8M elements
+// together, 32 bits: 224 MB in 53 us, one launch (4.2 TB/s).  A workgroup takes 2,048 elements of one tensor, which it finds in
+// descriptors that come as an argument, so that no table has to be copied to the device first.
 //
 // 8-bit states: m and the root of v as e4m3 codes, with one power of two for each 128 elements.  The update of p uses the new
 // m and v before they are rounded.  A root changes by 0.05 % a step, far less than the distance of two codes: rounded to
