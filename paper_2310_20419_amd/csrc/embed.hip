@@ -312,8 +312,8 @@ __global__ __launch_bounds__(SORT_THREADS) void k_sort_place(SortPass s)
 // through, whatever the length of a row), and sums the rows of one id after the other.  An id whose tokens end at most one chunk behind the chunk they start in is summed by
 // that chunk's lanes alone (they read on, and the next chunk's leave them out).  A longer one -- words as frequent as "the" --
 // leaves one partial sum per chunk, which k_grad_join adds in order, a whole block for each such id and slab.
-// Bound by memory, but for the sort before it (two passes for 300,000 or 1,000,000 rows): 1,000,000 x 96 float32 257 us, of which the sums
-// are 189 (768 MB, 4.1 TB/s) and the sort 63; 100,003 x 768 bfloat16 added to 300,000 float32 rows 145 us, sums 83, sort 33.
+// Bound by memory, but for the sort before it (two passes for 300,000 or 1,000,000 rows): 1,000,000 x 96 float32 235 us, of which the sums
+// are 168 (768 MB, 4.6 TB/s) and the sort 63; 100,003 x 768 bfloat16 added to 300,000 float32 rows 145 us, sums 83, sort 33.
 #define GRAD_UNROLL 8       // divides every chunk
 #define GRAD_SLOTS 2        // partial sums of a chunk: 0 = of an id that started before it, 1 = of the id that goes on after it
 #define JOIN_THREADS 512
@@ -376,16 +376,25 @@ __global__ __launch_bounds__(256) void k_grad_reduce(GradPar g)
 
     float acc[VEC] = {};
     bool some = false;
+    // the next tokens' names are fetched behind this trip's rows: a trip waits for one latency, not for two (1,000,000 x 96: 189 -> 168 us)
+    uint2 ahead[GRAD_UNROLL];
+#pragma unroll
+    for (int i = 0; i < GRAD_UNROLL; ++i) ahead[i] = g.item[begin + i < stop ? begin + i : stop - 1];
     for (u32 t = begin; t < stop; t += GRAD_UNROLL) {
         uint2 it[GRAD_UNROLL];
         Pack<DT, VEC> row[GRAD_UNROLL];
 #pragma unroll
-        for (int i = 0; i < GRAD_UNROLL; ++i) it[i] = g.item[t + i < stop ? t + i : stop - 1];
+        for (int i = 0; i < GRAD_UNROLL; ++i) it[i] = ahead[i];
 #pragma unroll
         for (int i = 0; i < GRAD_UNROLL; ++i) {
             const u32 at = t + i;
             if (at >= stop || (at >= end && it[i].x != last)) it[i].x = 0xFFFFFFFFu;      // nothing there for this chunk
             if (it[i].x < g.V && !(skip && first && it[i].x == id)) row[i] = load_pack<DT, VEC>(g.dout, ((u64)it[i].y * g.pieces + piece) * VEC);
+        }
+#pragma unroll
+        for (int i = 0; i < GRAD_UNROLL; ++i) {
+            const u32 at = t + GRAD_UNROLL + i;
+            ahead[i] = g.item[at < stop ? at : stop - 1];
         }
         bool done = false;
 #pragma unroll
