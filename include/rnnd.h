@@ -309,7 +309,7 @@ int rnnd_set_scan_launches(int mode);
  * Memory they work in is the caller's `workspace` (device, 16-byte aligned, as many bytes as the call's _workspace query
  * says, else RNND_ERR_SCRATCH; contents arbitrary; free for other use when the call's work on `stream` is done).
  * Pointers must be aligned to their elements (else RNND_ERR_BAD_PARAM); rows whose address and length allow 16-byte
- * accesses are faster.  Inputs and outputs must not overlap unless stated.  All sums are float32 and in an order that the
+ * accesses are faster.  Inputs and outputs must not overlap unless stated.  All sums are float32 and in an order that ids and
  * sizes alone decide: the same call gives the same bits. */
 #define RNND_MAX_ROW 65536          /* coordinates of a row */
 #define RNND_MAX_CONTRAST 1048576   /* queries and keys of rnnd_contrast */
