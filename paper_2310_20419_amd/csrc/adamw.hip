@@ -270,33 +270,31 @@ static void launch_adamw(const rnnd_adamw_tensor *tensors, int32_t count, const 
     a.rate = s.rate;
     a.root_scale = s.root_scale;
     a.eps = s.eps;
-    for (int32_t i = 0; i < count;) {
-        u64 tiles = 0;
-        a.count = 0;
-        for (; i < count && a.count < (u32)a.TENSORS; ++i) {
-            const rnnd_adamw_tensor &t = tensors[i];
-            if (t.state_bits != (EIGHT ? 8 : 32) || !t.n) continue;
-            const u64 more = ((u64)t.n + ADAMW_TILE - 1) / ADAMW_TILE;
-            if (tiles + more > 0x7FFFFFFFull) break;
-            AdamwTensor<EIGHT> &d = a.t[a.count++];
-            d.param = t.param;
-            d.grad = t.grad;
-            d.m_data = t.m;
-            d.v_data = t.v;
-            d.copy = t.copy;
-            if constexpr (EIGHT) {
-                d.m = t.m_scale;
-                d.v = t.v_scale;
-                d.counter = t.counter;
-            }
-            uintptr_t low = (uintptr_t)t.param | (uintptr_t)t.grad | (uintptr_t)t.copy;     // 16 bytes an access
-            low |= EIGHT ? ((uintptr_t)t.m | (uintptr_t)t.v) << 1 : (uintptr_t)t.m | (uintptr_t)t.v;    // codes: 8
-            d.n_types = (u64)t.n | (u64)t.grad_dtype << 48 | (u64)(t.copy ? t.copy_dtype : 0) << 52 | (u64)(low % 16 == 0) << 56;
-            d.first_tile = (u32)tiles;
-            tiles += more;
+    auto length = [&](int32_t i) { return tensors[i].state_bits == (EIGHT ? 8 : 32) ? (u64)tensors[i].n : 0; };
+    a.count = 0;
+    // a part starts at a multiple of a tile, so that its arrays are aligned as the tensor's are and its blocks of 128 are the tensor's
+    auto part = [&](int32_t i, u64 first, u64 n, u64 tiles) {
+        const rnnd_adamw_tensor &t = tensors[i];
+        AdamwTensor<EIGHT> &d = a.t[a.count++];
+        d.param = t.param + first;
+        d.grad = (const char *)t.grad + first * dt_size(t.grad_dtype);
+        d.m_data = (char *)t.m + first * (EIGHT ? 1 : 4);
+        d.v_data = (char *)t.v + first * (EIGHT ? 1 : 4);
+        d.copy = t.copy ? (char *)t.copy + first * 2 : nullptr;
+        if constexpr (EIGHT) {
+            d.m = t.m_scale + first / ADAMW_BLOCK;
+            d.v = t.v_scale + first / ADAMW_BLOCK;
+            d.counter = t.counter + first;
         }
-        if (a.count) hipLaunchKernelGGL(k_adamw<EIGHT>, dim3((u32)tiles), dim3(256), 0, st, a);
-    }
+        uintptr_t low = (uintptr_t)t.param | (uintptr_t)t.grad | (uintptr_t)t.copy;     // 16 bytes an access
+        low |= EIGHT ? ((uintptr_t)t.m | (uintptr_t)t.v) << 1 : (uintptr_t)t.m | (uintptr_t)t.v;    // codes: 8
+        d.n_types = n | (u64)t.grad_dtype << 48 | (u64)(t.copy ? t.copy_dtype : 0) << 52 | (u64)(low % 16 == 0) << 56;
+        d.first_tile = (u32)tiles;
+    };
+    cut_into_launches(count, ADAMW_TILE, most_blocks(256), a.TENSORS, length, part, [&](u64 tiles) {
+        hipLaunchKernelGGL(k_adamw<EIGHT>, dim3((u32)tiles), dim3(256), 0, st, a);
+        a.count = 0;
+    });
 }
 
 extern "C" int rnnd_adamw(const rnnd_adamw_tensor *tensors, int32_t count, int64_t step, double lr, double beta1, double beta2,

@@ -105,18 +105,18 @@ __device__ __forceinline__ void load4(const void *rows, size_t row, int d, int e
 
 // A wavefront per row: keys first, then queries.  A key's own part of its logits, a query's logit of its target.
 template <int DT, bool WIDE>
-__device__ __forceinline__ void contrast_rows(const ContrastPar &c, int key_blocks, int row_blocks)
+__device__ __forceinline__ void contrast_rows(const ContrastPar &c, int block, int key_blocks, int row_blocks)
 {
     __shared__ u32 most;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const bool keys = (int)blockIdx.x < key_blocks;
+    const bool keys = block < key_blocks;
     if (DT == DT_F16 && !keys) {        // (a whole block)
         if (threadIdx.x == 0) most = 0;
         __syncthreads();
     }
     const int blocks = keys ? key_blocks : row_blocks;
     const int padded = ((keys ? c.M : c.B) + CT_PAD - 1) / CT_PAD * CT_PAD;
-    for (int at = ((int)blockIdx.x - (keys ? 0 : key_blocks)) * 4 + wave; at < padded; at += blocks * 4) {
+    for (int at = (block - (keys ? 0 : key_blocks)) * 4 + wave; at < padded; at += blocks * 4) {
         if (keys) {
             const bool gone = at >= c.M || key_gone(c, at);
             float sum = 0.0f;
@@ -170,7 +170,7 @@ __device__ __forceinline__ void contrast_rows(const ContrastPar &c, int key_bloc
     }
     if (DT == DT_F16 && !keys) {
         __syncthreads();
-        if (threadIdx.x == 0) c.tops[(int)blockIdx.x - key_blocks] = most;
+        if (threadIdx.x == 0) c.tops[block - key_blocks] = most;
     }
 }
 
@@ -255,12 +255,13 @@ __device__ __forceinline__ void contrast_copy(const ContrastPar &c, int tile_r, 
     }
 }
 
-// Both in one launch (neither reads what the other writes): small calls are bound by the number of dependent launches.
+// Both in one launch (neither reads what the other writes): small calls are bound by the number of dependent launches.  first: here and
+// below, how many blocks earlier launches took (in_launches()).
 template <int DT, bool WIDE>
-__global__ __launch_bounds__(256) void k_contrast_prepare(ContrastPar c, int key_blocks, int row_blocks, int q_tiles, int across, int columns)
+__global__ __launch_bounds__(256) void k_contrast_prepare(ContrastPar c, u32 first, int key_blocks, int row_blocks, int q_tiles, int across, int columns)
 {
-    const int id = (int)blockIdx.x - key_blocks - row_blocks;
-    if (id < 0) contrast_rows<DT, WIDE>(c, key_blocks, row_blocks);
+    const int block = (int)(first + blockIdx.x), id = block - key_blocks - row_blocks;
+    if (id < 0) contrast_rows<DT, WIDE>(c, block, key_blocks, row_blocks);
     else contrast_copy<DT, WIDE>(c, id / across, id % across * 64, q_tiles, columns);
 }
 
@@ -643,14 +644,14 @@ __device__ __forceinline__ void leave_out(const SideLds<TILE> &side, int row, co
 
 // ------------------------------------------------------------------------------------------------ first product: largest and sum of every row
 template <int TILE, int DT, bool TERMS>
-__global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_contrast_sums(ContrastPar c, int tiles_q, int tiles_k)
+__global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_contrast_sums(ContrastPar c, u32 first, int tiles_q, int tiles_k)
 {
     constexpr int N = TILE / 32;
     __shared__ typename std::conditional<TERMS, TermsLds, ProductLds<TILE>>::type lds;
     __shared__ SideLds<TILE> side;
     f32x4 acc[N][N];
     int tr, tc;
-    tile_of(blockIdx.x, tiles_q, tiles_k, tr, tc);
+    tile_of((int)(first + blockIdx.x), tiles_q, tiles_k, tr, tc);
     logit_product<TILE, DT, TERMS>(c, tr, tc, lds, side, acc);
     const Place<TILE> at(tr, tc);
     float base[N];
@@ -754,14 +755,14 @@ __global__ __launch_bounds__(256) void k_contrast_loss(ContrastPar c, int row_bl
 
 // ------------------------------------------------------------------------------------------------ second product: g
 template <int TILE, int DT, bool TERMS>
-__global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_contrast_g(ContrastPar c, int tiles_q, int tiles_k)
+__global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_contrast_g(ContrastPar c, u32 first, int tiles_q, int tiles_k)
 {
     constexpr int N = TILE / 32, PLANES = planes_of<DT>();
     __shared__ typename std::conditional<TERMS, TermsLds, ProductLds<TILE>>::type lds;
     __shared__ SideLds<TILE> side;
     f32x4 acc[N][N];
     int tr, tc;
-    tile_of(blockIdx.x, tiles_q, tiles_k, tr, tc);
+    tile_of((int)(first + blockIdx.x), tiles_q, tiles_k, tr, tc);
     logit_product<TILE, DT, TERMS>(c, tr, tc, lds, side, acc);
     const Place<TILE> at(tr, tc);
     float base[N], col_sum[N] = {};
@@ -866,14 +867,15 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_contrast_
 // ------------------------------------------------------------------------------------------------ third and fourth: g k and g' q
 // One launch: the parts of dq's sums, then those of dk's.
 template <int TILE, int DT>
-__global__ __launch_bounds__(256, TILE == 256 || DT == DT_F32 ? 1 : 2) void k_contrast_grad(ContrastPar c, int tiles_q, int tiles_k, int tiles_d)
+__global__ __launch_bounds__(256, TILE == 256 || DT == DT_F32 ? 1 : 2) void k_contrast_grad(ContrastPar c, u32 first, int tiles_q, int tiles_k, int tiles_d)
 {
     constexpr int N = TILE / 32;
     __shared__ typename std::conditional<DT == DT_F32, TermsLds, ProductLds<TILE>>::type lds;
     f32x4 acc[N][N];
     const int of_q = tiles_q * tiles_d * c.splits_q;
-    const bool keys = (int)blockIdx.x >= of_q;
-    const int id = keys ? blockIdx.x - of_q : blockIdx.x, tiles = keys ? tiles_k : tiles_q, splits = keys ? c.splits_k : c.splits_q;
+    const int block = (int)(first + blockIdx.x);
+    const bool keys = block >= of_q;
+    const int id = keys ? block - of_q : block, tiles = keys ? tiles_k : tiles_q, splits = keys ? c.splits_k : c.splits_q;
     const int split = id / (tiles * tiles_d);
     int tr, tc;
     tile_of(id - split * tiles * tiles_d, tiles, tiles_d, tr, tc);
@@ -1122,15 +1124,22 @@ static void launch_products(ContrastPar &c, int want_grad, int row_blocks, hipSt
 {
     static_assert(DT != DT_F32 || TILE == 128, "g of three planes takes more registers than tiles of 256 leave");
     const int tq = ct_up(c.B, TILE) / TILE, tk = ct_up(c.M, TILE) / TILE;
-    hipLaunchKernelGGL((k_contrast_sums<TILE, DT, TERMS>), dim3((u32)tq * tk), dim3(256), 0, st, c, tq, tk);
+    in_launches((u64)tq * tk, 256, [&](u64 first, u64 blocks) {
+        hipLaunchKernelGGL((k_contrast_sums<TILE, DT, TERMS>), dim3((u32)blocks), dim3(256), 0, st, c, (u32)first, tq, tk);
+    });
     hipLaunchKernelGGL(k_contrast_loss<DT>, dim3((c.B + 3) / 4), dim3(256), 0, st, c, row_blocks);
-    if (want_grad) hipLaunchKernelGGL((k_contrast_g<TILE, DT, TERMS>), dim3((u32)tq * tk), dim3(256), 0, st, c, tq, tk);
+    if (!want_grad) return;
+    in_launches((u64)tq * tk, 256, [&](u64 first, u64 blocks) {
+        hipLaunchKernelGGL((k_contrast_g<TILE, DT, TERMS>), dim3((u32)blocks), dim3(256), 0, st, c, (u32)first, tq, tk);
+    });
 }
 template <int DT, int TILE>
 static void launch_grads(ContrastPar &c, hipStream_t st)
 {
     const int tq = ct_up(c.B, TILE) / TILE, tk = ct_up(c.M, TILE) / TILE, td = c.dr / TILE;
-    hipLaunchKernelGGL((k_contrast_grad<TILE, DT>), dim3((u32)td * (tq * c.splits_q + tk * c.splits_k)), dim3(256), 0, st, c, tq, tk, td);
+    in_launches((u64)td * (tq * c.splits_q + tk * c.splits_k), 256, [&](u64 first, u64 blocks) {
+        hipLaunchKernelGGL((k_contrast_grad<TILE, DT>), dim3((u32)blocks), dim3(256), 0, st, c, (u32)first, tq, tk, td);
+    });
 }
 
 template <int DT, bool WIDE>
@@ -1140,8 +1149,10 @@ static void launch_contrast(ContrastPar &c, const ContrastPlan &plan, int want_g
     const int key_blocks = Mr / 4 < CT_ROW_BLOCKS ? Mr / 4 : CT_ROW_BLOCKS, row_blocks = Br / 4 < CT_ROW_BLOCKS ? Br / 4 : CT_ROW_BLOCKS;
     // (by columns the padding of d up to a whole tile is written too: the products read it)
     const int across = (want_grad ? c.dr : c.dp) / 64;
-    hipLaunchKernelGGL((k_contrast_prepare<DT, WIDE>), dim3((u32)(key_blocks + row_blocks) + (u32)((Br + Mr) / 64) * across), dim3(256), 0, st, c,
-                       key_blocks, row_blocks, Br / 64, across, want_grad);
+    in_launches((u64)(key_blocks + row_blocks) + (u64)((Br + Mr) / 64) * across, 256, [&](u64 first, u64 blocks) {
+        hipLaunchKernelGGL((k_contrast_prepare<DT, WIDE>), dim3((u32)blocks), dim3(256), 0, st, c, (u32)first, key_blocks, row_blocks, Br / 64, across,
+                           want_grad);
+    });
     if constexpr (DT != DT_F32) {
         if (plan.tile == 256) launch_products<DT, 256, false>(c, want_grad, row_blocks, st);
         else launch_products<DT, 128, false>(c, want_grad, row_blocks, st);

@@ -54,9 +54,8 @@ static void launch_embed(const void *table, int64_t V, int d, const int32_t *ids
 {
     const int vec = row_vec(d, table, dt_size(DT), out, dt_size(OT));
     const u32 pieces = d / vec;
-    u64 rows = (256 * EMBED_ITEMS + pieces - 1) / pieces;      // one trip per block; small calls: one row per block at least
-    const u64 blocks_min = (n + rows - 1) / rows;
-    if (blocks_min > 0x7FFFFFFFull) rows = (n + 0x7FFFFFFEll) / 0x7FFFFFFFll;
+    // one trip per block; small calls: one row per block at least
+    const u64 rows = items_per_block(n, (256 * EMBED_ITEMS + pieces - 1) / pieces, most_blocks(256));
     const dim3 grid((u32)((n + rows - 1) / rows));
 #define RNND_EMBED(VEC) hipLaunchKernelGGL((k_embed<DT, OT, VEC>), grid, dim3(256), 0, st, table, (u32)V, pieces, ids, (u64)n, scale, out, (u32)rows)
     switch (vec) {
@@ -648,14 +647,14 @@ static void launch_grad_vec(GradPar &g, int d, const int32_t *small_ids, hipStre
         // 512 to 8,192 pieces for a block that clears: enough blocks, and each writes more than it reads of ids
         u32 pieces = 512;
         while (pieces < 8192 && (u64)g.V * g.pieces / pieces > 1024) pieces <<= 1;
-        g.clear_rows = pieces / g.pieces > 1 ? pieces / g.pieces : 1;
+        g.clear_rows = (u32)items_per_block(g.V, pieces / g.pieces > 1 ? pieces / g.pieces : 1, most_blocks(256) - g.reduce_blocks);
         const u32 clear_blocks = clear ? (g.V + g.clear_rows - 1) / g.clear_rows : 0;
         hipLaunchKernelGGL((k_grad_small<DT, GT, VEC>), dim3(g.reduce_blocks + clear_blocks), dim3(256), 0, st, g, small_ids, log_lanes, token_blocks);
         return;
     }
+    // (at most 2^23 blocks of sums, see rnnd_embed_grad(): 2^23 at least are left for the others)
     g.reduce_blocks = (u32)(((u64)g.chunks * g.pieces + 255) / 256);
-    g.clear_rows = 2048 / g.pieces > 1 ? 2048 / g.pieces : 1;
-    while (clear && (u64)g.V > (u64)g.clear_rows << 30) g.clear_rows <<= 1;
+    g.clear_rows = (u32)items_per_block(g.V, 2048 / g.pieces > 1 ? 2048 / g.pieces : 1, most_blocks(256) - g.reduce_blocks);
     const u32 clear_blocks = clear ? (g.V + g.clear_rows - 1) / g.clear_rows : 0;
     hipLaunchKernelGGL((k_grad_reduce<DT, GT, VEC>), dim3(g.reduce_blocks + clear_blocks), dim3(256), 0, st, g);
     if (g.pieces <= 8) launch_join<GT, VEC, 8>(g, st);
@@ -684,6 +683,7 @@ extern "C" int rnnd_embed_grad(const void *dout, int dtype, const int32_t *ids, 
     if ((uintptr_t)dout % dt_size(dtype) || (uintptr_t)ids % 4 || (uintptr_t)grad % dt_size(grad_dtype)) return RNND_ERR_BAD_PARAM;
     if (!n && accumulate) return RNND_OK;
     const GradPlan p = grad_plan(n, d, V);
+    if ((u64)p.chunks * d > (u64)256 << 23) return RNND_ERR_BAD_SHAPE;      // rows of 500 GB, which no device holds
     if (!workspace) return RNND_ERR_NULL;
     if ((uintptr_t)workspace % 16) return RNND_ERR_BAD_PARAM;
     if (workspace_bytes < p.bytes) return RNND_ERR_SCRATCH;

@@ -5,6 +5,7 @@
 
 #include "../../include/rnnd.h"
 #include "dist.h"
+#include "grid.h"
 
 template <int DT> struct RowType;
 template <> struct RowType<DT_F32> { typedef float T; };
