@@ -309,8 +309,8 @@ int rnnd_set_scan_launches(int mode);
  * Memory they work in is the caller's `workspace` (device, 16-byte aligned, as many bytes as the call's _workspace query
  * says, else RNND_ERR_SCRATCH; contents arbitrary; free for other use when the call's work on `stream` is done).
  * Pointers must be aligned to their elements (else RNND_ERR_BAD_PARAM); rows whose address and length allow 16-byte
- * accesses are faster.  Inputs and outputs must not overlap unless stated.  All sums are float32 and in an order that ids and
- * sizes alone decide: the same call gives the same bits. */
+ * accesses are faster.  Inputs and outputs must not overlap unless stated.  All sums are float32 and in an order that types,
+ * sizes and ids alone decide: the same call gives the same bits, wherever its arrays lie. */
 #define RNND_MAX_ROW 65536          /* coordinates of a row */
 #define RNND_MAX_CONTRAST 1048576   /* queries and keys of rnnd_contrast */
 
@@ -320,8 +320,9 @@ int rnnd_set_scan_launches(int mode);
 int rnnd_embed(const void *table, int64_t V, int32_t d, int dtype, const int32_t *ids, int64_t n, float scale,
                void *out, int out_dtype, void *stream);
 
-/* The gradient of the table for rnnd_embed: grad[v] = scale * sum of dout[t] over the t with ids[t] = v, in ascending t
- * (ids outside [0, V) are left out), summed in float32 and rounded once.
+/* The gradient of the table for rnnd_embed: grad[v] = scale * sum of dout[t] over the t with ids[t] = v
+ * (ids outside [0, V) are left out), summed in float32 and rounded once.  Few tokens of an id are added in ascending
+ * t; many are split into groups, each of which is summed by itself, and the groups' sums are added.
  *   dout        device, n x d of dtype; grad device, V x d of grad_dtype
  *   accumulate  0: every row of grad is written, those that no id names with zeros; 1: the sums are added to what grad
  *               holds, and rows that no id names are not touched */

@@ -4,9 +4,11 @@
 //   grad[v] (+)= scale * sum of dout[t] over the t with ids[t] = v, in ascending t
 //
 // Both only move rows: a lookup reads and writes n of them, a gradient reads n and writes V (added to what is there:
-// reads and writes the rows that are named).  The gradient's sums are in float32 and in an order that the sizes and ids alone decide:
-// up to SMALL_TOKENS tokens a block finds those of an id by itself, in one launch; more are sorted by id (stable), and every sum runs
-// over neighbours in that order.
+// reads and writes the rows that are named).  The gradient's sums are in float32 and in an order that types, sizes and ids decide, and
+// not where the rows lie: up to SMALL_TOKENS tokens a block finds those of an id by itself, in one launch; more are sorted by id (stable),
+// and every sum runs over neighbours in that order.  Tokens of one id that several groups of lanes share are summed by each group and the groups' sums
+// added one after the other; how many groups there are goes by the accesses that aligned rows allow, also where rows are not aligned and
+// are moved in shorter ones.
 #include "rows.h"
 
 // ------------------------------------------------------------------------------------------------ lookup
@@ -633,14 +635,15 @@ static void launch_join(GradPar &g, hipStream_t st)
     const u64 units = (u64)g.chunks * g.slabs;
     hipLaunchKernelGGL((k_grad_join<GT, VEC, G>), dim3((u32)(units < 1024 ? units : 1024)), dim3(JOIN_THREADS), 0, st, g);
 }
+// aligned_pieces: pieces of a row whose address allows the longest accesses that d does; decides the order of the sums
 template <int DT, int GT, int VEC>
-static void launch_grad_vec(GradPar &g, int d, const int32_t *small_ids, hipStream_t st)
+static void launch_grad_vec(GradPar &g, int d, u32 aligned_pieces, const int32_t *small_ids, hipStream_t st)
 {
     g.pieces = d / VEC;
     const bool clear = !g.accumulate;
     if (small_ids || !g.n) {
         u32 log_lanes = 3;
-        while (log_lanes < 6 && (1u << log_lanes) < g.pieces) ++log_lanes;
+        while (log_lanes < 6 && (1u << log_lanes) < aligned_pieces) ++log_lanes;
         g.slabs = (g.pieces + (1u << log_lanes) - 1) >> log_lanes;
         const u32 token_blocks = g.n > 1024 ? 1 : g.slabs < SMALL_SLABS ? g.slabs : SMALL_SLABS;
         g.reduce_blocks = g.n * token_blocks;
@@ -657,20 +660,21 @@ static void launch_grad_vec(GradPar &g, int d, const int32_t *small_ids, hipStre
     g.clear_rows = (u32)items_per_block(g.V, 2048 / g.pieces > 1 ? 2048 / g.pieces : 1, most_blocks(256) - g.reduce_blocks);
     const u32 clear_blocks = clear ? (g.V + g.clear_rows - 1) / g.clear_rows : 0;
     hipLaunchKernelGGL((k_grad_reduce<DT, GT, VEC>), dim3(g.reduce_blocks + clear_blocks), dim3(256), 0, st, g);
-    if (g.pieces <= 8) launch_join<GT, VEC, 8>(g, st);
-    else if (g.pieces <= 16) launch_join<GT, VEC, 16>(g, st);
-    else if (g.pieces <= 32) launch_join<GT, VEC, 32>(g, st);
+    if (aligned_pieces <= 8) launch_join<GT, VEC, 8>(g, st);
+    else if (aligned_pieces <= 16) launch_join<GT, VEC, 16>(g, st);
+    else if (aligned_pieces <= 32) launch_join<GT, VEC, 32>(g, st);
     else launch_join<GT, VEC, 64>(g, st);
 }
 template <int DT, int GT>
 static void launch_grad(GradPar &g, int d, const int32_t *small_ids, hipStream_t st)
 {
-    const int vec = row_vec(d, g.dout, dt_size(DT), g.grad, dt_size(GT));
-    if constexpr (DT != DT_F32)
-        if (vec == 8) return launch_grad_vec<DT, GT, 8>(g, d, small_ids, st);
-    if (vec >= 4) launch_grad_vec<DT, GT, 4>(g, d, small_ids, st);
-    else if (vec == 2) launch_grad_vec<DT, GT, 2>(g, d, small_ids, st);
-    else launch_grad_vec<DT, GT, 1>(g, d, small_ids, st);
+    constexpr int MOST = DT == DT_F32 ? 4 : 8;
+    const int aligned = row_vec(d, nullptr, dt_size(DT), nullptr, dt_size(GT)), vec = row_vec(d, g.dout, dt_size(DT), g.grad, dt_size(GT));
+    const u32 pieces = d / (aligned < MOST ? aligned : MOST);
+    if (vec >= MOST) launch_grad_vec<DT, GT, MOST>(g, d, pieces, small_ids, st);
+    else if (vec == 4) launch_grad_vec<DT, GT, 4>(g, d, pieces, small_ids, st);
+    else if (vec == 2) launch_grad_vec<DT, GT, 2>(g, d, pieces, small_ids, st);
+    else launch_grad_vec<DT, GT, 1>(g, d, pieces, small_ids, st);
 }
 
 extern "C" int rnnd_embed_grad(const void *dout, int dtype, const int32_t *ids, int64_t n, int32_t d, float scale, int64_t V,
