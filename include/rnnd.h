@@ -344,6 +344,9 @@ int rnnd_embed_grad_workspace(int64_t n, int32_t d, int64_t V, size_t *bytes);
  *   row_weight  device float [B] or NULL (1): 1 / B for the mean; a loss scale for float16 gradients
  *   loss        device float [B], not weighted
  *   dQ, dK      device, as Q and K; both NULL: only the loss
+ * Errors of a logit: float32 rows, some 2^-24 scale times the squares of the rows' distances from a point among the keys (distances do not
+ * change when all rows are moved, so the rows are taken from there); 16-bit rows, some 2^-24 scale (|q||k| + |k|^2): a program whose
+ * 16-bit rows are much farther from the origin than from each other subtracts a common row from them first.
  * 0 <= B <= RNND_MAX_CONTRAST, 1 <= M <= RNND_MAX_CONTRAST; the workspace holds two (float32 rows: six) 16-bit values per
  * pair for the gradients. */
 int rnnd_contrast(const void *Q, int64_t B, const void *K, int64_t M, int32_t d, int dtype, int metric,

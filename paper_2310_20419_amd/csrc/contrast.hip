@@ -14,6 +14,10 @@
 // What is exact, what is rounded:
 //   - 16-bit rows go to the matrix instructions as they are; float32 rows as three bfloat16 terms each (8 + 8 + 8 bits), of whose
 //     products the six largest are summed: what is left out is below 2^-24 of |a||b|.
+//   - a logit formed so is off by some 2^-24 scale |q||k| and 2^-24 scale |k|^2, in which distances between rows far from the origin
+//     drown (768 coordinates around 10, scale 5: losses off by 0.06; around 100: by 33).  Distances do not change when all rows are moved, so
+//     float32 rows are first taken from a point among the keys (k_contrast_centre), and the error goes with the rows' distances from it.
+//     16-bit rows stay as they are: their coordinates would no longer fit 16 bits.
 //   - all sums are float32.  The target is kept out of the row's sum: with x = lse over the others - s_t, loss = log(1 + e^x)
 //     and 1 - p_t = 1 - e^-loss, neither of which cancels when the loss is small.
 //   - g of the other keys is rounded to the type of the rows (float32 rows: three terms again; float16: scaled to below 2^15 by
@@ -57,6 +61,7 @@ struct ContrastPar {
     half_t *q, *k, *qt, *kt, *g, *gt;
     u32 *tops, *top;                // float16 rows: largest weight of each block of queries, and of all, as bits
     int *first, *count;             // [M] the first query whose target the key is, and how many they are
+    float *centre;                  // float32 rows: [dp] the point that they are taken from, zeros behind its d coordinates
     float *key_base;                // [M padded] (bias - scale |k|^2) log2(e), -inf where left out
     int *key_id;                    // [M padded]
     int2 *row_id;                   // [B padded] ids that a query leaves out: the target's, its own
@@ -103,6 +108,63 @@ __device__ __forceinline__ void load4(const void *rows, size_t row, int d, int e
         for (int k = 0; k < 4; ++k) x[k] = e + k < d ? (float)((const typename RowType<DT>::T *)rows)[row * d + e + k] : 0.0f;
 }
 
+// float32 rows: a point among the keys that count.  Of each sixteenth of the keys the first that counts is looked at, and every coordinate is the
+// median of theirs: a few keys far away from all others do not move it (as they would the mean).  Coordinates that are not finite count as the
+// largest; a median that is not is replaced by zero.
+#define CT_SAMPLES 16
+__global__ __launch_bounds__(64 * CT_SAMPLES) void k_contrast_centre(ContrastPar c)
+{
+    __shared__ int sample[CT_SAMPLES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int begin = (int)((long long)c.M * wave / CT_SAMPLES), end = (int)((long long)c.M * (wave + 1) / CT_SAMPLES);
+    int found = -1;
+    for (int j0 = begin; j0 < end && found < 0; j0 += 256) {
+        bool on[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) on[k] = j0 + k * 64 + lane < end && !key_gone(c, j0 + k * 64 + lane);
+#pragma unroll
+        for (int k = 3; k >= 0; --k) {
+            const u64 hit = __ballot(on[k]);
+            if (hit) found = j0 + k * 64 + __builtin_ctzll(hit);
+        }
+    }
+    if (lane == 0) sample[wave] = found;
+    __syncthreads();
+    const int e = blockIdx.x * (64 * CT_SAMPLES) + threadIdx.x;
+    if (e >= c.dp) return;
+    float x[CT_SAMPLES];
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < CT_SAMPLES; ++i) {
+        const int j = sample[i];
+        x[i] = j >= 0 && e < c.d ? ((const float *)c.K)[(size_t)j * c.d + e] : INFINITY;
+        count += j >= 0;
+    }
+#pragma unroll
+    for (int i = 0; i < CT_SAMPLES; ++i) x[i] = x[i] < INFINITY ? x[i] : INFINITY;      // NaN too
+    // neighbours exchanged, even and odd pairs in turn, until all are in order
+#pragma unroll
+    for (int pass = 0; pass < CT_SAMPLES; ++pass)
+#pragma unroll
+        for (int i = pass & 1; i + 1 < CT_SAMPLES; i += 2) {
+            const float low = fminf(x[i], x[i + 1]), high = fmaxf(x[i], x[i + 1]);
+            x[i] = low;
+            x[i + 1] = high;
+        }
+    float middle = 0.0f;
+#pragma unroll
+    for (int i = 0; i < CT_SAMPLES; ++i) middle = count && (count - 1) / 2 == i ? x[i] : middle;
+    c.centre[e] = fabsf(middle) < INFINITY ? middle : 0.0f;
+}
+
+// Four coordinates of a float32 row, taken from that point (x: as load4() left them)
+__device__ __forceinline__ void from_centre(const ContrastPar &c, int e, float (&x)[4])
+{
+    const f32x4 m = *(const f32x4 *)&c.centre[e];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] -= m[k];
+}
+
 // A wavefront per row: keys first, then queries.  A key's own part of its logits, a query's logit of its target.
 template <int DT, bool WIDE>
 __device__ __forceinline__ void contrast_rows(const ContrastPar &c, int block, int key_blocks, int row_blocks)
@@ -124,6 +186,7 @@ __device__ __forceinline__ void contrast_rows(const ContrastPar &c, int block, i
                 for (int e = lane * 4; e < c.d; e += 256) {
                     float x[4];
                     load4<DT, WIDE>(c.K, at, c.d, e, x);
+                    if constexpr (DT == DT_F32) from_centre(c, e, x);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) sum = fmaf(x[k], x[k], sum);
                 }
@@ -146,6 +209,10 @@ __device__ __forceinline__ void contrast_rows(const ContrastPar &c, int block, i
                     float x[4], y[4];
                     load4<DT, WIDE>(c.Q, at, c.d, e, x);
                     load4<DT, WIDE>(c.K, t, c.d, e, y);
+                    if constexpr (DT == DT_F32) {
+                        from_centre(c, e, x);
+                        from_centre(c, e, y);
+                    }
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         dot = fmaf(x[k], y[k], dot);
@@ -218,6 +285,7 @@ __device__ __forceinline__ void contrast_copy(const ContrastPar &c, int tile_r, 
             if (c0 + y + i < c.d) {
                 float four[4];
                 load4<DT, WIDE>(rows, r0 + x, c.d, c0 + y + i, four);
+                if constexpr (DT == DT_F32) from_centre(c, c0 + y + i, four);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[i + k] = four[k];
             }
@@ -945,9 +1013,11 @@ __global__ __launch_bounds__(256) void k_contrast_finish(ContrastPar c)
                 for (int k = 0; k < 4; ++k) a[k] += part[k];
             }
             load4<DT, WIDE>(mine, row, c.d, e, x);
+            float from[4] = {x[0], x[1], x[2], x[3]};       // as the products had it
+            if constexpr (DT == DT_F32) from_centre(c, e, from);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                a[k] = fmaf(-sum, x[k], a[k]);
+                a[k] = fmaf(-sum, from[k], a[k]);
                 if (DT == DT_F16) a[k] = ldexpf(a[k], down);
             }
         }
@@ -1070,6 +1140,7 @@ static size_t contrast_layout(ContrastPar &c, ContrastPlan &plan, int dtype, int
     take(c.top, 1);
     take(c.first, c.M);
     take(c.count, c.M);
+    if (planes == 3) take(c.centre, c.dp);
     take(c.key_base, Mr);
     take(c.key_id, Mr);
     take(c.row_id, Br);
@@ -1149,6 +1220,8 @@ static void launch_contrast(ContrastPar &c, const ContrastPlan &plan, int want_g
     const int key_blocks = Mr / 4 < CT_ROW_BLOCKS ? Mr / 4 : CT_ROW_BLOCKS, row_blocks = Br / 4 < CT_ROW_BLOCKS ? Br / 4 : CT_ROW_BLOCKS;
     // (by columns the padding of d up to a whole tile is written too: the products read it)
     const int across = (want_grad ? c.dr : c.dp) / 64;
+    if constexpr (DT == DT_F32)
+        hipLaunchKernelGGL(k_contrast_centre, dim3((c.dp + 64 * CT_SAMPLES - 1) / (64 * CT_SAMPLES)), dim3(64 * CT_SAMPLES), 0, st, c);
     in_launches((u64)(key_blocks + row_blocks) + (u64)((Br + Mr) / 64) * across, 256, [&](u64 first, u64 blocks) {
         hipLaunchKernelGGL((k_contrast_prepare<DT, WIDE>), dim3((u32)blocks), dim3(256), 0, st, c, (u32)first, key_blocks, row_blocks, Br / 64, across,
                            want_grad);
