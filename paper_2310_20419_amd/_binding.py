@@ -387,7 +387,8 @@ def rnnd_set_kernel_variant(variant: int):
 
 
 # ---- training the rows of an index.  These calls only enqueue their work.  Outputs and workspaces are allocated on the stream
-# the call runs on; inputs are marked as in use there if it is not the current one.
+# the call runs on; inputs are marked as in use there if it is not the current one.  They record no history for automatic
+# differentiation (the gradients are calls of their own), so tensors that ask for one are refused.
 _FLOAT_TYPES = {}
 
 
@@ -404,6 +405,13 @@ def _row_type(t, what):
 def _need(ok, message, *values):
     if not ok:
         raise ValueError(message % values)
+
+
+def _no_history(**tensors):
+    for what, x in tensors.items():
+        if x is not None and x.requires_grad and _torch().is_grad_enabled():
+            raise ValueError("%s requires a gradient, but this call records no history: pass %s.detach(), or call under torch.no_grad()"
+                             % (what, what))
 
 
 def _rows(x, what, d=None):
@@ -467,8 +475,10 @@ def _work(workspace, need, device):
 
 
 def rnnd_embed(table, ids, scale: float = 1.0, out_dtype=None, out=None, stream=None):
-    """rnnd_embed: returns scale * table[ids] ([n, d], of table's type or out_dtype); rows of zeros for ids outside the table."""
+    """rnnd_embed: returns scale * table[ids] ([n, d], of table's type or out_dtype); rows of zeros for ids outside the table.
+    Its gradient is rnnd_embed_grad; a table that requires gradients is refused outside torch.no_grad()."""
     torch = _torch()
+    _no_history(table=table, out=out)
     dt, device = _rows(table, "table"), table.device
     n, (V, d) = ids.shape[0] if ids.dim() == 1 else -1, table.shape
     pi = _vector(ids, "ids", None, torch.int32, device)
@@ -493,6 +503,7 @@ def rnnd_embed_grad(dout, ids, V: int, scale: float = 1.0, grad_dtype=None, grad
     """rnnd_embed_grad: returns the gradient of the table ([V, d], float32 or grad_dtype).  grad: where to put it, or
     (accumulate) what to add it to."""
     torch = _torch()
+    _no_history(dout=dout, grad=grad)
     dt, device = _rows(dout, "dout"), dout.device
     n, d = dout.shape
     pi = _vector(ids, "ids", n, torch.int32, device)
@@ -518,8 +529,10 @@ def rnnd_contrast_workspace(B: int, M: int, d: int, dtype: int, want_grad: bool 
 
 def rnnd_contrast(Q, K, target, scale: float, query_ids=None, key_ids=None, key_bias=None, row_weight=None,
                   want_grad: bool = True, metric: int = RNND_L2SQ, workspace=None, stream=None):
-    """rnnd_contrast: returns (loss [B] float32, dQ, dK), the gradients None without want_grad."""
+    """rnnd_contrast: returns (loss [B] float32, dQ, dK), the gradients None without want_grad.
+    Inputs that require gradients are refused outside torch.no_grad(): dQ and dK are what there is."""
     torch = _torch()
+    _no_history(Q=Q, K=K, key_bias=key_bias, row_weight=row_weight)
     dt, device = _rows(K, "K"), K.device
     M, d = K.shape
     _need(_rows(Q, "Q", d) == dt and Q.device == device, "Q and K must be of one type and on one device")
