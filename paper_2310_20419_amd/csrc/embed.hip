@@ -480,13 +480,16 @@ __global__ __launch_bounds__(JOIN_THREADS) void k_grad_join(GradPar g)
     }
 }
 
-// Few tokens: one launch, without a sort.  A block for each token looks through all ids; if an earlier token has the same id that token's
-// block sums them, else this one does: it lists the tokens of its id in order, its groups of G lanes sum pieces of the list, and
-// their sums are added in the groups' order.  The ids are a few KB that every block finds in its L2 -- 4,096 blocks read 64 MB of
+// Few tokens: one launch, without a sort.  A block for each token looks through all ids and lists the tokens of its own in order.  The blocks of
+// the tokens of one id share its row: the k-th takes every slab of it whose number is k modulo how many they are, and has nothing to do if there is none.  A slab
+// is what a group of lanes takes of a row; the groups of a block sum pieces of the list, and their sums are added in the groups' order.  An id of more than
+// SMALL_MANY tokens has groups of 8 lanes, the more of them.  (With one block for an id and always as many lanes as a row has pieces, up to 64, 4,096 tokens of
+// one id took 335 us with 768 coordinates and 3,328 with 8,192, sorted 47 and 40; now 26 and 27.)  The ids are a few KB that every block finds in its L2 -- 4,096 blocks read 64 MB of
 // them -- where a sort and its joins are four launches at least that wait for each other: 1,000 x 32 10.5 us (18 sorted), 4,096 x 32 10.4
 // (36), 4,096 x 768 f32 into 30,000 rows 32 (44).  The looking grows with the square of the tokens: 8,192 x 32 took 30 us, 8,192 x 768
 // 94, sorted 32 and 44.  Blocks behind the first reduce_blocks clear clear_rows rows each, but for those that an id names.
 #define SMALL_TOKENS 4096
+#define SMALL_MANY 256
 #define SMALL_SLABS 4           // blocks of a token, at most (more than 1,024 tokens fill the GPU with one each)
 #define SMALL_CLEAR 8192        // rows of a block that clears, at most
 
@@ -521,22 +524,26 @@ __global__ __launch_bounds__(256) void k_grad_small(GradPar g, const int *__rest
         }
         return;
     }
-    const u32 t = blockIdx.x / token_blocks, lanes = 1u << log_lanes, groups = 256 >> log_lanes;
+    const u32 t = blockIdx.x / token_blocks;
     const int key = ids[t];
     if ((u32)key >= g.V) return;        // a whole block
-    bool earlier = false;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
         const bool same = id[i] == key;     // (no token: -1, which is no key)
         const u64 all = __ballot(same);
         if (lane == 0) mask[i * 4 + (tid >> 6)] = all;
-        earlier |= same && i * 256 + tid < t;
     }
-    if (__syncthreads_or(earlier)) return;
+    __syncthreads();
     // a word's tokens follow those of the words before it: sums over the lanes, a word each
     static_assert(SMALL_TOKENS <= 64 * 64, "a word for each lane");
     const u32 mine = lane < (g.n + 63) / 64 ? __popcll(mask[lane]) : 0, upto = wave_inclusive(mine, lane);
     const u32 count = __builtin_amdgcn_readlane(upto, 63);
+    // this block's number among those of its id, and its first slab
+    const u32 rank = __builtin_amdgcn_readlane(upto - mine, __builtin_amdgcn_readfirstlane(t >> 6)) + __popcll(mask[t >> 6] & lanes_below(t & 63));
+    if (count > SMALL_MANY) log_lanes = 3;
+    const u32 lanes = 1u << log_lanes, groups = 256 >> log_lanes, slabs = (g.pieces + lanes - 1) >> log_lanes;
+    const u32 first = rank * token_blocks + blockIdx.x % token_blocks;
+    if (first >= slabs) return;         // a whole block
     if (count > 1) {
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
@@ -552,7 +559,7 @@ __global__ __launch_bounds__(256) void k_grad_small(GradPar g, const int *__rest
     if (each < GRAD_UNROLL) each = GRAD_UNROLL;
     const u32 begin = group * each < count ? group * each : count, end = begin + each < count ? begin + each : count;
     const u32 used = (count + each - 1) / each;
-    for (u32 slab = blockIdx.x % token_blocks; slab < g.slabs; slab += token_blocks) {
+    for (u32 slab = first; slab < slabs; slab += count * token_blocks) {
         const u32 piece = slab * lanes + at;
         float acc[VEC] = {};
         if (piece < g.pieces)
@@ -644,8 +651,8 @@ static void launch_grad_vec(GradPar &g, int d, u32 aligned_pieces, const int32_t
     if (small_ids || !g.n) {
         u32 log_lanes = 3;
         while (log_lanes < 6 && (1u << log_lanes) < aligned_pieces) ++log_lanes;
-        g.slabs = (g.pieces + (1u << log_lanes) - 1) >> log_lanes;
-        const u32 token_blocks = g.n > 1024 ? 1 : g.slabs < SMALL_SLABS ? g.slabs : SMALL_SLABS;
+        const u32 slabs = (g.pieces + (1u << log_lanes) - 1) >> log_lanes;
+        const u32 token_blocks = g.n > 1024 ? 1 : slabs < SMALL_SLABS ? slabs : SMALL_SLABS;
         g.reduce_blocks = g.n * token_blocks;
         // 512 to 8,192 pieces for a block that clears: enough blocks, and each writes more than it reads of ids
         u32 pieces = 512;
