@@ -23,6 +23,7 @@
 #include <mutex>
 
 #include "../../include/rnnd.h"
+#include "grid.h"
 #include "wave_prims.h"
 #include "round.h"
 
@@ -58,14 +59,14 @@ __device__ __forceinline__ int degree_class(int m, int use_classes)
 // ------------------------------------------------------------------ RandomGraph
 // Alg. 6, RandomGraph: S distinct random neighbours (wave_random_ids), their distances, sorted.
 template <int DT>
-__global__ __launch_bounds__(BLOCK) void k_random_graph(const void *X, long long N, int d, int vec_ok,
+__global__ __launch_bounds__(BLOCK) void k_random_graph(u32 first, const void *X, long long N, int d, int vec_ok,
                                                         int S, int R, u64 seed, u64 *keys, int *deg,
                                                         int8_t *vcls, int use_classes)
 {
     static_assert(SEARCH_MAX_L >= RNND_MAX_R, "the id / distance tables of the search hold a whole list");
     __shared__ SearchSmem s_tab[WAVES_PER_BLOCK];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const long long u = (long long)blockIdx.x * WAVES_PER_BLOCK + wave;
+    const long long u = (long long)(first + blockIdx.x) * WAVES_PER_BLOCK + wave;
     if (u >= N) return;
     int *ids = s_tab[wave].id;
     const size_t rowbytes = (size_t)d * dt_size(DT);
@@ -820,13 +821,13 @@ __device__ __forceinline__ void clear_cursors(u32 *misc, u32 *n_next)
 // v's bin once bins exist.
 // 16 lanes per vertex (lists are mostly short: a wavefront per vertex would leave most lanes idle and the
 // kernel is bound by its three dependent trips to memory: degree, list entry, arrival number).
-__global__ __launch_bounds__(BLOCK) void k_reverse_scatter(long long N, int R, const u64 *keys, const int *deg,
+__global__ __launch_bounds__(BLOCK) void k_reverse_scatter(u32 first, long long N, int R, const u64 *keys, const int *deg,
                                                            int *fill, u64 *inbox, u32 *late, u64 *over,
                                                            int8_t *mark, u32 *misc, u32 *n_next)
 {
-    clear_cursors(misc, n_next);
+    if (first == 0) clear_cursors(misc, n_next);
     const int lane = threadIdx.x & 63, sub = lane & 15, gsh = lane & ~15;
-    const long long u = ((long long)blockIdx.x * BLOCK + threadIdx.x) >> 4;
+    const long long u = ((long long)(first + blockIdx.x) * BLOCK + threadIdx.x) >> 4;
     const bool valid = u < N;
     const int m = valid ? deg[u] : 0;
     // the same number of trips for the four vertices of a wavefront (the ballot below is the wavefront's)
@@ -859,13 +860,13 @@ __global__ __launch_bounds__(BLOCK) void k_reverse_scatter(long long N, int R, c
 }
 
 // The late arrivals of k_reverse_scatter go to their targets' bins (which hold arrivals INBOX_CAP, ...).
-__global__ __launch_bounds__(BLOCK) void k_reverse_surplus(long long N, int R, const u64 *keys, const u32 *late,
+__global__ __launch_bounds__(BLOCK) void k_reverse_surplus(u32 first, long long N, int R, const u64 *keys, const u32 *late,
                                                            const u64 *over, const int8_t *mark,
                                                            const int *binoff, u64 *bins, const u32 *n_binned)
 {
     if (*n_binned == 0u) return;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const long long u = (long long)blockIdx.x * WAVES_PER_BLOCK + wave;
+    const long long u = (long long)(first + blockIdx.x) * WAVES_PER_BLOCK + wave;
     if (u >= N || !mark[u]) return;
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
@@ -1344,11 +1345,11 @@ __global__ void k_zero_u32(u32 *p, size_t n)
 }
 
 // vcls[u] for a snapshot handed in by the caller
-__global__ __launch_bounds__(BLOCK) void k_classify(long long N, int R, const u64 *keys, const int *deg,
+__global__ __launch_bounds__(BLOCK) void k_classify(u32 first, long long N, int R, const u64 *keys, const int *deg,
                                                     int8_t *vcls, int use_classes)
 {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const long long u = (long long)blockIdx.x * WAVES_PER_BLOCK + wave;
+    const long long u = (long long)(first + blockIdx.x) * WAVES_PER_BLOCK + wave;
     if (u >= N) return;
     int m = deg[u];
     if (m > R) m = R;
@@ -1358,10 +1359,10 @@ __global__ __launch_bounds__(BLOCK) void k_classify(long long N, int R, const u6
     if (lane == 0) vcls[u] = b ? (int8_t)degree_class(m, use_classes) : (int8_t)-1;
 }
 
-__global__ void k_export(long long N, int R, const u64 *keys, const int *deg, int *graph_out,
+__global__ void k_export(u32 first, long long N, int R, const u64 *keys, const int *deg, int *graph_out,
                          int *degree_out)
 {
-    long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+    long long i = (long long)(first + blockIdx.x) * blockDim.x + threadIdx.x;
     if (i >= N * R) return;
     long long u = i / R;
     int e = (int)(i - u * R);
@@ -1371,10 +1372,10 @@ __global__ void k_export(long long N, int R, const u64 *keys, const int *deg, in
 }
 
 // The same, four slots per thread (R a multiple of 4, graph_out 16-byte aligned).
-__global__ __launch_bounds__(256) void k_export4(long long N, int R4, const u64 *keys, const int *deg, int4 *graph_out,
+__global__ __launch_bounds__(256) void k_export4(u32 first, long long N, int R4, const u64 *keys, const int *deg, int4 *graph_out,
                                                  int *degree_out)
 {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;      // group of four slots
+    const long long i = (long long)(first + blockIdx.x) * 256 + threadIdx.x;      // group of four slots
     if (i >= N * R4) return;
     const long long u = i / R4;
     const int e = 4 * (int)(i - u * R4);
@@ -1394,12 +1395,13 @@ __global__ __launch_bounds__(256) void k_export4(long long N, int R4, const u64 
 static void launch_export(long long N, int R, const u64 *keys, const int *deg, int *graph_out, int *degree_out,
                           hipStream_t st)
 {
-    if (R % 4 == 0 && ((uintptr_t)graph_out & 15) == 0 && ((uintptr_t)keys & 15) == 0)
-        hipLaunchKernelGGL(k_export4, dim3((unsigned)(((size_t)N * (R / 4) + 255) / 256)), dim3(256), 0, st, N, R / 4, keys,
-                           deg, (int4 *)graph_out, degree_out);
-    else
-        hipLaunchKernelGGL(k_export, dim3((unsigned)(((size_t)N * R + 255) / 256)), dim3(256), 0, st, N, R, keys, deg,
-                           graph_out, degree_out);
+    const bool by_four = R % 4 == 0 && ((uintptr_t)graph_out & 15) == 0 && ((uintptr_t)keys & 15) == 0;
+    in_launches(((size_t)N * (by_four ? R / 4 : R) + 255) / 256, 256, [&](u64 first, u64 blocks) {
+        if (by_four)
+            hipLaunchKernelGGL(k_export4, dim3((u32)blocks), dim3(256), 0, st, (u32)first, N, R / 4, keys, deg, (int4 *)graph_out, degree_out);
+        else
+            hipLaunchKernelGGL(k_export, dim3((u32)blocks), dim3(256), 0, st, (u32)first, N, R, keys, deg, graph_out, degree_out);
+    });
 }
 
 // Measurement aid: random row gathers and nothing else.  Every wavefront draws row numbers from the
@@ -1716,7 +1718,9 @@ static void launch_prepare(const Workspace &w, const ScanPlan &p, const void *X,
     if (p.copy == COPY_NONE) return;
     if (p.copy == COPY_U8) {
         const size_t n = (size_t)N * d;
-        hipLaunchKernelGGL(k_prepare_u8, dim3((unsigned)((n / 16 + 255) / 256)), dim3(256), 0, st, (const uint8_t *)X, n, w.xs);
+        in_launches((n / 16 + 255) / 256, 256, [&](u64 first, u64 blocks) {
+            hipLaunchKernelGGL(k_prepare_u8, dim3((u32)blocks), dim3(256), 0, st, (u32)first, (const uint8_t *)X, n, w.xs);
+        });
         return;
     }
     const size_t threads = p.copy == COPY_U8_ROWS ? p.copy_bytes / 4 : p.copy_bytes / 16;
@@ -2103,13 +2107,16 @@ static hipError_t launch_reverse(const Workspace &w, long long N, int R, int use
         hipLaunchKernelGGL(k_bin_place, dim3(nr), dim3(PLACE_THREADS), 0, st, N, R, (const Prop *)w.props, (const u32 *)w.range_base,
                            (const int *)deg, w.fill, w.inbox, w.binoff, w.bins, w.misc + 0, w.cnt, cnt_in, cand);
     } else {
-        hipLaunchKernelGGL(k_reverse_scatter, dim3((unsigned)((N * 16 + BLOCK - 1) / BLOCK)), dim3(BLOCK), 0, st, N, W, keys, deg,
-                           w.fill, w.inbox, late, over, mark, w.misc, n_next);
+        in_launches((u64)(N * 16 + BLOCK - 1) / BLOCK, BLOCK, [&](u64 first, u64 blocks) {
+            hipLaunchKernelGGL(k_reverse_scatter, dim3((u32)blocks), dim3(BLOCK), 0, st, (u32)first, N, W, keys, deg, w.fill, w.inbox, late, over, mark, w.misc,
+                               n_next);
+        });
         hipLaunchKernelGGL(k_assign_bins, dim3(tb), dim3(1024), 0, st, N, w.fill, INBOX_CAP, INBOX_CAP, INBOX_CAP,
                            w.binoff, w.misc + 0, w.hubs, w.misc + 1, w.cnt, cnt_in, (u64 *)nullptr, deg, R, cand,
                            (const int8_t *)nullptr, (int *)nullptr, (u32 *)nullptr);
-        hipLaunchKernelGGL(k_reverse_surplus, dim3(vb), dim3(BLOCK), 0, st, N, W, keys, late, over, mark, w.binoff,
-                           w.bins, w.misc + 1);
+        in_launches(vb, BLOCK, [&](u64 first, u64 blocks) {
+            hipLaunchKernelGGL(k_reverse_surplus, dim3((u32)blocks), dim3(BLOCK), 0, st, (u32)first, N, W, keys, late, over, mark, w.binoff, w.bins, w.misc + 1);
+        });
     }
     static const int rmerge_per_cu = resident_blocks_per_cu(k_reverse_merge, 6);
     const int rm_blocks = cu_count() * rmerge_per_cu;
@@ -2376,8 +2383,9 @@ template <int DT>
 static void launch_random_graph_dt(const void *X, long long N, int d, int vec_ok, int S, int R, u64 seed, u64 *keys,
                                    int *deg, int8_t *vcls, int use_classes, hipStream_t st)
 {
-    hipLaunchKernelGGL(k_random_graph<DT>, dim3(vertex_blocks(N)), dim3(BLOCK), 0, st, X, N, d, vec_ok, S, R, seed, keys,
-                       deg, vcls, use_classes);
+    in_launches(vertex_blocks(N), BLOCK, [&](u64 first, u64 blocks) {
+        hipLaunchKernelGGL(k_random_graph<DT>, dim3((u32)blocks), dim3(BLOCK), 0, st, (u32)first, X, N, d, vec_ok, S, R, seed, keys, deg, vcls, use_classes);
+    });
 }
 
 static void launch_random_graph(const void *X, long long N, int d, int dtype, int vec_ok, int S, int R, u64 seed,
@@ -2635,8 +2643,9 @@ static int update_impl(const void *X, int64_t N, int32_t d, int dtype, int metri
     ws_clear(w, st);
     // (the copy first, where it does not depend on the lists: it runs while the other launches are submitted)
     if (!listed) HIPCHK(prepare_rows(w, plan, X, N, d, dtype, st, true, nullptr, &rows));
-    hipLaunchKernelGGL(k_classify, dim3(vertex_blocks(N)), dim3(BLOCK), 0, st, (long long)N, R, (const u64 *)keys,
-                       deg, w.vcls, plan.classes());
+    in_launches(vertex_blocks(N), BLOCK, [&](u64 first, u64 some) {
+        hipLaunchKernelGGL(k_classify, dim3((u32)some), dim3(BLOCK), 0, st, (u32)first, (long long)N, R, (const u64 *)keys, deg, w.vcls, plan.classes());
+    });
     if (!blocks) launch_compact_all(w, N, 0, st);
     if (listed) HIPCHK(prepare_rows(w, plan, X, N, d, dtype, st, true, &round, &rows));
     for (int t = 0; t < n_rounds; ++t) {

@@ -33,10 +33,10 @@ struct alignas(16) MfmaScanSmem {
 };
 
 // Once per build: Xs <- X - 128 as int8 (n bytes, a multiple of 16).
-__global__ __launch_bounds__(256) void k_prepare_u8(const uint8_t *__restrict__ X, size_t n,
+__global__ __launch_bounds__(256) void k_prepare_u8(u32 first, const uint8_t *__restrict__ X, size_t n,
                                                     int8_t *__restrict__ Xs)
 {
-    const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 16;
+    const size_t i = ((size_t)(first + blockIdx.x) * 256 + threadIdx.x) * 16;
     if (i < n) {
         v4i x = *(const v4i *)(X + i);
         x ^= (int)0x80808080;
