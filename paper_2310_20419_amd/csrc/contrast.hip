@@ -98,6 +98,17 @@ __device__ __forceinline__ float wave_sum(float v)
     return v;
 }
 
+// sums over the lanes up to each
+__device__ __forceinline__ int inclusive(int v, int lane)
+{
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) {
+        const int o = __shfl_up(v, k);
+        if (lane >= k) v += o;
+    }
+    return v;
+}
+
 // Four coordinates of a row, zeros behind its end; WIDE: all rows allow it in one access.
 template <int DT, bool WIDE>
 __device__ __forceinline__ void load4(const void *rows, size_t row, int d, int e, float (&x)[4])
@@ -976,81 +987,192 @@ __device__ __forceinline__ void store4(void *rows, size_t row, int d, int e, con
             if (e + k < d) ((typename RowType<DT>::T *)rows)[row * d + e + k] = (typename RowType<DT>::T)x[k];
 }
 
-// Joins the parts of a sum in order, takes off the row itself times the sum of its g, adds the target's term, and rounds.  A
-// wavefront per row, four coordinates a lane.
-template <int DT, bool WIDE>
-__global__ __launch_bounds__(256) void k_contrast_finish(ContrastPar c)
-{
-    const int at = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (at >= c.B + c.M) return;
-    const bool keys = at >= c.B;
-    const int row = keys ? at - c.B : at, rows = keys ? c.M : c.B, parts = keys ? c.parts_q : c.parts_k;
-    void *out = keys ? c.dK : c.dQ;
-    const void *mine = keys ? c.K : c.Q, *theirs = keys ? c.Q : c.K;
-    if (keys ? key_gone(c, row) : !row_counts(c, row)) {
-        const float zero[4] = {};
-        for (int e = lane * 4; e < c.d; e += 256) store4<DT, WIDE>(out, row, c.d, e, zero);
-        return;
+// A row of dQ or dK: the parts of its sum joined in order, less the row itself times the sum of its g.
+template <int DT, bool WIDE> struct GradRow {
+    const ContrastPar &c;
+    bool keys;
+    int row, splits, down;          // down: exponent of float16 rows' g
+    const void *mine;
+    const float *acc;
+    size_t plane;
+    float sum;
+    __device__ __forceinline__ GradRow(const ContrastPar &par, int at) : c(par)
+    {
+        keys = at >= c.B;
+        row = keys ? at - c.B : at;
+        const int lane = threadIdx.x & 63, rows = keys ? c.M : c.B, parts = keys ? c.parts_q : c.parts_k;
+        mine = keys ? c.K : c.Q;
+        splits = keys ? c.splits_k : c.splits_q;
+        const float *sums = (keys ? c.sum_k : c.sum_q) + (size_t)row * parts;
+        sum = 0.0f;
+        for (int t = lane; t < parts; t += 64) sum += sums[t];
+        sum = wave_sum(sum);
+        plane = (size_t)((rows + CT_PAD - 1) / CT_PAD * CT_PAD) * c.dr;
+        acc = (keys ? c.acc_k : c.acc_q) + (size_t)row * c.dr;
+        down = DT == DT_F16 ? -weight_exponent(*c.top) : 0;
     }
-    const float *sums = (keys ? c.sum_k : c.sum_q) + (size_t)row * parts;
-    float sum = 0.0f;
-    for (int t = lane; t < parts; t += 64) sum += sums[t];
-    sum = wave_sum(sum);
-    const size_t plane = (size_t)((rows + CT_PAD - 1) / CT_PAD * CT_PAD) * c.dr;
-    const float *acc = (keys ? c.acc_k : c.acc_q) + (size_t)row * c.dr;
-    const int splits = keys ? c.splits_k : c.splits_q;
-    const int down = DT == DT_F16 ? -weight_exponent(*c.top) : 0;       // of g
-    const int found = keys ? c.count[row] : 1, first = keys ? found ? c.first[row] : 0 : c.target[row];
-    const float f = 2.0f * c.scale;
-    for (int e0 = 0; e0 < c.d; e0 += 256) {        // all lanes stay: the search below needs them
+    // a: four coordinates of the sum; x: of the row
+    __device__ __forceinline__ void load(int e, float (&a)[4], float (&x)[4]) const
+    {
+        for (int s = 0; s < splits; ++s) {
+            const f32x4 part = *(const f32x4 *)&acc[s * plane + e];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) a[k] += part[k];
+        }
+        load4<DT, WIDE>(mine, row, c.d, e, x);
+        float from[4] = {x[0], x[1], x[2], x[3]};       // as the products had it
+        if constexpr (DT == DT_F32) from_centre(c, e, from);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            a[k] = fmaf(-sum, from[k], a[k]);
+            if (DT == DT_F16) a[k] = ldexpf(a[k], down);
+        }
+    }
+    __device__ __forceinline__ void store(int e, float (&a)[4]) const
+    {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) a[k] *= 2.0f * c.scale;
+        store4<DT, WIDE>(keys ? c.dK : c.dQ, row, c.d, e, a);
+    }
+};
+
+// A key that is the target of more than CT_SHARED queries takes their terms by a whole block: it looks for them in CT_LOOK targets at a time, each
+// wavefront sums a part of those found, in order, and the parts are added in the end.  8,192 x 16,384 x 768 bfloat16 with one target for all
+// queries, a tenth of them, each its own, us: 2,085, 1,175, 1,059 (a wavefront that looked for each and waited for it: 15,931, 2,557, 1,063);
+// 8,192 x 16 x 768 280 (1,366), 100,000 x 64 x 768 1,850 (5,633).
+#define CT_SHARED 8
+#define CT_LOOK 4096
+#define CT_ROWS 8           // rows that a wavefront has on the way
+#define CT_FINISH 4         // wavefronts of a block; 8 or 16 are faster here (1,641 and 1,434) and slower elsewhere (1,078 -> 1,087 and 1,104)
+struct SharedLds {
+    unsigned short list[CT_LOOK];
+    int found[CT_LOOK / 64];
+    f32x4 part[CT_FINISH - 1][64];
+};
+template <int DT, bool WIDE>
+__device__ __forceinline__ void contrast_shared(const ContrastPar &c, int at, SharedLds &lds)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row = at - c.B;
+    for (int e0 = 0; e0 < c.d; e0 += 256) {
         const int e = e0 + lane * 4;
         const bool in = e < c.d;
-        float a[4] = {}, x[4] = {};
-        if (in) {
-            for (int s = 0; s < splits; ++s) {
-                const f32x4 part = *(const f32x4 *)&acc[s * plane + e];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) a[k] += part[k];
+        float term[4] = {}, x[4] = {};
+        if (in) load4<DT, WIDE>(c.K, row, c.d, e, x);
+        int left = c.count[row];
+        for (int b = c.first[row]; left > 0 && b < c.B; b += CT_LOOK) {
+            constexpr int WORDS = CT_LOOK / 64 / CT_FINISH;     // ballots of a wavefront
+            u32 mine = 0;
+#pragma unroll 4
+            for (int w = 0; w < WORDS; ++w) {
+                const int i = b + (wave * WORDS + w) * 64 + lane;
+                mine |= (u32)(i < c.B && c.target[i] == row) << w;
             }
-            load4<DT, WIDE>(mine, row, c.d, e, x);
-            float from[4] = {x[0], x[1], x[2], x[3]};       // as the products had it
-            if constexpr (DT == DT_F32) from_centre(c, e, from);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                a[k] = fmaf(-sum, from[k], a[k]);
-                if (DT == DT_F16) a[k] = ldexpf(a[k], down);
+            for (int w = 0; w < WORDS; ++w) {
+                const u64 hit = __ballot(mine >> w & 1);
+                if (lane == 0) lds.found[wave * WORDS + w] = __popcll(hit);
             }
-        }
-        // the target's term; a key that is the target of several queries takes them in their order
-        int i = first;
-        for (int left = found; left > 0; --left) {
-            if (in) {
-                const float own = c.row_own[keys ? i : row];
-                float y[4];
-                load4<DT, WIDE>(theirs, i, c.d, e, y);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) a[k] = fmaf(own, y[k] - x[k], a[k]);
+            __syncthreads();
+            const int here = lds.found[lane], upto = inclusive(here, lane), n = __builtin_amdgcn_readlane(upto, 63);
+            for (int w = 0; w < WORDS; ++w) {
+                const int word = wave * WORDS + w;
+                const u64 hit = __ballot(mine >> w & 1);
+                if (mine >> w & 1)
+                    lds.list[__builtin_amdgcn_readlane(upto - here, word) + __popcll(hit & lanes_below(lane))] = (unsigned short)(word * 64 + lane);
             }
-            if (left == 1) break;
-            int next = -1;
-            for (int b = i + 1; b < c.B && next < 0; b += 256) {
-                int t[4];
+            __syncthreads();
+            const int end = n * (wave + 1) / CT_FINISH;
+            for (int j = n * wave / CT_FINISH; in && j < end; j += CT_ROWS) {
+                float y[CT_ROWS][4], own[CT_ROWS];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) t[k] = b + k * 64 + lane < c.B ? c.target[b + k * 64 + lane] : -1;
-#pragma unroll
-                for (int k = 3; k >= 0; --k) {
-                    const u64 hit = __ballot(t[k] == row);
-                    if (hit) next = b + k * 64 + __builtin_ctzll(hit);
+                for (int k = 0; k < CT_ROWS; ++k) {
+                    const int i = b + lds.list[j + k < end ? j + k : end - 1];
+                    own[k] = c.row_own[i];
+                    load4<DT, WIDE>(c.Q, i, c.d, e, y[k]);
                 }
-            }
-            if (next < 0) break;
-            i = next;
-        }
-        if (!in) continue;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) a[k] *= f;
-        store4<DT, WIDE>(out, row, c.d, e, a);
+                for (int k = 0; k < CT_ROWS; ++k)
+                    if (j + k < end)
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) term[h] = fmaf(own[k], y[k][h] - x[h], term[h]);
+            }
+            left -= n;
+            __syncthreads();        // the lists are used again
+        }
+        if (wave) lds.part[wave - 1][lane] = (f32x4){term[0], term[1], term[2], term[3]};
+        __syncthreads();
+        if (wave == 0) {
+            const GradRow<DT, WIDE> mine(c, at);
+            if (in) {
+                float a[4] = {};
+                mine.load(e, a, x);
+                for (int w = 0; w < CT_FINISH - 1; ++w)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) term[k] += lds.part[w][lane][k];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) a[k] += term[k];
+                mine.store(e, a);
+            }
+        }
+        __syncthreads();
     }
+}
+
+// Joins the parts of a sum, takes off the row itself times the sum of its g, adds the target's term, and rounds.  A wavefront per row,
+// four coordinates a lane; then the block's keys that many queries share.  The rows of a block lie gridDim.x apart, so that neighbouring keys of this kind
+// are those of different blocks.  Every wavefront sees for itself whether there are any: a barrier for all would hold the fast ones back (8,192 x
+// 16,384 x 768, random targets: 1,091 -> 1,107 us).  Eight wavefronts per SIMD, though contrast_shared() spills then: five cost every call more (1,078 -> 1,087).
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(64 * CT_FINISH, 8) void k_contrast_finish(ContrastPar c)
+{
+    __shared__ SharedLds lds;
+    const int lane = threadIdx.x & 63, total = c.B + c.M, mine_at = (int)(blockIdx.x + lane * gridDim.x);
+    const u64 shared = __ballot(lane < CT_FINISH && mine_at >= c.B && mine_at < total && c.count[mine_at - c.B] > CT_SHARED);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = (int)(blockIdx.x + wave * gridDim.x);
+    const bool keys = at >= c.B;
+    const int row = keys ? at - c.B : at;
+    if (at >= total || shared >> wave & 1) {
+    } else if (keys ? key_gone(c, row) : !row_counts(c, row)) {
+        const float zero[4] = {};
+        for (int e = lane * 4; e < c.d; e += 256) store4<DT, WIDE>(keys ? c.dK : c.dQ, row, c.d, e, zero);
+    } else {
+        const int found = keys ? c.count[row] : 1, first = keys ? found ? c.first[row] : 0 : c.target[row];
+        const GradRow<DT, WIDE> mine(c, at);
+        const void *theirs = keys ? c.Q : c.K;
+        for (int e0 = 0; e0 < c.d; e0 += 256) {        // all lanes stay: the search below needs them
+            const int e = e0 + lane * 4;
+            const bool in = e < c.d;
+            float a[4] = {}, x[4] = {};
+            if (in) mine.load(e, a, x);
+            // the target's term; a key that is the target of several queries takes them in their order
+            int i = first;
+            for (int left = found; left > 0; --left) {
+                if (in) {
+                    const float own = c.row_own[keys ? i : row];
+                    float y[4];
+                    load4<DT, WIDE>(theirs, i, c.d, e, y);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) a[k] = fmaf(own, y[k] - x[k], a[k]);
+                }
+                if (left == 1) break;
+                int next = -1;
+                for (int b = i + 1; b < c.B && next < 0; b += 256) {
+                    int t[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) t[k] = b + k * 64 + lane < c.B ? c.target[b + k * 64 + lane] : -1;
+#pragma unroll
+                    for (int k = 3; k >= 0; --k) {
+                        const u64 hit = __ballot(t[k] == row);
+                        if (hit) next = b + k * 64 + __builtin_ctzll(hit);
+                    }
+                }
+                if (next < 0) break;
+                i = next;
+            }
+            if (in) mine.store(e, a);
+        }
+    }
+    for (u64 left = shared; left; left &= left - 1) contrast_shared<DT, WIDE>(c, (int)(blockIdx.x + __builtin_ctzll(left) * gridDim.x), lds);
 }
 
 __global__ void k_contrast_zero(unsigned short *p, size_t n)
@@ -1237,7 +1359,7 @@ static void launch_contrast(ContrastPar &c, const ContrastPlan &plan, int want_g
         else launch_grads<DT, 128>(c, st);
     } else
         launch_grads<DT, 128>(c, st);
-    hipLaunchKernelGGL((k_contrast_finish<DT, WIDE>), dim3((c.B + c.M + 3) / 4), dim3(256), 0, st, c);
+    hipLaunchKernelGGL((k_contrast_finish<DT, WIDE>), dim3((c.B + c.M + CT_FINISH - 1) / CT_FINISH), dim3(64 * CT_FINISH), 0, st, c);
 }
 
 extern "C" int rnnd_contrast(const void *Q, int64_t B, const void *K, int64_t M, int32_t d, int dtype, int metric, const int32_t *target,
