@@ -344,6 +344,9 @@ int rnnd_embed_grad_workspace(int64_t n, int32_t d, int64_t V, size_t *bytes);
  *   row_weight  device float [B] or NULL (1): 1 / B for the mean; a loss scale for float16 gradients
  *   loss        device float [B], not weighted
  *   dQ, dK      device, as Q and K; both NULL: only the loss
+ * Held in fewer bits than float32: for the products that form dQ and dK, row_weight[i] times the probability of a key that is not the target
+ * is rounded to the rows' type (float16: after scaling all weights by a power of two; float32: 24 bits); the target's own term is float32, and
+ * the sums that are taken off with the row itself are those of the rounded values.
  * Errors of a logit: float32 rows, some 2^-24 scale times the squares of the rows' distances from a point among the keys (distances do not
  * change when all rows are moved, so the rows are taken from there); 16-bit rows, some 2^-24 scale (|q||k| + |k|^2): a program whose
  * 16-bit rows are much farther from the origin than from each other subtracts a common row from them first.

@@ -560,7 +560,8 @@ class AdamwTensors:
     """The tensors of an AdamW step, described once.  Each is a dict of 1-D views or whole contiguous tensors:
     param (float32), grad, m, v (float32, or one byte an element for 8-bit states with m_scale and v_scale, one
     byte per 128 elements), copy (float16 or bfloat16, optional) and counter (8 bits; by default the tensors' own elements,
-    counted through, each starting at a multiple of 128)."""
+    counted through, each starting at a multiple of 128).  The descriptors hold the tensors' addresses, and this object keeps the tensors: a program
+    writes its gradients into the same tensors every step (rnnd_embed_grad's grad=); for gradients in new tensors it is made anew."""
 
     def __init__(self, tensors):
         torch = _torch()

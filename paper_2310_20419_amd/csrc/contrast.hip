@@ -1220,7 +1220,10 @@ static ContrastPlan contrast_plan(ContrastPar &c, int planes)
     // 3,000 x 12,000, d = 32 332 / 361, 128 381 / 415, 256 586 / 599, 384 807 / 799, 768 1,501 / 1,412; 2,200 x 2,200 x 128 (324 tiles)
     // 83 / 94, 700 x 4,000 x 300 (192 tiles) 119 / 101, 100 x 1,100 x 32 49.0 / 45.6
     p.terms = planes == 3 && (c.d > 320 || tiles(c.B, 128) * tiles(c.M, 128) <= 256);
-    // the gradient products: also by how much of the last tile of d would be padding
+    // the gradient products: also by how much of the last tile of d would be padding.  The whole call, tiles of 128 / 256, us: 500 x 1,000 x 768
+    // (18 tiles of 256) 63 / 77, 1,700 x 3,400 x 768 (63) 86 / 97, 2,048 x 4,096 x 768 (72) 91 / 100, 1,000 x 11,000 x 768 (141) 153 / 148,
+    // 8,192 x 16,384 x 768 (288) 1,127 / 1,052; by padding, 4,096 x 8,192: d = 300 (512 for 384) 163 / 177, 600 (768 for 640) 266 / 262, 1,100 (1,280 for
+    // 1,152) 410 / 438, 64 103 / 118.  (Between 64 and about 128 tiles, and at lengths like 1,100, tiles of 128 would be up to 10 % ahead.)
     const int d128 = ct_up(c.d, 128), d256 = ct_up(c.d, 256);
     p.tile_g = planes == 1 && (tiles(c.B, 256) + tiles(c.M, 256)) * (d256 / 256) >= 64 && d256 * 4 <= d128 * 5 ? 256 : 128;
     c.dp = ct_up(c.d, CT_K);
@@ -1230,7 +1233,8 @@ static ContrastPlan contrast_plan(ContrastPar &c, int planes)
     c.parts_k = 2 * (int)tiles(c.M, p.tile);
     c.parts_q = 2 * (int)tiles(c.B, p.tile);
     // parts of the gradients' sums: few tiles are split over the workgroups that run at a time; a part costs about 24 steps of the
-    // product, for what it starts with and for its results, written and read again
+    // product, for what it starts with and for its results, written and read again.  With 6 / 24 / 80 steps, us: 1,700 x 3,400 x 768 99 / 86 / 86,
+    // 4,096 x 8,192 x 300 176 / 162 / 162, x 600 306 / 262 / 262, x 1,100 445 / 438 / 425, float32 2,000 x 10,000 x 100 234 / 233 / 242
     static const int choices[] = {1, 2, 3, 4, 6, 8, 12, 16};
     const long long tq = tiles(c.B, p.tile_g) * (c.dr / p.tile_g), tk = tiles(c.M, p.tile_g) * (c.dr / p.tile_g);
     const int steps_q = c.Mp / CT_K * (planes == 3 ? 6 : 1), steps_k = c.Bp / CT_K * (planes == 3 ? 6 : 1);
