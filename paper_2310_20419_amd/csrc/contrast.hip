@@ -28,10 +28,10 @@
 //
 // What bounds it.  The work that the loss cannot do without is three products; forming the logits again is a fourth, which costs less
 // than writing them in 32 bits and reading them back.  8,192 x 16,384 x 768 bfloat16, 1.08 ms (three library products of that shape: 0.64):
-// preparation 34 us; largest and sums 263 (784 TFLOP/s); g 364 (567, and 537 MB written: one wavefront per SIMD, so that what
-// follows a tile's product is not hidden behind another's); g k and g' q 428 (963; the library's products 971); joining the parts 46.  Float32 rows of
-// 100 coordinates, 2,000 x 10,000, 231 us: six products for each, and g in three terms twice, 250 MB written by the second product (74 us)
-// and read by the third (94).  Small calls are six launches that wait for each other: 100 x 1,100 x 32 45 us.
+// preparation 34 us; largest and sums 264 (781 TFLOP/s); g 365 (565, and 537 MB written: one wavefront per SIMD, so that what
+// follows a tile's product is not hidden behind another's); g k and g' q 427 (965; the library's products 971 to 1,003); joining the parts 47.  Float32 rows of
+// 100 coordinates, 2,000 x 10,000, 239 us: six products for each, and g in three terms twice, 250 MB written by the second product (74 us)
+// and read by the third (93).  Small calls are seven launches that wait for each other (16-bit rows six): 100 x 1,100 x 32 50 us.
 #include <cmath>
 #include <type_traits>
 #include <utility>
@@ -121,7 +121,7 @@ __device__ __forceinline__ void load4(const void *rows, size_t row, int d, int e
 
 // float32 rows: a point among the keys that count.  Of each sixteenth of the keys the first that counts is looked at, and every coordinate is the
 // median of theirs: a few keys far away from all others do not move it (as they would the mean).  Coordinates that are not finite count as the
-// largest; a median that is not is replaced by zero.
+// largest; a median that is not is replaced by zero.  A launch of 4 to 6 us.
 #define CT_SAMPLES 16
 __global__ __launch_bounds__(64 * CT_SAMPLES) void k_contrast_centre(ContrastPar c)
 {
@@ -1042,7 +1042,6 @@ template <int DT, bool WIDE> struct GradRow {
 // 8,192 x 16 x 768 280 (1,366), 100,000 x 64 x 768 1,850 (5,633).
 #define CT_SHARED 8
 #define CT_LOOK 4096
-#define CT_ROWS 8           // rows that a wavefront has on the way
 #define CT_FINISH 4         // wavefronts of a block; 8 or 16 are faster here (1,641 and 1,434) and slower elsewhere (1,078 -> 1,087 and 1,104)
 struct SharedLds {
     unsigned short list[CT_LOOK];
@@ -1082,16 +1081,18 @@ __device__ __forceinline__ void contrast_shared(const ContrastPar &c, int at, Sh
             }
             __syncthreads();
             const int end = n * (wave + 1) / CT_FINISH;
-            for (int j = n * wave / CT_FINISH; in && j < end; j += CT_ROWS) {
-                float y[CT_ROWS][4], own[CT_ROWS];
+            // rows that a wavefront has on the way; eight of float32 spill so much that every call pays for it (2,000 x 10,000 x 100: 241 us, four 239)
+            constexpr int ROWS = DT == DT_F32 ? 4 : 8;
+            for (int j = n * wave / CT_FINISH; in && j < end; j += ROWS) {
+                float y[ROWS][4], own[ROWS];
 #pragma unroll
-                for (int k = 0; k < CT_ROWS; ++k) {
+                for (int k = 0; k < ROWS; ++k) {
                     const int i = b + lds.list[j + k < end ? j + k : end - 1];
                     own[k] = c.row_own[i];
                     load4<DT, WIDE>(c.Q, i, c.d, e, y[k]);
                 }
 #pragma unroll
-                for (int k = 0; k < CT_ROWS; ++k)
+                for (int k = 0; k < ROWS; ++k)
                     if (j + k < end)
 #pragma unroll
                         for (int h = 0; h < 4; ++h) term[h] = fmaf(own[k], y[k][h] - x[h], term[h]);
