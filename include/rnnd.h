@@ -358,6 +358,52 @@ int rnnd_contrast(const void *Q, int64_t B, const void *K, int64_t M, int32_t d,
                   size_t workspace_bytes, void *stream);
 int rnnd_contrast_workspace(int64_t B, int64_t M, int32_t d, int dtype, int want_grad, size_t *bytes);
 
+/* Distillation: the divergence of the softmax over squared distances from what another model (the teacher) said about each query's
+ * most probable keys, with gradients.  Logits s_ij, the keys that are left out (key_ids[j] < 0, key_bias[j] = -infinity, for query i those with
+ * key_ids[j] = query_ids[i]), biases, weights and errors as for rnnd_contrast; P_ij = exp(s_ij) / sum over the keys that are not left out.
+ * The list of query i is teacher_ids[i][0 .. entries), positions of keys, with teacher_logits beside them.  An entry is absent, and counts nowhere,
+ * where its position is outside [0, M), its key is left out, its logit is -infinity, or an earlier entry that is not absent names the same key.
+ *   tail = 0   p = softmax of the list's logits; loss[i] = sum_t p_t (log p_t - log P_t)
+ *   tail = 1   the logits are log probabilities (rnnd_logprob gives them): p_t = exp(logit), and r = max(0, 1 - sum p), what the teacher gave to the
+ *              other keys, is one more outcome (p over its sum where that is above 1):
+ *              loss[i] = sum_t p_t (log p_t - log P_t) + r (log r - log R), R the sum of P over the keys off the list
+ *              (where all keys that count are on the list: p over its sum, no r)
+ *   dQ, dK     gradients of sum_i row_weight[i] * loss[i]
+ * A query without an entry does not count: loss 0, gradient 0, whatever its row holds.
+ *   Q, K, query_ids, key_ids, key_bias, row_weight, loss, dQ, dK   as for rnnd_contrast
+ *   teacher_ids     device int32 [B x entries], 1 <= entries <= RNND_MAX_LISTED, in any order
+ *   teacher_logits  device float [B x entries], no NaN or +infinity (they make the query's loss and gradients NaN)
+ * Held in fewer bits than float32: for the products that form dQ and dK the gradients with respect to the logits, as for rnnd_contrast,
+ * those of listed keys among them.  The probabilities of a list are formed and summed in double precision.
+ * 0 <= B <= RNND_MAX_CONTRAST, 1 <= M <= RNND_MAX_CONTRAST; the workspace holds two (float32 rows: six) 16-bit values per
+ * pair for the gradients. */
+#define RNND_MAX_LISTED 128         /* entries of a teacher's list; alternatives of rnnd_logprob */
+int rnnd_distill(const void *Q, int64_t B, const void *K, int64_t M, int32_t d, int dtype, int metric,
+                 const int32_t *teacher_ids, const float *teacher_logits, int32_t entries, int tail, const int32_t *query_ids,
+                 const int32_t *key_ids, const float *key_bias, const float *row_weight, float scale, float *loss, void *dQ,
+                 void *dK, void *workspace, size_t workspace_bytes, void *stream);
+int rnnd_distill_workspace(int64_t B, int64_t M, int32_t d, int dtype, int32_t entries, int want_grad, size_t *bytes);
+
+/* Log probabilities under the softmax over squared distances: of a given key, the entropy, and the most probable keys.  Logits s_ij and
+ * the keys that are left out as for rnnd_distill; lse_i = log(sum_j exp s_ij), log P_ij = s_ij - lse_i.
+ *   logprob[i]      log P of key target[i]; 0 where target[i] is outside [0, M) or names a key that is left out (also the query's own)
+ *   entropy[i]      -sum_j P_ij log P_ij
+ *   top_ids[i]      the `alternatives` most probable keys (positions), most probable first, the lowest position first where their logits are equal;
+ *                   -1 where there are fewer
+ *   top_logprob[i]  their log P; -infinity where there are fewer
+ * The order of the alternatives is that of the logits in double precision (each distance summed in double precision from the rows as
+ * they are), whatever the error of the sums; it costs more where very many keys are within that error of each other.  The sums are float32,
+ * with rnnd_contrast's errors of a logit; with at most 8 queries the distances are summed from differences and have no error from far origins.
+ * Where no key counts: logprob and entropy 0, no alternatives.  Where a logit that counts is NaN or +infinity: NaN, no alternatives (-1 and NaN).
+ *   target       device int32 [B] or NULL with logprob NULL; entropy device float [B] or NULL
+ *   alternatives 0 <= alternatives <= RNND_MAX_LISTED; top_ids device int32 [B x alternatives], top_logprob device float [B x alternatives] (NULL if 0)
+ * 0 <= B <= RNND_MAX_CONTRAST, 1 <= M <= RNND_MAX_CONTRAST. */
+int rnnd_logprob(const void *Q, int64_t B, const void *K, int64_t M, int32_t d, int dtype, int metric, const int32_t *target,
+                 const int32_t *query_ids, const int32_t *key_ids, const float *key_bias, float scale, int32_t alternatives,
+                 float *logprob, float *entropy, int32_t *top_ids, float *top_logprob, void *workspace, size_t workspace_bytes,
+                 void *stream);
+int rnnd_logprob_workspace(int64_t B, int64_t M, int32_t d, int dtype, int32_t alternatives, size_t *bytes);
+
 /* One tensor of an AdamW step: n elements each.  state_bits 32: m, v are float arrays.  state_bits 8: m, v are n bytes of
  * codes of the OCP 8-bit float with 4 bits of exponent and 3 of fraction, m_scale, v_scale one byte b per 128 elements, and the moment
  * is m = code * 2^(b - 127) and v = (code * 2^(b - 127))^2; b = 255 says that the block held a value that is not finite.

@@ -127,6 +127,10 @@ def load_library():
         L.rnnd_embed_grad_workspace.argtypes = [i64, i32, i64, c.POINTER(sz)]
         L.rnnd_contrast.argtypes = [vp, i64, vp, i64, i32, c.c_int, c.c_int, vp, vp, vp, vp, vp, f32, vp, vp, vp, vp, sz, vp]
         L.rnnd_contrast_workspace.argtypes = [i64, i64, i32, c.c_int, c.c_int, c.POINTER(sz)]
+        L.rnnd_distill.argtypes = [vp, i64, vp, i64, i32, c.c_int, c.c_int, vp, vp, i32, c.c_int, vp, vp, vp, vp, f32, vp, vp, vp, vp, sz, vp]
+        L.rnnd_distill_workspace.argtypes = [i64, i64, i32, c.c_int, i32, c.c_int, c.POINTER(sz)]
+        L.rnnd_logprob.argtypes = [vp, i64, vp, i64, i32, c.c_int, c.c_int, vp, vp, vp, vp, f32, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.rnnd_logprob_workspace.argtypes = [i64, i64, i32, c.c_int, i32, c.POINTER(sz)]
         L.rnnd_adamw.argtypes = [c.POINTER(AdamwTensor), i32, i64, f64, f64, f64, f64, f64, f64, u64, vp]
         L.rnnd_strerror.argtypes = [c.c_int]
         L.rnnd_strerror.restype = c.c_char_p
@@ -138,7 +142,7 @@ def load_library():
                      "rnnd_set_workspace_poison", "rnnd_add_reverse_edges_wide", "rnnd_set_transpose_path",
                      "rnnd_set_event_timing", "rnnd_probe_gather_map", "rnnd_set_scan_launches",
                      "rnnd_embed", "rnnd_embed_grad", "rnnd_embed_grad_workspace", "rnnd_contrast",
-                     "rnnd_contrast_workspace", "rnnd_adamw"):
+                     "rnnd_contrast_workspace", "rnnd_distill", "rnnd_distill_workspace", "rnnd_logprob", "rnnd_logprob_workspace", "rnnd_adamw"):
             getattr(L, name).restype = c.c_int
         _lib = L
     return _lib
@@ -551,6 +555,79 @@ def rnnd_contrast(Q, K, target, scale: float, query_ids=None, key_ids=None, key_
                                             loss.data_ptr(), dQ.data_ptr() if want_grad else None,
                                             dK.data_ptr() if want_grad else None, w.data_ptr(), w.numel() * w.element_size(), st))
     return loss, dQ, dK
+
+
+def rnnd_distill_workspace(B: int, M: int, d: int, dtype: int, entries: int, want_grad: bool = True) -> int:
+    b = ctypes.c_size_t(0)
+    _check(load_library().rnnd_distill_workspace(B, M, d, dtype, entries, 1 if want_grad else 0, ctypes.byref(b)))
+    return b.value
+
+
+def rnnd_distill(Q, K, teacher_ids, teacher_logits, scale: float, tail: bool = False, query_ids=None, key_ids=None, key_bias=None,
+                 row_weight=None, want_grad: bool = True, metric: int = RNND_L2SQ, workspace=None, stream=None):
+    """rnnd_distill: returns (loss [B] float32, dQ, dK), the gradients None without want_grad.  teacher_ids (int32) and teacher_logits
+    (float32) are [B, entries], as rnnd_logprob of the teacher returns them (tail=True) or any scores of candidates.
+    Inputs that require gradients are refused outside torch.no_grad(): dQ and dK are what there is."""
+    torch = _torch()
+    _no_history(Q=Q, K=K, teacher_logits=teacher_logits, key_bias=key_bias, row_weight=row_weight)
+    dt, device = _rows(K, "K"), K.device
+    M, d = K.shape
+    _need(_rows(Q, "Q", d) == dt and Q.device == device, "Q and K must be of one type and on one device")
+    B = Q.shape[0]
+    _need(teacher_ids.dim() == 2 and teacher_ids.shape[0] == B and teacher_logits.shape == teacher_ids.shape,
+          "teacher_ids and teacher_logits must both be [%s, entries]", B)
+    entries = teacher_ids.shape[1]
+    for what, x, t in (("teacher_ids", teacher_ids, torch.int32), ("teacher_logits", teacher_logits, torch.float32)):
+        _need(x.is_cuda and x.device == device and x.is_contiguous() and x.dtype == t, "%s must be a contiguous %s tensor on the same device", what, t)
+    pq = _vector(query_ids, "query_ids", B, torch.int32, device)
+    pk = _vector(key_ids, "key_ids", M, torch.int32, device)
+    pb = _vector(key_bias, "key_bias", M, torch.float32, device)
+    pw = _vector(row_weight, "row_weight", B, torch.float32, device)
+    need = rnnd_distill_workspace(B, M, d, dt, entries, want_grad)
+    with _On(device, stream, (Q, K, teacher_ids, teacher_logits, query_ids, key_ids, key_bias, row_weight, workspace)) as st:
+        loss = torch.empty(B, dtype=torch.float32, device=device)
+        dQ, dK = (torch.empty_like(Q), torch.empty_like(K)) if want_grad else (None, None)
+        w = _work(workspace, need, device)
+        _check(load_library().rnnd_distill(Q.data_ptr(), B, K.data_ptr(), M, d, dt, metric, teacher_ids.data_ptr(), teacher_logits.data_ptr(),
+                                           entries, 1 if tail else 0, pq, pk, pb, pw, scale, loss.data_ptr(),
+                                           dQ.data_ptr() if want_grad else None, dK.data_ptr() if want_grad else None,
+                                           w.data_ptr(), w.numel() * w.element_size(), st))
+    return loss, dQ, dK
+
+
+def rnnd_logprob_workspace(B: int, M: int, d: int, dtype: int, alternatives: int = 0) -> int:
+    b = ctypes.c_size_t(0)
+    _check(load_library().rnnd_logprob_workspace(B, M, d, dtype, alternatives, ctypes.byref(b)))
+    return b.value
+
+
+def rnnd_logprob(Q, K, scale: float, target=None, alternatives: int = 0, query_ids=None, key_ids=None, key_bias=None,
+                 metric: int = RNND_L2SQ, workspace=None, stream=None):
+    """rnnd_logprob: returns (logprob [B] of the targets or None, entropy [B], top_ids int32 [B, alternatives], top_logprob
+    [B, alternatives]), the last two None without alternatives.
+    Inputs that require gradients are refused outside torch.no_grad(): the call records no history (rnnd_contrast has the gradients)."""
+    torch = _torch()
+    _no_history(Q=Q, K=K, key_bias=key_bias)
+    dt, device = _rows(K, "K"), K.device
+    M, d = K.shape
+    _need(_rows(Q, "Q", d) == dt and Q.device == device, "Q and K must be of one type and on one device")
+    B = Q.shape[0]
+    pt = _vector(target, "target", B, torch.int32, device)
+    pq = _vector(query_ids, "query_ids", B, torch.int32, device)
+    pk = _vector(key_ids, "key_ids", M, torch.int32, device)
+    pb = _vector(key_bias, "key_bias", M, torch.float32, device)
+    need = rnnd_logprob_workspace(B, M, d, dt, alternatives)
+    with _On(device, stream, (Q, K, target, query_ids, key_ids, key_bias, workspace)) as st:
+        logprob = torch.empty(B, dtype=torch.float32, device=device) if target is not None else None
+        entropy = torch.empty(B, dtype=torch.float32, device=device)
+        ids = torch.empty((B, alternatives), dtype=torch.int32, device=device) if alternatives else None
+        top = torch.empty((B, alternatives), dtype=torch.float32, device=device) if alternatives else None
+        w = _work(workspace, need, device)
+        _check(load_library().rnnd_logprob(Q.data_ptr(), B, K.data_ptr(), M, d, dt, metric, pt, pq, pk, pb, scale, alternatives,
+                                           None if logprob is None else logprob.data_ptr(), entropy.data_ptr(),
+                                           None if ids is None else ids.data_ptr(), None if top is None else top.data_ptr(),
+                                           w.data_ptr(), w.numel() * w.element_size(), st))
+    return logprob, entropy, ids, top
 
 
 _ADAMW_KEYS = {"param", "grad", "m", "v", "m_scale", "v_scale", "copy", "counter"}

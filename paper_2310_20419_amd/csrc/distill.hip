@@ -1,0 +1,477 @@
+// Distillation: the divergence of the softmax over squared distances from what another model said, and its gradients.
+//
+//   s_ij   = bias_j - scale |q_i - k_j|^2,  P_ij = exp(s_ij - lse_i)          the student, over all keys that are not left out
+//   p_it   = the teacher's probability of entry t of the list of query i; r_i what it leaves to the keys off the list
+//   loss_i = sum_t p_it (log p_it - log P_it) + r_i (log r_i - log R_i),  R_i the student's mass off the list
+//   g_ij   = w_i (P_ij - p_ij) on the list, w_i P_ij (1 - r_i / R_i) off it   (without a rest: w_i P_ij)
+//   dq_i   = 2 scale sum_j g_ij (k_j - q_i),  dk_j = 2 scale sum_i g_ij (q_i - k_j)
+//
+// The products are those of rnnd_contrast (contrast.h), with lists in the place of targets: the sums of a row are of the keys off its
+// list, so that neither R nor what follows from it is a small difference of large numbers, and the logits of listed keys are written
+// out by the tile that they lie in.  The lists are sorted by key, with the place where every tile begins, so a tile marks its listed
+// keys in a bitmap in LDS while its first loads are under way; a key's place in the list is the number of marks before it in its row.
+// Off the list g is a factor of the row times 2^(s - reference), with w (R - r) and the log of the sum off the list: again no difference
+// of large numbers where a key has little of both.  Listed keys take g = w (P - p), formed in float32 from the logits; like all of g it
+// is rounded to the type of the rows for the products (float32 rows: three terms), which bounds its error by half a step of its own
+// size, also where teacher and student nearly agree.  The teacher's probabilities are summed in double precision: 1 - sum p of a
+// teacher that is sure is a small difference, and there are few of them.
+#include <cmath>
+
+#include "contrast.h"
+
+struct DistillPar : ContrastPar {
+    const int *ids;             // [B][entries]
+    const float *logits;
+    int entries, tail;
+    int tiles_k;                // tiles of the logits across the keys
+    int *list_key;              // [B padded][entries] keys that count, ascending; from here on a row's lists are in this order
+    float *list_p, *list_s, *list_g;    // the teacher's probability; the logit in base 2; g (float16: scaled)
+    float2 *list_sum;           // [B] sum of the list's p, r
+    unsigned char *list_at;     // [B padded][tiles_k + 1] place of a tile's first key; of the end
+};
+
+__device__ __forceinline__ bool entry_counts(const DistillPar &c, int i, int e)
+{
+    const int j = c.ids[(size_t)i * c.entries + e];
+    return (u32)j < (u32)c.M && !(c.logits[(size_t)i * c.entries + e] == -INFINITY) && !key_gone(c, j) &&
+           !(c.query_ids && c.key_ids[j] == c.query_ids[i]);
+}
+__device__ __forceinline__ bool row_counts(const DistillPar &c, int i)
+{
+    for (int e = 0; e < c.entries; ++e)
+        if (entry_counts(c, i, e)) return true;
+    return false;
+}
+
+// ------------------------------------------------------------------------------------------------ a row's marks in a tile
+template <> constexpr bool has_lists<DistillPar>() { return true; }
+
+template <int TILE> struct ListLds<TILE, DistillPar> {
+    static constexpr int ROOM = TILE * 4;       // values of g; those of more entries stay in memory
+    u32 bits[TILE * TILE / 32];
+    float value[ROOM];
+    unsigned short at[TILE];                    // of a row's first value
+    unsigned char first[TILE], count[TILE];     // place of the row's first key of this tile in its list, and how many they are
+    u32 used;
+};
+
+template <int TILE>
+__device__ __forceinline__ void load_lists(const DistillPar &c, ListLds<TILE, DistillPar> &lists, int row0, int tile_c, bool values)
+{
+    const int t = threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < TILE * TILE / 32 / 256; ++i) lists.bits[i * 256 + t] = 0;
+    if (t == 0) lists.used = 0;
+    __syncthreads();
+    if (t >= TILE) return;
+    const unsigned char *ends = &c.list_at[(size_t)(row0 + t) * (c.tiles_k + 1) + tile_c];
+    const int first = ends[0], n = ends[1] - first;
+    lists.first[t] = (unsigned char)first;
+    lists.count[t] = (unsigned char)n;
+    if (!n) return;
+    const u32 place = values ? atomicAdd(&lists.used, (u32)n) : 0;
+    lists.at[t] = (unsigned short)place;        // at most 256 rows of 128
+    const size_t from = (size_t)(row0 + t) * c.entries + first;
+    for (int e = 0; e < n; ++e) {
+        const int col = c.list_key[from + e] - tile_c * TILE;
+        atomicOr(&lists.bits[(t * TILE + col) >> 5], 1u << (col & 31));
+        if (values && place + e < (u32)ListLds<TILE, DistillPar>::ROOM) lists.value[place + e] = c.list_g[from + e];
+    }
+}
+
+template <int TILE>
+__device__ __forceinline__ u32 marks_at(const ListLds<TILE, DistillPar> &lists, int row, int col)
+{
+    return lists.bits[(row * TILE + col) >> 5] >> (col & 31) & ((1u << (TILE / 32)) - 1);
+}
+// marks of the row before the column
+template <int TILE>
+__device__ __forceinline__ int marks_before(const ListLds<TILE, DistillPar> &lists, int row, int col)
+{
+    if (lists.count[row] < 2) return 0;
+    const u32 *words = &lists.bits[row * TILE >> 5];
+    int n = __popc(words[col >> 5] & ((1u << (col & 31)) - 1));
+    for (int w = 0; w < col >> 5; ++w) n += __popc(words[w]);
+    return n;
+}
+
+// Four rows' logits: those of listed keys are written out, and become -infinity
+template <int TILE, int N>
+__device__ __forceinline__ void take_listed(const DistillPar &c, const ListLds<TILE, DistillPar> &lists, int row0, int row, int col, float (&s)[4][N])
+{
+    u32 marks[4], any = 0;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) any |= marks[r] = marks_at(lists, row + r, col);
+    if (!__any(any)) return;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        if (marks[r]) {
+            float *to = &c.list_s[(size_t)(row0 + row + r) * c.entries + lists.first[row + r] + marks_before(lists, row + r, col)];
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+                if (marks[r] >> n & 1) {
+                    *to++ = s[r][n];
+                    s[r][n] = -INFINITY;
+                }
+        }
+    }
+}
+
+// A row's g: those of listed keys
+template <int TILE, int N>
+__device__ __forceinline__ void put_listed(const DistillPar &c, const ListLds<TILE, DistillPar> &lists, int row0, int row, int col, float (&g)[N])
+{
+    const u32 marks = marks_at(lists, row, col);
+    if (!__any(marks)) return;
+    if (marks) {
+        const int before = marks_before(lists, row, col);
+        u32 at = lists.at[row] + (u32)before;
+        const float *from = &c.list_g[(size_t)(row0 + row) * c.entries + lists.first[row] + before];
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            if (marks >> n & 1) {
+                g[n] = at < (u32)ListLds<TILE, DistillPar>::ROOM ? lists.value[at] : *from;
+                ++at;
+                ++from;
+            }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ preparation
+__device__ __forceinline__ double wave_sum_f64(double v)
+{
+#pragma unroll
+    for (int s = 32; s; s >>= 1) v += __shfl_xor(v, s);
+    return v;
+}
+__device__ __forceinline__ float wave_max_f32(float v)
+{
+#pragma unroll
+    for (int s = 32; s; s >>= 1) v = fmaxf(v, __shfl_xor(v, s));
+    return v;
+}
+
+// A query's list, by a wavefront: entries that count in the order of their keys, each key once (the first entry that names it), and
+// the teacher's probabilities.  keys: the wavefront's own place in LDS.
+#define DS_MAX RNND_MAX_LISTED
+__device__ __forceinline__ void distill_row(const DistillPar &c, int i, int lane, int *keys, int logit_tile)
+{
+    const size_t from = (size_t)i * c.entries;
+    u64 k[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int e = r * 64 + lane;
+        k[r] = i < c.B && e < c.entries && entry_counts(c, i, e) ? (u64)(u32)c.ids[from + e] << 8 | (u32)e : ~0ull;
+    }
+    wave_sort<2>(k);
+    const u64 before[2] = {shfl_up1_u64(k[0]), shfl_up1_u64(k[1])}, last = shfl_u64(k[0], 63);
+    bool on[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const u64 b = lane ? before[r] : r ? last : ~0ull;
+        on[r] = k[r] != ~0ull && (b == ~0ull || b >> 8 != k[r] >> 8);
+    }
+    const u64 m0 = __ballot(on[0]), m1 = __ballot(on[1]);
+    const int n0 = (int)__popcll(m0), n = n0 + (int)__popcll(m1);
+    const int at[2] = {(int)__popcll(m0 & lanes_below(lane)), n0 + (int)__popcll(m1 & lanes_below(lane))};
+    float l[2];
+    double p[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) l[r] = on[r] ? c.logits[from + (k[r] & 0xFF)] : -INFINITY;
+    const float top = c.tail || !n ? 0.0f : wave_max_f32(fmaxf(l[0], l[1]));
+#pragma unroll
+    for (int r = 0; r < 2; ++r) p[r] = on[r] ? exp((double)l[r] - (double)top) : 0.0;
+    const double sum = wave_sum_f64(p[0] + p[1]);
+    const double rest = c.tail && sum < 1.0 ? 1.0 - sum : 0.0, mass = n ? sum + rest : 1.0;
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+        if (on[r]) {
+            keys[at[r]] = (int)(k[r] >> 8);
+            c.list_key[from + at[r]] = (int)(k[r] >> 8);
+            c.list_p[from + at[r]] = (float)(p[r] / mass);
+        }
+    wave_sync();
+    unsigned char *ends = &c.list_at[(size_t)i * (c.tiles_k + 1)];
+    for (int t = lane; t <= c.tiles_k; t += 64) {
+        int lo = 0, hi = n;         // keys below the tile's first
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (keys[mid] < t * logit_tile) lo = mid + 1;
+            else hi = mid;
+        }
+        ends[t] = (unsigned char)lo;
+    }
+    wave_sync();
+    if (lane == 0) {
+        if (i < c.B) c.list_sum[i] = make_float2((float)(sum / mass), (float)(rest / mass));
+        c.row_id[i] = make_int2(CT_NEVER, n && c.query_ids ? c.query_ids[i] : CT_NEVER);
+        const float w = n ? c.row_weight ? c.row_weight[i] : 1.0f : 0.0f;
+        c.row_g[i] = make_float2(INFINITY, w);
+        c.row_own[i] = w;
+    }
+}
+
+// A wavefront per row, keys first; then the copies of the rows (contrast_copy()), in the same launch.
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(256) void k_distill_prepare(DistillPar c, u32 first, int key_blocks, int row_blocks, int q_tiles, int across, int columns, int logit_tile)
+{
+    __shared__ int keys_of[4][DS_MAX];
+    __shared__ u32 most;
+    const int block = (int)(first + blockIdx.x), id = block - key_blocks - row_blocks;
+    if (id >= 0) {
+        contrast_copy<DT, WIDE>(c, id / across, id % across * 64, q_tiles, columns);
+        return;
+    }
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (block < key_blocks) {
+        for (int at = block * 4 + wave; at < ct_up(c.M, CT_PAD); at += key_blocks * 4) key_side<DT, WIDE>(c, at, lane);
+        return;
+    }
+    if (threadIdx.x == 0) most = 0;
+    __syncthreads();
+    for (int at = (block - key_blocks) * 4 + wave; at < ct_up(c.B, CT_PAD); at += row_blocks * 4) {
+        distill_row(c, at, lane, keys_of[wave], logit_tile);
+        if (DT == DT_F16 && lane == 0) {
+            const u32 bits = __float_as_uint(c.row_own[at]) & 0x7FFFFFFFu;
+            if (bits < 0x7F800000u) atomicMax(&most, bits);
+        }
+    }
+    __syncthreads();
+    if (DT == DT_F16 && threadIdx.x == 0) c.tops[block - key_blocks] = most;
+}
+
+// ------------------------------------------------------------------------------------------------ the loss
+// A wavefront per query joins the parts of its sum and its list: the loss, and what the second product needs.
+template <int DT>
+__global__ __launch_bounds__(256) void k_distill_loss(DistillPar c, int row_blocks)
+{
+    const int i = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    int up = 0;
+    if constexpr (DT == DT_F16) {
+        __shared__ u32 most;
+        if (threadIdx.x == 0) most = 0;
+        __syncthreads();
+        u32 top = 0;
+        for (int b = threadIdx.x; b < row_blocks; b += 256) top = c.tops[b] > top ? c.tops[b] : top;
+        atomicMax(&most, top);
+        __syncthreads();
+        up = weight_exponent(most);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *c.top = most;
+    }
+    if (i >= c.B) return;
+    const int n = c.list_at[(size_t)i * (c.tiles_k + 1) + c.tiles_k];
+    if (!n) {
+        if (lane == 0) c.loss[i] = 0.0f;
+        return;
+    }
+    float top = -INFINITY, sum = 0.0f;
+    for (int t = lane; t < c.parts_k; t += 64) {
+        const float2 part = c.part[(size_t)i * c.parts_k + t];
+        join_parts(top, sum, part.x, part.y);
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) join_parts(top, sum, __shfl_xor(top, s), __shfl_xor(sum, s));
+    float s[2], p[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int e = r * 64 + lane;
+        s[r] = e < n ? c.list_s[(size_t)i * c.entries + e] : -INFINITY;
+        p[r] = e < n ? c.list_p[(size_t)i * c.entries + e] : 0.0f;
+    }
+    const float2 mass = c.list_sum[i];
+    const bool others = top > -INFINITY || !(sum == 0.0f);      // keys off the list
+    float rest = mass.y;
+    if (!others && rest > 0.0f) {       // nothing can have what the teacher left: the list alone
+        rest = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) p[r] /= mass.x;
+    }
+    const float m = fmaxf(top, wave_max_f32(fmaxf(s[0], s[1]))), ref = m == -INFINITY ? 0.0f : m;
+    const float x[2] = {s[0] - ref, s[1] - ref}, e[2] = {__builtin_amdgcn_exp2f(x[0]), __builtin_amdgcn_exp2f(x[1])};
+    const float off = others ? sum * __builtin_amdgcn_exp2f(top - ref) : 0.0f, total = off + wave_sum(e[0] + e[1]), log_total = log2f(total);
+    const float w = c.row_own[i], up_w = ldexpf(w, up);
+    float loss = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int at = r * 64 + lane;
+        if (at >= n) continue;
+        // (an entry whose probability is below the smallest float has none)
+        if (!(p[r] == 0.0f)) loss = fmaf(p[r], (log2f(p[r]) - (x[r] - log_total)) * 0.693147181f, loss);
+        c.list_g[(size_t)i * c.entries + at] = up_w * (e[r] / total - p[r]);
+    }
+    loss = wave_sum(loss);
+    if (lane) return;
+    if (rest > 0.0f) {
+        const float log_off = top - ref + log2f(sum);
+        loss = fmaf(rest, (log2f(rest) - (log_off - log_total)) * 0.693147181f, loss);
+        c.row_g[i] = make_float2(top + log2f(sum), up_w * (off / total - rest));
+    } else if (others)
+        c.row_g[i] = make_float2(ref + log_total, up_w);
+    c.loss[i] = loss;
+}
+
+// ------------------------------------------------------------------------------------------------ joining the gradients' parts
+// A wavefront per row, four coordinates a lane.
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(256) void k_distill_finish(DistillPar c)
+{
+    const int lane = threadIdx.x & 63, at = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (at >= c.B + c.M) return;
+    const bool keys = at >= c.B;
+    const int row = keys ? at - c.B : at;
+    if (keys ? key_gone(c, row) : !c.list_at[(size_t)row * (c.tiles_k + 1) + c.tiles_k]) {
+        const float zero[4] = {};
+        for (int e = lane * 4; e < c.d; e += 256) store4<DT, WIDE>(keys ? c.dK : c.dQ, row, c.d, e, zero);
+        return;
+    }
+    const GradRow<DT, WIDE> mine(c, at);
+    for (int e = lane * 4; e < c.d; e += 256) {
+        float a[4] = {}, x[4] = {};
+        mine.load(e, a, x);
+        mine.store(e, a);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+static size_t layout(DistillPar &c, ContrastPlan &plan, int dtype, int want_grad, char *base)
+{
+    return contrast_layout(c, plan, dtype, want_grad, base, [&](auto &take) {
+        const size_t Br = ct_up(c.B, CT_PAD);
+        c.tiles_k = c.parts_k / 2;
+        take(c.list_key, Br * c.entries);
+        take(c.list_p, Br * c.entries);
+        take(c.list_s, Br * c.entries);
+        take(c.list_g, Br * c.entries);
+        take(c.list_sum, Br);
+        take(c.list_at, Br * (c.tiles_k + 1));
+    });
+}
+
+static int check_distill(int64_t B, int64_t M, int32_t d, int dtype, int32_t entries)
+{
+    const int rc = check_contrast(B, M, d, dtype);
+    if (rc) return rc;
+    return entries < 1 || entries > DS_MAX ? RNND_ERR_BAD_PARAM : RNND_OK;
+}
+
+extern "C" int rnnd_distill_workspace(int64_t B, int64_t M, int32_t d, int dtype, int32_t entries, int want_grad, size_t *bytes)
+{
+    const int rc = check_distill(B, M, d, dtype, entries);
+    if (rc) return rc;
+    if (!bytes) return RNND_ERR_NULL;
+    if (!B) {
+        *bytes = 0;
+        return RNND_OK;
+    }
+    DistillPar c = {};
+    ContrastPlan plan;
+    c.B = (int)B;
+    c.M = (int)M;
+    c.d = d;
+    c.entries = entries;
+    *bytes = layout(c, plan, dtype, want_grad, nullptr);
+    return RNND_OK;
+}
+
+template <int DT, int TILE, bool TERMS>
+static void launch_products(DistillPar &c, int want_grad, int row_blocks, hipStream_t st)
+{
+    const int tq = ct_up(c.B, TILE) / TILE, tk = ct_up(c.M, TILE) / TILE;
+    in_launches((u64)tq * tk, 256, [&](u64 first, u64 blocks) {
+        hipLaunchKernelGGL((k_contrast_sums<TILE, DT, TERMS, DistillPar>), dim3((u32)blocks), dim3(256), 0, st, c, (u32)first, tq, tk);
+    });
+    hipLaunchKernelGGL(k_distill_loss<DT>, dim3((c.B + 3) / 4), dim3(256), 0, st, c, row_blocks);
+    if (!want_grad) return;
+    in_launches((u64)tq * tk, 256, [&](u64 first, u64 blocks) {
+        hipLaunchKernelGGL((k_contrast_g<TILE, DT, TERMS, DistillPar>), dim3((u32)blocks), dim3(256), 0, st, c, (u32)first, tq, tk);
+    });
+}
+
+template <int DT, bool WIDE>
+static void launch_distill(DistillPar &c, const ContrastPlan &plan, int want_grad, hipStream_t st)
+{
+    const int Br = ct_up(c.B, CT_PAD), Mr = ct_up(c.M, CT_PAD);
+    const int key_blocks = Mr / 4 < CT_ROW_BLOCKS ? Mr / 4 : CT_ROW_BLOCKS, row_blocks = Br / 4 < CT_ROW_BLOCKS ? Br / 4 : CT_ROW_BLOCKS;
+    const int across = (want_grad ? c.dr : c.dp) / 64;
+    if constexpr (DT == DT_F32)
+        hipLaunchKernelGGL(k_contrast_centre<DistillPar>, dim3((c.dp + 64 * CT_SAMPLES - 1) / (64 * CT_SAMPLES)), dim3(64 * CT_SAMPLES), 0, st, c);
+    in_launches((u64)(key_blocks + row_blocks) + (u64)((Br + Mr) / 64) * across, 256, [&](u64 first, u64 blocks) {
+        hipLaunchKernelGGL((k_distill_prepare<DT, WIDE>), dim3((u32)blocks), dim3(256), 0, st, c, (u32)first, key_blocks, row_blocks, Br / 64, across,
+                           want_grad, plan.tile);
+    });
+    if constexpr (DT != DT_F32) {
+        if (plan.tile == 256) launch_products<DT, 256, false>(c, want_grad, row_blocks, st);
+        else launch_products<DT, 128, false>(c, want_grad, row_blocks, st);
+    } else if (plan.terms) launch_products<DT, 128, true>(c, want_grad, row_blocks, st);
+    else launch_products<DT, 128, false>(c, want_grad, row_blocks, st);
+    if (!want_grad) return;
+    if constexpr (DT != DT_F32) {
+        if (plan.tile_g == 256) launch_grads<DT, 256>(c, st);
+        else launch_grads<DT, 128>(c, st);
+    } else
+        launch_grads<DT, 128>(c, st);
+    hipLaunchKernelGGL((k_distill_finish<DT, WIDE>), dim3((c.B + c.M + 3) / 4), dim3(256), 0, st, c);
+}
+
+extern "C" int rnnd_distill(const void *Q, int64_t B, const void *K, int64_t M, int32_t d, int dtype, int metric, const int32_t *teacher_ids,
+                            const float *teacher_logits, int32_t entries, int tail, const int32_t *query_ids, const int32_t *key_ids,
+                            const float *key_bias, const float *row_weight, float scale, float *loss, void *dQ, void *dK, void *workspace,
+                            size_t workspace_bytes, void *stream)
+{
+    const int rc = check_distill(B, M, d, dtype, entries);
+    if (rc) return rc;
+    if (metric != RNND_L2SQ) return RNND_ERR_UNSUPPORTED;
+    if (!K || (B && (!Q || !teacher_ids || !teacher_logits || !loss)) || (query_ids && !key_ids)) return RNND_ERR_NULL;
+    if (B && (dQ == nullptr) != (dK == nullptr)) return RNND_ERR_NULL;
+    const size_t size = dt_size(dtype);
+    if (((uintptr_t)Q | (uintptr_t)K | (uintptr_t)dQ | (uintptr_t)dK) % size) return RNND_ERR_BAD_PARAM;
+    if (((uintptr_t)teacher_ids | (uintptr_t)teacher_logits | (uintptr_t)query_ids | (uintptr_t)key_ids | (uintptr_t)key_bias | (uintptr_t)row_weight |
+         (uintptr_t)loss) % 4)
+        return RNND_ERR_BAD_PARAM;
+    if (!std::isfinite(scale) || (tail != 0 && tail != 1)) return RNND_ERR_BAD_PARAM;
+    const int want_grad = dK != nullptr;
+    if (!B) {       // no query: no gradient reaches a key
+        if (!want_grad) return RNND_OK;
+        const size_t n = (size_t)M * d * size / 2, blocks = (n + 1023) / 1024;
+        hipLaunchKernelGGL(k_contrast_zero<DistillPar>, dim3((u32)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, (hipStream_t)stream,
+                           (unsigned short *)dK, n);
+        return launched("rnnd_distill");
+    }
+    DistillPar c = {};
+    ContrastPlan plan;
+    c.Q = Q;
+    c.K = K;
+    c.ids = teacher_ids;
+    c.logits = teacher_logits;
+    c.entries = entries;
+    c.tail = tail;
+    c.query_ids = query_ids;
+    c.key_ids = key_ids;
+    c.bias = key_bias;
+    c.row_weight = row_weight;
+    c.scale = scale;
+    c.c1 = (float)(2.0 * scale * 1.4426950408889634);
+    c.B = (int)B;
+    c.M = (int)M;
+    c.d = d;
+    c.loss = loss;
+    c.dQ = dQ;
+    c.dK = dK;
+    if (!workspace) return RNND_ERR_NULL;
+    if ((uintptr_t)workspace % 16) return RNND_ERR_BAD_PARAM;
+    if (workspace_bytes < layout(c, plan, dtype, want_grad, (char *)workspace)) return RNND_ERR_SCRATCH;
+    hipStream_t st = (hipStream_t)stream;
+    int vec = row_vec(d, Q, (int)size, K, (int)size);
+    if (want_grad) {
+        const int vg = row_vec(d, dQ, (int)size, dK, (int)size);
+        vec = vg < vec ? vg : vec;
+    }
+#define RNND_DISTILL(DT) \
+    if (vec >= 4) launch_distill<DT, true>(c, plan, want_grad, st); \
+    else launch_distill<DT, false>(c, plan, want_grad, st)
+    if (dtype == RNND_F32) { RNND_DISTILL(DT_F32); }
+    else if (dtype == RNND_F16) { RNND_DISTILL(DT_F16); }
+    else { RNND_DISTILL(DT_BF16); }
+#undef RNND_DISTILL
+    return launched("rnnd_distill");
+}

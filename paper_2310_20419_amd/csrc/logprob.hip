@@ -1,0 +1,799 @@
+// Log probabilities under the softmax over squared distances, its entropy, and the most probable keys in their exact order.
+//
+//   s_ij = bias_j - scale |q_i - k_j|^2,  lse_i = log sum_j exp s_ij,  log P_ij = s_ij - lse_i,  H_i = -sum_j P_ij log P_ij
+//
+// In one pass over the logits: of every row and part of the keys the largest logit m, sum exp(s - m) and sum exp(s - m) (s - m), which join
+// like the first two do (all terms of the third have one sign: H = log sum - third / sum loses nothing), all in float32 and base 2.
+//
+// Alternatives.  The same pass keeps of each group of keys (8, or 4 with small tiles) the largest and the second largest logit; the number of the
+// largest one's key stands in the lowest bits of its significand.  k keys are at least as large as the k-th largest of any values that are
+// logits of different keys, so a bound on the k-th logit follows from the parts' largest, a better one from the groups of those parts, and
+// what lies above the better one is little more than k keys.  Their distances are summed again in double precision from the rows as
+// they are, and these decide the order.  The first pass is off by some error E (bounds(), from the norms): keys down to 2 E below
+// the bound are taken along, so E costs time but changes no answer.  Where more keys than there is room for lie that close
+// together (thousands of copies of a row), all groups above the bound are gone through in double precision instead.
+#include <cmath>
+
+#include "contrast.h"
+
+#define LP_ROOM 512             // groups above the bound, and keys among them, that a wavefront has room for
+#define LP_PARTS 512            // parts looked at together
+#define LP_NONE (-3.0e38f)      // stands for -infinity where bits are put into the significand
+#define LP_LOG2E 1.4426950408889634
+#define LP_FEW 8                // queries
+
+struct LogprobPar : ContrastPar {
+    int alternatives;
+    float *logprob, *entropy, *top_logprob;
+    int *top_ids;
+    float *part_w;              // [B padded][parts_k] sum of 2^(s - top) (s - top), s in base 2
+    float2 *groups;             // [B padded][parts_k][groups of a part] largest and second largest
+    int group_shift, part_shift;    // keys of a group, groups of a part: powers of two
+    float *most;                // [2][CT_ROW_BLOCKS] largest |k|^2 and |bias| of a block of keys
+    int most_blocks;
+    int few;                    // logits are from differences: the whole of s
+};
+
+__device__ __forceinline__ bool row_counts(const LogprobPar &, int) { return true; }
+
+__device__ __forceinline__ bool leaves_out(const LogprobPar &c, int i, int j)
+{
+    return key_gone(c, j) || (c.query_ids && c.key_ids[j] == c.query_ids[i]);
+}
+
+// ------------------------------------------------------------------------------------------------ preparation
+// The largest |k|^2 and |bias| of a block's keys; what is not a number counts as infinite.
+struct MostLds { u32 norm, bias; };
+__device__ __forceinline__ void most_of(MostLds &most, const LogprobPar &c, int j, float norm)
+{
+    if (j >= c.M || key_gone(c, j)) return;
+    const float b = c.bias ? fabsf(c.bias[j]) : 0.0f;
+    atomicMax(&most.norm, __float_as_uint(norm < INFINITY ? norm : INFINITY));
+    atomicMax(&most.bias, __float_as_uint(b < INFINITY ? b : INFINITY));
+}
+
+// A wavefront per row, keys first; then the copies of the rows (contrast_copy()).  key_tiles: 0 where the keys have been prepared.
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(256) void k_logprob_prepare(LogprobPar c, u32 first, int key_blocks, int row_blocks, int q_tiles, int across)
+{
+    __shared__ MostLds most;
+    const int block = (int)(first + blockIdx.x), id = block - key_blocks - row_blocks;
+    if (id >= 0) {
+        contrast_copy<DT, WIDE>(c, id / across, id % across * 64, q_tiles, 0);
+        return;
+    }
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (block < key_blocks) {
+        if (threadIdx.x == 0) most = {0, 0};
+        __syncthreads();
+        for (int at = block * 4 + wave; at < ct_up(c.M, CT_PAD); at += key_blocks * 4) {
+            const float norm = key_side<DT, WIDE>(c, at, lane);
+            if (lane == 0) most_of(most, c, at, norm);
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            c.most[block] = __uint_as_float(most.norm);
+            c.most[CT_ROW_BLOCKS + block] = __uint_as_float(most.bias);
+        }
+        return;
+    }
+    for (int at = (block - key_blocks) * 256 + threadIdx.x; at < ct_up(c.B, CT_PAD); at += row_blocks * 256) {
+        c.row_id[at] = make_int2(CT_NEVER, at < c.B && c.query_ids ? c.query_ids[at] : CT_NEVER);
+        c.row_g[at] = make_float2(0.0f, 0.0f);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ the logits by tiles
+// Puts a logit into the largest two of its group.
+__device__ __forceinline__ void into_group(float &most, float &second, float s, int n, int group)
+{
+    const float x = __uint_as_float((__float_as_uint(fmaxf(s, LP_NONE)) & ~(u32)(group - 1)) | (u32)n);
+    second = __builtin_amdgcn_fmed3f(most, second, x);      // most >= second
+    most = fmaxf(most, x);
+}
+
+template <int TILE, int DT, bool TERMS, bool TOPS>
+__global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_logprob_sums(LogprobPar c, u32 first, int tiles_q, int tiles_k)
+{
+    constexpr int N = TILE / 32;
+    __shared__ typename std::conditional<TERMS, TermsLds, ProductLds<TILE>>::type lds;
+    __shared__ SideLds<TILE> side;
+    f32x4 acc[N][N];
+    int tr, tc;
+    tile_of((int)(first + blockIdx.x), tiles_q, tiles_k, tr, tc);
+    logit_product<TILE, DT, TERMS>(c, tr, tc, lds, side, acc, []() {});
+    const Place<TILE> at(tr, tc);
+    float base[N];
+    int id[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        base[n] = side.base[at.in_col + n];
+        id[n] = side.id[at.in_col + n];
+    }
+    // as in k_contrast_sums; and a lane's N columns of a row are a group
+    float keep_top[N / 4], keep_sum[N / 4], keep_w[N / 4];
+#pragma unroll
+    for (int m = 0; m < N; ++m) {
+        float s[4][N], top[4], sum[4], w[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int n = 0; n < N; ++n) s[r][n] = fmaf(acc[m][n][r], c.c1, base[n]);
+        leave_out(side, at.in_row + m * 4, id, s);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            if constexpr (TOPS) {
+                float most = -INFINITY, second = -INFINITY;
+#pragma unroll
+                for (int n = 0; n < N; ++n) into_group(most, second, s[r][n], n, N);
+                c.groups[((size_t)(at.row + m * 4 + r) * c.parts_k + at.half_c) * 16 + (threadIdx.x & 15)] = make_float2(most, second);
+            }
+            top[r] = s[r][0];
+#pragma unroll
+            for (int n = 1; n < N; ++n) top[r] = fmaxf(top[r], s[r][n]);
+        }
+        row16_max(top);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float ref = top[r] == -INFINITY ? 0.0f : top[r];
+            sum[r] = w[r] = 0.0f;
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const float x = s[r][n] - ref, e = __builtin_amdgcn_exp2f(x);
+                sum[r] += e;
+                w[r] = fmaf(e, fmaxf(x, LP_NONE), w[r]);
+            }
+        }
+        row16_sum(sum);
+        row16_sum(w);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const bool mine = (int)(threadIdx.x & 15) == m % 4 * 4 + r;
+            keep_top[m / 4] = mine ? top[r] : m % 4 || r ? keep_top[m / 4] : 0.0f;
+            keep_sum[m / 4] = mine ? sum[r] : m % 4 || r ? keep_sum[m / 4] : 0.0f;
+            keep_w[m / 4] = mine ? w[r] : m % 4 || r ? keep_w[m / 4] : 0.0f;
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < N / 4; ++h) {
+        const size_t to = (size_t)(at.row + h * 16 + (threadIdx.x & 15)) * c.parts_k + at.half_c;
+        c.part[to] = make_float2(keep_top[h], keep_sum[h]);
+        c.part_w[to] = keep_w[h];
+    }
+}
+
+// (largest, sum, weighted sum) of two parts; a NaN in either sum stays
+__device__ __forceinline__ void join_three(float &top, float &sum, float &w, float ot, float os, float ow)
+{
+    const float m = fmaxf(top, ot), ref = m == -INFINITY ? 0.0f : m;
+    const float da = fmaxf(top - ref, LP_NONE), db = fmaxf(ot - ref, LP_NONE), fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
+    w = fa * fmaf(sum, da, w) + fb * fmaf(os, db, ow);
+    sum = sum * fa + os * fb;
+    top = m;
+}
+
+// ------------------------------------------------------------------------------------------------ the logits of a few queries
+// Up to 8 queries: no matrix tile would be filled, and the call is bound by reading the keys once.  8 lanes take a row, 16 bytes each, a
+// wavefront 16 rows at a time; distances are summed from differences.  Query coordinates come from LDS, as many of all queries as
+// fit at a time.  A block takes a part of the keys; its wavefronts then take the sums of a query each.
+#define LP_CHUNK 8192           // coordinates in LDS
+#define LP_PASS 64              // keys of a block's pass
+template <int DT, int NB, bool WIDE>
+__global__ __launch_bounds__(256) void k_logprob_few(LogprobPar c, int part_keys)
+{
+    constexpr int V = DT == DT_F32 ? 4 : 8, R = 2;
+    __shared__ __align__(16) float query[LP_CHUNK];
+    __shared__ float logit[NB][LP_PASS];
+    __shared__ MostLds most;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane & 7;
+    const int chunk = c.d <= LP_CHUNK / NB ? (c.d + 7) & ~7 : LP_CHUNK / NB;
+    const int key0 = blockIdx.x * part_keys;
+    auto stage = [&](int e0) {
+        for (int t = threadIdx.x; t < NB * chunk; t += 256) {
+            const int b = t / chunk, e = e0 + t - b * chunk;
+            query[t] = e < c.d ? (float)((const typename RowType<DT>::T *)c.Q)[(size_t)(b < c.B ? b : c.B - 1) * c.d + e] : 0.0f;
+        }
+    };
+    if (threadIdx.x == 0) most = {0, 0};
+    if (chunk >= c.d) stage(0);
+    __syncthreads();
+    // of the queries wave, wave + 4
+    float top[(NB + 3) / 4], sum[(NB + 3) / 4], w[(NB + 3) / 4];
+#pragma unroll
+    for (int h = 0; h < (NB + 3) / 4; ++h) {
+        top[h] = -INFINITY;
+        sum[h] = w[h] = 0.0f;
+    }
+    for (int pass = 0; pass < part_keys; pass += LP_PASS) {
+        int key[R];
+        float acc[NB][R] = {};
+#pragma unroll
+        for (int r = 0; r < R; ++r) key[r] = key0 + pass + wave * 16 + r * 8 + (lane >> 3);
+        for (int e0 = 0; e0 < c.d; e0 += chunk) {
+            if (chunk < c.d) {
+                __syncthreads();
+                stage(e0);
+                __syncthreads();
+            }
+            const int end = c.d - e0 < chunk ? c.d - e0 : chunk;
+#pragma unroll 2
+            for (int e = sub * V; e < end; e += 8 * V) {
+                float x[R][V];
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const size_t row = key[r] < c.M ? key[r] : c.M - 1;
+                    if constexpr (WIDE) unpack<DT, V>(load_pack<DT, V>(c.K, row * c.d + e0 + e), x[r]);
+                    else
+#pragma unroll
+                        for (int k = 0; k < V; ++k)
+                            x[r][k] = e + k < end ? (float)((const typename RowType<DT>::T *)c.K)[row * c.d + e0 + e + k] : 0.0f;
+                }
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int k = 0; k < V; k += 4) {
+                        const f32x4 q = *(const f32x4 *)&query[b * chunk + e + k];
+#pragma unroll
+                        for (int r = 0; r < R; ++r)
+#pragma unroll
+                            for (int h = 0; h < 4; ++h) {
+                                const float diff = x[r][k + h] - q[h];
+                                acc[b][r] = fmaf(diff, diff, acc[b][r]);
+                            }
+                    }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                acc[b][r] += xor_lane_f32<1>(acc[b][r]);
+                acc[b][r] += xor_lane_f32<2>(acc[b][r]);
+                acc[b][r] += xor_lane_f32<7>(acc[b][r]);
+            }
+            // lane b of the 8 writes query b
+            float far = acc[0][r];
+#pragma unroll
+            for (int b = 1; b < NB; ++b) far = sub == b ? acc[b][r] : far;
+            if (sub < NB) {
+                const int j = key[r];
+                const bool out = j >= c.M || sub >= c.B || leaves_out(c, sub, j);
+                logit[sub][wave * 16 + r * 8 + (lane >> 3)] =
+                    out ? -INFINITY : ((c.bias ? c.bias[j] : 0.0f) - c.scale * far) * 1.44269504f;
+                if (sub == 0) most_of(most, c, j, 0.0f);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < (NB + 3) / 4; ++h) {
+            const int b = wave + h * 4;
+            if (b >= c.B) break;
+            const float s = logit[b][lane];
+            if (c.alternatives) {       // 8 lanes are a group
+                float x = __uint_as_float((__float_as_uint(fmaxf(s, LP_NONE)) & ~7u) | (u32)sub), y = LP_NONE;
+                auto with = [&](float ox, float oy) {
+                    y = fmaxf(fminf(x, ox), fmaxf(y, oy));
+                    x = fmaxf(x, ox);
+                };
+                with(xor_lane_f32<1>(x), xor_lane_f32<1>(y));
+                with(xor_lane_f32<2>(x), xor_lane_f32<2>(y));
+                with(xor_lane_f32<7>(x), xor_lane_f32<7>(y));
+                if (sub == 0) c.groups[((size_t)b * gridDim.x + blockIdx.x) * (part_keys / 8) + pass / 8 + (lane >> 3)] = make_float2(x, y);
+            }
+            const float m = fmaxf(top[h], s), ref = m == -INFINITY ? 0.0f : m;      // a lane's own
+            const float da = fmaxf(top[h] - ref, LP_NONE), x = s - ref, fa = __builtin_amdgcn_exp2f(da), e = __builtin_amdgcn_exp2f(x);
+            w[h] = fmaf(e, fmaxf(x, LP_NONE), fa * fmaf(sum[h], da, w[h]));
+            sum[h] = fmaf(sum[h], fa, e);
+            top[h] = m;
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int h = 0; h < (NB + 3) / 4; ++h) {
+        const int b = wave + h * 4;
+        if (b >= c.B) break;
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) join_three(top[h], sum[h], w[h], __shfl_xor(top[h], s), __shfl_xor(sum[h], s), __shfl_xor(w[h], s));
+        if (lane == 0) {
+            c.part[(size_t)b * gridDim.x + blockIdx.x] = make_float2(top[h], sum[h]);
+            c.part_w[(size_t)b * gridDim.x + blockIdx.x] = w[h];
+        }
+    }
+    if (c.alternatives && threadIdx.x == 0) c.most[blockIdx.x] = __uint_as_float(most.bias);
+}
+
+// ------------------------------------------------------------------------------------------------ the answers
+// |q_i - k_j|^2 in double precision, by 8 lanes
+template <int DT, bool WIDE>
+__device__ __forceinline__ double exact_distance(const LogprobPar &c, int i, int j, int sub)
+{
+    constexpr int V = DT == DT_F32 ? 4 : 8;
+    double sum = 0.0;
+    const size_t q = (size_t)i * c.d, k = (size_t)j * c.d;
+#pragma unroll 4
+    for (int e = sub * V; e < c.d; e += 8 * V) {
+        float x[V], y[V];
+        if constexpr (WIDE) {
+            unpack<DT, V>(load_pack<DT, V>(c.Q, q + e), x);
+            unpack<DT, V>(load_pack<DT, V>(c.K, k + e), y);
+        } else
+#pragma unroll
+            for (int h = 0; h < V; ++h) {
+                const bool in = e + h < c.d;
+                x[h] = in ? (float)((const typename RowType<DT>::T *)c.Q)[q + e + h] : 0.0f;
+                y[h] = in ? (float)((const typename RowType<DT>::T *)c.K)[k + e + h] : 0.0f;
+            }
+#pragma unroll
+        for (int h = 0; h < V; ++h) {
+            const double diff = (double)x[h] - (double)y[h];
+            sum = fma(diff, diff, sum);
+        }
+    }
+    sum += __shfl_xor(sum, 1);
+    sum += __shfl_xor(sum, 2);
+    sum += __shfl_xor(sum, 4);
+    return sum;
+}
+
+// What the product's logits leave out: |q - centre|^2, by a wavefront
+template <int DT, bool WIDE>
+__device__ __forceinline__ double query_norm(const LogprobPar &c, int i, int lane)
+{
+    double sum = 0.0;
+    for (int e = lane * 4; e < c.d; e += 256) {
+        float x[4];
+        load4<DT, WIDE>(c.Q, i, c.d, e, x);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const double v = (double)x[k] - (DT == DT_F32 && e + k < c.d ? (double)c.centre[e + k] : 0.0);
+            sum = fma(v, v, sum);
+        }
+    }
+#pragma unroll
+    for (int s = 32; s; s >>= 1) sum += __shfl_xor(sum, s);
+    return sum;
+}
+
+__device__ __forceinline__ u32 in_order(float x)        // unsigned integers in the order of the numbers
+{
+    const u32 b = __float_as_uint(x);
+    return b ^ (b >> 31 ? 0xFFFFFFFFu : 0x80000000u);
+}
+__device__ __forceinline__ float from_order(u32 o) { return __uint_as_float(o ^ (o >> 31 ? 0x80000000u : 0xFFFFFFFFu)); }
+
+// A bound from below on the k-th largest of n values (-infinity where there are fewer), by a wavefront: the highest 24 bits of it.
+template <typename F>
+__device__ __forceinline__ float kth_largest(int n, int k, int lane, F value)
+{
+    u32 at = 0;
+    for (int bit = 31; bit >= 8; --bit) {
+        const u32 t = at | 1u << bit;
+        int count = 0;
+        for (int e = 0; e < n; e += 64) count += (int)__popcll(__ballot(e + lane < n && in_order(value(e)) >= t));
+        if (count >= k) at = t;
+    }
+    return at >= in_order(-INFINITY) ? from_order(at) : -INFINITY;
+}
+
+struct FinishLds {
+    float most[LP_ROOM], second[LP_ROOM];
+    int group[LP_ROOM], key[LP_ROOM];
+    double value[LP_ROOM];
+    int part[LP_PARTS];
+};
+
+// A wavefront per query.
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(128) void k_logprob_finish(LogprobPar c)
+{
+    __shared__ FinishLds of_waves[2];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = blockIdx.x * 2 + wave, sub = lane & 7;
+    if (i >= c.B) return;
+    FinishLds &lds = of_waves[wave];
+    float top = -INFINITY, sum = 0.0f, w = 0.0f, first = -INFINITY, second = -INFINITY;
+    const float2 *part = c.part + (size_t)i * c.parts_k;
+#pragma unroll 4
+    for (int t = lane; t < c.parts_k; t += 64) {
+        const float2 p = part[t];
+        join_three(top, sum, w, p.x, p.y, c.part_w[(size_t)i * c.parts_k + t]);
+        second = fmaxf(second, fminf(first, p.x));
+        first = fmaxf(first, p.x);
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) join_three(top, sum, w, __shfl_xor(top, s), __shfl_xor(sum, s), __shfl_xor(w, s));
+    const bool none = sum == 0.0f, bad = !(sum >= 0.0f && sum < INFINITY);
+    const double lse = (double)top + log2((double)sum), norm = c.few ? 0.0 : query_norm<DT, WIDE>(c, i, lane);
+    auto exactly = [&](int j) {     // in base 2 and the frame of the sums; by 8 lanes
+        return ((c.bias ? (double)c.bias[j] : 0.0) - (double)c.scale * (exact_distance<DT, WIDE>(c, i, j, sub) - norm)) * LP_LOG2E;
+    };
+    auto log_of = [&](double s) {   // (a probability is not above 1)
+        const double l = (s - lse) * 0.69314718055994531;
+        return bad ? NAN : (float)(l < 0.0 ? l : 0.0);
+    };
+    if (c.entropy && lane == 0) c.entropy[i] = none ? 0.0f : bad ? NAN : (log2f(sum) - w / sum) * 0.693147181f;
+    if (c.logprob) {
+        const int t = c.target[i];
+        const bool on = (u32)t < (u32)c.M && !leaves_out(c, i, t);
+        const float l = on ? log_of(exactly(t)) : 0.0f;
+        if (lane == 0) c.logprob[i] = l;
+    }
+    const int k = c.alternatives;
+    if (!k) return;
+    int *ids = c.top_ids + (size_t)i * k;
+    float *tops = c.top_logprob + (size_t)i * k;
+    if (none || bad) {
+        for (int e = lane; e < k; e += 64) {
+            ids[e] = -1;
+            tops[e] = bad ? NAN : -INFINITY;
+        }
+        return;
+    }
+    // how far a logit of the first pass may be off, in base 2: a sum of d products of one rounding each (float32 rows: six times as many), its
+    // scaling, the key's own sum and bias; for a few queries a sum of d squares, which with the bias make up the logit
+    float norms = 0.0f, biases = 0.0f;
+    for (int b = lane; b < c.most_blocks; b += 64) {
+        if (!c.few) norms = fmaxf(norms, c.most[b]);
+        biases = fmaxf(biases, c.most[c.few ? b : CT_ROW_BLOCKS + b]);
+    }
+#pragma unroll
+    for (int s = 32; s; s >>= 1) {
+        norms = fmaxf(norms, __shfl_xor(norms, s));
+        biases = fmaxf(biases, __shfl_xor(biases, s));
+    }
+    const float u = 1.19209290e-7f, terms = DT == DT_F32 ? 6.0f : 1.0f;
+    const float error = c.few ? u * (float)(c.d + 16) * biases * 1.45f
+                              : 1.45f * (u * fabsf(c.scale) * (2.0f * (terms * c.d + 16.0f) * sqrtf((float)norm * norms) + (float)(c.d + 16) * norms) + 2.0f * u * biases);
+    auto below = [&](float t) {     // t: a bound on the k-th logit as the first pass has it, with the key's number in it
+        if (t <= LP_NONE) return -INFINITY;
+        const float cut = t - 2.0f * error - fabsf(t) * (4.0e-6f + (c.few ? 2.0f * u * (float)(c.d + 16) : 0.0f));
+        return cut > LP_NONE ? cut : -INFINITY;
+    };
+    float cut = below(kth_largest(128, k, lane, [&](int e) { return e ? second : first; }));
+    int n = 0;
+    bool full = false;
+    // the groups above the bound: keeps those that are above a better one
+    auto tighten = [&]() {
+        if (n < k) return;
+        wave_sync();
+        cut = fmaxf(cut, below(kth_largest(n, k, lane, [&](int e) { return lds.most[e + lane]; })));
+        int kept = 0;
+        for (int e = 0; e < n; e += 64) {
+            const bool in = e + lane < n;
+            const float a = in ? lds.most[e + lane] : 0.0f, b = in ? lds.second[e + lane] : 0.0f;
+            const int g = in ? lds.group[e + lane] : 0;
+            const u64 on = __ballot(in && a >= cut);
+            wave_sync();
+            if (on >> lane & 1) {
+                const int to = kept + (int)__popcll(on & lanes_below(lane));
+                lds.most[to] = a;
+                lds.second[to] = b;
+                lds.group[to] = g;
+            }
+            kept += (int)__popcll(on);
+            wave_sync();
+        }
+        n = kept;
+    };
+    const float2 *groups = c.groups + ((size_t)i * c.parts_k << c.part_shift);
+    for (int p0 = 0; p0 < c.parts_k && !full; p0 += LP_PARTS) {
+        int parts = 0;
+#pragma unroll
+        for (int h = 0; h < LP_PARTS; h += 64) {
+            const int p = p0 + h + lane;
+            const float largest = p < c.parts_k ? part[p].x : -INFINITY;
+            const u64 on = __ballot(largest > -INFINITY && largest >= cut);
+            if (on >> lane & 1) lds.part[parts + (int)__popcll(on & lanes_below(lane))] = p;
+            parts += (int)__popcll(on);
+        }
+        wave_sync();
+        const int items = parts << c.part_shift;
+        for (int t0 = 0; t0 < items && !full; t0 += 256) {
+            float2 v[4];
+            int g[4];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const int t = t0 + h * 64 + lane;
+                g[h] = t < items ? (lds.part[t >> c.part_shift] << c.part_shift) + (t & ((1 << c.part_shift) - 1)) : -1;
+                v[h] = g[h] >= 0 ? groups[g[h]] : make_float2(-INFINITY, -INFINITY);
+            }
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                u64 on = __ballot(v[h].x > LP_NONE * 0.99f && v[h].x >= cut);
+                if (!on) continue;
+                if (n + (int)__popcll(on) > LP_ROOM && !full) {
+                    tighten();
+                    on = __ballot(v[h].x > LP_NONE * 0.99f && v[h].x >= cut);
+                    full = n + (int)__popcll(on) > LP_ROOM;
+                }
+                if (full) continue;
+                if (on >> lane & 1) {
+                    const int to = n + (int)__popcll(on & lanes_below(lane));
+                    lds.most[to] = v[h].x;
+                    lds.second[to] = v[h].y;
+                    lds.group[to] = g[h];
+                }
+                n += (int)__popcll(on);
+            }
+        }
+        wave_sync();
+    }
+    const int size = 1 << c.group_shift;
+    int found = 0;
+    if (!full) {
+        tighten();
+        wave_sync();
+        // the keys: the largest of a group, or all where the second is above the bound too
+        for (int e = 0; e < n && !full; e += 64) {
+            const bool in = e + lane < n && lds.most[e + lane] >= cut;
+            const int g = in ? lds.group[e + lane] : 0, mine = !in ? 0 : lds.second[e + lane] >= cut && lds.second[e + lane] > LP_NONE * 0.99f ? size : 1;
+            int upto = inclusive(mine, lane);
+            const int all = __builtin_amdgcn_readlane(upto, 63);
+            if (found + all > LP_ROOM) {
+                full = true;
+                break;
+            }
+            upto += found - mine;
+            if (mine == 1) lds.key[upto] = (g << c.group_shift) + (int)(__float_as_uint(lds.most[e + lane]) & (u32)(size - 1));
+            else
+                for (int h = 0; h < mine; ++h) lds.key[upto + h] = (g << c.group_shift) + h;
+            found += all;
+        }
+    }
+    if (!full) {
+        wave_sync();
+        for (int e = 0; e < found; e += 8) {
+            const int at = e + (lane >> 3), j = at < found ? lds.key[at] : c.M;
+            const bool on = j < c.M && !leaves_out(c, i, j);
+            const double s = exactly(on ? j : 0);
+            if (sub == 0 && at < found) {
+                lds.value[at] = s;
+                if (!on || !(s > -INFINITY)) lds.key[at] = -1;
+            }
+        }
+        wave_sync();
+        int valid = 0;
+        for (int e = 0; e < found; e += 64) {
+            const int j = e + lane < found ? lds.key[e + lane] : -1;
+            const double s = j >= 0 ? lds.value[e + lane] : 0.0;
+            int rank = 0;
+            for (int o = 0; o < found; ++o) {
+                const double os = lds.value[o];
+                const int oj = lds.key[o];
+                rank += oj >= 0 && (os > s || (os == s && oj < j));
+            }
+            if (j >= 0 && rank < k) {
+                ids[rank] = j;
+                tops[rank] = log_of(s);
+            }
+            valid += (int)__popcll(__ballot(j >= 0));
+        }
+        for (int e = valid + lane; e < k; e += 64) {
+            ids[e] = -1;
+            tops[e] = -INFINITY;
+        }
+        return;
+    }
+    // No room: every key of a group above the bound, in the order of their positions, into a list of the k best so far.  The bound stays valid:
+    // keys that are not looked at are below k others.
+    wave_sync();
+    found = 0;
+    for (int g0 = 0; g0 < c.parts_k << c.part_shift; g0 += 64) {
+        const int g = g0 + lane;
+        const float largest = g < c.parts_k << c.part_shift ? groups[g].x : -INFINITY;
+        for (u64 on = __ballot(largest > LP_NONE * 0.99f && largest >= cut); on; on &= on - 1) {
+            const int key0 = (g0 + __builtin_ctzll(on)) << c.group_shift, j = key0 + (lane >> 3);
+            bool in = lane >> 3 < size && j < c.M && !leaves_out(c, i, j);
+            const double s = exactly(in ? j : 0);
+            in &= s > -INFINITY;
+            for (int h = 0; h < size; ++h) {
+                if (!__builtin_amdgcn_readlane((int)in, h * 8)) continue;
+                const double x = __shfl(s, h * 8);
+                // its place: behind those that are at least as large
+                const double a = lane < found ? lds.value[lane] : 0.0, b = 64 + lane < found ? lds.value[64 + lane] : 0.0;
+                const int ka = lane < found ? lds.key[lane] : 0, kb = 64 + lane < found ? lds.key[64 + lane] : 0;
+                const int at = (int)__popcll(__ballot(lane < found && a >= x)) + (int)__popcll(__ballot(64 + lane < found && b >= x));
+                if (at >= k) continue;
+                wave_sync();
+                if (lane >= at && lane < found && lane + 1 < k) {
+                    lds.value[lane + 1] = a;
+                    lds.key[lane + 1] = ka;
+                }
+                if (64 + lane >= at && 64 + lane < found && 65 + lane < k) {
+                    lds.value[65 + lane] = b;
+                    lds.key[65 + lane] = kb;
+                }
+                if (lane == 0) {
+                    lds.value[at] = x;
+                    lds.key[at] = key0 + h;
+                }
+                found = found < k ? found + 1 : k;
+                wave_sync();
+            }
+        }
+    }
+    for (int e = lane; e < k; e += 64) {
+        ids[e] = e < found ? lds.key[e] : -1;
+        tops[e] = e < found ? log_of(lds.value[e]) : -INFINITY;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+struct LogprobPlan {
+    ContrastPlan tiles;
+    int slab;           // queries of a run through the keys
+    int part_keys;      // a few queries: keys of a block
+};
+
+#define LP_BYTES ((size_t)1 << 28)      // of a run's parts and groups
+
+static size_t layout(LogprobPar &c, LogprobPlan &plan, int dtype, char *base)
+{
+    size_t off = 0;
+    auto take = [&](auto *&p, size_t count) {
+        p = (typename std::remove_reference<decltype(p)>::type)(base + off);
+        off += ws_align(count * sizeof(*p));
+    };
+    const int queries = c.B;
+    c.few = c.B <= LP_FEW;
+    if (c.few) {
+        // parts: a wavefront joins them in the end, so not more than some 2,000
+        plan.part_keys = LP_PASS;
+        while ((c.M + plan.part_keys - 1) / plan.part_keys > 2048) plan.part_keys *= 2;
+        plan.slab = c.B;
+        c.parts_k = (c.M + plan.part_keys - 1) / plan.part_keys;
+        c.group_shift = 3;
+        c.part_shift = __builtin_ctz(plan.part_keys / 8);
+        c.most_blocks = c.parts_k;
+        take(c.most, c.parts_k);
+        take(c.part, (size_t)c.B * c.parts_k);
+        take(c.part_w, (size_t)c.B * c.parts_k);
+        if (c.alternatives) take(c.groups, (size_t)c.B * c.parts_k << c.part_shift);
+        return off;
+    }
+    plan.tiles = contrast_plan(c, dtype == RNND_F32 ? 3 : 1);
+    c.part_shift = 4;
+    const size_t row = (size_t)c.parts_k * (12 + (c.alternatives ? 16 * 8 : 0));
+    const size_t rows = LP_BYTES / row / CT_PAD * CT_PAD;
+    plan.slab = rows < CT_PAD ? CT_PAD : rows < (size_t)queries ? (int)rows : queries;
+    c.B = plan.slab < queries ? plan.slab : queries;
+    off = contrast_layout(c, plan.tiles, dtype, 0, base, [](auto &) {});     // (tiles for the queries of a run)
+    c.group_shift = plan.tiles.tile == 256 ? 3 : 2;
+    const size_t Br = ct_up(c.B, CT_PAD);
+    take(c.most, 2 * CT_ROW_BLOCKS);
+    take(c.part_w, Br * c.parts_k);
+    if (c.alternatives) take(c.groups, (Br * c.parts_k) << c.part_shift);
+    c.B = queries;
+    return off;
+}
+
+static int check_logprob(int64_t B, int64_t M, int32_t d, int dtype, int32_t alternatives)
+{
+    const int rc = check_contrast(B, M, d, dtype);
+    if (rc) return rc;
+    return alternatives < 0 || alternatives > RNND_MAX_LISTED ? RNND_ERR_BAD_PARAM : RNND_OK;
+}
+
+extern "C" int rnnd_logprob_workspace(int64_t B, int64_t M, int32_t d, int dtype, int32_t alternatives, size_t *bytes)
+{
+    const int rc = check_logprob(B, M, d, dtype, alternatives);
+    if (rc) return rc;
+    if (!bytes) return RNND_ERR_NULL;
+    if (!B) {
+        *bytes = 0;
+        return RNND_OK;
+    }
+    LogprobPar c = {};
+    LogprobPlan plan;
+    c.B = (int)B;
+    c.M = (int)M;
+    c.d = d;
+    c.alternatives = alternatives;
+    *bytes = layout(c, plan, dtype, nullptr);
+    return RNND_OK;
+}
+
+template <int DT, int TILE, bool TERMS>
+static void launch_sums(LogprobPar &c, hipStream_t st)
+{
+    const int tq = ct_up(c.B, TILE) / TILE, tk = ct_up(c.M, TILE) / TILE;
+    in_launches((u64)tq * tk, 256, [&](u64 first, u64 blocks) {
+        if (c.alternatives) hipLaunchKernelGGL((k_logprob_sums<TILE, DT, TERMS, true>), dim3((u32)blocks), dim3(256), 0, st, c, (u32)first, tq, tk);
+        else hipLaunchKernelGGL((k_logprob_sums<TILE, DT, TERMS, false>), dim3((u32)blocks), dim3(256), 0, st, c, (u32)first, tq, tk);
+    });
+}
+
+template <int DT, bool WIDE>
+static void launch_logprob(LogprobPar &c, const LogprobPlan &plan, bool wide_few, hipStream_t st)
+{
+    if (c.few) {
+        const dim3 grid(c.parts_k), block(256);
+#define LP_LAUNCH(NB) \
+        if (wide_few) hipLaunchKernelGGL((k_logprob_few<DT, NB, true>), grid, block, 0, st, c, plan.part_keys); \
+        else hipLaunchKernelGGL((k_logprob_few<DT, NB, false>), grid, block, 0, st, c, plan.part_keys)
+        if (c.B == 1) { LP_LAUNCH(1); }
+        else if (c.B == 2) { LP_LAUNCH(2); }
+        else if (c.B <= 4) { LP_LAUNCH(4); }
+        else { LP_LAUNCH(8); }
+#undef LP_LAUNCH
+    } else {
+        const int Br = ct_up(c.B, CT_PAD), Mr = ct_up(c.M, CT_PAD), across = c.dp / 64;
+        const bool keys = c.most_blocks == 0;       // not yet prepared
+        const int key_blocks = !keys ? 0 : Mr / 4 < CT_ROW_BLOCKS ? Mr / 4 : CT_ROW_BLOCKS, row_blocks = Br / CT_PAD < CT_ROW_BLOCKS ? Br / CT_PAD : CT_ROW_BLOCKS;
+        if (keys) c.most_blocks = key_blocks;
+        if constexpr (DT == DT_F32)
+            if (keys)
+                hipLaunchKernelGGL(k_contrast_centre<LogprobPar>, dim3((c.dp + 64 * CT_SAMPLES - 1) / (64 * CT_SAMPLES)), dim3(64 * CT_SAMPLES), 0, st, c);
+        in_launches((u64)(key_blocks + row_blocks) + (u64)((Br + (keys ? Mr : 0)) / 64) * across, 256, [&](u64 first, u64 blocks) {
+            hipLaunchKernelGGL((k_logprob_prepare<DT, WIDE>), dim3((u32)blocks), dim3(256), 0, st, c, (u32)first, key_blocks, row_blocks, Br / 64, across);
+        });
+        if constexpr (DT != DT_F32) {
+            if (plan.tiles.tile == 256) launch_sums<DT, 256, false>(c, st);
+            else launch_sums<DT, 128, false>(c, st);
+        } else if (plan.tiles.terms) launch_sums<DT, 128, true>(c, st);
+        else launch_sums<DT, 128, false>(c, st);
+    }
+    if (wide_few) hipLaunchKernelGGL((k_logprob_finish<DT, true>), dim3((c.B + 1) / 2), dim3(128), 0, st, c);
+    else hipLaunchKernelGGL((k_logprob_finish<DT, false>), dim3((c.B + 1) / 2), dim3(128), 0, st, c);
+}
+
+extern "C" int rnnd_logprob(const void *Q, int64_t B, const void *K, int64_t M, int32_t d, int dtype, int metric, const int32_t *target,
+                            const int32_t *query_ids, const int32_t *key_ids, const float *key_bias, float scale, int32_t alternatives,
+                            float *logprob, float *entropy, int32_t *top_ids, float *top_logprob, void *workspace, size_t workspace_bytes,
+                            void *stream)
+{
+    const int rc = check_logprob(B, M, d, dtype, alternatives);
+    if (rc) return rc;
+    if (metric != RNND_L2SQ) return RNND_ERR_UNSUPPORTED;
+    if (!K || (B && !Q) || (query_ids && !key_ids)) return RNND_ERR_NULL;
+    if (B && ((target == nullptr) != (logprob == nullptr) || (alternatives && (!top_ids || !top_logprob)))) return RNND_ERR_NULL;
+    const size_t size = dt_size(dtype);
+    if (((uintptr_t)Q | (uintptr_t)K) % size) return RNND_ERR_BAD_PARAM;
+    if (((uintptr_t)target | (uintptr_t)query_ids | (uintptr_t)key_ids | (uintptr_t)key_bias | (uintptr_t)logprob | (uintptr_t)entropy |
+         (uintptr_t)top_ids | (uintptr_t)top_logprob) % 4)
+        return RNND_ERR_BAD_PARAM;
+    if (!std::isfinite(scale)) return RNND_ERR_BAD_PARAM;
+    if (!B) return RNND_OK;
+    LogprobPar c = {};
+    LogprobPlan plan;
+    c.Q = Q;
+    c.K = K;
+    c.target = target;
+    c.query_ids = query_ids;
+    c.key_ids = key_ids;
+    c.bias = key_bias;
+    c.scale = scale;
+    c.c1 = (float)(2.0 * scale * LP_LOG2E);
+    c.B = (int)B;
+    c.M = (int)M;
+    c.d = d;
+    c.alternatives = alternatives;
+    c.logprob = logprob;
+    c.entropy = entropy;
+    c.top_ids = top_ids;
+    c.top_logprob = top_logprob;
+    if (!workspace) return RNND_ERR_NULL;
+    if ((uintptr_t)workspace % 16) return RNND_ERR_BAD_PARAM;
+    if (workspace_bytes < layout(c, plan, dtype, (char *)workspace)) return RNND_ERR_SCRATCH;
+    hipStream_t st = (hipStream_t)stream;
+    const int vec = row_vec(d, Q, (int)size, K, (int)size);
+    const bool wide_few = vec >= (dtype == RNND_F32 ? 4 : 8);
+    const int queries = c.B;
+    for (int q0 = 0; q0 < queries; q0 += plan.slab) {
+        c.B = queries - q0 < plan.slab ? queries - q0 : plan.slab;
+        c.Q = (const char *)Q + (size_t)q0 * d * size;
+        c.target = target ? target + q0 : nullptr;
+        c.query_ids = query_ids ? query_ids + q0 : nullptr;
+        c.logprob = logprob ? logprob + q0 : nullptr;
+        c.entropy = entropy ? entropy + q0 : nullptr;
+        c.top_ids = top_ids ? top_ids + (size_t)q0 * alternatives : nullptr;
+        c.top_logprob = top_logprob ? top_logprob + (size_t)q0 * alternatives : nullptr;
+#define RNND_LOGPROB(DT) \
+        if (vec >= 4) launch_logprob<DT, true>(c, plan, wide_few, st); \
+        else launch_logprob<DT, false>(c, plan, wide_few, st)
+        if (dtype == RNND_F32) { RNND_LOGPROB(DT_F32); }
+        else if (dtype == RNND_F16) { RNND_LOGPROB(DT_F16); }
+        else { RNND_LOGPROB(DT_BF16); }
+#undef RNND_LOGPROB
+    }
+    return launched("rnnd_logprob");
+}
