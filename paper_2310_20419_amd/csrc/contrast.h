@@ -584,7 +584,7 @@ template <int TILE> struct SideLds {
     u32 maybe[TILE];        // whether the row may leave out a key of the tile
     u32 seen[(1 << CT_HASH) / 32];
 };
-// Keys that have a value of their own in a row's list, by tiles: distill.hip.
+// Keys that a row lists are kept out of its sums and of g: distill.hip.
 template <typename PAR> constexpr bool has_lists() { return false; }
 template <int TILE, typename PAR> struct ListLds {};
 __device__ __forceinline__ u32 id_hash(int id) { return (u32)id * 0x9E3779B1u >> (32 - CT_HASH); }
@@ -648,7 +648,7 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_contrast_
     int tr, tc;
     tile_of((int)(first + blockIdx.x), tiles_q, tiles_k, tr, tc);
     logit_product<TILE, DT, TERMS>(c, tr, tc, lds, side, acc, [&]() {
-        if constexpr (has_lists<PAR>()) load_lists(c, lists, tr * TILE, tc, false);
+        if constexpr (has_lists<PAR>()) load_lists(c, lists, tr * TILE, tc);
     });
     const Place<TILE> at(tr, tc);
     float base[N];
@@ -668,7 +668,7 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_contrast_
 #pragma unroll
             for (int n = 0; n < N; ++n) s[r][n] = fmaf(acc[m][n][r], c.c1, base[n]);
         leave_out(side, at.in_row + m * 4, id, s);
-        if constexpr (has_lists<PAR>()) take_listed(c, lists, tr * TILE, at.in_row + m * 4, at.in_col, s);
+        if constexpr (has_lists<PAR>()) take_listed(std::true_type(), c, lists, tr * TILE, at.in_row + m * 4, at.in_col, s);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             top[r] = s[r][0];
@@ -717,7 +717,7 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_contrast_
     int tr, tc;
     tile_of((int)(first + blockIdx.x), tiles_q, tiles_k, tr, tc);
     logit_product<TILE, DT, TERMS>(c, tr, tc, lds, side, acc, [&]() {
-        if constexpr (has_lists<PAR>()) load_lists(c, lists, tr * TILE, tc, true);
+        if constexpr (has_lists<PAR>()) load_lists(c, lists, tr * TILE, tc);
     });
     const Place<TILE> at(tr, tc);
     float base[N], col_sum[N] = {};
@@ -747,15 +747,12 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_contrast_
 #pragma unroll
                     for (int n = 0; n < N; ++n) logit[r][n] = fmaf(acc[pair * 2 + r8 / 4][n][r], c.c1, base[n]);
                 leave_out(side, at.in_row + pair * 8 + r8, id, logit);
+                if constexpr (has_lists<PAR>()) take_listed(std::false_type(), c, lists, tr * TILE, at.in_row + pair * 8 + r8, at.in_col, logit);
             }
             const float2 info = side.row_g[at.in_row + pair * 8 + r8];
-            float value[N];
-#pragma unroll
-            for (int n = 0; n < N; ++n) value[n] = __builtin_amdgcn_exp2f(logit[r8 % 4][n] - info.x) * info.y;
-            if constexpr (has_lists<PAR>()) put_listed(c, lists, tr * TILE, at.in_row + pair * 8 + r8, at.in_col, value);
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                const float g = value[n];
+                const float g = __builtin_amdgcn_exp2f(logit[r8 % 4][n] - info.x) * info.y;
                 half_t x[PLANES];
                 to_planes<DT>(g, x);
                 float rounded = 0.0f;

@@ -11,10 +11,11 @@
 // out by the tile that they lie in.  The lists are sorted by key, with the place where every tile begins, so a tile marks its listed
 // keys in a bitmap in LDS while its first loads are under way; a key's place in the list is the number of marks before it in its row.
 // Off the list g is a factor of the row times 2^(s - reference), with w (R - r) and the log of the sum off the list: again no difference
-// of large numbers where a key has little of both.  Listed keys take g = w (P - p), formed in float32 from the logits; like all of g it
-// is rounded to the type of the rows for the products (float32 rows: three terms), which bounds its error by half a step of its own
-// size, also where teacher and student nearly agree.  The teacher's probabilities are summed in double precision: 1 - sum p of a
-// teacher that is sure is a small difference, and there are few of them.
+// of large numbers where a key has little of both.  It is rounded to the type of the rows for the products (float32 rows: three terms).
+// Listed keys have the largest g, of both signs, and often rows that lie close together, so that rounded ones would leave an error of the
+// size of the gradient (float16, 300 queries, lists of 7: 3.5e-4 of its norm, where rounding the result costs 2.1e-4): theirs is float32, kept
+// out of the products, and added row by row at the end.  For the gradient of a key a bitmap says which queries list it.
+// The teacher's probabilities are summed in double precision: 1 - sum p of a teacher that is sure is a small difference, and there are few of them.
 #include <cmath>
 
 #include "contrast.h"
@@ -25,9 +26,12 @@ struct DistillPar : ContrastPar {
     int entries, tail;
     int tiles_k;                // tiles of the logits across the keys
     int *list_key;              // [B padded][entries] keys that count, ascending; from here on a row's lists are in this order
-    float *list_p, *list_s, *list_g;    // the teacher's probability; the logit in base 2; g (float16: scaled)
+    float *list_p, *list_s, *list_g;    // the teacher's probability; the logit in base 2; g
     float2 *list_sum;           // [B] sum of the list's p, r
     unsigned char *list_at;     // [B padded][tiles_k + 1] place of a tile's first key; of the end
+    u32 *marks;                 // [M][words] the queries that list a key
+    int words;
+    int *count;                 // [M] how many they are
 };
 
 __device__ __forceinline__ bool entry_counts(const DistillPar &c, int i, int e)
@@ -47,35 +51,26 @@ __device__ __forceinline__ bool row_counts(const DistillPar &c, int i)
 template <> constexpr bool has_lists<DistillPar>() { return true; }
 
 template <int TILE> struct ListLds<TILE, DistillPar> {
-    static constexpr int ROOM = TILE * 4;       // values of g; those of more entries stay in memory
     u32 bits[TILE * TILE / 32];
-    float value[ROOM];
-    unsigned short at[TILE];                    // of a row's first value
     unsigned char first[TILE], count[TILE];     // place of the row's first key of this tile in its list, and how many they are
-    u32 used;
 };
 
 template <int TILE>
-__device__ __forceinline__ void load_lists(const DistillPar &c, ListLds<TILE, DistillPar> &lists, int row0, int tile_c, bool values)
+__device__ __forceinline__ void load_lists(const DistillPar &c, ListLds<TILE, DistillPar> &lists, int row0, int tile_c)
 {
     const int t = threadIdx.x;
 #pragma unroll
     for (int i = 0; i < TILE * TILE / 32 / 256; ++i) lists.bits[i * 256 + t] = 0;
-    if (t == 0) lists.used = 0;
     __syncthreads();
     if (t >= TILE) return;
     const unsigned char *ends = &c.list_at[(size_t)(row0 + t) * (c.tiles_k + 1) + tile_c];
     const int first = ends[0], n = ends[1] - first;
     lists.first[t] = (unsigned char)first;
     lists.count[t] = (unsigned char)n;
-    if (!n) return;
-    const u32 place = values ? atomicAdd(&lists.used, (u32)n) : 0;
-    lists.at[t] = (unsigned short)place;        // at most 256 rows of 128
-    const size_t from = (size_t)(row0 + t) * c.entries + first;
+    const int *keys = &c.list_key[(size_t)(row0 + t) * c.entries + first];
     for (int e = 0; e < n; ++e) {
-        const int col = c.list_key[from + e] - tile_c * TILE;
+        const int col = keys[e] - tile_c * TILE;
         atomicOr(&lists.bits[(t * TILE + col) >> 5], 1u << (col & 31));
-        if (values && place + e < (u32)ListLds<TILE, DistillPar>::ROOM) lists.value[place + e] = c.list_g[from + e];
     }
 }
 
@@ -95,9 +90,9 @@ __device__ __forceinline__ int marks_before(const ListLds<TILE, DistillPar> &lis
     return n;
 }
 
-// Four rows' logits: those of listed keys are written out, and become -infinity
-template <int TILE, int N>
-__device__ __forceinline__ void take_listed(const DistillPar &c, const ListLds<TILE, DistillPar> &lists, int row0, int row, int col, float (&s)[4][N])
+// Four rows' logits: those of listed keys become -infinity, and are written out before
+template <bool WRITE, int TILE, int N>
+__device__ __forceinline__ void take_listed(std::integral_constant<bool, WRITE>, const DistillPar &c, const ListLds<TILE, DistillPar> &lists, int row0, int row, int col, float (&s)[4][N])
 {
     u32 marks[4], any = 0;
 #pragma unroll
@@ -105,35 +100,16 @@ __device__ __forceinline__ void take_listed(const DistillPar &c, const ListLds<T
     if (!__any(any)) return;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        if (marks[r]) {
-            float *to = &c.list_s[(size_t)(row0 + row + r) * c.entries + lists.first[row + r] + marks_before(lists, row + r, col)];
+        if constexpr (WRITE) {
+            if (marks[r]) {
+                float *to = &c.list_s[(size_t)(row0 + row + r) * c.entries + lists.first[row + r] + marks_before(lists, row + r, col)];
 #pragma unroll
-            for (int n = 0; n < N; ++n)
-                if (marks[r] >> n & 1) {
-                    *to++ = s[r][n];
-                    s[r][n] = -INFINITY;
-                }
-        }
-    }
-}
-
-// A row's g: those of listed keys
-template <int TILE, int N>
-__device__ __forceinline__ void put_listed(const DistillPar &c, const ListLds<TILE, DistillPar> &lists, int row0, int row, int col, float (&g)[N])
-{
-    const u32 marks = marks_at(lists, row, col);
-    if (!__any(marks)) return;
-    if (marks) {
-        const int before = marks_before(lists, row, col);
-        u32 at = lists.at[row] + (u32)before;
-        const float *from = &c.list_g[(size_t)(row0 + row) * c.entries + lists.first[row] + before];
-#pragma unroll
-        for (int n = 0; n < N; ++n)
-            if (marks >> n & 1) {
-                g[n] = at < (u32)ListLds<TILE, DistillPar>::ROOM ? lists.value[at] : *from;
-                ++at;
-                ++from;
+                for (int n = 0; n < N; ++n)
+                    if (marks[r] >> n & 1) *to++ = s[r][n];
             }
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) s[r][n] = marks[r] >> n & 1 ? -INFINITY : s[r][n];
     }
 }
 
@@ -224,7 +200,12 @@ __global__ __launch_bounds__(256) void k_distill_prepare(DistillPar c, u32 first
     }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (block < key_blocks) {
-        for (int at = block * 4 + wave; at < ct_up(c.M, CT_PAD); at += key_blocks * 4) key_side<DT, WIDE>(c, at, lane);
+        for (int at = block * 4 + wave; at < ct_up(c.M, CT_PAD); at += key_blocks * 4) {
+            key_side<DT, WIDE>(c, at, lane);
+            if (!c.dK || at >= c.M) continue;
+            if (lane == 0) c.count[at] = 0;
+            for (int t = lane; t < c.words; t += 64) c.marks[(size_t)at * c.words + t] = 0;
+        }
         return;
     }
     if (threadIdx.x == 0) most = 0;
@@ -297,7 +278,11 @@ __global__ __launch_bounds__(256) void k_distill_loss(DistillPar c, int row_bloc
         if (at >= n) continue;
         // (an entry whose probability is below the smallest float has none)
         if (!(p[r] == 0.0f)) loss = fmaf(p[r], (log2f(p[r]) - (x[r] - log_total)) * 0.693147181f, loss);
-        c.list_g[(size_t)i * c.entries + at] = up_w * (e[r] / total - p[r]);
+        if (!c.dK) continue;
+        c.list_g[(size_t)i * c.entries + at] = w * (e[r] / total - p[r]);
+        const int j = c.list_key[(size_t)i * c.entries + at];
+        atomicOr(&c.marks[(size_t)j * c.words + (i >> 5)], 1u << (i & 31));
+        atomicAdd(&c.count[j], 1);
     }
     loss = wave_sum(loss);
     if (lane) return;
@@ -311,24 +296,145 @@ __global__ __launch_bounds__(256) void k_distill_loss(DistillPar c, int row_bloc
 }
 
 // ------------------------------------------------------------------------------------------------ joining the gradients' parts
-// A wavefront per row, four coordinates a lane.
+// A wavefront per row: the listed terms, four coordinates a lane and DS_WIDE of these at a time.  A key that more than DS_SHARED queries list is
+// summed by the whole block, a part of the queries to each wavefront, and their sums are added in order.  The rows of a block lie gridDim.x
+// apart, so that neighbouring keys of this kind are those of different blocks.
+#define DS_FINISH 16            // wavefronts of a block
+#define DS_SHARED 128
+#define DS_WIDE 4
+#define DS_RUN 64               // words of marks looked at together, one for each lane; by a whole block fewer, so that all its wavefronts have some
+#define DS_RUN_SHARED 4
+#define DS_ROWS 4               // rows on the way
+struct KeyLds {
+    unsigned short list[DS_FINISH][DS_RUN * 32];
+    f32x4 part[DS_FINISH][64];
+};
+
+typedef float Sums[DS_WIDE][4];
+
+// Adds g (row - x) of n entries; lane e holds entry e: its row's number and its g.  e0: the first coordinate; x: the row of the sum.
 template <int DT, bool WIDE>
-__global__ __launch_bounds__(256) void k_distill_finish(DistillPar c)
+__device__ __forceinline__ void add_terms(const DistillPar &c, const void *rows, int e0, const Sums &x, int number, float g, int n, int lane, Sums &sum)
 {
-    const int lane = threadIdx.x & 63, at = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (at >= c.B + c.M) return;
+    for (int j = 0; j < n; j += DS_ROWS) {
+#pragma unroll
+        for (int h = 0; h < DS_WIDE; ++h) {
+            const int e = e0 + h * 256 + lane * 4;
+            if (e >= c.d) continue;
+            float y[DS_ROWS][4];
+#pragma unroll
+            for (int r = 0; r < DS_ROWS; ++r) load4<DT, WIDE>(rows, __builtin_amdgcn_readlane(number, j + r < n ? j + r : n - 1), c.d, e, y[r]);
+#pragma unroll
+            for (int r = 0; r < DS_ROWS; ++r) {
+                const float own = j + r < n ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), j + r < n ? j + r : n - 1)) : 0.0f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum[h][k] = fmaf(own, y[r][k] - x[h][k], sum[h][k]);
+            }
+        }
+    }
+}
+
+// Terms of the queries that list key j, of the runs of RUN words of marks first, first + step, ..; list: the wavefront's own.
+template <int RUN, int DT, bool WIDE>
+__device__ __forceinline__ void add_queries(const DistillPar &c, int j, int e0, const Sums &x, int first, int step, unsigned short *list, int lane, Sums &sum)
+{
+    for (int run = first; run * RUN < c.words; run += step) {
+        const int at = run * RUN + lane;
+        u32 marks = lane < RUN && at < c.words ? c.marks[(size_t)j * c.words + at] : 0;
+        const int here = (int)__popc(marks), upto = inclusive(here, lane), n = __builtin_amdgcn_readlane(upto, 63);
+        for (int to = upto - here; marks; marks &= marks - 1) list[to++] = (unsigned short)(lane * 32 + __builtin_ctz(marks));
+        wave_sync();
+        for (int t = 0; t < n; t += 64) {
+            const int i = t + lane < n ? run * RUN * 32 + list[t + lane] : -1;
+            float g = 0.0f;
+            if (i >= 0) {
+                const int *keys = &c.list_key[(size_t)i * c.entries];
+                int lo = 0, hi = c.list_at[(size_t)i * (c.tiles_k + 1) + c.tiles_k] - 1;        // it is there
+                while (lo < hi) {
+                    const int mid = (lo + hi) >> 1;
+                    if (keys[mid] < j) lo = mid + 1;
+                    else hi = mid;
+                }
+                g = c.list_g[(size_t)i * c.entries + lo];
+            }
+            add_terms<DT, WIDE>(c, c.Q, e0, x, i, g, n - t < 64 ? n - t : 64, lane, sum);
+        }
+        wave_sync();
+    }
+}
+
+template <int DT, bool WIDE>
+__device__ __forceinline__ void load_row(const DistillPar &c, const void *rows, int row, int e0, int lane, Sums &x)
+{
+#pragma unroll
+    for (int h = 0; h < DS_WIDE; ++h)
+        if (e0 + h * 256 + lane * 4 < c.d) load4<DT, WIDE>(rows, row, c.d, e0 + h * 256 + lane * 4, x[h]);
+}
+// The parts of the products and the listed terms, rounded
+template <int DT, bool WIDE>
+__device__ __forceinline__ void finish_row(const DistillPar &c, int at, int e0, int lane, const Sums &sum)
+{
+    const GradRow<DT, WIDE> mine(c, at);
+#pragma unroll
+    for (int h = 0; h < DS_WIDE; ++h) {
+        const int e = e0 + h * 256 + lane * 4;
+        if (e >= c.d) continue;
+        float a[4] = {}, own[4];
+        mine.load(e, a, own);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) a[k] += sum[h][k];
+        mine.store(e, a);
+    }
+}
+
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(64 * DS_FINISH, 4) void k_distill_finish(DistillPar c)
+{
+    __shared__ KeyLds lds;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), total = c.B + c.M;
+    const int at = (int)(blockIdx.x + wave * gridDim.x), lanes_row = (int)(blockIdx.x + (lane & (DS_FINISH - 1)) * gridDim.x);
+    const u64 shared = __ballot(lane < DS_FINISH && lanes_row >= c.B && lanes_row < total && c.count[lanes_row - c.B] > DS_SHARED);
     const bool keys = at >= c.B;
-    const int row = keys ? at - c.B : at;
-    if (keys ? key_gone(c, row) : !c.list_at[(size_t)row * (c.tiles_k + 1) + c.tiles_k]) {
+    const int row = keys ? at - c.B : at, n = at < total && !keys ? c.list_at[(size_t)row * (c.tiles_k + 1) + c.tiles_k] : 0;
+    if (at >= total || shared >> wave & 1) {
+    } else if (keys ? key_gone(c, row) : !n) {
         const float zero[4] = {};
         for (int e = lane * 4; e < c.d; e += 256) store4<DT, WIDE>(keys ? c.dK : c.dQ, row, c.d, e, zero);
-        return;
-    }
-    const GradRow<DT, WIDE> mine(c, at);
-    for (int e = lane * 4; e < c.d; e += 256) {
-        float a[4] = {}, x[4] = {};
-        mine.load(e, a, x);
-        mine.store(e, a);
+    } else
+        for (int e0 = 0; e0 < c.d; e0 += 256 * DS_WIDE) {
+            Sums x = {}, sum = {};
+            load_row<DT, WIDE>(c, keys ? c.K : c.Q, row, e0, lane, x);
+            if (keys) {
+                if (c.count[row]) add_queries<DS_RUN, DT, WIDE>(c, row, e0, x, 0, 1, lds.list[wave], lane, sum);
+            } else
+                for (int t = 0; t < n; t += 64) {
+                    const size_t e = (size_t)row * c.entries + t + lane;
+                    const bool in = t + lane < n;
+                    add_terms<DT, WIDE>(c, c.K, e0, x, in ? c.list_key[e] : 0, in ? c.list_g[e] : 0.0f, n - t < 64 ? n - t : 64, lane, sum);
+                }
+            finish_row<DT, WIDE>(c, at, e0, lane, sum);
+        }
+    if (!shared) return;        // a whole block
+    __syncthreads();
+    for (u64 left = shared; left; left &= left - 1) {
+        const int key = (int)(blockIdx.x + __builtin_ctzll(left) * gridDim.x) - c.B;
+        for (int e0 = 0; e0 < c.d; e0 += 256 * DS_WIDE) {
+            Sums x = {}, sum = {};
+            load_row<DT, WIDE>(c, c.K, key, e0, lane, x);
+            add_queries<DS_RUN_SHARED, DT, WIDE>(c, key, e0, x, wave, DS_FINISH, lds.list[wave], lane, sum);
+#pragma unroll
+            for (int h = 0; h < DS_WIDE; ++h) {
+                if (e0 + h * 256 >= c.d) break;
+                lds.part[wave][lane] = (f32x4){sum[h][0], sum[h][1], sum[h][2], sum[h][3]};
+                __syncthreads();
+                if (wave == 0)
+                    for (int w = 1; w < DS_FINISH; ++w)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) sum[h][k] += lds.part[w][lane][k];
+                __syncthreads();
+            }
+            if (wave == 0) finish_row<DT, WIDE>(c, key + c.B, e0, lane, sum);
+        }
     }
 }
 
@@ -344,6 +450,11 @@ static size_t layout(DistillPar &c, ContrastPlan &plan, int dtype, int want_grad
         take(c.list_g, Br * c.entries);
         take(c.list_sum, Br);
         take(c.list_at, Br * (c.tiles_k + 1));
+        if (want_grad) {
+            c.words = (c.B + 31) / 32;
+            take(c.marks, (size_t)c.M * c.words);
+            take(c.count, c.M);
+        }
     });
 }
 
@@ -410,7 +521,7 @@ static void launch_distill(DistillPar &c, const ContrastPlan &plan, int want_gra
         else launch_grads<DT, 128>(c, st);
     } else
         launch_grads<DT, 128>(c, st);
-    hipLaunchKernelGGL((k_distill_finish<DT, WIDE>), dim3((c.B + c.M + 3) / 4), dim3(256), 0, st, c);
+    hipLaunchKernelGGL((k_distill_finish<DT, WIDE>), dim3((c.B + c.M + DS_FINISH - 1) / DS_FINISH), dim3(64 * DS_FINISH), 0, st, c);
 }
 
 extern "C" int rnnd_distill(const void *Q, int64_t B, const void *K, int64_t M, int32_t d, int dtype, int metric, const int32_t *teacher_ids,

@@ -319,3 +319,30 @@ def test_streams_of_their_own_give_the_same_bits(rn):
         for u, v in zip(got, want):
             assert torch.equal(u, v)
         del junk
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_keys_that_many_queries_list(rn, dtype):
+    """One key in every list, one in a fifth of them: a whole block sums these; row for row against float64."""
+    c = case(1300, 90, 24, 5, dtype, 15)
+    g = np.random.Generator(np.random.PCG64(16))
+    c["teacher_ids"][:, 1], c["teacher_ids"][g.random(1300) < 0.2, 2] = 17, 18
+    for j in (17, 18):
+        c["key_ids"][j], c["key_bias"][j] = 1000 + j, 0.0
+    check(rn, c, 3.0, True)
+
+
+def test_a_gradient_that_is_a_small_difference(rn):
+    """Teacher and student differ only in how they divide the probability between two keys that lie close together: g of the two is large and
+    of both signs, the gradient small.  Its terms are float32, so the gradient is off by little more than the rounding of its own values."""
+    import torch
+    c = case(40, 200, 64, 2, "float16", 17, ids=False, bias=False, weight=False)
+    K = c["K"].float()
+    K[1::2] = K[0::2] + 0.01 * K[1::2]
+    c["K"], c["Q"] = K.half(), (K[0:80:2] + 0.05 * c["Q"].float()).half()
+    c["teacher_ids"] = np.arange(80).reshape(40, 2).astype(np.int32)
+    c["teacher_logits"] = np.tile(np.log(np.array([[0.8, 0.2]])), (40, 1)).astype(np.float32)
+    _, dq, _, *_ = reference(c, 20.0, True)
+    got = call(rn, c, 20.0, True)[1].double().cpu().numpy()
+    # half a step for the rounding of the result, as much again for all else: g off the list is below 2^-8 here, rounded with 2^-11 of itself
+    assert np.sqrt(np.square(got - dq).sum()) <= 2 * 2.0 ** -11 * np.sqrt(np.square(dq).sum())
