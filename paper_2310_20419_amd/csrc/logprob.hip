@@ -16,11 +16,11 @@
 
 #include "contrast.h"
 
-#define LP_ROOM 512             // groups above the bound, and keys among them, that a wavefront has room for
-#define LP_PARTS 512            // parts looked at together
+#define LP_ROOM 256             // groups above the bound, and keys among them, that a wavefront has room for
 #define LP_NONE (-3.0e38f)      // stands for -infinity where bits are put into the significand
 #define LP_LOG2E 1.4426950408889634
 #define LP_FEW 8                // queries
+#define LP_ALONE 512            // queries, for each of which there is room for a block of eight wavefronts
 
 struct LogprobPar : ContrastPar {
     int alternatives;
@@ -173,102 +173,116 @@ __device__ __forceinline__ void join_three(float &top, float &sum, float &w, flo
 }
 
 // ------------------------------------------------------------------------------------------------ the logits of a few queries
-// Up to 8 queries: no matrix tile would be filled, and the call is bound by reading the keys once.  8 lanes take a row, 16 bytes each, a
-// wavefront 16 rows at a time; distances are summed from differences.  Query coordinates come from LDS, as many of all queries as
-// fit at a time.  A block takes a part of the keys; its wavefronts then take the sums of a query each.
-#define LP_CHUNK 8192           // coordinates in LDS
-#define LP_PASS 64              // keys of a block's pass
+// Up to 8 queries: no matrix tile would be filled, and the call is bound by reading the keys once.  8 lanes take a row, 16 bytes each; distances
+// are summed from differences.  Query coordinates come from LDS, as many of all queries as fit at a time.  A wavefront takes 16, 32 or 64 keys
+// at a time by itself, and then a lane each of them for the sums; a block of four takes a part of the keys.
+#define LP_CHUNK 8192           // coordinates in LDS, at most
+template <int NB> constexpr int few_rows() { return NB <= 2 ? 4 : 2; }      // of a lane at a time
+
 template <int DT, int NB, bool WIDE>
-__global__ __launch_bounds__(256) void k_logprob_few(LogprobPar c, int part_keys)
+__global__ __launch_bounds__(256) void k_logprob_few(LogprobPar c, int wave_keys, int passes)
 {
-    constexpr int V = DT == DT_F32 ? 4 : 8, R = 2;
-    __shared__ __align__(16) float query[LP_CHUNK];
-    __shared__ float logit[NB][LP_PASS];
-    __shared__ MostLds most;
+    constexpr int V = DT == DT_F32 ? 4 : 8, R = few_rows<NB>(), AHEAD = 8 / R;
+    extern __shared__ __align__(16) float query[];         // [NB][chunk], then [4][NB][64] distances
+    __shared__ float sums[4][NB][3];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane & 7;
     const int chunk = c.d <= LP_CHUNK / NB ? (c.d + 7) & ~7 : LP_CHUNK / NB;
-    const int key0 = blockIdx.x * part_keys;
+    float *const far_of = query + NB * chunk + wave * NB * 64;
     auto stage = [&](int e0) {
-        for (int t = threadIdx.x; t < NB * chunk; t += 256) {
-            const int b = t / chunk, e = e0 + t - b * chunk;
-            query[t] = e < c.d ? (float)((const typename RowType<DT>::T *)c.Q)[(size_t)(b < c.B ? b : c.B - 1) * c.d + e] : 0.0f;
-        }
+        for (int b = 0; b < NB; ++b)
+            for (int t = threadIdx.x; t < chunk; t += 256)
+                query[b * chunk + t] = e0 + t < c.d ? (float)((const typename RowType<DT>::T *)c.Q)[(size_t)(b < c.B ? b : c.B - 1) * c.d + e0 + t] : 0.0f;
     };
-    if (threadIdx.x == 0) most = {0, 0};
     if (chunk >= c.d) stage(0);
     __syncthreads();
-    // of the queries wave, wave + 4
-    float top[(NB + 3) / 4], sum[(NB + 3) / 4], w[(NB + 3) / 4];
+    float top[NB], sum[NB], w[NB], biases = 0.0f;
 #pragma unroll
-    for (int h = 0; h < (NB + 3) / 4; ++h) {
-        top[h] = -INFINITY;
-        sum[h] = w[h] = 0.0f;
+    for (int b = 0; b < NB; ++b) {
+        top[b] = -INFINITY;
+        sum[b] = w[b] = 0.0f;
     }
-    for (int pass = 0; pass < part_keys; pass += LP_PASS) {
-        int key[R];
-        float acc[NB][R] = {};
+    const int part_keys = wave_keys * 4 * passes;
+    for (int pass = 0; pass < passes; ++pass) {
+        const int in_part = (pass * 4 + wave) * wave_keys, key0 = blockIdx.x * part_keys + in_part;
+        // what the lane's key needs besides its distances, while these are formed
+        const int mine = key0 + lane;
+        const bool on = lane < wave_keys && mine < c.M && !key_gone(c, mine);
+        const float bias = on && c.bias ? c.bias[mine] : 0.0f;
+        const int name = on && c.query_ids ? c.key_ids[mine] : 0;
+        for (int r0 = 0; r0 < wave_keys; r0 += 8 * R) {
+            float acc[NB][R] = {};
+            size_t row[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) key[r] = key0 + pass + wave * 16 + r * 8 + (lane >> 3);
-        for (int e0 = 0; e0 < c.d; e0 += chunk) {
-            if (chunk < c.d) {
-                __syncthreads();
-                stage(e0);
-                __syncthreads();
+            for (int r = 0; r < R; ++r) {
+                const int j = key0 + r0 + r * 8 + (lane >> 3);
+                row[r] = (size_t)(j < c.M ? j : c.M - 1) * c.d;
             }
-            const int end = c.d - e0 < chunk ? c.d - e0 : chunk;
-#pragma unroll 2
-            for (int e = sub * V; e < end; e += 8 * V) {
-                float x[R][V];
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const size_t row = key[r] < c.M ? key[r] : c.M - 1;
-                    if constexpr (WIDE) unpack<DT, V>(load_pack<DT, V>(c.K, row * c.d + e0 + e), x[r]);
-                    else
-#pragma unroll
-                        for (int k = 0; k < V; ++k)
-                            x[r][k] = e + k < end ? (float)((const typename RowType<DT>::T *)c.K)[row * c.d + e0 + e + k] : 0.0f;
+            for (int e0 = 0; e0 < c.d; e0 += chunk) {
+                if (chunk < c.d) {
+                    __syncthreads();
+                    stage(e0);
+                    __syncthreads();
                 }
+                const int end = c.d - e0 < chunk ? c.d - e0 : chunk;
+                for (int e1 = 0; e1 < end; e1 += AHEAD * 8 * V) {
+                    Pack<DT, V> packs[AHEAD][R];
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
+                    for (int a = 0; a < AHEAD; ++a) {
+                        const int e = e1 + a * 8 * V + sub * V, from = e < end ? e : 0;
 #pragma unroll
-                    for (int k = 0; k < V; k += 4) {
-                        const f32x4 q = *(const f32x4 *)&query[b * chunk + e + k];
+                        for (int r = 0; r < R; ++r) {
+                            typedef typename RowType<DT>::T T;
+                            if constexpr (WIDE) packs[a][r] = load_pack<DT, V>(c.K, row[r] + e0 + from);
+                            else
 #pragma unroll
-                        for (int r = 0; r < R; ++r)
+                                for (int k = 0; k < V; ++k) packs[a][r].v[k] = from + k < end ? ((const T *)c.K)[row[r] + e0 + from + k] : (T)0.0f;
+                        }
+                    }
 #pragma unroll
-                            for (int h = 0; h < 4; ++h) {
-                                const float diff = x[r][k + h] - q[h];
-                                acc[b][r] = fmaf(diff, diff, acc[b][r]);
+                    for (int a = 0; a < AHEAD; ++a) {
+                        const int e = e1 + a * 8 * V + sub * V;
+                        __builtin_amdgcn_sched_barrier(0);      // (packs stay packed until their turn: half the registers)
+                        if (e >= end) continue;
+                        float x[R][V];
+#pragma unroll
+                        for (int r = 0; r < R; ++r) unpack<DT, V>(packs[a][r], x[r]);
+#pragma unroll
+                        for (int b = 0; b < NB; ++b)
+#pragma unroll
+                            for (int k = 0; k < V; k += 4) {
+                                const f32x4 q = *(const f32x4 *)&query[b * chunk + e + k];
+#pragma unroll
+                                for (int r = 0; r < R; ++r)
+#pragma unroll
+                                    for (int h = 0; h < 4; ++h) {
+                                        const float diff = x[r][k + h] - q[h];
+                                        acc[b][r] = fmaf(diff, diff, acc[b][r]);
+                                    }
                             }
                     }
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    acc[b][r] += xor_lane_f32<1>(acc[b][r]);
+                    acc[b][r] += xor_lane_f32<2>(acc[b][r]);
+                    acc[b][r] += xor_lane_f32<7>(acc[b][r]);
+                }
+                // lane b of the 8 writes query b
+                float far = acc[0][r];
+#pragma unroll
+                for (int b = 1; b < NB; ++b) far = sub == b ? acc[b][r] : far;
+                if (sub < NB) far_of[sub * 64 + r0 + r * 8 + (lane >> 3)] = far;
             }
         }
+        wave_sync();
+        if (on) biases = fmaxf(biases, fabsf(bias) < INFINITY ? fabsf(bias) : INFINITY);
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                acc[b][r] += xor_lane_f32<1>(acc[b][r]);
-                acc[b][r] += xor_lane_f32<2>(acc[b][r]);
-                acc[b][r] += xor_lane_f32<7>(acc[b][r]);
-            }
-            // lane b of the 8 writes query b
-            float far = acc[0][r];
-#pragma unroll
-            for (int b = 1; b < NB; ++b) far = sub == b ? acc[b][r] : far;
-            if (sub < NB) {
-                const int j = key[r];
-                const bool out = j >= c.M || sub >= c.B || leaves_out(c, sub, j);
-                logit[sub][wave * 16 + r * 8 + (lane >> 3)] =
-                    out ? -INFINITY : ((c.bias ? c.bias[j] : 0.0f) - c.scale * far) * 1.44269504f;
-                if (sub == 0) most_of(most, c, j, 0.0f);
-            }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int h = 0; h < (NB + 3) / 4; ++h) {
-            const int b = wave + h * 4;
+        for (int b = 0; b < NB; ++b) {
             if (b >= c.B) break;
-            const float s = logit[b][lane];
+            const float s = !on || (c.query_ids && name == c.query_ids[b]) ? -INFINITY : (bias - c.scale * far_of[b * 64 + lane]) * 1.44269504f;
             if (c.alternatives) {       // 8 lanes are a group
                 float x = __uint_as_float((__float_as_uint(fmaxf(s, LP_NONE)) & ~7u) | (u32)sub), y = LP_NONE;
                 auto with = [&](float ox, float oy) {
@@ -278,28 +292,43 @@ __global__ __launch_bounds__(256) void k_logprob_few(LogprobPar c, int part_keys
                 with(xor_lane_f32<1>(x), xor_lane_f32<1>(y));
                 with(xor_lane_f32<2>(x), xor_lane_f32<2>(y));
                 with(xor_lane_f32<7>(x), xor_lane_f32<7>(y));
-                if (sub == 0) c.groups[((size_t)b * gridDim.x + blockIdx.x) * (part_keys / 8) + pass / 8 + (lane >> 3)] = make_float2(x, y);
+                if (sub == 0 && lane < wave_keys)
+                    c.groups[((size_t)b * gridDim.x + blockIdx.x) * (part_keys / 8) + (in_part + lane) / 8] = make_float2(x, y);
             }
-            const float m = fmaxf(top[h], s), ref = m == -INFINITY ? 0.0f : m;      // a lane's own
-            const float da = fmaxf(top[h] - ref, LP_NONE), x = s - ref, fa = __builtin_amdgcn_exp2f(da), e = __builtin_amdgcn_exp2f(x);
-            w[h] = fmaf(e, fmaxf(x, LP_NONE), fa * fmaf(sum[h], da, w[h]));
-            sum[h] = fmaf(sum[h], fa, e);
-            top[h] = m;
+            const float m = fmaxf(top[b], s), ref = m == -INFINITY ? 0.0f : m;      // a lane's own
+            const float da = fmaxf(top[b] - ref, LP_NONE), x = s - ref, fa = __builtin_amdgcn_exp2f(da), e = __builtin_amdgcn_exp2f(x);
+            w[b] = fmaf(e, fmaxf(x, LP_NONE), fa * fmaf(sum[b], da, w[b]));
+            sum[b] = fmaf(sum[b], fa, e);
+            top[b] = m;
         }
-        __syncthreads();
+        wave_sync();
     }
 #pragma unroll
-    for (int h = 0; h < (NB + 3) / 4; ++h) {
-        const int b = wave + h * 4;
+    for (int b = 0; b < NB; ++b) {
         if (b >= c.B) break;
 #pragma unroll
-        for (int s = 1; s < 64; s <<= 1) join_three(top[h], sum[h], w[h], __shfl_xor(top[h], s), __shfl_xor(sum[h], s), __shfl_xor(w[h], s));
+        for (int s = 1; s < 64; s <<= 1) join_three(top[b], sum[b], w[b], __shfl_xor(top[b], s), __shfl_xor(sum[b], s), __shfl_xor(w[b], s));
         if (lane == 0) {
-            c.part[(size_t)b * gridDim.x + blockIdx.x] = make_float2(top[h], sum[h]);
-            c.part_w[(size_t)b * gridDim.x + blockIdx.x] = w[h];
+            sums[wave][b][0] = top[b];
+            sums[wave][b][1] = sum[b];
+            sums[wave][b][2] = w[b];
         }
     }
-    if (c.alternatives && threadIdx.x == 0) c.most[blockIdx.x] = __uint_as_float(most.bias);
+#pragma unroll
+    for (int s = 32; s; s >>= 1) biases = fmaxf(biases, __shfl_xor(biases, s));
+    if (lane == 0) far_of[0] = biases;
+    __syncthreads();
+    const int b = threadIdx.x;
+    if (b < NB && b < c.B) {
+        float t = sums[0][b][0], u = sums[0][b][1], v = sums[0][b][2];
+        for (int h = 1; h < 4; ++h) {
+            join_three(t, u, v, sums[h][b][0], sums[h][b][1], sums[h][b][2]);
+            biases = fmaxf(biases, far_of[h * NB * 64]);        // (of the first wavefront; it reads the others')
+        }
+        c.part[(size_t)b * gridDim.x + blockIdx.x] = make_float2(t, u);
+        c.part_w[(size_t)b * gridDim.x + blockIdx.x] = v;
+        if (b == 0) c.most[blockIdx.x] = biases;
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ the answers
@@ -307,26 +336,38 @@ __global__ __launch_bounds__(256) void k_logprob_few(LogprobPar c, int part_keys
 template <int DT, bool WIDE>
 __device__ __forceinline__ double exact_distance(const LogprobPar &c, int i, int j, int sub)
 {
-    constexpr int V = DT == DT_F32 ? 4 : 8;
+    typedef typename RowType<DT>::T T;
+    constexpr int V = DT == DT_F32 ? 4 : 8, AHEAD = WIDE ? 4 : 1;
     double sum = 0.0;
     const size_t q = (size_t)i * c.d, k = (size_t)j * c.d;
-#pragma unroll 4
-    for (int e = sub * V; e < c.d; e += 8 * V) {
-        float x[V], y[V];
-        if constexpr (WIDE) {
-            unpack<DT, V>(load_pack<DT, V>(c.Q, q + e), x);
-            unpack<DT, V>(load_pack<DT, V>(c.K, k + e), y);
-        } else
+    for (int e1 = sub * V; e1 < c.d; e1 += AHEAD * 8 * V) {
+        Pack<DT, V> px[AHEAD], py[AHEAD];
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            const int e = e1 + a * 8 * V, from = e < c.d ? e : e1;
+            if constexpr (WIDE) {
+                py[a] = load_pack<DT, V>(c.K, k + from);
+                px[a] = load_pack<DT, V>(c.Q, q + from);
+            } else
+#pragma unroll
+                for (int h = 0; h < V; ++h) {
+                    const bool in = from + h < c.d;
+                    px[a].v[h] = in ? ((const T *)c.Q)[q + from + h] : (T)0.0f;
+                    py[a].v[h] = in ? ((const T *)c.K)[k + from + h] : (T)0.0f;
+                }
+        }
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (e1 + a * 8 * V >= c.d) continue;
+            float x[V], y[V];
+            unpack<DT, V>(px[a], x);
+            unpack<DT, V>(py[a], y);
 #pragma unroll
             for (int h = 0; h < V; ++h) {
-                const bool in = e + h < c.d;
-                x[h] = in ? (float)((const typename RowType<DT>::T *)c.Q)[q + e + h] : 0.0f;
-                y[h] = in ? (float)((const typename RowType<DT>::T *)c.K)[k + e + h] : 0.0f;
+                const double diff = (double)x[h] - (double)y[h];
+                sum = fma(diff, diff, sum);
             }
-#pragma unroll
-        for (int h = 0; h < V; ++h) {
-            const double diff = (double)x[h] - (double)y[h];
-            sum = fma(diff, diff, sum);
         }
     }
     sum += __shfl_xor(sum, 1);
@@ -361,211 +402,280 @@ __device__ __forceinline__ u32 in_order(float x)        // unsigned integers in 
 }
 __device__ __forceinline__ float from_order(u32 o) { return __uint_as_float(o ^ (o >> 31 ? 0x80000000u : 0xFFFFFFFFu)); }
 
-// A bound from below on the k-th largest of n values (-infinity where there are fewer), by a wavefront: the highest 24 bits of it.
-template <typename F>
-__device__ __forceinline__ float kth_largest(int n, int k, int lane, F value)
+// A bound from below on the k-th largest of a wavefront's values (-infinity where there are fewer): the highest 24 bits of it.
+__device__ __forceinline__ float kth_largest(const float (&v)[LP_ROOM / 64], int k)
 {
-    u32 at = 0;
+    u32 o[LP_ROOM / 64], at = 0;
+#pragma unroll
+    for (int h = 0; h < LP_ROOM / 64; ++h) o[h] = in_order(v[h]);
     for (int bit = 31; bit >= 8; --bit) {
         const u32 t = at | 1u << bit;
         int count = 0;
-        for (int e = 0; e < n; e += 64) count += (int)__popcll(__ballot(e + lane < n && in_order(value(e)) >= t));
+#pragma unroll
+        for (int h = 0; h < LP_ROOM / 64; ++h) count += (int)__popcll(__ballot(o[h] >= t));
         if (count >= k) at = t;
     }
     return at >= in_order(-INFINITY) ? from_order(at) : -INFINITY;
 }
 
-struct FinishLds {
-    float most[LP_ROOM], second[LP_ROOM];
-    int group[LP_ROOM], key[LP_ROOM];
-    double value[LP_ROOM];
-    int part[LP_PARTS];
+// A query's selection.  The keys' values overlay the groups' logits, which are no longer needed then; one place more for the target.
+template <int PARTS> struct FinishLds {
+    union {
+        struct { float most[LP_ROOM], second[LP_ROOM]; };
+        double value[LP_ROOM];
+    };
+    int group[LP_ROOM];
+    union {
+        int part[2 * PARTS];        // until the groups are known
+        struct { int key[LP_ROOM + 1]; float bias[LP_ROOM + 1]; };
+    };
+    double target, lse, norm;
+    int found;                      // keys; -1: no room
+    bool bad;
 };
 
-// A wavefront per query.
-template <int DT, bool WIDE>
-__global__ __launch_bounds__(128) void k_logprob_finish(LogprobPar c)
+// A query by WAVES wavefronts (1: two queries a block).  The first selects; all form the distances of the keys that are left.  A query by
+// itself waits for dependent loads most of the time, so with few queries eight wavefronts take one.
+template <int DT, bool WIDE, int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) void k_logprob_finish(LogprobPar c)
 {
-    __shared__ FinishLds of_waves[2];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = blockIdx.x * 2 + wave, sub = lane & 7;
-    if (i >= c.B) return;
-    FinishLds &lds = of_waves[wave];
-    float top = -INFINITY, sum = 0.0f, w = 0.0f, first = -INFINITY, second = -INFINITY;
+    constexpr int QUERIES = WAVES == 1 ? 2 : 1, PARTS = WAVES == 1 ? 256 : 512, DEEP = WAVES == 1 ? 4 : 8;
+    __shared__ FinishLds<PARTS> of_queries[QUERIES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sub = lane & 7;
+    const int i = WAVES == 1 ? blockIdx.x * 2 + wave : blockIdx.x, worker = WAVES == 1 ? 0 : wave;
+    if (i >= c.B) return;       // (blocks of one query: never)
+    FinishLds<PARTS> &lds = of_queries[WAVES == 1 ? wave : 0];
+    const int k = c.alternatives, size = 1 << c.group_shift;
     const float2 *part = c.part + (size_t)i * c.parts_k;
-#pragma unroll 4
-    for (int t = lane; t < c.parts_k; t += 64) {
-        const float2 p = part[t];
-        join_three(top, sum, w, p.x, p.y, c.part_w[(size_t)i * c.parts_k + t]);
-        second = fmaxf(second, fminf(first, p.x));
-        first = fmaxf(first, p.x);
-    }
+    const float2 *groups = c.groups + ((size_t)i * c.parts_k << c.part_shift);
+    int *ids = c.top_ids + (size_t)i * k;
+    float *tops = c.top_logprob + (size_t)i * k;
+    float cut = -INFINITY;
+    bool asked = false;         // for a target that can be
+    int target = 0;
+    if (worker == 0) {
+        float top = -INFINITY, sum = 0.0f, w = 0.0f, first = -INFINITY, second = -INFINITY, norms = 0.0f, biases = 0.0f;
+        if (c.logprob) target = c.target[i];
+        for (int t0 = lane; t0 < c.parts_k; t0 += 64 * DEEP) {
+            float2 p[DEEP];
+            float pw[DEEP], most[DEEP];
 #pragma unroll
-    for (int s = 1; s < 64; s <<= 1) join_three(top, sum, w, __shfl_xor(top, s), __shfl_xor(sum, s), __shfl_xor(w, s));
-    const bool none = sum == 0.0f, bad = !(sum >= 0.0f && sum < INFINITY);
-    const double lse = (double)top + log2((double)sum), norm = c.few ? 0.0 : query_norm<DT, WIDE>(c, i, lane);
-    auto exactly = [&](int j) {     // in base 2 and the frame of the sums; by 8 lanes
-        return ((c.bias ? (double)c.bias[j] : 0.0) - (double)c.scale * (exact_distance<DT, WIDE>(c, i, j, sub) - norm)) * LP_LOG2E;
+            for (int h = 0; h < DEEP; ++h) {
+                const int t = t0 + h * 64;
+                p[h] = t < c.parts_k ? part[t] : make_float2(-INFINITY, 0.0f);
+                pw[h] = t < c.parts_k ? c.part_w[(size_t)i * c.parts_k + t] : 0.0f;
+                most[h] = c.few && t < c.parts_k ? c.most[t] : 0.0f;
+            }
+#pragma unroll
+            for (int h = 0; h < DEEP; ++h) {
+                join_three(top, sum, w, p[h].x, p[h].y, pw[h]);
+                second = fmaxf(second, fminf(first, p[h].x));
+                first = fmaxf(first, p[h].x);
+                biases = fmaxf(biases, most[h]);
+            }
+        }
+        if (!c.few && k)
+#pragma unroll
+            for (int h = 0; h < CT_ROW_BLOCKS / 256; ++h) {     // (a multiple of 64 blocks)
+                const int b = h * 256 + lane * 4;
+                if (b >= c.most_blocks) continue;
+                const f32x4 x = *(const f32x4 *)&c.most[b], y = *(const f32x4 *)&c.most[CT_ROW_BLOCKS + b];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    norms = fmaxf(norms, x[e]);
+                    biases = fmaxf(biases, y[e]);
+                }
+            }
+        if (c.logprob) asked = (u32)target < (u32)c.M && !leaves_out(c, i, target);
+        const double norm = c.few ? 0.0 : query_norm<DT, WIDE>(c, i, lane);
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) {
+            join_three(top, sum, w, __shfl_xor(top, s), __shfl_xor(sum, s), __shfl_xor(w, s));
+            norms = fmaxf(norms, __shfl_xor(norms, s));
+            biases = fmaxf(biases, __shfl_xor(biases, s));
+        }
+        const bool none = sum == 0.0f, bad = !(sum >= 0.0f && sum < INFINITY);
+        if (c.entropy && lane == 0) c.entropy[i] = none ? 0.0f : bad ? NAN : (log2f(sum) - w / sum) * 0.693147181f;
+        int n = 0, found = 0;
+        bool full = false;
+        if (none || bad) {
+            for (int e = lane; e < k; e += 64) {
+                ids[e] = -1;
+                tops[e] = bad ? NAN : -INFINITY;
+            }
+        } else if (k) {
+            // how far a logit of the first pass may be off, in base 2: a sum of d products of one rounding each (float32 rows: six times as many),
+            // its scaling, the key's own sum and bias; for a few queries a sum of d squares, which with the bias make up the logit
+            const float u = 1.19209290e-7f, terms = DT == DT_F32 ? 6.0f : 1.0f;
+            const float error = c.few ? u * (float)(c.d + 16) * biases * 1.45f
+                                      : 1.45f * (u * fabsf(c.scale) * (2.0f * (terms * c.d + 16.0f) * sqrtf((float)norm * norms) + (float)(c.d + 16) * norms) +
+                                                 2.0f * u * biases);
+            auto below = [&](float t) {     // t: a bound on the k-th logit as the first pass has it, with the key's number in it
+                if (t <= LP_NONE) return -INFINITY;
+                const float b = t - 2.0f * error - fabsf(t) * (4.0e-6f + (c.few ? 2.0f * u * (float)(c.d + 16) : 0.0f));
+                return b > LP_NONE ? b : -INFINITY;
+            };
+            {
+                float v[LP_ROOM / 64];
+#pragma unroll
+                for (int h = 0; h < LP_ROOM / 64; ++h) v[h] = h == 0 ? first : h == 1 ? second : -INFINITY;
+                cut = below(kth_largest(v, k));
+            }
+            // of the groups above the bound, those above a better one
+            auto tighten = [&]() {
+                if (n < k) return;
+                wave_sync();
+                float a[LP_ROOM / 64], b[LP_ROOM / 64];
+                int g[LP_ROOM / 64];
+#pragma unroll
+                for (int h = 0; h < LP_ROOM / 64; ++h) {
+                    const int e = h * 64 + lane;
+                    a[h] = e < n ? lds.most[e] : -INFINITY;
+                    b[h] = e < n ? lds.second[e] : -INFINITY;
+                    g[h] = e < n ? lds.group[e] : 0;
+                }
+                cut = fmaxf(cut, below(kth_largest(a, k)));
+                wave_sync();
+                n = 0;
+#pragma unroll
+                for (int h = 0; h < LP_ROOM / 64; ++h) {
+                    const u64 on = __ballot(a[h] > -INFINITY && a[h] >= cut);
+                    if (on >> lane & 1) {
+                        const int to = n + (int)__popcll(on & lanes_below(lane));
+                        lds.most[to] = a[h];
+                        lds.second[to] = b[h];
+                        lds.group[to] = g[h];
+                    }
+                    n += (int)__popcll(on);
+                }
+                wave_sync();
+            };
+            int parts = 0;
+            for (int p0 = 0; p0 < c.parts_k && !full; p0 += PARTS) {
+                float largest[PARTS / 64];
+#pragma unroll
+                for (int h = 0; h < PARTS / 64; ++h) largest[h] = p0 + h * 64 + lane < c.parts_k ? part[p0 + h * 64 + lane].x : -INFINITY;
+#pragma unroll
+                for (int h = 0; h < PARTS / 64; ++h) {
+                    const u64 on = __ballot(largest[h] > -INFINITY && largest[h] >= cut);
+                    if (on >> lane & 1) lds.part[parts + (int)__popcll(on & lanes_below(lane))] = p0 + h * 64 + lane;
+                    parts += (int)__popcll(on);
+                }
+                if (parts <= PARTS && p0 + PARTS < c.parts_k) continue;        // there is room for the next ones
+                wave_sync();
+                const int items = parts << c.part_shift;
+                for (int t0 = 0; t0 < items && !full; t0 += 64 * DEEP) {
+                    float2 v[DEEP];
+                    int g[DEEP];
+#pragma unroll
+                    for (int h = 0; h < DEEP; ++h) {
+                        const int t = t0 + h * 64 + lane;
+                        g[h] = t < items ? (lds.part[t >> c.part_shift] << c.part_shift) + (t & ((1 << c.part_shift) - 1)) : -1;
+                        v[h] = g[h] >= 0 ? groups[g[h]] : make_float2(-INFINITY, -INFINITY);
+                    }
+#pragma unroll
+                    for (int h = 0; h < DEEP; ++h) {
+                        u64 on = __ballot(v[h].x > LP_NONE * 0.99f && v[h].x >= cut);
+                        if (!on) continue;
+                        if (n + (int)__popcll(on) > LP_ROOM && !full) {
+                            tighten();
+                            on = __ballot(v[h].x > LP_NONE * 0.99f && v[h].x >= cut);
+                            full = n + (int)__popcll(on) > LP_ROOM;
+                        }
+                        if (full) continue;
+                        if (on >> lane & 1) {
+                            const int to = n + (int)__popcll(on & lanes_below(lane));
+                            lds.most[to] = v[h].x;
+                            lds.second[to] = v[h].y;
+                            lds.group[to] = g[h];
+                        }
+                        n += (int)__popcll(on);
+                    }
+                }
+                wave_sync();
+                parts = 0;
+            }
+            if (!full) tighten();
+            wave_sync();
+            // the keys: the largest of a group, or all where the second is above the bound too
+            for (int e = 0; e < n && !full; e += 64) {
+                const bool in = e + lane < n && lds.most[e + lane] >= cut;
+                const int g = in ? lds.group[e + lane] : 0;
+                const int mine = !in ? 0 : lds.second[e + lane] >= cut && lds.second[e + lane] > LP_NONE * 0.99f ? size : 1;
+                int upto = inclusive(mine, lane);
+                const int all = __builtin_amdgcn_readlane(upto, 63);
+                if (found + all > LP_ROOM) {
+                    full = true;
+                    break;
+                }
+                upto += found - mine;
+                if (mine == 1) lds.key[upto] = (g << c.group_shift) + (int)(__float_as_uint(lds.most[e + lane]) & (u32)(size - 1));
+                else
+                    for (int h = 0; h < mine; ++h) lds.key[upto + h] = (g << c.group_shift) + h;
+                found += all;
+            }
+            wave_sync();
+            for (int e = lane; e < found && !full; e += 64) {
+                const int j = lds.key[e];
+                const bool on = j < c.M && !leaves_out(c, i, j);
+                if (!on) lds.key[e] = -1;
+                lds.bias[e] = on && c.bias ? c.bias[j] : 0.0f;
+            }
+        }
+        if (lane == 0) {
+            lds.key[LP_ROOM] = asked ? target : -1;
+            lds.bias[LP_ROOM] = asked && c.bias ? c.bias[target] : 0.0f;
+            lds.lse = (double)top + log2((double)sum);
+            lds.norm = norm;
+            lds.found = full ? -1 : found;
+            lds.bad = bad;
+        }
+    }
+    if constexpr (WAVES > 1) __syncthreads();
+    else wave_sync();
+    const double norm = lds.norm, lse = lds.lse;
+    const bool bad = lds.bad;
+    int found = lds.found;
+    const bool full = found < 0;
+    auto logit = [&](float bias, int j) {       // in base 2 and the frame of the sums; by 8 lanes
+        return ((double)bias - (double)c.scale * (exact_distance<DT, WIDE>(c, i, j, sub) - norm)) * LP_LOG2E;
     };
     auto log_of = [&](double s) {   // (a probability is not above 1)
         const double l = (s - lse) * 0.69314718055994531;
         return bad ? NAN : (float)(l < 0.0 ? l : 0.0);
     };
-    if (c.entropy && lane == 0) c.entropy[i] = none ? 0.0f : bad ? NAN : (log2f(sum) - w / sum) * 0.693147181f;
-    if (c.logprob) {
-        const int t = c.target[i];
-        const bool on = (u32)t < (u32)c.M && !leaves_out(c, i, t);
-        const float l = on ? log_of(exactly(t)) : 0.0f;
-        if (lane == 0) c.logprob[i] = l;
-    }
-    const int k = c.alternatives;
-    if (!k) return;
-    int *ids = c.top_ids + (size_t)i * k;
-    float *tops = c.top_logprob + (size_t)i * k;
-    if (none || bad) {
-        for (int e = lane; e < k; e += 64) {
-            ids[e] = -1;
-            tops[e] = bad ? NAN : -INFINITY;
+    // the target behind the keys
+    for (int e = worker * 8; e < (full ? 0 : found) + 1; e += WAVES * 8) {
+        const int n = full ? 0 : found, at = e + (lane >> 3) < n ? e + (lane >> 3) : LP_ROOM, j = lds.key[at];
+        const double s = logit(lds.bias[at], j < 0 ? 0 : j);
+        if (sub == 0 && e + (lane >> 3) <= n) {
+            if (at < LP_ROOM) lds.value[at] = s;
+            else lds.target = s;
         }
-        return;
     }
-    // how far a logit of the first pass may be off, in base 2: a sum of d products of one rounding each (float32 rows: six times as many), its
-    // scaling, the key's own sum and bias; for a few queries a sum of d squares, which with the bias make up the logit
-    float norms = 0.0f, biases = 0.0f;
-    for (int b = lane; b < c.most_blocks; b += 64) {
-        if (!c.few) norms = fmaxf(norms, c.most[b]);
-        biases = fmaxf(biases, c.most[c.few ? b : CT_ROW_BLOCKS + b]);
-    }
-#pragma unroll
-    for (int s = 32; s; s >>= 1) {
-        norms = fmaxf(norms, __shfl_xor(norms, s));
-        biases = fmaxf(biases, __shfl_xor(biases, s));
-    }
-    const float u = 1.19209290e-7f, terms = DT == DT_F32 ? 6.0f : 1.0f;
-    const float error = c.few ? u * (float)(c.d + 16) * biases * 1.45f
-                              : 1.45f * (u * fabsf(c.scale) * (2.0f * (terms * c.d + 16.0f) * sqrtf((float)norm * norms) + (float)(c.d + 16) * norms) + 2.0f * u * biases);
-    auto below = [&](float t) {     // t: a bound on the k-th logit as the first pass has it, with the key's number in it
-        if (t <= LP_NONE) return -INFINITY;
-        const float cut = t - 2.0f * error - fabsf(t) * (4.0e-6f + (c.few ? 2.0f * u * (float)(c.d + 16) : 0.0f));
-        return cut > LP_NONE ? cut : -INFINITY;
-    };
-    float cut = below(kth_largest(128, k, lane, [&](int e) { return e ? second : first; }));
-    int n = 0;
-    bool full = false;
-    // the groups above the bound: keeps those that are above a better one
-    auto tighten = [&]() {
-        if (n < k) return;
-        wave_sync();
-        cut = fmaxf(cut, below(kth_largest(n, k, lane, [&](int e) { return lds.most[e + lane]; })));
-        int kept = 0;
-        for (int e = 0; e < n; e += 64) {
-            const bool in = e + lane < n;
-            const float a = in ? lds.most[e + lane] : 0.0f, b = in ? lds.second[e + lane] : 0.0f;
-            const int g = in ? lds.group[e + lane] : 0;
-            const u64 on = __ballot(in && a >= cut);
-            wave_sync();
-            if (on >> lane & 1) {
-                const int to = kept + (int)__popcll(on & lanes_below(lane));
-                lds.most[to] = a;
-                lds.second[to] = b;
-                lds.group[to] = g;
-            }
-            kept += (int)__popcll(on);
-            wave_sync();
-        }
-        n = kept;
-    };
-    const float2 *groups = c.groups + ((size_t)i * c.parts_k << c.part_shift);
-    for (int p0 = 0; p0 < c.parts_k && !full; p0 += LP_PARTS) {
-        int parts = 0;
-#pragma unroll
-        for (int h = 0; h < LP_PARTS; h += 64) {
-            const int p = p0 + h + lane;
-            const float largest = p < c.parts_k ? part[p].x : -INFINITY;
-            const u64 on = __ballot(largest > -INFINITY && largest >= cut);
-            if (on >> lane & 1) lds.part[parts + (int)__popcll(on & lanes_below(lane))] = p;
-            parts += (int)__popcll(on);
-        }
-        wave_sync();
-        const int items = parts << c.part_shift;
-        for (int t0 = 0; t0 < items && !full; t0 += 256) {
-            float2 v[4];
-            int g[4];
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                const int t = t0 + h * 64 + lane;
-                g[h] = t < items ? (lds.part[t >> c.part_shift] << c.part_shift) + (t & ((1 << c.part_shift) - 1)) : -1;
-                v[h] = g[h] >= 0 ? groups[g[h]] : make_float2(-INFINITY, -INFINITY);
-            }
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                u64 on = __ballot(v[h].x > LP_NONE * 0.99f && v[h].x >= cut);
-                if (!on) continue;
-                if (n + (int)__popcll(on) > LP_ROOM && !full) {
-                    tighten();
-                    on = __ballot(v[h].x > LP_NONE * 0.99f && v[h].x >= cut);
-                    full = n + (int)__popcll(on) > LP_ROOM;
-                }
-                if (full) continue;
-                if (on >> lane & 1) {
-                    const int to = n + (int)__popcll(on & lanes_below(lane));
-                    lds.most[to] = v[h].x;
-                    lds.second[to] = v[h].y;
-                    lds.group[to] = g[h];
-                }
-                n += (int)__popcll(on);
-            }
-        }
-        wave_sync();
-    }
-    const int size = 1 << c.group_shift;
-    int found = 0;
+    if constexpr (WAVES > 1) __syncthreads();
+    else wave_sync();
+    if (worker) return;
+    if (c.logprob && lane == 0) c.logprob[i] = lds.key[LP_ROOM] >= 0 ? log_of(lds.target) : 0.0f;
+    if (!k || bad || lse == -INFINITY) return;
     if (!full) {
-        tighten();
-        wave_sync();
-        // the keys: the largest of a group, or all where the second is above the bound too
-        for (int e = 0; e < n && !full; e += 64) {
-            const bool in = e + lane < n && lds.most[e + lane] >= cut;
-            const int g = in ? lds.group[e + lane] : 0, mine = !in ? 0 : lds.second[e + lane] >= cut && lds.second[e + lane] > LP_NONE * 0.99f ? size : 1;
-            int upto = inclusive(mine, lane);
-            const int all = __builtin_amdgcn_readlane(upto, 63);
-            if (found + all > LP_ROOM) {
-                full = true;
-                break;
-            }
-            upto += found - mine;
-            if (mine == 1) lds.key[upto] = (g << c.group_shift) + (int)(__float_as_uint(lds.most[e + lane]) & (u32)(size - 1));
-            else
-                for (int h = 0; h < mine; ++h) lds.key[upto + h] = (g << c.group_shift) + h;
-            found += all;
-        }
-    }
-    if (!full) {
-        wave_sync();
-        for (int e = 0; e < found; e += 8) {
-            const int at = e + (lane >> 3), j = at < found ? lds.key[at] : c.M;
-            const bool on = j < c.M && !leaves_out(c, i, j);
-            const double s = exactly(on ? j : 0);
-            if (sub == 0 && at < found) {
-                lds.value[at] = s;
-                if (!on || !(s > -INFINITY)) lds.key[at] = -1;
-            }
-        }
-        wave_sync();
         int valid = 0;
         for (int e = 0; e < found; e += 64) {
             const int j = e + lane < found ? lds.key[e + lane] : -1;
             const double s = j >= 0 ? lds.value[e + lane] : 0.0;
+            const bool on = j >= 0 && s > -INFINITY;
             int rank = 0;
+#pragma unroll 4
             for (int o = 0; o < found; ++o) {
                 const double os = lds.value[o];
                 const int oj = lds.key[o];
                 rank += oj >= 0 && (os > s || (os == s && oj < j));
             }
-            if (j >= 0 && rank < k) {
+            if (on && rank < k) {
                 ids[rank] = j;
                 tops[rank] = log_of(s);
             }
-            valid += (int)__popcll(__ballot(j >= 0));
+            valid += (int)__popcll(__ballot(on));
         }
         for (int e = valid + lane; e < k; e += 64) {
             ids[e] = -1;
@@ -575,7 +685,6 @@ __global__ __launch_bounds__(128) void k_logprob_finish(LogprobPar c)
     }
     // No room: every key of a group above the bound, in the order of their positions, into a list of the k best so far.  The bound stays valid:
     // keys that are not looked at are below k others.
-    wave_sync();
     found = 0;
     for (int g0 = 0; g0 < c.parts_k << c.part_shift; g0 += 64) {
         const int g = g0 + lane;
@@ -583,7 +692,7 @@ __global__ __launch_bounds__(128) void k_logprob_finish(LogprobPar c)
         for (u64 on = __ballot(largest > LP_NONE * 0.99f && largest >= cut); on; on &= on - 1) {
             const int key0 = (g0 + __builtin_ctzll(on)) << c.group_shift, j = key0 + (lane >> 3);
             bool in = lane >> 3 < size && j < c.M && !leaves_out(c, i, j);
-            const double s = exactly(in ? j : 0);
+            const double s = logit(in && c.bias ? c.bias[j] : 0.0f, in ? j : 0);
             in &= s > -INFINITY;
             for (int h = 0; h < size; ++h) {
                 if (!__builtin_amdgcn_readlane((int)in, h * 8)) continue;
@@ -621,7 +730,7 @@ __global__ __launch_bounds__(128) void k_logprob_finish(LogprobPar c)
 struct LogprobPlan {
     ContrastPlan tiles;
     int slab;           // queries of a run through the keys
-    int part_keys;      // a few queries: keys of a block
+    int wave_keys, passes;      // a few queries: keys of a wavefront at a time, and how many times
 };
 
 #define LP_BYTES ((size_t)1 << 28)      // of a run's parts and groups
@@ -637,12 +746,15 @@ static size_t layout(LogprobPar &c, LogprobPlan &plan, int dtype, char *base)
     c.few = c.B <= LP_FEW;
     if (c.few) {
         // parts: a wavefront joins them in the end, so not more than some 2,000
-        plan.part_keys = LP_PASS;
-        while ((c.M + plan.part_keys - 1) / plan.part_keys > 2048) plan.part_keys *= 2;
+        plan.wave_keys = c.B <= 2 ? 32 : 16;
+        plan.passes = 1;
+        auto parts = [&]() { return (c.M + plan.wave_keys * 4 * plan.passes - 1) / (plan.wave_keys * 4 * plan.passes); };
+        while (plan.wave_keys < 64 && parts() > 512) plan.wave_keys *= 2;
+        while (parts() > 2048) plan.passes *= 2;
         plan.slab = c.B;
-        c.parts_k = (c.M + plan.part_keys - 1) / plan.part_keys;
+        c.parts_k = parts();
         c.group_shift = 3;
-        c.part_shift = __builtin_ctz(plan.part_keys / 8);
+        c.part_shift = __builtin_ctz(plan.wave_keys * plan.passes / 2);
         c.most_blocks = c.parts_k;
         take(c.most, c.parts_k);
         take(c.part, (size_t)c.B * c.parts_k);
@@ -708,8 +820,10 @@ static void launch_logprob(LogprobPar &c, const LogprobPlan &plan, bool wide_few
     if (c.few) {
         const dim3 grid(c.parts_k), block(256);
 #define LP_LAUNCH(NB) \
-        if (wide_few) hipLaunchKernelGGL((k_logprob_few<DT, NB, true>), grid, block, 0, st, c, plan.part_keys); \
-        else hipLaunchKernelGGL((k_logprob_few<DT, NB, false>), grid, block, 0, st, c, plan.part_keys)
+        const int chunk = c.d <= LP_CHUNK / NB ? (c.d + 7) & ~7 : LP_CHUNK / NB; \
+        const size_t bytes = (size_t)(NB * chunk + 4 * NB * 64) * 4; \
+        if (wide_few) hipLaunchKernelGGL((k_logprob_few<DT, NB, true>), grid, block, bytes, st, c, plan.wave_keys, plan.passes); \
+        else hipLaunchKernelGGL((k_logprob_few<DT, NB, false>), grid, block, bytes, st, c, plan.wave_keys, plan.passes)
         if (c.B == 1) { LP_LAUNCH(1); }
         else if (c.B == 2) { LP_LAUNCH(2); }
         else if (c.B <= 4) { LP_LAUNCH(4); }
@@ -732,8 +846,12 @@ static void launch_logprob(LogprobPar &c, const LogprobPlan &plan, bool wide_few
         } else if (plan.tiles.terms) launch_sums<DT, 128, true>(c, st);
         else launch_sums<DT, 128, false>(c, st);
     }
-    if (wide_few) hipLaunchKernelGGL((k_logprob_finish<DT, true>), dim3((c.B + 1) / 2), dim3(128), 0, st, c);
-    else hipLaunchKernelGGL((k_logprob_finish<DT, false>), dim3((c.B + 1) / 2), dim3(128), 0, st, c);
+#define LP_LAUNCH(WAVES, BLOCKS, THREADS) \
+    if (wide_few) hipLaunchKernelGGL((k_logprob_finish<DT, true, WAVES>), dim3(BLOCKS), dim3(THREADS), 0, st, c); \
+    else hipLaunchKernelGGL((k_logprob_finish<DT, false, WAVES>), dim3(BLOCKS), dim3(THREADS), 0, st, c)
+    if (c.B <= LP_ALONE) { LP_LAUNCH(8, c.B, 512); }
+    else { LP_LAUNCH(1, (c.B + 1) / 2, 128); }
+#undef LP_LAUNCH
 }
 
 extern "C" int rnnd_logprob(const void *Q, int64_t B, const void *K, int64_t M, int32_t d, int dtype, int metric, const int32_t *target,
