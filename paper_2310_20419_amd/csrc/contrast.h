@@ -27,9 +27,11 @@ struct ContrastPar {
     float scale, c1;                // c1 = 2 scale log2(e)
     int B, M, d;
     int dp, Bp, Mp, dr;             // padded to CT_K; dr: d padded to the tile of the gradient products
+    bool keys_as_they_are;          // no copy of all of them
+    int key0;                       // the first key that copies are made of and logits are formed with
     int ld_g, ld_gt;                // rows of g by rows and by columns: M and B padded to the largest tile
     size_t plane_q, plane_k, plane_qt, plane_kt, plane_g, plane_gt;     // elements
-    half_t *q, *k, *qt, *kt, *g, *gt;
+    half_t *q, *k, *qt, *kt, *g, *gt;       // copies (k: NULL where the keys are read as they are)
     u32 *tops, *top;                // float16 rows: largest weight of each block of queries, and of all, as bits
     int *first, *count;             // [M] the first query whose target the key is, and how many they are
     float *centre;                  // float32 rows: [dp] the point that they are taken from, zeros behind its d coordinates
@@ -148,13 +150,14 @@ __device__ __forceinline__ void from_centre(const ContrastPar &c, int e, float (
     for (int k = 0; k < 4; ++k) x[k] -= m[k];
 }
 
-// A key's own part of its logits, by a wavefront; at < M padded
-template <int DT, bool WIDE>
+// A key's own part of its logits, by a wavefront; at < M padded.  ALL: the products read the rows of keys that are left out, too.  Zero times what is
+// not a number is not zero, so those of which some are not get a base that is NaN.
+template <int DT, bool WIDE, bool ALL = false>
 __device__ __forceinline__ float key_side(const ContrastPar &c, int at, int lane)
 {
     const bool gone = at >= c.M || key_gone(c, at);
     float sum = 0.0f;
-    if (!gone)
+    if (ALL ? at < c.M : !gone)
         for (int e = lane * 4; e < c.d; e += 256) {
             float x[4];
             load4<DT, WIDE>(c.K, at, c.d, e, x);
@@ -164,7 +167,7 @@ __device__ __forceinline__ float key_side(const ContrastPar &c, int at, int lane
         }
     sum = wave_sum(sum);
     if (lane == 0) {
-        c.key_base[at] = gone ? -INFINITY : ((c.bias ? c.bias[at] : 0.0f) - c.scale * sum) * 1.44269504f;
+        c.key_base[at] = gone ? ALL && !(sum < INFINITY) ? NAN : -INFINITY : ((c.bias ? c.bias[at] : 0.0f) - c.scale * sum) * 1.44269504f;
         c.key_id[at] = gone ? -1 : c.key_ids ? c.key_ids[at] : at;
     }
     return sum;
@@ -201,7 +204,7 @@ __device__ __forceinline__ void contrast_copy(const PAR &c, int tile_r, int c0, 
     constexpr int PLANES = planes_of<DT>();
     __shared__ u32 tile[64][33];        // [column][two rows]
     const bool keys = tile_r >= q_tiles;
-    const int r0 = (keys ? tile_r - q_tiles : tile_r) * 64;
+    const int r0 = keys ? (tile_r - q_tiles) * 64 + c.key0 : tile_r * 64;
     const void *rows = keys ? c.K : c.Q;
     half_t *by_row = keys ? c.k : c.q, *by_col = keys ? c.kt : c.qt;
     const size_t plane_r = keys ? c.plane_k : c.plane_q, plane_c = keys ? c.plane_kt : c.plane_qt;
@@ -266,7 +269,8 @@ __device__ __forceinline__ void contrast_copy(const PAR &c, int tile_r, int c0, 
 //
 // LDS traffic a step: each wavefront reads TILE rows, all write 2 TILE: (4 + 2) * TILE * 128 bytes at 128 a clock, against
 // TILE^2 * 128 / 4096 clocks of matrix work: 768 against 512 clocks with TILE = 128, 1,536 against 2,048 with TILE = 256.
-struct Operand { const half_t *p; size_t plane; int ld; };      // rows of ld elements, ld a multiple of CT_K
+// Rows of ld elements, ld a multiple of CT_K; rows behind the last are zeros (copies are padded to whole tiles, so they have none).
+struct Operand { const half_t *p; size_t plane; int ld, rows = 0x7FFFFFFF; };
 
 template <int TILE> struct ProductLds { half_t a[2][TILE * CT_K], b[2][TILE * CT_K]; };
 
@@ -308,10 +312,13 @@ template <int DT> __device__ __forceinline__ f32x4 mfma(const us8 &a, const us8 
 
 template <int N> struct Half { us8 a[N], b[N]; };      // what half a step multiplies
 
-// `meanwhile` runs while the first loads are under way; what it leaves in LDS is there behind the product.
-template <int TILE, int DT, typename F>
+struct Nothing { __device__ __forceinline__ void operator()(const us8 &, int) const {} };
+
+// `meanwhile` runs while the first loads are under way; what it leaves in LDS is there behind the product.  also(b, j) is given all that is
+// multiplied of B: of the lane's column j, a quarter of every step.
+template <int TILE, int DT, typename F, typename G = Nothing>
 __device__ __forceinline__ void product(const Operand &A, const Operand &B, int row_a, int row_b, int k_begin, int k_end,
-                                        ProductLds<TILE> &lds, f32x4 (&acc)[TILE / 32][TILE / 32], F meanwhile)
+                                        ProductLds<TILE> &lds, f32x4 (&acc)[TILE / 32][TILE / 32], F meanwhile, G also = G())
 {
     constexpr int N = TILE / 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -330,6 +337,7 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int 
         vb[i] = (col_at<TILE>(p) * B.ld + piece * 8) * 2;
     }
     const half_t *pa = A.p + (size_t)row_a * A.ld, *pb = B.p + (size_t)row_b * B.ld;
+    const int bytes_a = (A.rows - row_a < TILE ? A.rows - row_a : TILE) * A.ld * 2, bytes_b = (B.rows - row_b < TILE ? B.rows - row_b : TILE) * B.ld * 2;
     // 1 / N of a step's loads
     auto fetch = [&](int s, int buf, int i) {
         int kk = s;
@@ -341,8 +349,8 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int 
             qb += (pair == 1 || pair == 3 ? 1 : pair == 4 ? 2 : 0) * B.plane;
         }
         const int at = (k_begin + kk * CT_K) * 2, place = (wave * (TILE / 4) + i * 8) * CT_K;
-        to_lds(qa, TILE * A.ld * 2, &lds.a[buf][place], va[i], at);
-        to_lds(qb, TILE * B.ld * 2, &lds.b[buf][place], vb[i], at);
+        to_lds(qa, bytes_a, &lds.a[buf][place], va[i], at);
+        to_lds(qb, bytes_b, &lds.b[buf][place], vb[i], at);
     };
     const int ra0 = ((wave >> 1) * (TILE / 2) + (lane & 15)) * CT_K, rb0 = ((wave & 1) * (TILE / 2) + (lane & 15)) * CT_K;
     const int piece0 = ((lane >> 4) ^ (lane & 7)) * 8;
@@ -386,6 +394,7 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int 
                 read(h1, s & 1, 1, 2 * i + 1);
             }
             multiply(h0, i);
+            also(h0.b[i], i);
             __builtin_amdgcn_sched_barrier(0);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // the next step is there
@@ -401,15 +410,22 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int 
                 read(h0, (s + 1) & 1, 0, 2 * i - N + 1);
             }
             multiply(h1, i);
+            also(h1.b[i], i);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) read(h1, (steps - 1) & 1, 1, i);
 #pragma unroll
-    for (int i = 0; i < N; ++i) multiply(h0, i);
+    for (int i = 0; i < N; ++i) {
+        multiply(h0, i);
+        also(h0.b[i], i);
+    }
 #pragma unroll
-    for (int i = 0; i < N; ++i) multiply(h1, i);
+    for (int i = 0; i < N; ++i) {
+        multiply(h1, i);
+        also(h1.b[i], i);
+    }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if constexpr (TILE == 256) {
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");       // a result may be read 18 clocks behind its instruction
@@ -588,7 +604,8 @@ template <int TILE> struct SideLds {
 template <typename PAR> constexpr bool has_lists() { return false; }
 template <int TILE, typename PAR> struct ListLds {};
 __device__ __forceinline__ u32 id_hash(int id) { return (u32)id * 0x9E3779B1u >> (32 - CT_HASH); }
-template <int TILE> __device__ __forceinline__ void load_side(const ContrastPar &c, SideLds<TILE> &side, int row0, int col0)
+// PREPARED: by key_side(); else the base is without -scale |k|^2.
+template <int TILE, bool PREPARED> __device__ __forceinline__ void load_side(const ContrastPar &c, SideLds<TILE> &side, int row0, int col0)
 {
     const int t = threadIdx.x;
     int id = -1;
@@ -598,8 +615,15 @@ template <int TILE> __device__ __forceinline__ void load_side(const ContrastPar 
     if (t < TILE) {
         side.row_id[t] = out = c.row_id[row0 + t];
         side.row_g[t] = c.row_g[row0 + t];
-        side.base[t] = c.key_base[col0 + t];
-        side.id[t] = id = c.key_id[col0 + t];
+        if constexpr (!PREPARED) {
+            const int j = col0 + t;
+            const bool gone = j >= c.M || key_gone(c, j);
+            side.base[t] = gone ? -INFINITY : c.bias ? c.bias[j] * 1.44269504f : 0.0f;
+            side.id[t] = id = gone ? -1 : c.key_ids ? c.key_ids[j] : j;
+        } else {
+            side.base[t] = c.key_base[col0 + t];
+            side.id[t] = id = c.key_id[col0 + t];
+        }
     }
     __syncthreads();
     if (t < TILE && id >= 0) atomicOr(&side.seen[id_hash(id) >> 5], 1u << (id_hash(id) & 31));
@@ -608,21 +632,22 @@ template <int TILE> __device__ __forceinline__ void load_side(const ContrastPar 
 }
 
 // q k' of a tile, its side tables read meanwhile
-template <int TILE, int DT, bool TERMS, typename LDS, typename F>
-__device__ __forceinline__ void logit_product(const ContrastPar &c, int tr, int tc, LDS &lds, SideLds<TILE> &side, f32x4 (&acc)[TILE / 32][TILE / 32], F lists)
+template <int TILE, int DT, bool TERMS, bool PREPARED = true, typename LDS, typename F, typename G = Nothing>
+__device__ __forceinline__ void logit_product(const ContrastPar &c, int tr, int tc, LDS &lds, SideLds<TILE> &side, f32x4 (&acc)[TILE / 32][TILE / 32], F lists,
+                                              G also = G())
 {
-    const Operand q = {c.q, c.plane_q, c.dp}, k = {c.k, c.plane_k, c.dp};
+    const Operand q = {c.q, c.plane_q, c.dp}, k = !c.k ? Operand{(const half_t *)c.K, 0, c.d, c.M} : Operand{c.k, c.plane_k, c.dp};
     const auto tables = [&]() {
-        load_side(c, side, tr * TILE, tc * TILE);
+        load_side<TILE, PREPARED>(c, side, tr * TILE, tc * TILE);
         lists();
     };
     if constexpr (TERMS) product_of_terms(q, k, tr * TILE, tc * TILE, 0, c.dp, lds, acc, tables);
-    else product<TILE, DT>(q, k, tr * TILE, tc * TILE, 0, c.dp, lds, acc, tables);
+    else product<TILE, DT>(q, k, tr * TILE, tc * TILE, 0, c.dp, lds, acc, tables, also);
 }
 
-// Logits of the keys that rows leave out become -infinity; nothing to do for most rows.
+// Logits of the keys that rows leave out become -infinity, or what stands for it; nothing to do for most rows.
 template <int TILE, int R, int N>
-__device__ __forceinline__ void leave_out(const SideLds<TILE> &side, int row, const int (&id)[N], float (&s)[R][N])
+__device__ __forceinline__ void leave_out(const SideLds<TILE> &side, int row, const int (&id)[N], float (&s)[R][N], float none = -INFINITY)
 {
     u32 maybe = 0;
 #pragma unroll
@@ -632,7 +657,7 @@ __device__ __forceinline__ void leave_out(const SideLds<TILE> &side, int row, co
     for (int r = 0; r < R; ++r) {
         const int2 out = side.row_id[row + r];
 #pragma unroll
-        for (int n = 0; n < N; ++n) s[r][n] = id[n] == out.x || id[n] == out.y ? -INFINITY : s[r][n];
+        for (int n = 0; n < N; ++n) s[r][n] = id[n] == out.x || id[n] == out.y ? none : s[r][n];
     }
 }
 
@@ -1013,7 +1038,8 @@ static size_t contrast_layout(ContrastPar &c, ContrastPlan &plan, int dtype, int
     take(c.row_own, Br);
     take(c.part, Br * c.parts_k);
     take(c.q, planes * (c.plane_q = Br * c.dp));
-    take(c.k, planes * (c.plane_k = Mr * c.dp));
+    c.plane_k = Mr * c.dp;
+    if (!c.keys_as_they_are) take(c.k, planes * c.plane_k);
     if (want_grad) {
         take(c.qt, planes * (c.plane_qt = (size_t)c.dr * c.Bp));
         take(c.kt, planes * (c.plane_kt = (size_t)c.dr * c.Mp));

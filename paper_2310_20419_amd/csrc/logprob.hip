@@ -31,6 +31,7 @@ struct LogprobPar : ContrastPar {
     int group_shift, part_shift;    // keys of a group, groups of a part: powers of two
     float *most;                // [2][CT_ROW_BLOCKS] largest |k|^2 and |bias| of a block of keys
     int most_blocks;
+    bool squares;               // |k|^2 comes from the product's pass over the keys
     int few;                    // logits are from differences: the whole of s
 };
 
@@ -67,7 +68,7 @@ __global__ __launch_bounds__(256) void k_logprob_prepare(LogprobPar c, u32 first
         if (threadIdx.x == 0) most = {0, 0};
         __syncthreads();
         for (int at = block * 4 + wave; at < ct_up(c.M, CT_PAD); at += key_blocks * 4) {
-            const float norm = key_side<DT, WIDE>(c, at, lane);
+            const float norm = c.keys_as_they_are ? key_side<DT, WIDE, true>(c, at, lane) : key_side<DT, WIDE>(c, at, lane);
             if (lane == 0) most_of(most, c, at, norm);
         }
         __syncthreads();
@@ -81,18 +82,32 @@ __global__ __launch_bounds__(256) void k_logprob_prepare(LogprobPar c, u32 first
         c.row_id[at] = make_int2(CT_NEVER, at < c.B && c.query_ids ? c.query_ids[at] : CT_NEVER);
         c.row_g[at] = make_float2(0.0f, 0.0f);
     }
+    if (c.squares && block == key_blocks && threadIdx.x < 8) c.most[(threadIdx.x >> 2) * CT_ROW_BLOCKS + (threadIdx.x & 3)] = 0.0f;
 }
 
 // ------------------------------------------------------------------------------------------------ the logits by tiles
 // Puts a logit into the largest two of its group.
 __device__ __forceinline__ void into_group(float &most, float &second, float s, int n, int group)
 {
-    const float x = __uint_as_float((__float_as_uint(fmaxf(s, LP_NONE)) & ~(u32)(group - 1)) | (u32)n);
+    const float x = __uint_as_float((__float_as_uint(s) & ~(u32)(group - 1)) | (u32)n);
     second = __builtin_amdgcn_fmed3f(most, second, x);      // most >= second
     most = fmaxf(most, x);
 }
 
-template <int TILE, int DT, bool TERMS, bool TOPS>
+// Sums of squares of what the product multiplies: |k|^2 without another pass over the keys.  (The dot product instruction of bfloat16 pairs rounds
+// in between: |k|^2 = 1 of 768 coordinates was off by 2 %.)
+template <int DT, int N> struct SquaresOf {
+    float (&sum)[N];
+    __device__ __forceinline__ void operator()(const us8 &b, int j) const
+    {
+#pragma unroll
+        for (int h = 0; h < 8; ++h) sum[j] = fmaf(value16<DT>(b[h]), value16<DT>(b[h]), sum[j]);
+    }
+};
+
+// Keys as they are: rows of those that are left out are multiplied too; what is not a number stays in its own column.
+// Left-out keys have LP_NONE for a logit, and logits below it count as it; NaN stays NaN, and makes the sum NaN.
+template <int TILE, int DT, bool TERMS, bool TOPS, bool SQUARES>
 __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_logprob_sums(LogprobPar c, u32 first, int tiles_q, int tiles_k)
 {
     constexpr int N = TILE / 32;
@@ -101,14 +116,51 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_logprob_s
     f32x4 acc[N][N];
     int tr, tc;
     tile_of((int)(first + blockIdx.x), tiles_q, tiles_k, tr, tc);
-    logit_product<TILE, DT, TERMS>(c, tr, tc, lds, side, acc, []() {});
+    tc += c.key0 / TILE;
+    float base[N], norm[N] = {};
+    if constexpr (SQUARES) logit_product<TILE, DT, TERMS, false>(c, tr, tc, lds, side, acc, []() {}, SquaresOf<DT, N>{norm});
+    else logit_product<TILE, DT, TERMS>(c, tr, tc, lds, side, acc, []() {});
     const Place<TILE> at(tr, tc);
-    float base[N];
     int id[N];
+    bool odd[N], any_odd = false;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
         base[n] = side.base[at.in_col + n];
         id[n] = side.id[at.in_col + n];
+        const bool gone = id[n] < 0;
+        if constexpr (SQUARES) {
+            norm[n] += __shfl_xor(norm[n], 16);
+            norm[n] += __shfl_xor(norm[n], 32);
+            odd[n] = gone && !(norm[n] < INFINITY);
+            if (!gone) base[n] = fmaf(-c.scale * norm[n], 1.44269504f, base[n]);
+        } else {
+            odd[n] = gone && base[n] != base[n];
+            if (odd[n]) base[n] = LP_NONE;
+        }
+        any_odd |= odd[n];
+        base[n] = base[n] < LP_NONE ? LP_NONE : base[n];        // (NaN stays)
+    }
+    any_odd = __any(any_odd);
+    if constexpr (SQUARES && TOPS) {
+        if (tr == 0 && threadIdx.x < 128) {         // the two wavefronts that have all columns
+            float most = 0.0f, bias = 0.0f;
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                if (id[n] < 0 || odd[n]) continue;
+                most = fmaxf(most, norm[n] < INFINITY ? norm[n] : INFINITY);
+                const float b = c.bias ? fabsf(side.base[at.in_col + n]) * 0.7f : 0.0f;
+                bias = fmaxf(bias, b < INFINITY ? b : INFINITY);
+            }
+#pragma unroll
+            for (int x = 8; x; x >>= 1) {
+                most = fmaxf(most, __shfl_xor(most, x));
+                bias = fmaxf(bias, __shfl_xor(bias, x));
+            }
+            if ((threadIdx.x & 63) == 0) {
+                atomicMax((u32 *)&c.most[0], __float_as_uint(most));
+                atomicMax((u32 *)&c.most[CT_ROW_BLOCKS], __float_as_uint(bias));
+            }
+        }
     }
     // as in k_contrast_sums; and a lane's N columns of a row are a group
     float keep_top[N / 4], keep_sum[N / 4], keep_w[N / 4];
@@ -118,30 +170,39 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_logprob_s
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int n = 0; n < N; ++n) s[r][n] = fmaf(acc[m][n][r], c.c1, base[n]);
-        leave_out(side, at.in_row + m * 4, id, s);
+            for (int n = 0; n < N; ++n) s[r][n] = __builtin_elementwise_maximum(fmaf(acc[m][n][r], c.c1, base[n]), LP_NONE);
+        leave_out(side, at.in_row + m * 4, id, s, LP_NONE);
+        if constexpr (DT != DT_F32)
+            if (any_odd)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int n = 0; n < N; ++n) s[r][n] = odd[n] ? LP_NONE : s[r][n];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            if constexpr (TOPS) {
-                float most = -INFINITY, second = -INFINITY;
+            if constexpr (TOPS) {       // (with the key's number in the lowest bits it does for the reference, too)
+                float most = LP_NONE, second = LP_NONE;
 #pragma unroll
                 for (int n = 0; n < N; ++n) into_group(most, second, s[r][n], n, N);
                 c.groups[((size_t)(at.row + m * 4 + r) * c.parts_k + at.half_c) * 16 + (threadIdx.x & 15)] = make_float2(most, second);
-            }
-            top[r] = s[r][0];
+                top[r] = most;
+            } else {
+                top[r] = s[r][0];
 #pragma unroll
-            for (int n = 1; n < N; ++n) top[r] = fmaxf(top[r], s[r][n]);
+                for (int n = 1; n < N; ++n) top[r] = fmaxf(top[r], s[r][n]);
+            }
         }
         row16_max(top);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const float ref = top[r] == -INFINITY ? 0.0f : top[r];
+            const float ref = top[r] > LP_NONE * 0.99f ? top[r] : 0.0f;
+            top[r] = top[r] > LP_NONE * 0.99f ? top[r] : -INFINITY;
             sum[r] = w[r] = 0.0f;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 const float x = s[r][n] - ref, e = __builtin_amdgcn_exp2f(x);
                 sum[r] += e;
-                w[r] = fmaf(e, fmaxf(x, LP_NONE), w[r]);
+                w[r] = fmaf(e, x, w[r]);
             }
         }
         row16_sum(sum);
@@ -495,7 +556,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) 
             biases = fmaxf(biases, __shfl_xor(biases, s));
         }
         const bool none = sum == 0.0f, bad = !(sum >= 0.0f && sum < INFINITY);
-        if (c.entropy && lane == 0) c.entropy[i] = none ? 0.0f : bad ? NAN : (log2f(sum) - w / sum) * 0.693147181f;
+        if (c.entropy && lane == 0) c.entropy[i] = none ? 0.0f : bad ? NAN : fmaxf(0.0f, (log2f(sum) - w / sum) * 0.693147181f);
         int n = 0, found = 0;
         bool full = false;
         if (none || bad) {
@@ -730,11 +791,17 @@ __global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) 
 struct LogprobPlan {
     ContrastPlan tiles;
     int slab;           // queries of a run through the keys
+    half_t *spare;      // room for copies of key_rows keys, where the keys could be read as they are but for where they lie
+    int key_rows;
+    bool copied;
     int wave_keys, passes;      // a few queries: keys of a wavefront at a time, and how many times
 };
 
 #define LP_BYTES ((size_t)1 << 28)      // of a run's parts and groups
 
+// Keys of 16 bits whose rows are whole steps of the product are read where they are.  Where they do not lie at a multiple of 16 bytes they are copied after
+// all, as many at a time as there is room for: neither the workspace nor the order of sums goes by addresses.
+#define LP_SPARE 16384
 static size_t layout(LogprobPar &c, LogprobPlan &plan, int dtype, char *base)
 {
     size_t off = 0;
@@ -763,6 +830,10 @@ static size_t layout(LogprobPar &c, LogprobPlan &plan, int dtype, char *base)
         return off;
     }
     plan.tiles = contrast_plan(c, dtype == RNND_F32 ? 3 : 1);
+    c.keys_as_they_are = dtype != RNND_F32 && c.d % CT_K == 0;
+    // Their norms come from the product's pass over them where few tiles do that for every key.  Norms by themselves / along with the product, us:
+    // bfloat16, 200 x 300,000 x 768 (one row of tiles) 600 / 300, 8,192 x 16,384 x 768 (32) 430 / 470; float16, 1,000 x 11,000 x 768 54 / 51
+    c.squares = c.keys_as_they_are && c.B <= 1024;
     c.part_shift = 4;
     const size_t row = (size_t)c.parts_k * (12 + (c.alternatives ? 16 * 8 : 0));
     const size_t rows = LP_BYTES / row / CT_PAD * CT_PAD;
@@ -773,6 +844,8 @@ static size_t layout(LogprobPar &c, LogprobPlan &plan, int dtype, char *base)
     const size_t Br = ct_up(c.B, CT_PAD);
     take(c.most, 2 * CT_ROW_BLOCKS);
     take(c.part_w, Br * c.parts_k);
+    plan.key_rows = ct_up(c.M, CT_PAD) < LP_SPARE ? ct_up(c.M, CT_PAD) : LP_SPARE;
+    if (c.keys_as_they_are) take(plan.spare, (size_t)plan.key_rows * c.dp);
     if (c.alternatives) take(c.groups, (Br * c.parts_k) << c.part_shift);
     c.B = queries;
     return off;
@@ -795,7 +868,7 @@ extern "C" int rnnd_logprob_workspace(int64_t B, int64_t M, int32_t d, int dtype
         return RNND_OK;
     }
     LogprobPar c = {};
-    LogprobPlan plan;
+    LogprobPlan plan = {};
     c.B = (int)B;
     c.M = (int)M;
     c.d = d;
@@ -805,12 +878,19 @@ extern "C" int rnnd_logprob_workspace(int64_t B, int64_t M, int32_t d, int dtype
 }
 
 template <int DT, int TILE, bool TERMS>
-static void launch_sums(LogprobPar &c, hipStream_t st)
+static void launch_sums(const LogprobPar &c, int keys, hipStream_t st)
 {
-    const int tq = ct_up(c.B, TILE) / TILE, tk = ct_up(c.M, TILE) / TILE;
+    const int tq = ct_up(c.B, TILE) / TILE, tk = ct_up(keys, TILE) / TILE;
     in_launches((u64)tq * tk, 256, [&](u64 first, u64 blocks) {
-        if (c.alternatives) hipLaunchKernelGGL((k_logprob_sums<TILE, DT, TERMS, true>), dim3((u32)blocks), dim3(256), 0, st, c, (u32)first, tq, tk);
-        else hipLaunchKernelGGL((k_logprob_sums<TILE, DT, TERMS, false>), dim3((u32)blocks), dim3(256), 0, st, c, (u32)first, tq, tk);
+        const dim3 grid((u32)blocks), block(256);
+        if constexpr (DT != DT_F32)
+            if (c.squares) {
+                if (c.alternatives) hipLaunchKernelGGL((k_logprob_sums<TILE, DT, TERMS, true, true>), grid, block, 0, st, c, (u32)first, tq, tk);
+                else hipLaunchKernelGGL((k_logprob_sums<TILE, DT, TERMS, false, true>), grid, block, 0, st, c, (u32)first, tq, tk);
+                return;
+            }
+        if (c.alternatives) hipLaunchKernelGGL((k_logprob_sums<TILE, DT, TERMS, true, false>), grid, block, 0, st, c, (u32)first, tq, tk);
+        else hipLaunchKernelGGL((k_logprob_sums<TILE, DT, TERMS, false, false>), grid, block, 0, st, c, (u32)first, tq, tk);
     });
 }
 
@@ -832,19 +912,35 @@ static void launch_logprob(LogprobPar &c, const LogprobPlan &plan, bool wide_few
     } else {
         const int Br = ct_up(c.B, CT_PAD), Mr = ct_up(c.M, CT_PAD), across = c.dp / 64;
         const bool keys = c.most_blocks == 0;       // not yet prepared
-        const int key_blocks = !keys ? 0 : Mr / 4 < CT_ROW_BLOCKS ? Mr / 4 : CT_ROW_BLOCKS, row_blocks = Br / CT_PAD < CT_ROW_BLOCKS ? Br / CT_PAD : CT_ROW_BLOCKS;
-        if (keys) c.most_blocks = key_blocks;
+        const int key_blocks = !keys || c.squares ? 0 : Mr / 4 < CT_ROW_BLOCKS ? Mr / 4 : CT_ROW_BLOCKS, row_blocks = Br / CT_PAD < CT_ROW_BLOCKS ? Br / CT_PAD : CT_ROW_BLOCKS;
+        if (keys) c.most_blocks = c.squares ? 4 : key_blocks;      // (with squares: one, which all tiles go into)
         if constexpr (DT == DT_F32)
             if (keys)
                 hipLaunchKernelGGL(k_contrast_centre<LogprobPar>, dim3((c.dp + 64 * CT_SAMPLES - 1) / (64 * CT_SAMPLES)), dim3(64 * CT_SAMPLES), 0, st, c);
-        in_launches((u64)(key_blocks + row_blocks) + (u64)((Br + (keys ? Mr : 0)) / 64) * across, 256, [&](u64 first, u64 blocks) {
-            hipLaunchKernelGGL((k_logprob_prepare<DT, WIDE>), dim3((u32)blocks), dim3(256), 0, st, c, (u32)first, key_blocks, row_blocks, Br / 64, across);
-        });
-        if constexpr (DT != DT_F32) {
-            if (plan.tiles.tile == 256) launch_sums<DT, 256, false>(c, st);
-            else launch_sums<DT, 128, false>(c, st);
-        } else if (plan.tiles.terms) launch_sums<DT, 128, true>(c, st);
-        else launch_sums<DT, 128, false>(c, st);
+        // keys' sides, queries' ids and copies of rows, by blocks
+        auto prepare = [&](const LogprobPar &p, int sides, int ids, int query_rows, int key_rows) {
+            in_launches((u64)(sides + ids) + (u64)((query_rows + key_rows) / 64) * across, 256, [&](u64 first, u64 blocks) {
+                hipLaunchKernelGGL((k_logprob_prepare<DT, WIDE>), dim3((u32)blocks), dim3(256), 0, st, p, (u32)first, sides, ids, query_rows / 64, across);
+            });
+        };
+        auto sums = [&](const LogprobPar &p, int keys_of_it) {
+            if constexpr (DT != DT_F32) {
+                if (plan.tiles.tile == 256) launch_sums<DT, 256, false>(p, keys_of_it, st);
+                else launch_sums<DT, 128, false>(p, keys_of_it, st);
+            } else if (plan.tiles.terms) launch_sums<DT, 128, true>(p, keys_of_it, st);
+            else launch_sums<DT, 128, false>(p, keys_of_it, st);
+        };
+        prepare(c, key_blocks, row_blocks, Br, keys && !c.keys_as_they_are ? Mr : 0);
+        if (!plan.copied) sums(c, c.M);
+        else
+            for (int key0 = 0; key0 < c.M; key0 += plan.key_rows) {
+                LogprobPar p = c;
+                p.key0 = key0;
+                p.k = plan.spare - (size_t)key0 * c.dp;     // rows go by the keys' numbers
+                const int rows = Mr - key0 < plan.key_rows ? Mr - key0 : plan.key_rows;
+                prepare(p, 0, 0, 0, rows);
+                sums(p, rows);
+            }
     }
 #define LP_LAUNCH(WAVES, BLOCKS, THREADS) \
     if (wide_few) hipLaunchKernelGGL((k_logprob_finish<DT, true, WAVES>), dim3(BLOCKS), dim3(THREADS), 0, st, c); \
@@ -872,7 +968,7 @@ extern "C" int rnnd_logprob(const void *Q, int64_t B, const void *K, int64_t M, 
     if (!std::isfinite(scale)) return RNND_ERR_BAD_PARAM;
     if (!B) return RNND_OK;
     LogprobPar c = {};
-    LogprobPlan plan;
+    LogprobPlan plan = {};
     c.Q = Q;
     c.K = K;
     c.target = target;
@@ -892,6 +988,7 @@ extern "C" int rnnd_logprob(const void *Q, int64_t B, const void *K, int64_t M, 
     if (!workspace) return RNND_ERR_NULL;
     if ((uintptr_t)workspace % 16) return RNND_ERR_BAD_PARAM;
     if (workspace_bytes < layout(c, plan, dtype, (char *)workspace)) return RNND_ERR_SCRATCH;
+    plan.copied = c.keys_as_they_are && (uintptr_t)K % 16;
     hipStream_t st = (hipStream_t)stream;
     const int vec = row_vec(d, Q, (int)size, K, (int)size);
     const bool wide_few = vec >= (dtype == RNND_F32 ? 4 : 8);

@@ -201,10 +201,10 @@ def test_float32_rows_far_from_the_origin(rn, far):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("B", [3, 33])
-def test_what_is_left_out_is_never_read_as_a_number(rn, B, dtype):
+@pytest.mark.parametrize("B,d", [(3, 40), (33, 40), (33, 64), (3, 64)])
+def test_what_is_left_out_is_never_read_as_a_number(rn, B, d, dtype):
     import torch
-    c = case(B, 500, 40, dtype, 12)
+    c = case(B, 500, d, dtype, 12)
     want = call(rn, c, 3.0, 8)
     gone = torch.from_numpy((c["key_ids"] < 0) | (c["key_bias"] == -np.inf)).cuda()
     c["K"][gone] = float("nan")
@@ -264,10 +264,11 @@ def test_tiles_of_256(rn):
     check(rn, case(300, 70_000, 392, "float16", 16), 3.0, 33)
 
 
-@pytest.mark.parametrize("B", [1, 40])
-def test_rows_that_are_not_aligned(rn, B):
+@pytest.mark.parametrize("B,M,d", [(1, 400, 64), (40, 400, 64), (300, 33_000, 64), (40, 400, 62)])
+def test_rows_that_are_not_aligned(rn, B, M, d):
+    """(Of 33,000 keys not all fit the room for copies at once.)"""
     import torch
-    c = case(B, 400, 64, "bfloat16", 17)
+    c = case(B, M, d, "bfloat16", 17)
     want = call(rn, c, 3.0, 7)
     for name in ("Q", "K"):
         room = torch.empty(c[name].numel() + 1, dtype=torch.bfloat16, device="cuda")
