@@ -683,6 +683,7 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_contrast_
         base[n] = side.base[at.in_col + n];
         id[n] = side.id[at.in_col + n];
     }
+    if constexpr (has_lists<PAR>()) __syncthreads();        // all have read their operands
     // four rows at a time without a branch, so that their chains of instructions overlap; lane l of 16 keeps the rows l, l + 16
     float keep_top[N / 4], keep_sum[N / 4];
 #pragma unroll
@@ -693,7 +694,7 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_contrast_
 #pragma unroll
             for (int n = 0; n < N; ++n) s[r][n] = fmaf(acc[m][n][r], c.c1, base[n]);
         leave_out(side, at.in_row + m * 4, id, s);
-        if constexpr (has_lists<PAR>()) take_listed(std::true_type(), c, lists, tr * TILE, at.in_row + m * 4, at.in_col, s);
+        if constexpr (has_lists<PAR>()) take_listed(std::true_type(), c, lists, (float *)&lds, tr * TILE, at.in_row + m * 4, at.in_col, s);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             top[r] = s[r][0];
@@ -719,6 +720,7 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_contrast_
 #pragma unroll
     for (int h = 0; h < N / 4; ++h)
         c.part[(size_t)(at.row + h * 16 + (threadIdx.x & 15)) * c.parts_k + at.half_c] = make_float2(keep_top[h], keep_sum[h]);
+    if constexpr (has_lists<PAR>()) write_listed(c, lists, (const float *)&lds, tr * TILE, tc);
 }
 
 // (largest, sum) of two parts; a NaN in either stays
@@ -772,7 +774,7 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_contrast_
 #pragma unroll
                     for (int n = 0; n < N; ++n) logit[r][n] = fmaf(acc[pair * 2 + r8 / 4][n][r], c.c1, base[n]);
                 leave_out(side, at.in_row + pair * 8 + r8, id, logit);
-                if constexpr (has_lists<PAR>()) take_listed(std::false_type(), c, lists, tr * TILE, at.in_row + pair * 8 + r8, at.in_col, logit);
+                if constexpr (has_lists<PAR>()) take_listed(std::false_type(), c, lists, nullptr, tr * TILE, at.in_row + pair * 8 + r8, at.in_col, logit);
             }
             const float2 info = side.row_g[at.in_row + pair * 8 + r8];
 #pragma unroll

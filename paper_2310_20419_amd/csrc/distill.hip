@@ -31,7 +31,6 @@ struct DistillPar : ContrastPar {
     unsigned char *list_at;     // [B padded][tiles_k + 1] place of a tile's first key; of the end
     u32 *marks;                 // [M][words] the queries that list a key
     int words;
-    int *count;                 // [M] how many they are
 };
 
 __device__ __forceinline__ bool entry_counts(const DistillPar &c, int i, int e)
@@ -52,6 +51,7 @@ template <> constexpr bool has_lists<DistillPar>() { return true; }
 
 template <int TILE> struct ListLds<TILE, DistillPar> {
     u32 bits[TILE * TILE / 32];
+    u32 cols[TILE];                             // of the row's first four keys of this tile, a byte each
     unsigned char first[TILE], count[TILE];     // place of the row's first key of this tile in its list, and how many they are
 };
 
@@ -68,10 +68,13 @@ __device__ __forceinline__ void load_lists(const DistillPar &c, ListLds<TILE, Di
     lists.first[t] = (unsigned char)first;
     lists.count[t] = (unsigned char)n;
     const int *keys = &c.list_key[(size_t)(row0 + t) * c.entries + first];
+    u32 cols = 0;
     for (int e = 0; e < n; ++e) {
         const int col = keys[e] - tile_c * TILE;
         atomicOr(&lists.bits[(t * TILE + col) >> 5], 1u << (col & 31));
+        if (e < 4) cols |= (u32)col << (8 * e);
     }
+    lists.cols[t] = cols;
 }
 
 template <int TILE>
@@ -90,9 +93,12 @@ __device__ __forceinline__ int marks_before(const ListLds<TILE, DistillPar> &lis
     return n;
 }
 
-// Four rows' logits: those of listed keys become -infinity, and are written out before
+// Four rows' logits: those of listed keys become -infinity.  WRITE: the first of a lane's N columns goes to `room` (LDS, a place for each row and lane of
+// the 32 that share it), from where write_listed() takes it; others, which are rare, go to their place at once.  (Finding that place for
+// every listed key here held the wavefront up: 8,192 x 16,384 x 768, lists of 32, 366 us for the logits and their sums.)
 template <bool WRITE, int TILE, int N>
-__device__ __forceinline__ void take_listed(std::integral_constant<bool, WRITE>, const DistillPar &c, const ListLds<TILE, DistillPar> &lists, int row0, int row, int col, float (&s)[4][N])
+__device__ __forceinline__ void take_listed(std::integral_constant<bool, WRITE>, const DistillPar &c, const ListLds<TILE, DistillPar> &lists, float *room,
+                                            int row0, int row, int col, float (&s)[4][N])
 {
     u32 marks[4], any = 0;
 #pragma unroll
@@ -101,15 +107,38 @@ __device__ __forceinline__ void take_listed(std::integral_constant<bool, WRITE>,
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         if constexpr (WRITE) {
-            if (marks[r]) {
-                float *to = &c.list_s[(size_t)(row0 + row + r) * c.entries + lists.first[row + r] + marks_before(lists, row + r, col)];
+            const u32 more = marks[r] & (marks[r] - 1);
+            if (__any(more)) {
+                if (more) {
+                    float *to = &c.list_s[(size_t)(row0 + row + r) * c.entries + lists.first[row + r] + marks_before(lists, row + r, col)];
 #pragma unroll
-                for (int n = 0; n < N; ++n)
-                    if (marks[r] >> n & 1) *to++ = s[r][n];
+                    for (int n = 0; n < N; ++n)
+                        if (marks[r] >> n & 1) *to++ = s[r][n];
+                }
             }
+            float first = s[r][N - 1];
+#pragma unroll
+            for (int n = N - 2; n >= 0; --n) first = marks[r] >> n & 1 ? s[r][n] : first;
+            if (marks[r]) room[(row + r) * 32 + col / N] = first;
         }
 #pragma unroll
         for (int n = 0; n < N; ++n) s[r][n] = marks[r] >> n & 1 ? -INFINITY : s[r][n];
+    }
+}
+
+template <int TILE>
+__device__ __forceinline__ void write_listed(const DistillPar &c, const ListLds<TILE, DistillPar> &lists, const float *room, int row0, int tile_c)
+{
+    constexpr int N = TILE / 32;
+    __syncthreads();
+    const int t = threadIdx.x;
+    if (t >= TILE) return;
+    const size_t from = (size_t)(row0 + t) * c.entries + lists.first[t];
+    const int n = lists.count[t];
+    const u32 cols = lists.cols[t];
+    for (int e = 0; e < n; ++e) {
+        const int col = e < 4 ? (int)(cols >> (8 * e) & 0xFF) : c.list_key[from + e] - tile_c * TILE;
+        if (!(marks_at(lists, t, col & ~(N - 1)) & ((1u << (col & (N - 1))) - 1))) c.list_s[from + e] = room[t * 32 + col / N];
     }
 }
 
@@ -203,7 +232,6 @@ __global__ __launch_bounds__(256) void k_distill_prepare(DistillPar c, u32 first
         for (int at = block * 4 + wave; at < ct_up(c.M, CT_PAD); at += key_blocks * 4) {
             key_side<DT, WIDE>(c, at, lane);
             if (!c.dK || at >= c.M) continue;
-            if (lane == 0) c.count[at] = 0;
             for (int t = lane; t < c.words; t += 64) c.marks[(size_t)at * c.words + t] = 0;
         }
         return;
@@ -282,7 +310,6 @@ __global__ __launch_bounds__(256) void k_distill_loss(DistillPar c, int row_bloc
         c.list_g[(size_t)i * c.entries + at] = w * (e[r] / total - p[r]);
         const int j = c.list_key[(size_t)i * c.entries + at];
         atomicOr(&c.marks[(size_t)j * c.words + (i >> 5)], 1u << (i & 31));
-        atomicAdd(&c.count[j], 1);
     }
     loss = wave_sum(loss);
     if (lane) return;
@@ -296,56 +323,68 @@ __global__ __launch_bounds__(256) void k_distill_loss(DistillPar c, int row_bloc
 }
 
 // ------------------------------------------------------------------------------------------------ joining the gradients' parts
-// A wavefront per row: the listed terms, four coordinates a lane and DS_WIDE of these at a time.  A key that more than DS_SHARED queries list is
-// summed by the whole block, a part of the queries to each wavefront, and their sums are added in order.  The rows of a block lie gridDim.x
+// A wavefront per row, queries first: the listed terms, four coordinates a lane and H of these at a time.  A key that more than DS_SHARED queries
+// list is summed by the whole block, a part of the queries to each wavefront, and their sums are added in order.  The keys of a block lie
 // apart, so that neighbouring keys of this kind are those of different blocks.
-#define DS_FINISH 16            // wavefronts of a block
+#define DS_FINISH 8             // wavefronts of a block
 #define DS_SHARED 128
-#define DS_WIDE 4
 #define DS_RUN 64               // words of marks looked at together, one for each lane; by a whole block fewer, so that all its wavefronts have some
-#define DS_RUN_SHARED 4
+#define DS_RUN_SHARED 4         // (no more than DS_SHARED queries)
 #define DS_ROWS 4               // rows on the way
 struct KeyLds {
-    unsigned short list[DS_FINISH][DS_RUN * 32];
+    unsigned short list[DS_FINISH][DS_SHARED];
     f32x4 part[DS_FINISH][64];
+    u32 shared;                 // wavefronts whose keys these are
 };
 
-typedef float Sums[DS_WIDE][4];
-
 // Adds g (row - x) of n entries; lane e holds entry e: its row's number and its g.  e0: the first coordinate; x: the row of the sum.
-template <int DT, bool WIDE>
-__device__ __forceinline__ void add_terms(const DistillPar &c, const void *rows, int e0, const Sums &x, int number, float g, int n, int lane, Sums &sum)
+template <int DT, bool WIDE, int H>
+__device__ __forceinline__ void add_terms(const DistillPar &c, const void *rows, int e0, const float (&x)[H][4], int number, float g, int n, int lane,
+                                          float (&sum)[H][4])
 {
+    typedef typename RowType<DT>::T T;
     for (int j = 0; j < n; j += DS_ROWS) {
+        Pack<DT, 4> packs[DS_ROWS][H];
 #pragma unroll
-        for (int h = 0; h < DS_WIDE; ++h) {
-            const int e = e0 + h * 256 + lane * 4;
-            if (e >= c.d) continue;
-            float y[DS_ROWS][4];
+        for (int r = 0; r < DS_ROWS; ++r) {
+            const T *row = (const T *)rows + (size_t)__builtin_amdgcn_readlane(number, j + r < n ? j + r : n - 1) * c.d;
 #pragma unroll
-            for (int r = 0; r < DS_ROWS; ++r) load4<DT, WIDE>(rows, __builtin_amdgcn_readlane(number, j + r < n ? j + r : n - 1), c.d, e, y[r]);
+            for (int h = 0; h < H; ++h) {
+                const int e = e0 + h * 256 + lane * 4, from = e < c.d ? e : 0;      // (what lies behind the row is not stored)
+                if constexpr (WIDE) packs[r][h] = load_pack<DT, 4>(row, from);
+                else
 #pragma unroll
-            for (int r = 0; r < DS_ROWS; ++r) {
-                const float own = j + r < n ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), j + r < n ? j + r : n - 1)) : 0.0f;
+                    for (int k = 0; k < 4; ++k) packs[r][h].v[k] = from + k < c.d ? row[from + k] : (T)0.0f;
+            }
+        }
 #pragma unroll
-                for (int k = 0; k < 4; ++k) sum[h][k] = fmaf(own, y[r][k] - x[h][k], sum[h][k]);
+        for (int r = 0; r < DS_ROWS; ++r) {
+            const float own = j + r < n ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), j + r < n ? j + r : n - 1)) : 0.0f;
+#pragma unroll
+            for (int h = 0; h < H; ++h) {
+                float y[4];
+                unpack<DT, 4>(packs[r][h], y);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum[h][k] = fmaf(own, y[k] - x[h][k], sum[h][k]);
             }
         }
     }
 }
 
-// Terms of the queries that list key j, of the runs of RUN words of marks first, first + step, ..; list: the wavefront's own.
-template <int RUN, int DT, bool WIDE>
-__device__ __forceinline__ void add_queries(const DistillPar &c, int j, int e0, const Sums &x, int first, int step, unsigned short *list, int lane, Sums &sum)
+// Terms of the queries that list key j, of the runs of `words` words of marks first, first + step, ..; list: the wavefront's own.
+template <int DT, bool WIDE, int H>
+__device__ __forceinline__ void add_queries(const DistillPar &c, int j, int e0, const float (&x)[H][4], int words, int first, int step, unsigned short *list,
+                                            int lane, float (&sum)[H][4])
 {
-    for (int run = first; run * RUN < c.words; run += step) {
-        const int at = run * RUN + lane;
-        u32 marks = lane < RUN && at < c.words ? c.marks[(size_t)j * c.words + at] : 0;
+    for (int run = first; run * words < c.words; run += step) {
+        const int at = run * words + lane;
+        u32 marks = lane < words && at < c.words ? c.marks[(size_t)j * c.words + at] : 0;
         const int here = (int)__popc(marks), upto = inclusive(here, lane), n = __builtin_amdgcn_readlane(upto, 63);
+        if (!n) continue;
         for (int to = upto - here; marks; marks &= marks - 1) list[to++] = (unsigned short)(lane * 32 + __builtin_ctz(marks));
         wave_sync();
         for (int t = 0; t < n; t += 64) {
-            const int i = t + lane < n ? run * RUN * 32 + list[t + lane] : -1;
+            const int i = t + lane < n ? run * words * 32 + list[t + lane] : -1;
             float g = 0.0f;
             if (i >= 0) {
                 const int *keys = &c.list_key[(size_t)i * c.entries];
@@ -357,26 +396,27 @@ __device__ __forceinline__ void add_queries(const DistillPar &c, int j, int e0, 
                 }
                 g = c.list_g[(size_t)i * c.entries + lo];
             }
-            add_terms<DT, WIDE>(c, c.Q, e0, x, i, g, n - t < 64 ? n - t : 64, lane, sum);
+            add_terms<DT, WIDE, H>(c, c.Q, e0, x, i, g, n - t < 64 ? n - t : 64, lane, sum);
         }
         wave_sync();
     }
 }
 
-template <int DT, bool WIDE>
-__device__ __forceinline__ void load_row(const DistillPar &c, const void *rows, int row, int e0, int lane, Sums &x)
+template <int DT, bool WIDE, int H>
+__device__ __forceinline__ void load_row(const DistillPar &c, const void *rows, int row, int e0, int lane, float (&x)[H][4])
 {
 #pragma unroll
-    for (int h = 0; h < DS_WIDE; ++h)
-        if (e0 + h * 256 + lane * 4 < c.d) load4<DT, WIDE>(rows, row, c.d, e0 + h * 256 + lane * 4, x[h]);
+    for (int h = 0; h < H; ++h) {
+        const int e = e0 + h * 256 + lane * 4;
+        load4<DT, WIDE>(rows, row, c.d, e < c.d ? e : 0, x[h]);
+    }
 }
 // The parts of the products and the listed terms, rounded
-template <int DT, bool WIDE>
-__device__ __forceinline__ void finish_row(const DistillPar &c, int at, int e0, int lane, const Sums &sum)
+template <int DT, bool WIDE, int H>
+__device__ __forceinline__ void finish_row(const DistillPar &c, const GradRow<DT, WIDE> &mine, int e0, int lane, const float (&sum)[H][4])
 {
-    const GradRow<DT, WIDE> mine(c, at);
 #pragma unroll
-    for (int h = 0; h < DS_WIDE; ++h) {
+    for (int h = 0; h < H; ++h) {
         const int e = e0 + h * 256 + lane * 4;
         if (e >= c.d) continue;
         float a[4] = {}, own[4];
@@ -388,52 +428,94 @@ __device__ __forceinline__ void finish_row(const DistillPar &c, int at, int e0, 
 }
 
 template <int DT, bool WIDE>
-__global__ __launch_bounds__(64 * DS_FINISH, 4) void k_distill_finish(DistillPar c)
+__device__ __forceinline__ void no_gradient(const DistillPar &c, void *to, int row, int lane)
+{
+    const float zero[4] = {};
+    for (int e = lane * 4; e < c.d; e += 256) store4<DT, WIDE>(to, row, c.d, e, zero);
+}
+
+// how many queries list a key
+__device__ __forceinline__ int queries_of(const DistillPar &c, int j, int lane)
+{
+    const u32 *marks = &c.marks[(size_t)j * c.words];
+    int n = 0;
+    for (int t = lane; t < c.words; t += 256) {
+        u32 m[4];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) m[h] = t + h * 64 < c.words ? marks[t + h * 64] : 0;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) n += (int)__popc(m[h]);
+    }
+#pragma unroll
+    for (int s = 32; s; s >>= 1) n += __shfl_xor(n, s);
+    return __builtin_amdgcn_readfirstlane(n);
+}
+
+template <int DT, bool WIDE, int H>
+__global__ __launch_bounds__(64 * DS_FINISH) void k_distill_finish(DistillPar c, int query_blocks)
 {
     __shared__ KeyLds lds;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), total = c.B + c.M;
-    const int at = (int)(blockIdx.x + wave * gridDim.x), lanes_row = (int)(blockIdx.x + (lane & (DS_FINISH - 1)) * gridDim.x);
-    const u64 shared = __ballot(lane < DS_FINISH && lanes_row >= c.B && lanes_row < total && c.count[lanes_row - c.B] > DS_SHARED);
-    const bool keys = at >= c.B;
-    const int row = keys ? at - c.B : at, n = at < total && !keys ? c.list_at[(size_t)row * (c.tiles_k + 1) + c.tiles_k] : 0;
-    if (at >= total || shared >> wave & 1) {
-    } else if (keys ? key_gone(c, row) : !n) {
-        const float zero[4] = {};
-        for (int e = lane * 4; e < c.d; e += 256) store4<DT, WIDE>(keys ? c.dK : c.dQ, row, c.d, e, zero);
-    } else
-        for (int e0 = 0; e0 < c.d; e0 += 256 * DS_WIDE) {
-            Sums x = {}, sum = {};
-            load_row<DT, WIDE>(c, keys ? c.K : c.Q, row, e0, lane, x);
-            if (keys) {
-                if (c.count[row]) add_queries<DS_RUN, DT, WIDE>(c, row, e0, x, 0, 1, lds.list[wave], lane, sum);
-            } else
-                for (int t = 0; t < n; t += 64) {
-                    const size_t e = (size_t)row * c.entries + t + lane;
-                    const bool in = t + lane < n;
-                    add_terms<DT, WIDE>(c, c.K, e0, x, in ? c.list_key[e] : 0, in ? c.list_g[e] : 0.0f, n - t < 64 ? n - t : 64, lane, sum);
-                }
-            finish_row<DT, WIDE>(c, at, e0, lane, sum);
-        }
-    if (!shared) return;        // a whole block
-    __syncthreads();
-    for (u64 left = shared; left; left &= left - 1) {
-        const int key = (int)(blockIdx.x + __builtin_ctzll(left) * gridDim.x) - c.B;
-        for (int e0 = 0; e0 < c.d; e0 += 256 * DS_WIDE) {
-            Sums x = {}, sum = {};
-            load_row<DT, WIDE>(c, c.K, key, e0, lane, x);
-            add_queries<DS_RUN_SHARED, DT, WIDE>(c, key, e0, x, wave, DS_FINISH, lds.list[wave], lane, sum);
-#pragma unroll
-            for (int h = 0; h < DS_WIDE; ++h) {
-                if (e0 + h * 256 >= c.d) break;
-                lds.part[wave][lane] = (f32x4){sum[h][0], sum[h][1], sum[h][2], sum[h][3]};
-                __syncthreads();
-                if (wave == 0)
-                    for (int w = 1; w < DS_FINISH; ++w)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) sum[h][k] += lds.part[w][lane][k];
-                __syncthreads();
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if ((int)blockIdx.x < query_blocks) {
+        const int i = blockIdx.x * DS_FINISH + wave;
+        if (i >= c.B) return;
+        const int n = c.list_at[(size_t)i * (c.tiles_k + 1) + c.tiles_k];
+        if (!n) return no_gradient<DT, WIDE>(c, c.dQ, i, lane);
+        const GradRow<DT, WIDE> mine(c, i);
+        for (int e0 = 0; e0 < c.d; e0 += 256 * H) {
+            float x[H][4], sum[H][4] = {};
+            load_row<DT, WIDE, H>(c, c.Q, i, e0, lane, x);
+            for (int t = 0; t < n; t += 64) {
+                const size_t e = (size_t)i * c.entries + t + lane;
+                const bool on = t + lane < n;
+                add_terms<DT, WIDE, H>(c, c.K, e0, x, on ? c.list_key[e] : 0, on ? c.list_g[e] : 0.0f, n - t < 64 ? n - t : 64, lane, sum);
             }
-            if (wave == 0) finish_row<DT, WIDE>(c, key + c.B, e0, lane, sum);
+            finish_row<DT, WIDE, H>(c, mine, e0, lane, sum);
+        }
+        return;
+    }
+    const int first = blockIdx.x - query_blocks, apart = gridDim.x - query_blocks;
+    if (threadIdx.x == 0) lds.shared = 0;
+    __syncthreads();
+    // a key of the wavefront's own, then those of the block that are summed together
+    int j = first + wave * apart;
+    bool alone = false;
+    if (j < c.M) {
+        if (key_gone(c, j)) no_gradient<DT, WIDE>(c, c.dK, j, lane);
+        else if (queries_of(c, j, lane) <= DS_SHARED) alone = true;
+        else if (lane == 0) atomicOr(&lds.shared, 1u << wave);
+    }
+    u32 left = 0;
+    for (bool own = true;; own = false) {
+        if (!own) {
+            if (!left) break;
+            j = first + __builtin_ctz(left) * apart;
+            left &= left - 1;
+        }
+        if (!own || alone) {
+            const GradRow<DT, WIDE> mine(c, c.B + j);
+            for (int e0 = 0; e0 < c.d; e0 += 256 * H) {
+                float x[H][4], sum[H][4] = {};
+                load_row<DT, WIDE, H>(c, c.K, j, e0, lane, x);
+                add_queries<DT, WIDE, H>(c, j, e0, x, own ? DS_RUN : DS_RUN_SHARED, own ? 0 : wave, own ? 1 : DS_FINISH, lds.list[wave], lane, sum);
+                if (!own) {
+#pragma unroll
+                    for (int h = 0; h < H; ++h) {
+                        __syncthreads();
+                        lds.part[wave][lane] = (f32x4){sum[h][0], sum[h][1], sum[h][2], sum[h][3]};
+                        __syncthreads();
+                        for (int w = 1; wave == 0 && w < DS_FINISH; ++w)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) sum[h][k] += lds.part[w][lane][k];
+                    }
+                    if (wave) continue;
+                }
+                finish_row<DT, WIDE, H>(c, mine, e0, lane, sum);
+            }
+        }
+        if (own) {
+            __syncthreads();
+            left = lds.shared;
         }
     }
 }
@@ -453,7 +535,6 @@ static size_t layout(DistillPar &c, ContrastPlan &plan, int dtype, int want_grad
         if (want_grad) {
             c.words = (c.B + 31) / 32;
             take(c.marks, (size_t)c.M * c.words);
-            take(c.count, c.M);
         }
     });
 }
@@ -521,7 +602,11 @@ static void launch_distill(DistillPar &c, const ContrastPlan &plan, int want_gra
         else launch_grads<DT, 128>(c, st);
     } else
         launch_grads<DT, 128>(c, st);
-    hipLaunchKernelGGL((k_distill_finish<DT, WIDE>), dim3((c.B + c.M + DS_FINISH - 1) / DS_FINISH), dim3(64 * DS_FINISH), 0, st, c);
+    const int query_blocks = (c.B + DS_FINISH - 1) / DS_FINISH;
+    const dim3 grid(query_blocks + (c.M + DS_FINISH - 1) / DS_FINISH), block(64 * DS_FINISH);
+    if (c.d <= 256) hipLaunchKernelGGL((k_distill_finish<DT, WIDE, 1>), grid, block, 0, st, c, query_blocks);
+    else if (c.d <= 512) hipLaunchKernelGGL((k_distill_finish<DT, WIDE, 2>), grid, block, 0, st, c, query_blocks);
+    else hipLaunchKernelGGL((k_distill_finish<DT, WIDE, 3>), grid, block, 0, st, c, query_blocks);
 }
 
 extern "C" int rnnd_distill(const void *Q, int64_t B, const void *K, int64_t M, int32_t d, int dtype, int metric, const int32_t *teacher_ids,
