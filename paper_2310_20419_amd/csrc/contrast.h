@@ -589,8 +589,9 @@ template <int TILE> struct Place {
 
 // What the logits of a tile need besides the product, in LDS while its first loads are under way: behind it nothing else hides the
 // latency of loads from memory (one wavefront per SIMD).
-// A row leaves out few keys, so most rows leave out none of a tile's.  16,384 bits say which hashes the tile's keys have; a row
-// whose two ids are not among them needs no comparison (4 instructions of 14 for each logit).
+// A row leaves out few keys, so most rows leave out none of a tile's.  16,384 bits say which hashes the tile's keys have, two of each; a row
+// whose two ids are not among them needs no comparison (4 instructions of 14 for each logit; one hash alone is there by chance for one
+// of 40 rows, and 16 rows are looked at together).
 #define CT_HASH 14
 template <int TILE> struct SideLds {
     int2 row_id[TILE];
@@ -604,6 +605,8 @@ template <int TILE> struct SideLds {
 template <typename PAR> constexpr bool has_lists() { return false; }
 template <int TILE, typename PAR> struct ListLds {};
 __device__ __forceinline__ u32 id_hash(int id) { return (u32)id * 0x9E3779B1u >> (32 - CT_HASH); }
+__device__ __forceinline__ u32 id_hash2(int id) { return (u32)id * 0x85EBCA77u >> (32 - CT_HASH); }
+__device__ __forceinline__ u32 bit_at(const u32 *bits, u32 at) { return bits[at >> 5] >> (at & 31) & 1; }
 // PREPARED: by key_side(); else the base is without -scale |k|^2.
 template <int TILE, bool PREPARED> __device__ __forceinline__ void load_side(const ContrastPar &c, SideLds<TILE> &side, int row0, int col0)
 {
@@ -626,9 +629,13 @@ template <int TILE, bool PREPARED> __device__ __forceinline__ void load_side(con
         }
     }
     __syncthreads();
-    if (t < TILE && id >= 0) atomicOr(&side.seen[id_hash(id) >> 5], 1u << (id_hash(id) & 31));
+    if (t < TILE && id >= 0) {
+        atomicOr(&side.seen[id_hash(id) >> 5], 1u << (id_hash(id) & 31));
+        atomicOr(&side.seen[id_hash2(id) >> 5], 1u << (id_hash2(id) & 31));
+    }
     __syncthreads();
-    if (t < TILE) side.maybe[t] = (side.seen[id_hash(out.x) >> 5] >> (id_hash(out.x) & 31) | side.seen[id_hash(out.y) >> 5] >> (id_hash(out.y) & 31)) & 1;
+    if (t < TILE)
+        side.maybe[t] = (bit_at(side.seen, id_hash(out.x)) & bit_at(side.seen, id_hash2(out.x))) | (bit_at(side.seen, id_hash(out.y)) & bit_at(side.seen, id_hash2(out.y)));
 }
 
 // q k' of a tile, its side tables read meanwhile

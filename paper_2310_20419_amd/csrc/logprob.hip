@@ -86,12 +86,27 @@ __global__ __launch_bounds__(256) void k_logprob_prepare(LogprobPar c, u32 first
 }
 
 // ------------------------------------------------------------------------------------------------ the logits by tiles
+// Larger of two, NaN if one is: one instruction (fmaxf() first makes sure that both are no signalling NaN, two more where they come from bits)
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+// over the 16 lanes that share a row
+template <int R> __device__ __forceinline__ void row16_larger(float (&v)[R])
+{
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = larger(v[r], xor_lane_f32<1>(v[r]));
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = larger(v[r], xor_lane_f32<2>(v[r]));
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = larger(v[r], xor_lane_f32<7>(v[r]));
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = larger(v[r], xor_lane_f32<15>(v[r]));
+}
+
 // Puts a logit into the largest two of its group.
 __device__ __forceinline__ void into_group(float &most, float &second, float s, int n, int group)
 {
     const float x = __uint_as_float((__float_as_uint(s) & ~(u32)(group - 1)) | (u32)n);
     second = __builtin_amdgcn_fmed3f(most, second, x);      // most >= second
-    most = fmaxf(most, x);
+    most = larger(most, x);
 }
 
 // Sums of squares of what the product multiplies: |k|^2 without another pass over the keys.  (The dot product instruction of bfloat16 pairs rounds
@@ -170,7 +185,7 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_logprob_s
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int n = 0; n < N; ++n) s[r][n] = __builtin_elementwise_maximum(fmaf(acc[m][n][r], c.c1, base[n]), LP_NONE);
+            for (int n = 0; n < N; ++n) s[r][n] = larger(fmaf(acc[m][n][r], c.c1, base[n]), LP_NONE);
         leave_out(side, at.in_row + m * 4, id, s, LP_NONE);
         if constexpr (DT != DT_F32)
             if (any_odd)
@@ -189,10 +204,10 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_logprob_s
             } else {
                 top[r] = s[r][0];
 #pragma unroll
-                for (int n = 1; n < N; ++n) top[r] = fmaxf(top[r], s[r][n]);
+                for (int n = 1; n < N; ++n) top[r] = larger(top[r], s[r][n]);
             }
         }
-        row16_max(top);
+        row16_larger(top);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const float ref = top[r] > LP_NONE * 0.99f ? top[r] : 0.0f;
