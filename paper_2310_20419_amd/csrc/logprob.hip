@@ -954,7 +954,7 @@ static void launch_logprob(LogprobPar &c, const LogprobPlan &plan, bool wide_few
                 p.k = plan.spare - (size_t)key0 * c.dp;     // rows go by the keys' numbers
                 const int rows = Mr - key0 < plan.key_rows ? Mr - key0 : plan.key_rows;
                 prepare(p, 0, 0, 0, rows);
-                sums(p, rows);
+                sums(p, c.M - key0 < rows ? c.M - key0 : rows);     // (tiles behind the last key have no place)
             }
     }
 #define LP_LAUNCH(WAVES, BLOCKS, THREADS) \
