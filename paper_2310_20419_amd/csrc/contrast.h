@@ -272,7 +272,11 @@ __device__ __forceinline__ void contrast_copy(const PAR &c, int tile_r, int c0, 
 // Rows of ld elements, ld a multiple of CT_K; rows behind the last are zeros (copies are padded to whole tiles, so they have none).
 struct Operand { const half_t *p; size_t plane; int ld, rows = 0x7FFFFFFF; };
 
-template <int TILE> struct ProductLds { half_t a[2][TILE * CT_K], b[2][TILE * CT_K]; };
+// One step.  The two that a kernel has are variables of their own: the compiler lets reads of one go past loads into the other, but would have
+// reads of a variable wait for all loads into it (in the middle of every step, for those just sent off).
+template <int TILE> struct ProductLds { half_t a[TILE * CT_K], b[TILE * CT_K]; };
+struct NoLds {};
+#define CT_TOUCH 4          // steps ahead (see product())
 
 template <int TILE> __device__ __forceinline__ int row_at(int p)      // row of A that stands at place p
 {
@@ -288,10 +292,13 @@ template <int TILE> __device__ __forceinline__ int col_at(int p)      // row of 
 }
 
 // 16 bytes of every lane from base + v + at (bytes; `bytes` of them may be read) to 1 KB of LDS, in the lanes' order
+template <int SIZE = 16>
 __device__ __forceinline__ void to_lds(const half_t *base, int bytes, half_t *lds, int v, int at)
 {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)base, 0, bytes, 0x00027000),
-                                             (__attribute__((address_space(3))) void *)lds, 16, v, at, 0, 0);
+    const auto from = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, bytes, 0x00027000);
+    const auto to = (__attribute__((address_space(3))) void *)lds;
+    if constexpr (SIZE == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 16, v, at, 0, 0);
+    else __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 4, v, at, 0, 0);
 }
 
 // With tiles of 256 the results take all 256 accumulation registers.  Left to itself the compiler moves some of them to and fro (180
@@ -315,11 +322,15 @@ template <int N> struct Half { us8 a[N], b[N]; };      // what half a step multi
 struct Nothing { __device__ __forceinline__ void operator()(const us8 &, int) const {} };
 
 // `meanwhile` runs while the first loads are under way; what it leaves in LDS is there behind the product.  also(b, j) is given all that is
-// multiplied of B: of the lane's column j, a quarter of every step.
-template <int TILE, int DT, typename F, typename G = Nothing>
+// multiplied of B: of the lane's column j, a quarter of every step.  TOUCH: B comes from memory, whose latency is more than the step that a load
+// has.  So every thread loads 4 bytes of a row some steps ahead, to nowhere (1 KB of LDS that nobody reads), and the step's own
+// loads find the row in L2.  It is the last load of a step, and the only one that is not waited for.
+template <int TILE, int DT, bool TOUCH = false, typename F, typename G = Nothing>
 __device__ __forceinline__ void product(const Operand &A, const Operand &B, int row_a, int row_b, int k_begin, int k_end,
-                                        ProductLds<TILE> &lds, f32x4 (&acc)[TILE / 32][TILE / 32], F meanwhile, G also = G())
+                                        ProductLds<TILE> &even, ProductLds<TILE> &odd, f32x4 (&acc)[TILE / 32][TILE / 32], F meanwhile, G also = G(),
+                                        half_t *nowhere = nullptr)
 {
+    static_assert(!TOUCH || (TILE == 256 && DT != DT_F32), "a row for each thread, one plane");
     constexpr int N = TILE / 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int per = (k_end - k_begin) / CT_K;
@@ -339,7 +350,7 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int 
     const half_t *pa = A.p + (size_t)row_a * A.ld, *pb = B.p + (size_t)row_b * B.ld;
     const int bytes_a = (A.rows - row_a < TILE ? A.rows - row_a : TILE) * A.ld * 2, bytes_b = (B.rows - row_b < TILE ? B.rows - row_b : TILE) * B.ld * 2;
     // 1 / N of a step's loads
-    auto fetch = [&](int s, int buf, int i) {
+    auto fetch = [&](int s, ProductLds<TILE> &lds, int i) {
         int kk = s;
         const half_t *qa = pa, *qb = pb;
         if (DT == DT_F32) {         // planes (0, 0) (0, 1) (1, 0) (1, 1) (0, 2) (2, 0)
@@ -349,15 +360,15 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int 
             qb += (pair == 1 || pair == 3 ? 1 : pair == 4 ? 2 : 0) * B.plane;
         }
         const int at = (k_begin + kk * CT_K) * 2, place = (wave * (TILE / 4) + i * 8) * CT_K;
-        to_lds(qa, bytes_a, &lds.a[buf][place], va[i], at);
-        to_lds(qb, bytes_b, &lds.b[buf][place], vb[i], at);
+        to_lds(qa, bytes_a, &lds.a[place], va[i], at);
+        to_lds(qb, bytes_b, &lds.b[place], vb[i], at);
     };
     const int ra0 = ((wave >> 1) * (TILE / 2) + (lane & 15)) * CT_K, rb0 = ((wave & 1) * (TILE / 2) + (lane & 15)) * CT_K;
     const int piece0 = ((lane >> 4) ^ (lane & 7)) * 8;
-    auto read = [&](Half<N> &f, int buf, int h, int i) {
+    auto read = [&](Half<N> &f, const ProductLds<TILE> &lds, int h, int i) {
         const int at = piece0 ^ (h * 32);
-        f.a[i] = *(const us8 *)&lds.a[buf][ra0 + i * 16 * CT_K + at];
-        f.b[i] = *(const us8 *)&lds.b[buf][rb0 + i * 16 * CT_K + at];
+        f.a[i] = *(const us8 *)&lds.a[ra0 + i * 16 * CT_K + at];
+        f.b[i] = *(const us8 *)&lds.b[rb0 + i * 16 * CT_K + at];
     };
     auto multiply = [&](const Half<N> &f, int i) {
 #pragma unroll
@@ -375,47 +386,68 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int 
     }
     Half<N> h0, h1;
 #pragma unroll
-    for (int i = 0; i < N; ++i) fetch(0, 0, i);
+    for (int i = 0; i < N; ++i) fetch(0, even, i);
+    const int touch_at = (int)threadIdx.x * B.ld * 2;
+    auto touch = [&](int s) {
+        if constexpr (TOUCH) to_lds<4>(pb, bytes_b, nowhere + wave * 128, touch_at, (k_begin + (s < steps ? s : steps - 1) * CT_K) * 2);
+    };
+    if (TOUCH)
+#pragma unroll
+        for (int s = 1; s < CT_TOUCH; ++s) touch(s);
     meanwhile();
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (steps > 1)
 #pragma unroll
-        for (int i = 0; i < N; ++i) fetch(1, 1, i);
+        for (int i = 0; i < N; ++i) fetch(1, odd, i);
+    touch(CT_TOUCH);
 #pragma unroll
-    for (int i = 0; i < N; ++i) read(h0, 0, 0, i);
+    for (int i = 0; i < N; ++i) read(h0, even, 0, i);
     // A wavefront issues in order: reads and loads in one lump would hold its matrix instructions back until they are accepted.  So
     // a few of them go before each N matrix instructions, the reads early enough to be there for the next half.
-    for (int s = 0; s + 1 < steps; ++s) {
+    auto step = [&](int s, ProductLds<TILE> &now, ProductLds<TILE> &other) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             if (i < N / 2) {
-                read(h1, s & 1, 1, 2 * i);
-                read(h1, s & 1, 1, 2 * i + 1);
+                read(h1, now, 1, 2 * i);
+                read(h1, now, 1, 2 * i + 1);
             }
             multiply(h0, i);
             also(h0.b[i], i);
             __builtin_amdgcn_sched_barrier(0);
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // the next step is there
-        __syncthreads();                                        // ... for all, and all have read this one
+        // the next step is there for all, and all have read this one
+        if constexpr (TOUCH) asm volatile("s_waitcnt vmcnt(1) lgkmcnt(0)" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
         const int next = s + 2 < steps ? s + 2 : s + 1;         // (the last one is read by nobody)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             if (i < N / 2) {
-                fetch(next, s & 1, 2 * i);
-                fetch(next, s & 1, 2 * i + 1);
+                fetch(next, now, 2 * i);
+                fetch(next, now, 2 * i + 1);
+                if (2 * i + 2 == N) touch(s + 1 + CT_TOUCH);
             } else {
-                read(h0, (s + 1) & 1, 0, 2 * i - N);
-                read(h0, (s + 1) & 1, 0, 2 * i - N + 1);
+                read(h0, other, 0, 2 * i - N);
+                read(h0, other, 0, 2 * i - N + 1);
             }
             multiply(h1, i);
             also(h1.b[i], i);
             __builtin_amdgcn_sched_barrier(0);
         }
+    };
+    for (int s = 0; s + 1 < steps; s += 2) {
+        step(s, even, odd);
+        if (s + 2 < steps) step(s + 1, odd, even);
     }
+    if (steps & 1) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) read(h1, (steps - 1) & 1, 1, i);
+        for (int i = 0; i < N; ++i) read(h1, even, 1, i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) read(h1, odd, 1, i);
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         multiply(h0, i);
@@ -639,9 +671,9 @@ template <int TILE, bool PREPARED> __device__ __forceinline__ void load_side(con
 }
 
 // q k' of a tile, its side tables read meanwhile
-template <int TILE, int DT, bool TERMS, bool PREPARED = true, typename LDS, typename F, typename G = Nothing>
-__device__ __forceinline__ void logit_product(const ContrastPar &c, int tr, int tc, LDS &lds, SideLds<TILE> &side, f32x4 (&acc)[TILE / 32][TILE / 32], F lists,
-                                              G also = G())
+template <int TILE, int DT, bool TERMS, bool PREPARED = true, bool TOUCH = false, typename LDS, typename LDS2, typename F, typename G = Nothing>
+__device__ __forceinline__ void logit_product(const ContrastPar &c, int tr, int tc, LDS &lds, LDS2 &lds2, SideLds<TILE> &side, f32x4 (&acc)[TILE / 32][TILE / 32], F lists,
+                                              G also = G(), half_t *nowhere = nullptr)
 {
     const Operand q = {c.q, c.plane_q, c.dp}, k = !c.k ? Operand{(const half_t *)c.K, 0, c.d, c.M} : Operand{c.k, c.plane_k, c.dp};
     const auto tables = [&]() {
@@ -649,7 +681,7 @@ __device__ __forceinline__ void logit_product(const ContrastPar &c, int tr, int 
         lists();
     };
     if constexpr (TERMS) product_of_terms(q, k, tr * TILE, tc * TILE, 0, c.dp, lds, acc, tables);
-    else product<TILE, DT>(q, k, tr * TILE, tc * TILE, 0, c.dp, lds, acc, tables, also);
+    else product<TILE, DT, TOUCH>(q, k, tr * TILE, tc * TILE, 0, c.dp, lds, lds2, acc, tables, also, nowhere);
 }
 
 // Logits of the keys that rows leave out become -infinity, or what stands for it; nothing to do for most rows.
@@ -674,12 +706,13 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_contrast_
 {
     constexpr int N = TILE / 32;
     __shared__ typename std::conditional<TERMS, TermsLds, ProductLds<TILE>>::type lds;
+    __shared__ typename std::conditional<TERMS, NoLds, ProductLds<TILE>>::type lds2;
     __shared__ SideLds<TILE> side;
     __shared__ ListLds<TILE, PAR> lists;
     f32x4 acc[N][N];
     int tr, tc;
     tile_of((int)(first + blockIdx.x), tiles_q, tiles_k, tr, tc);
-    logit_product<TILE, DT, TERMS>(c, tr, tc, lds, side, acc, [&]() {
+    logit_product<TILE, DT, TERMS>(c, tr, tc, lds, lds2, side, acc, [&]() {
         if constexpr (has_lists<PAR>()) load_lists(c, lists, tr * TILE, tc);
     });
     const Place<TILE> at(tr, tc);
@@ -745,12 +778,13 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_contrast_
 {
     constexpr int N = TILE / 32, PLANES = planes_of<DT>();
     __shared__ typename std::conditional<TERMS, TermsLds, ProductLds<TILE>>::type lds;
+    __shared__ typename std::conditional<TERMS, NoLds, ProductLds<TILE>>::type lds2;
     __shared__ SideLds<TILE> side;
     __shared__ ListLds<TILE, PAR> lists;
     f32x4 acc[N][N];
     int tr, tc;
     tile_of((int)(first + blockIdx.x), tiles_q, tiles_k, tr, tc);
-    logit_product<TILE, DT, TERMS>(c, tr, tc, lds, side, acc, [&]() {
+    logit_product<TILE, DT, TERMS>(c, tr, tc, lds, lds2, side, acc, [&]() {
         if constexpr (has_lists<PAR>()) load_lists(c, lists, tr * TILE, tc);
     });
     const Place<TILE> at(tr, tc);
@@ -763,7 +797,9 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_contrast_
     }
     constexpr int H = TILE / 2;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    half_t *turn = (half_t *)&lds + wave * H * H * (PLANES == 3 ? 2 : 1);
+    constexpr int room = H * H * (PLANES == 3 ? 2 : 1), fit = sizeof(lds) / 2 / room;       // of a wavefront; how many go into the first
+    half_t *turn = wave < fit ? (half_t *)&lds + wave * room : (half_t *)&lds2 + (wave - fit) * room;
+    static_assert(fit >= 4 || sizeof(lds2) / 2 / room >= 4 - fit, "every wavefront has its room");
     us8 third[PLANES == 3 ? N / 2 : 1][N];
     auto turn_at = [&](int n, int pair) { return ((lane & 15) * N + n) * H + (((lane >> 4) * (N / 2) + pair) ^ (lane & 7)) * 8; };
     __syncthreads();        // all have read their operands
@@ -861,6 +897,7 @@ __global__ __launch_bounds__(256, TILE == 256 || DT == DT_F32 ? 1 : 2) void k_co
 {
     constexpr int N = TILE / 32;
     __shared__ typename std::conditional<DT == DT_F32, TermsLds, ProductLds<TILE>>::type lds;
+    __shared__ typename std::conditional<DT == DT_F32, NoLds, ProductLds<TILE>>::type lds2;
     f32x4 acc[N][N];
     const int of_q = tiles_q * tiles_d * c.splits_q;
     const int block = (int)(first + blockIdx.x);
@@ -874,7 +911,7 @@ __global__ __launch_bounds__(256, TILE == 256 || DT == DT_F32 ? 1 : 2) void k_co
     const Operand a = keys ? Operand{c.gt, c.plane_gt, c.ld_gt} : Operand{c.g, c.plane_g, c.ld_g};
     const Operand b = keys ? Operand{c.qt, c.plane_qt, c.Bp} : Operand{c.kt, c.plane_kt, c.Mp};
     if constexpr (DT == DT_F32) product_of_terms(a, b, tr * TILE, tc * TILE, k0, k1, lds, acc, []() {});
-    else product<TILE, DT>(a, b, tr * TILE, tc * TILE, k0, k1, lds, acc, []() {});
+    else product<TILE, DT>(a, b, tr * TILE, tc * TILE, k0, k1, lds, lds2, acc, []() {});
     const Place<TILE> at(tr, tc);
     const size_t rows = (size_t)((keys ? c.M : c.B) + CT_PAD - 1) / CT_PAD * CT_PAD;
     float *out = (keys ? c.acc_k : c.acc_q) + (size_t)split * rows * c.dr;
