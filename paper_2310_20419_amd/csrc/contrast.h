@@ -276,7 +276,6 @@ struct Operand { const half_t *p; size_t plane; int ld, rows = 0x7FFFFFFF; };
 // reads of a variable wait for all loads into it (in the middle of every step, for those just sent off).
 template <int TILE> struct ProductLds { half_t a[TILE * CT_K], b[TILE * CT_K]; };
 struct NoLds {};
-#define CT_TOUCH 4          // steps ahead (see product())
 
 template <int TILE> __device__ __forceinline__ int row_at(int p)      // row of A that stands at place p
 {
@@ -292,13 +291,10 @@ template <int TILE> __device__ __forceinline__ int col_at(int p)      // row of 
 }
 
 // 16 bytes of every lane from base + v + at (bytes; `bytes` of them may be read) to 1 KB of LDS, in the lanes' order
-template <int SIZE = 16>
 __device__ __forceinline__ void to_lds(const half_t *base, int bytes, half_t *lds, int v, int at)
 {
-    const auto from = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, bytes, 0x00027000);
-    const auto to = (__attribute__((address_space(3))) void *)lds;
-    if constexpr (SIZE == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 16, v, at, 0, 0);
-    else __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 4, v, at, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc((void *)base, 0, bytes, 0x00027000),
+                                             (__attribute__((address_space(3))) void *)lds, 16, v, at, 0, 0);
 }
 
 // With tiles of 256 the results take all 256 accumulation registers.  Left to itself the compiler moves some of them to and fro (180
@@ -322,15 +318,11 @@ template <int N> struct Half { us8 a[N], b[N]; };      // what half a step multi
 struct Nothing { __device__ __forceinline__ void operator()(const us8 &, int) const {} };
 
 // `meanwhile` runs while the first loads are under way; what it leaves in LDS is there behind the product.  also(b, j) is given all that is
-// multiplied of B: of the lane's column j, a quarter of every step.  TOUCH: B comes from memory, whose latency is more than the step that a load
-// has.  So every thread loads 4 bytes of a row some steps ahead, to nowhere (1 KB of LDS that nobody reads), and the step's own
-// loads find the row in L2.  It is the last load of a step, and the only one that is not waited for.
-template <int TILE, int DT, bool TOUCH = false, typename F, typename G = Nothing>
+// multiplied of B: of the lane's column j, a quarter of every step.
+template <int TILE, int DT, typename F, typename G = Nothing>
 __device__ __forceinline__ void product(const Operand &A, const Operand &B, int row_a, int row_b, int k_begin, int k_end,
-                                        ProductLds<TILE> &even, ProductLds<TILE> &odd, f32x4 (&acc)[TILE / 32][TILE / 32], F meanwhile, G also = G(),
-                                        half_t *nowhere = nullptr)
+                                        ProductLds<TILE> &even, ProductLds<TILE> &odd, f32x4 (&acc)[TILE / 32][TILE / 32], F meanwhile, G also = G())
 {
-    static_assert(!TOUCH || (TILE == 256 && DT != DT_F32), "a row for each thread, one plane");
     constexpr int N = TILE / 32;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int per = (k_end - k_begin) / CT_K;
@@ -387,20 +379,12 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int 
     Half<N> h0, h1;
 #pragma unroll
     for (int i = 0; i < N; ++i) fetch(0, even, i);
-    const int touch_at = (int)threadIdx.x * B.ld * 2;
-    auto touch = [&](int s) {
-        if constexpr (TOUCH) to_lds<4>(pb, bytes_b, nowhere + wave * 128, touch_at, (k_begin + (s < steps ? s : steps - 1) * CT_K) * 2);
-    };
-    if (TOUCH)
-#pragma unroll
-        for (int s = 1; s < CT_TOUCH; ++s) touch(s);
     meanwhile();
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (steps > 1)
 #pragma unroll
         for (int i = 0; i < N; ++i) fetch(1, odd, i);
-    touch(CT_TOUCH);
 #pragma unroll
     for (int i = 0; i < N; ++i) read(h0, even, 0, i);
     // A wavefront issues in order: reads and loads in one lump would hold its matrix instructions back until they are accepted.  So
@@ -417,8 +401,7 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int 
             __builtin_amdgcn_sched_barrier(0);
         }
         // the next step is there for all, and all have read this one
-        if constexpr (TOUCH) asm volatile("s_waitcnt vmcnt(1) lgkmcnt(0)" ::: "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         const int next = s + 2 < steps ? s + 2 : s + 1;         // (the last one is read by nobody)
@@ -427,7 +410,6 @@ __device__ __forceinline__ void product(const Operand &A, const Operand &B, int 
             if (i < N / 2) {
                 fetch(next, now, 2 * i);
                 fetch(next, now, 2 * i + 1);
-                if (2 * i + 2 == N) touch(s + 1 + CT_TOUCH);
             } else {
                 read(h0, other, 0, 2 * i - N);
                 read(h0, other, 0, 2 * i - N + 1);
@@ -671,9 +653,9 @@ template <int TILE, bool PREPARED> __device__ __forceinline__ void load_side(con
 }
 
 // q k' of a tile, its side tables read meanwhile
-template <int TILE, int DT, bool TERMS, bool PREPARED = true, bool TOUCH = false, typename LDS, typename LDS2, typename F, typename G = Nothing>
+template <int TILE, int DT, bool TERMS, bool PREPARED = true, typename LDS, typename LDS2, typename F, typename G = Nothing>
 __device__ __forceinline__ void logit_product(const ContrastPar &c, int tr, int tc, LDS &lds, LDS2 &lds2, SideLds<TILE> &side, f32x4 (&acc)[TILE / 32][TILE / 32], F lists,
-                                              G also = G(), half_t *nowhere = nullptr)
+                                              G also = G())
 {
     const Operand q = {c.q, c.plane_q, c.dp}, k = !c.k ? Operand{(const half_t *)c.K, 0, c.d, c.M} : Operand{c.k, c.plane_k, c.dp};
     const auto tables = [&]() {
@@ -681,7 +663,7 @@ __device__ __forceinline__ void logit_product(const ContrastPar &c, int tr, int 
         lists();
     };
     if constexpr (TERMS) product_of_terms(q, k, tr * TILE, tc * TILE, 0, c.dp, lds, acc, tables);
-    else product<TILE, DT, TOUCH>(q, k, tr * TILE, tc * TILE, 0, c.dp, lds, lds2, acc, tables, also, nowhere);
+    else product<TILE, DT>(q, k, tr * TILE, tc * TILE, 0, c.dp, lds, lds2, acc, tables, also);
 }
 
 // Logits of the keys that rows leave out become -infinity, or what stands for it; nothing to do for most rows.

@@ -134,10 +134,8 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_logprob_s
     tile_of((int)(first + blockIdx.x), tiles_q, tiles_k, tr, tc);
     tc += c.key0 / TILE;
     float base[N], norm[N] = {};
-    constexpr bool TOUCH = TILE == 256;
-    __shared__ half_t nowhere[TOUCH ? 512 : 1];
-    if constexpr (SQUARES) logit_product<TILE, DT, TERMS, false, TOUCH>(c, tr, tc, lds, lds2, side, acc, []() {}, SquaresOf<DT, N>{norm}, nowhere);
-    else logit_product<TILE, DT, TERMS, true, TOUCH>(c, tr, tc, lds, lds2, side, acc, []() {}, Nothing(), nowhere);
+    if constexpr (SQUARES) logit_product<TILE, DT, TERMS, false>(c, tr, tc, lds, lds2, side, acc, []() {}, SquaresOf<DT, N>{norm});
+    else logit_product<TILE, DT, TERMS>(c, tr, tc, lds, lds2, side, acc, []() {});
     const Place<TILE> at(tr, tc);
     int id[N];
     bool odd[N], any_odd = false;
