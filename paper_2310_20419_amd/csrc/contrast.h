@@ -150,27 +150,40 @@ __device__ __forceinline__ void from_centre(const ContrastPar &c, int e, float (
     for (int k = 0; k < 4; ++k) x[k] -= m[k];
 }
 
-// A key's own part of its logits, by a wavefront; at < M padded.  ALL: the products read the rows of keys that are left out, too.  Zero times what is
-// not a number is not zero, so those of which some are not get a base that is NaN.
-template <int DT, bool WIDE, bool ALL = false>
-__device__ __forceinline__ float key_side(const ContrastPar &c, int at, int lane)
+// The own parts of R keys' logits, by a wavefront, and |k|^2; at < M padded, or a key is left alone.  ALL: the products read the rows of keys that are
+// left out, too.  Zero times what is not a number is not zero, so those of which some are not get a base that is NaN.
+template <int DT, bool WIDE, int R, bool ALL = false>
+__device__ __forceinline__ void key_sides(const ContrastPar &c, const int (&at)[R], int padded, int lane, float (&sum)[R])
 {
-    const bool gone = at >= c.M || key_gone(c, at);
-    float sum = 0.0f;
-    if (ALL ? at < c.M : !gone)
-        for (int e = lane * 4; e < c.d; e += 256) {
-            float x[4];
-            load4<DT, WIDE>(c.K, at, c.d, e, x);
-            if constexpr (DT == DT_F32) from_centre(c, e, x);
+    bool read[R];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sum = fmaf(x[k], x[k], sum);
-        }
-    sum = wave_sum(sum);
-    if (lane == 0) {
-        c.key_base[at] = gone ? ALL && !(sum < INFINITY) ? NAN : -INFINITY : ((c.bias ? c.bias[at] : 0.0f) - c.scale * sum) * 1.44269504f;
-        c.key_id[at] = gone ? -1 : c.key_ids ? c.key_ids[at] : at;
+    for (int r = 0; r < R; ++r) {
+        read[r] = at[r] < c.M && (ALL || !key_gone(c, at[r]));
+        sum[r] = 0.0f;
     }
-    return sum;
+    for (int e = lane * 4; e < c.d; e += 256) {
+        float x[R][4];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (read[r]) load4<DT, WIDE>(c.K, at[r], c.d, e, x[r]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (!read[r]) continue;
+            if constexpr (DT == DT_F32) from_centre(c, e, x[r]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum[r] = fmaf(x[r][k], x[r][k], sum[r]);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) sum[r] = wave_sum(sum[r]);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (lane != r || at[r] >= padded) continue;
+        const int j = at[r];
+        const bool gone = j >= c.M || key_gone(c, j);
+        c.key_base[j] = gone ? ALL && !(sum[r] < INFINITY) ? NAN : -INFINITY : ((c.bias ? c.bias[j] : 0.0f) - c.scale * sum[r]) * 1.44269504f;
+        c.key_id[j] = gone ? -1 : c.key_ids ? c.key_ids[j] : j;
+    }
 }
 
 __device__ __forceinline__ half_t bits16(__bf16 x) { return __builtin_bit_cast(half_t, x); }

@@ -51,7 +51,9 @@ __device__ __forceinline__ void contrast_rows(const ContrastPar &c, int block, i
     const int padded = ((keys ? c.M : c.B) + CT_PAD - 1) / CT_PAD * CT_PAD;
     for (int at = (block - (keys ? 0 : key_blocks)) * 4 + wave; at < padded; at += blocks * 4) {
         if (keys) {
-            key_side<DT, WIDE>(c, at, lane);
+            const int one[1] = {at};
+            float norm[1];
+            key_sides<DT, WIDE, 1>(c, one, padded, lane, norm);
             if (lane == 0 && at < c.M) {
                 c.first[at] = 0x7FFFFFFF;
                 c.count[at] = 0;

@@ -229,10 +229,13 @@ __global__ __launch_bounds__(256) void k_distill_prepare(DistillPar c, u32 first
     }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (block < key_blocks) {
-        for (int at = block * 4 + wave; at < ct_up(c.M, CT_PAD); at += key_blocks * 4) {
-            key_side<DT, WIDE>(c, at, lane);
-            if (!c.dK || at >= c.M) continue;
-            for (int t = lane; t < c.words; t += 64) c.marks[(size_t)at * c.words + t] = 0;
+        const int padded = ct_up(c.M, CT_PAD);
+        for (int at = (block * 4 + wave) * 4; at < padded; at += key_blocks * 16) {
+            const int four[4] = {at, at + 1, at + 2, at + 3};
+            float norm[4];
+            key_sides<DT, WIDE, 4>(c, four, padded, lane, norm);
+            if (!c.dK) continue;
+            for (int t = lane; t < (c.M - at < 4 ? c.M - at : 4) * c.words; t += 64) c.marks[(size_t)at * c.words + t] = 0;
         }
         return;
     }

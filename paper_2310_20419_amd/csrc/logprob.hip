@@ -19,7 +19,7 @@
 #define LP_ROOM 256             // groups above the bound, and keys among them, that a wavefront has room for
 #define LP_NONE (-3.0e38f)      // stands for -infinity where bits are put into the significand
 #define LP_LOG2E 1.4426950408889634
-#define LP_FEW 8                // queries
+#define LP_FEW 8                // queries at a time that are summed from differences
 #define LP_ALONE 512            // queries, for each of which there is room for a block of eight wavefronts
 
 struct LogprobPar : ContrastPar {
@@ -67,9 +67,15 @@ __global__ __launch_bounds__(256) void k_logprob_prepare(LogprobPar c, u32 first
     if (block < key_blocks) {
         if (threadIdx.x == 0) most = {0, 0};
         __syncthreads();
-        for (int at = block * 4 + wave; at < ct_up(c.M, CT_PAD); at += key_blocks * 4) {
-            const float norm = c.keys_as_they_are ? key_side<DT, WIDE, true>(c, at, lane) : key_side<DT, WIDE>(c, at, lane);
-            if (lane == 0) most_of(most, c, at, norm);
+        const int padded = ct_up(c.M, CT_PAD);
+        for (int at = (block * 4 + wave) * 4; at < padded; at += key_blocks * 16) {
+            const int four[4] = {at, at + 1, at + 2, at + 3};
+            float norm[4];
+            if (c.keys_as_they_are) key_sides<DT, WIDE, 4, true>(c, four, padded, lane, norm);
+            else key_sides<DT, WIDE, 4>(c, four, padded, lane, norm);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (lane == r) most_of(most, c, at + r, norm[r]);
         }
         __syncthreads();
         if (threadIdx.x == 0) {
@@ -813,7 +819,16 @@ struct LogprobPlan {
     int wave_keys, passes;      // a few queries: keys of a wavefront at a time, and how many times
 };
 
-#define LP_BYTES ((size_t)1 << 28)      // of a run's parts and groups
+#define LP_BYTES ((size_t)1 << 30)      // of a run's parts and groups
+
+// Up to 8 queries at a time by differences, or all by tiles.  Float32 keys have to be copied in three terms for the tiles, which costs as much as many
+// runs of 8 through a large table: 1,000,000 x 96, 8 queries 128 us, 64 by tiles 945.  A run takes some 20 us and 1.3 us a million coordinates, tiles
+// 45 and 9.  (16-bit keys: 300,000 x 768, 8 queries 155 us, 9 to 256 by tiles 223.)
+static bool few_queries(int B, int M, int d, int dtype)
+{
+    const double size = 1e-6 * M * d;
+    return B <= LP_FEW || (dtype == RNND_F32 && (B + LP_FEW - 1) / LP_FEW * (20.0 + 1.3 * size) < 45.0 + 9.0 * size);
+}
 
 // Keys of 16 bits whose rows are whole steps of the product are read where they are.  Where they do not lie at a multiple of 16 bytes they are copied after
 // all, as many at a time as there is room for: neither the workspace nor the order of sums goes by addresses.
@@ -826,8 +841,9 @@ static size_t layout(LogprobPar &c, LogprobPlan &plan, int dtype, char *base)
         off += ws_align(count * sizeof(*p));
     };
     const int queries = c.B;
-    c.few = c.B <= LP_FEW;
+    c.few = few_queries(c.B, c.M, c.d, dtype);
     if (c.few) {
+        if (c.B > LP_FEW) c.B = LP_FEW;
         // parts: a wavefront joins them in the end, so not more than some 2,000
         plan.wave_keys = c.B <= 2 ? 32 : 16;
         plan.passes = 1;
@@ -835,14 +851,14 @@ static size_t layout(LogprobPar &c, LogprobPlan &plan, int dtype, char *base)
         while (plan.wave_keys < 64 && parts() > 512) plan.wave_keys *= 2;
         while (parts() > 2048) plan.passes *= 2;
         plan.slab = c.B;
-        c.parts_k = parts();
+        c.parts_k = c.most_blocks = parts();
         c.group_shift = 3;
         c.part_shift = __builtin_ctz(plan.wave_keys * plan.passes / 2);
-        c.most_blocks = c.parts_k;
         take(c.most, c.parts_k);
         take(c.part, (size_t)c.B * c.parts_k);
         take(c.part_w, (size_t)c.B * c.parts_k);
         if (c.alternatives) take(c.groups, (size_t)c.B * c.parts_k << c.part_shift);
+        c.B = queries;
         return off;
     }
     plan.tiles = contrast_plan(c, dtype == RNND_F32 ? 3 : 1);
