@@ -151,8 +151,8 @@ __device__ __forceinline__ void from_centre(const ContrastPar &c, int e, float (
 }
 
 // The own parts of R keys' logits, by a wavefront, and |k|^2; at < M padded, or a key is left alone.  ALL: the products read the rows of keys that are
-// left out, too.  Zero times what is not a number is not zero, so those of which some are not get a base that is NaN.
-template <int DT, bool WIDE, int R, bool ALL = false>
+// left out, too.  Zero times what is not a number is not zero, so those of which some are not get a base that is NaN.  ONCE: the base is rounded once, at the end.
+template <int DT, bool WIDE, int R, bool ALL = false, bool ONCE = true>
 __device__ __forceinline__ void key_sides(const ContrastPar &c, const int (&at)[R], int padded, int lane, float (&sum)[R])
 {
     bool read[R];
@@ -181,7 +181,9 @@ __device__ __forceinline__ void key_sides(const ContrastPar &c, const int (&at)[
         if (lane != r || at[r] >= padded) continue;
         const int j = at[r];
         const bool gone = j >= c.M || key_gone(c, j);
-        c.key_base[j] = gone ? ALL && !(sum[r] < INFINITY) ? NAN : -INFINITY : ((c.bias ? c.bias[j] : 0.0f) - c.scale * sum[r]) * 1.44269504f;
+        const float bias = c.bias ? c.bias[j] : 0.0f;
+        const float base = ONCE ? (float)(((double)bias - (double)c.scale * (double)sum[r]) * 1.4426950408889634) : (bias - c.scale * sum[r]) * 1.44269504f;
+        c.key_base[j] = gone ? ALL && !(sum[r] < INFINITY) ? NAN : -INFINITY : base;
         c.key_id[j] = gone ? -1 : c.key_ids ? c.key_ids[j] : j;
     }
 }

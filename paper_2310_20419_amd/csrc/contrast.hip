@@ -53,7 +53,7 @@ __device__ __forceinline__ void contrast_rows(const ContrastPar &c, int block, i
         if (keys) {
             const int one[1] = {at};
             float norm[1];
-            key_sides<DT, WIDE, 1>(c, one, padded, lane, norm);
+            key_sides<DT, WIDE, 1, false, false>(c, one, padded, lane, norm);
             if (lane == 0 && at < c.M) {
                 c.first[at] = 0x7FFFFFFF;
                 c.count[at] = 0;

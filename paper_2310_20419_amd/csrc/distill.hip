@@ -298,31 +298,33 @@ __global__ __launch_bounds__(256) void k_distill_loss(DistillPar c, int row_bloc
 #pragma unroll
         for (int r = 0; r < 2; ++r) p[r] /= mass.x;
     }
+    // The loss is a difference of sums that are larger than it where teacher and student agree, so it is formed in double precision: its error is that
+    // of the logits and their sums.
     const float m = fmaxf(top, wave_max_f32(fmaxf(s[0], s[1]))), ref = m == -INFINITY ? 0.0f : m;
-    const float x[2] = {s[0] - ref, s[1] - ref}, e[2] = {__builtin_amdgcn_exp2f(x[0]), __builtin_amdgcn_exp2f(x[1])};
-    const float off = others ? sum * __builtin_amdgcn_exp2f(top - ref) : 0.0f, total = off + wave_sum(e[0] + e[1]), log_total = log2f(total);
+    const double x[2] = {(double)s[0] - (double)ref, (double)s[1] - (double)ref}, e[2] = {exp2(x[0]), exp2(x[1])};
+    const double off = others ? (double)sum * exp2((double)top - (double)ref) : 0.0, total = off + wave_sum_f64(e[0] + e[1]), log_total = log2(total);
     const float w = c.row_own[i], up_w = ldexpf(w, up);
-    float loss = 0.0f;
+    double loss = 0.0;
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         const int at = r * 64 + lane;
         if (at >= n) continue;
         // (an entry whose probability is below the smallest float has none)
-        if (!(p[r] == 0.0f)) loss = fmaf(p[r], (log2f(p[r]) - (x[r] - log_total)) * 0.693147181f, loss);
+        if (!(p[r] == 0.0f)) loss = fma((double)p[r], log2((double)p[r]) - (x[r] - log_total), loss);
         if (!c.dK) continue;
-        c.list_g[(size_t)i * c.entries + at] = w * (e[r] / total - p[r]);
+        c.list_g[(size_t)i * c.entries + at] = w * (float)(e[r] / total - (double)p[r]);
         const int j = c.list_key[(size_t)i * c.entries + at];
         atomicOr(&c.marks[(size_t)j * c.words + (i >> 5)], 1u << (i & 31));
     }
-    loss = wave_sum(loss);
+    loss = wave_sum_f64(loss);
     if (lane) return;
     if (rest > 0.0f) {
-        const float log_off = top - ref + log2f(sum);
-        loss = fmaf(rest, (log2f(rest) - (log_off - log_total)) * 0.693147181f, loss);
-        c.row_g[i] = make_float2(top + log2f(sum), up_w * (off / total - rest));
+        const double log_off = (double)top - (double)ref + log2((double)sum);
+        loss = fma((double)rest, log2((double)rest) - (log_off - log_total), loss);
+        c.row_g[i] = make_float2(top + log2f(sum), up_w * (float)(off / total - (double)rest));
     } else if (others)
-        c.row_g[i] = make_float2(ref + log_total, up_w);
-    c.loss[i] = loss;
+        c.row_g[i] = make_float2((float)((double)ref + log_total), up_w);
+    c.loss[i] = (float)(loss * 0.69314718055994531);
 }
 
 // ------------------------------------------------------------------------------------------------ joining the gradients' parts

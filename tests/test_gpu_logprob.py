@@ -227,7 +227,9 @@ def test_no_key_at_all(rn, B):
     lp, ent, ids, tops = call(rn, c, 3.0, 5)
     # its probability is 1; the first pass has its logit with an error of u ((16 + 4) 2 scale |q||k| + (16 + 4) scale (|q|^2 + |k|^2)), and |q|, |k| < 2
     one = U * (20 * 6 * 4 + 20 * 3 * 8)
-    assert abs(lp[1]) <= one and abs(tops[1, 0]) <= one and ent[1] == 0 and ids[1].tolist() == [7, -1, -1, -1, -1] and (ids[0] == -1).all()
+    # its entropy is log2(sum) - w / sum in base 2, with sum = 2^x and w = x sum for some x near zero: the sum is off by 2 u, its logarithm by 3 u for that
+    # and 2 u for itself, the quotient by 3 u of |x| < 1
+    assert abs(lp[1]) <= one and abs(tops[1, 0]) <= one and 0 <= ent[1] <= 8 * U and ids[1].tolist() == [7, -1, -1, -1, -1] and (ids[0] == -1).all()
 
 
 @pytest.mark.parametrize("B", [2, 12])
