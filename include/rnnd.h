@@ -372,9 +372,9 @@ int rnnd_contrast_workspace(int64_t B, int64_t M, int32_t d, int dtype, int want
  * A query without an entry does not count: loss 0, gradient 0, whatever its row holds.
  *   Q, K, query_ids, key_ids, key_bias, row_weight, loss, dQ, dK   as for rnnd_contrast
  *   teacher_ids     device int32 [B x entries], 1 <= entries <= RNND_MAX_LISTED, in any order
- *   teacher_logits  device float [B x entries], no NaN or +infinity (they make the query's loss and gradients NaN)
- * Held in fewer bits than float32: for the products that form dQ and dK the gradients with respect to the logits, as for rnnd_contrast,
- * those of listed keys among them.  The probabilities of a list are formed and summed in double precision.
+ *   teacher_logits  device float [B x entries], no NaN or +infinity (they make the query's loss and gradients NaN, and those of the keys on its list)
+ * Held in fewer bits than float32: for the products that form dQ and dK the gradients with respect to the logits of keys off the list, as for
+ * rnnd_contrast; those of listed keys are float32.  The probabilities of a list, and the loss, are formed in double precision.
  * 0 <= B <= RNND_MAX_CONTRAST, 1 <= M <= RNND_MAX_CONTRAST; the workspace holds two (float32 rows: six) 16-bit values per
  * pair for the gradients. */
 #define RNND_MAX_LISTED 128         /* entries of a teacher's list; alternatives of rnnd_logprob */
@@ -392,12 +392,15 @@ int rnnd_distill_workspace(int64_t B, int64_t M, int32_t d, int dtype, int32_t e
  *                   -1 where there are fewer
  *   top_logprob[i]  their log P; -infinity where there are fewer
  * The order of the alternatives is that of the logits in double precision (each distance summed in double precision from the rows as
- * they are), whatever the error of the sums; it costs more where very many keys are within that error of each other.  The sums are float32,
- * with rnnd_contrast's errors of a logit; with at most 8 queries the distances are summed from differences and have no error from far origins.
- * Where no key counts: logprob and entropy 0, no alternatives.  Where a logit that counts is NaN or +infinity: NaN, no alternatives (-1 and NaN).
+ * they are), whatever the error of the sums; it costs more where very many keys are within that error of each other.  The logits whose
+ * log probabilities are given are from double precision too.  The sums over all keys are float32, with rnnd_contrast's errors of a logit; for up to
+ * 8 queries (and more against a large table of float32 rows) the distances are summed from differences and have no error from far origins.
+ * Where no key counts: logprob and entropy 0, no alternatives.  Logits below -2e38 count as -infinity (a bias of the lowest float leaves its key out
+ * of sums and alternatives).  Where a logit that counts is NaN or +infinity: NaN, no alternatives (-1 and NaN).
  *   target       device int32 [B] or NULL with logprob NULL; entropy device float [B] or NULL
  *   alternatives 0 <= alternatives <= RNND_MAX_LISTED; top_ids device int32 [B x alternatives], top_logprob device float [B x alternatives] (NULL if 0)
- * 0 <= B <= RNND_MAX_CONTRAST, 1 <= M <= RNND_MAX_CONTRAST. */
+ * 0 <= B <= RNND_MAX_CONTRAST, 1 <= M <= RNND_MAX_CONTRAST; many queries go through the keys in runs, so that the workspace stays at about a GB beside
+ * copies of the rows (16-bit keys whose rows are multiples of 64 coordinates are read where they are). */
 int rnnd_logprob(const void *Q, int64_t B, const void *K, int64_t M, int32_t d, int dtype, int metric, const int32_t *target,
                  const int32_t *query_ids, const int32_t *key_ids, const float *key_bias, float scale, int32_t alternatives,
                  float *logprob, float *entropy, int32_t *top_ids, float *top_logprob, void *workspace, size_t workspace_bytes,

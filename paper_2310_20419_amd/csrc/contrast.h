@@ -27,6 +27,7 @@ struct ContrastPar {
     float scale, c1;                // c1 = 2 scale log2(e)
     int B, M, d;
     int dp, Bp, Mp, dr;             // padded to CT_K; dr: d padded to the tile of the gradient products
+    int tile, terms_from;           // of the logits, where a call has rules of its own (0: those of contrast_plan())
     bool keys_as_they_are;          // no copy of all of them
     int key0;                       // the first key that copies are made of and logits are formed with
     int ld_g, ld_gt;                // rows of g by rows and by columns: M and B padded to the largest tile
@@ -1017,19 +1018,20 @@ static ContrastPlan contrast_plan(ContrastPar &c, int planes)
 {
     ContrastPlan p;
     auto tiles = [](int x, int t) { return (long long)(x + t - 1) / t; };
-    // logits: tiles of 128 come two to a CU, one's product beside the other's logits, which is the longer part of short rows.  Sums and g
-    // of 8,192 x 16,384, tiles of 128 / 256, us: d = 64 216 / 266, 256 349 / 357, 768 635 / 604, 1,536 1,035 / 944; of 1,000 x 11,000: d = 768
-    // 69 / 76 (172 tiles of 256 for 256 CUs), 1,536 117 / 119
-    p.tile = planes == 1 && c.d > 384 && tiles(c.B, 256) * tiles(c.M, 256) >= 512 ? 256 : 128;
+    // logits: tiles of 128 come two to a CU, one's product beside the other's logits, which is the longer part of short rows.  The whole call with
+    // gradients, tiles of 128 / 256, us: 8,192 x 16,384, d = 64 418 / 464, 256 543 / 565, 384 684 / 691, 768 1,007 / 978, 1,536 1,699 / 1,601;
+    // 1,000 x 11,000: d = 768 140 / 145 (172 tiles of 256 for 256 CUs), 1,536 242 / 244
+    p.tile = c.tile ? c.tile : planes == 1 && c.d > 384 && tiles(c.B, 256) * tiles(c.M, 256) >= 512 ? 256 : 128;
     // float32 rows: product_of_terms() takes the LDS of a CU, so a second workgroup no longer works on its logits meanwhile.  It is ahead
-    // where rows are long or every workgroup has a CU of its own.  The whole call with two workgroups / with the terms together, us:
-    // 3,000 x 12,000, d = 32 332 / 361, 128 381 / 415, 256 586 / 599, 384 807 / 799, 768 1,501 / 1,412; 2,200 x 2,200 x 128 (324 tiles)
-    // 83 / 94, 700 x 4,000 x 300 (192 tiles) 119 / 101, 100 x 1,100 x 32 49.0 / 45.6
-    p.terms = planes == 3 && (c.d > 320 || tiles(c.B, 128) * tiles(c.M, 128) <= 256);
+    // where every workgroup has a CU of its own.  The whole call with two workgroups / with the terms together, us: 3,000 x 12,000,
+    // d = 32 328 / 364, 128 368 / 416, 256 559 / 597, 384 754 / 800, 768 1,390 / 1,413, 1,536 2,680 / 2,678, 2,048 3,414 / 3,372; 2,200 x 2,200 x 128 (324 tiles)
+    // 84 / 96, 700 x 4,000 x 300 (192 tiles) 109 / 104, 100 x 1,100 x 32 49.5 / 48.6.  (rnnd_contrast takes it from 321 coordinates on, where it was ahead
+    // before the other product stopped waiting for its loads: its sums keep their order.)
+    p.terms = planes == 3 && (c.d > (c.terms_from ? c.terms_from : 320) || tiles(c.B, 128) * tiles(c.M, 128) <= 256);
     // the gradient products: also by how much of the last tile of d would be padding.  The whole call, tiles of 128 / 256, us: 500 x 1,000 x 768
-    // (18 tiles of 256) 63 / 77, 1,700 x 3,400 x 768 (63) 86 / 97, 2,048 x 4,096 x 768 (72) 91 / 100, 1,000 x 11,000 x 768 (141) 153 / 148,
-    // 8,192 x 16,384 x 768 (288) 1,127 / 1,052; by padding, 4,096 x 8,192: d = 300 (512 for 384) 163 / 177, 600 (768 for 640) 266 / 262, 1,100 (1,280 for
-    // 1,152) 410 / 438, 64 103 / 118.  (Between 64 and about 128 tiles, and at lengths like 1,100, tiles of 128 would be up to 10 % ahead.)
+    // (18 tiles of 256) 57 / 71, 1,700 x 3,400 x 768 (63) 85 / 94, 2,048 x 4,096 x 768 (72) 88 / 98, 1,000 x 11,000 x 768 (141) 145 / 139,
+    // 8,192 x 16,384 x 768 (288) 1,061 / 978; by padding, 4,096 x 8,192: d = 300 (512 for 384) 153 / 167, 600 (768 for 640) 237 / 248, 1,100 (1,280 for
+    // 1,152) 393 / 409, 64 103 / 118.  (Between 64 and about 128 tiles, and at lengths like 600 and 1,100, tiles of 128 would be up to 10 % ahead.)
     const int d128 = ct_up(c.d, 128), d256 = ct_up(c.d, 256);
     p.tile_g = planes == 1 && (tiles(c.B, 256) + tiles(c.M, 256)) * (d256 / 256) >= 64 && d256 * 4 <= d128 * 5 ? 256 : 128;
     c.dp = ct_up(c.d, CT_K);

@@ -528,6 +528,7 @@ __global__ __launch_bounds__(64 * DS_FINISH) void k_distill_finish(DistillPar c,
 // ------------------------------------------------------------------------------------------------ host side
 static size_t layout(DistillPar &c, ContrastPlan &plan, int dtype, int want_grad, char *base)
 {
+    c.terms_from = 1536;
     return contrast_layout(c, plan, dtype, want_grad, base, [&](auto &take) {
         const size_t Br = ct_up(c.B, CT_PAD);
         c.tiles_k = c.parts_k / 2;

@@ -861,6 +861,13 @@ static size_t layout(LogprobPar &c, LogprobPlan &plan, int dtype, char *base)
         c.B = queries;
         return off;
     }
+    // Tiles: as contrast_plan(), but that there is one product.  16-bit rows, tiles of 128 / 256, us: up to 128 queries, where half of one of 256 would be padding,
+    // 100 x 300,000, d = 128 99 / 108, 256 105 / 125, 768 195 / 224; more of them read the keys once instead of twice, 200 x 300,000, d = 64 103 / 100, 128 107 / 111,
+    // 192 135 / 121, 256 153 / 130, 768 254 / 224, 400 x 300,000 x 256 255 / 238; 8,192 x 16,384, d = 128 146 / 157, 256 179 / 180, 384 211 / 209, 768 311 / 289.
+    // Float32 rows, two workgroups / terms together: 3,000 x 12,000, d = 100 97 / 124, 768 361 / 386, 1,536 693 / 712; 700 x 4,000 x 300 57 / 54.
+    const bool large = (c.B + 255LL) / 256 * ((c.M + 255LL) / 256) >= 512 && c.B > 128 && c.d > (c.B <= 1024 ? 160 : 320);
+    c.tile = dtype != RNND_F32 && large ? 256 : 128;
+    c.terms_from = 1536;
     plan.tiles = contrast_plan(c, dtype == RNND_F32 ? 3 : 1);
     c.keys_as_they_are = dtype != RNND_F32 && c.d % CT_K == 0;
     // Their norms come from the product's pass over them where few tiles do that for every key.  Norms by themselves / along with the product, us:
