@@ -255,6 +255,24 @@ __device__ __forceinline__ void join_three(float &top, float &sum, float &w, flo
     top = m;
 }
 
+// V coordinates of a row from e on, of which those behind `end` are zeros.  WIDE: all rows allow it in one aligned access.  Others are loaded in one access
+// all the same where they are whole (the hardware takes any address of a global load), and one by one at the end of the row.
+template <int DT, int V, bool WIDE>
+__device__ __forceinline__ Pack<DT, V> load_piece(const void *rows, size_t row, int e, int end)
+{
+    typedef typename RowType<DT>::T T;
+    if constexpr (WIDE) return load_pack<DT, V>(rows, row + e);
+    else {
+        const T *from = (const T *)rows + row + e;
+        Pack<DT, V> p;
+        if (e + V <= end) __builtin_memcpy(&p, from, sizeof(p));
+        else
+#pragma unroll
+            for (int k = 0; k < V; ++k) p.v[k] = e + k < end ? from[k] : (T)0.0f;
+        return p;
+    }
+}
+
 // ------------------------------------------------------------------------------------------------ the logits of a few queries
 // Up to 8 queries: no matrix tile would be filled, and the call is bound by reading the keys once.  8 lanes take a row, 16 bytes each; distances
 // are summed from differences.  Query coordinates come from LDS, as many of all queries as fit at a time.  A wavefront takes 16, 32 or 64 keys
@@ -313,13 +331,7 @@ __global__ __launch_bounds__(256) void k_logprob_few(LogprobPar c, int wave_keys
                     for (int a = 0; a < AHEAD; ++a) {
                         const int e = e1 + a * 8 * V + sub * V, from = e < end ? e : 0;
 #pragma unroll
-                        for (int r = 0; r < R; ++r) {
-                            typedef typename RowType<DT>::T T;
-                            if constexpr (WIDE) packs[a][r] = load_pack<DT, V>(c.K, row[r] + e0 + from);
-                            else
-#pragma unroll
-                                for (int k = 0; k < V; ++k) packs[a][r].v[k] = from + k < end ? ((const T *)c.K)[row[r] + e0 + from + k] : (T)0.0f;
-                        }
+                        for (int r = 0; r < R; ++r) packs[a][r] = load_piece<DT, V, WIDE>(c.K, row[r] + e0, from, end);
                     }
 #pragma unroll
                     for (int a = 0; a < AHEAD; ++a) {
@@ -419,8 +431,7 @@ __global__ __launch_bounds__(256) void k_logprob_few(LogprobPar c, int wave_keys
 template <int DT, bool WIDE>
 __device__ __forceinline__ double exact_distance(const LogprobPar &c, int i, int j, int sub)
 {
-    typedef typename RowType<DT>::T T;
-    constexpr int V = DT == DT_F32 ? 4 : 8, AHEAD = WIDE ? 4 : 1;
+    constexpr int V = DT == DT_F32 ? 4 : 8, AHEAD = WIDE ? 4 : 2;
     double sum = 0.0;
     const size_t q = (size_t)i * c.d, k = (size_t)j * c.d;
     for (int e1 = sub * V; e1 < c.d; e1 += AHEAD * 8 * V) {
@@ -428,16 +439,8 @@ __device__ __forceinline__ double exact_distance(const LogprobPar &c, int i, int
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a) {
             const int e = e1 + a * 8 * V, from = e < c.d ? e : e1;
-            if constexpr (WIDE) {
-                py[a] = load_pack<DT, V>(c.K, k + from);
-                px[a] = load_pack<DT, V>(c.Q, q + from);
-            } else
-#pragma unroll
-                for (int h = 0; h < V; ++h) {
-                    const bool in = from + h < c.d;
-                    px[a].v[h] = in ? ((const T *)c.Q)[q + from + h] : (T)0.0f;
-                    py[a].v[h] = in ? ((const T *)c.K)[k + from + h] : (T)0.0f;
-                }
+            py[a] = load_piece<DT, V, WIDE>(c.K, k, from, c.d);
+            px[a] = load_piece<DT, V, WIDE>(c.Q, q, from, c.d);
         }
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a) {
