@@ -27,11 +27,11 @@
 //     the formulas have it.
 //
 // What bounds it.  The work that the loss cannot do without is three products; forming the logits again is a fourth, which costs less
-// than writing them in 32 bits and reading them back.  8,192 x 16,384 x 768 bfloat16, 1.08 ms (three library products of that shape: 0.64):
-// preparation 34 us; largest and sums 264 (781 TFLOP/s); g 365 (565, and 537 MB written: one wavefront per SIMD, so that what
-// follows a tile's product is not hidden behind another's); g k and g' q 427 (965; the library's products 971 to 1,003); joining the parts 47.  Float32 rows of
-// 100 coordinates, 2,000 x 10,000, 239 us: six products for each, and g in three terms twice, 250 MB written by the second product (74 us)
-// and read by the third (93).  Small calls are seven launches that wait for each other (16-bit rows six): 100 x 1,100 x 32 50 us.
+// than writing them in 32 bits and reading them back.  8,192 x 16,384 x 768 bfloat16, 0.98-1.00 ms (three library products of that shape: 0.64):
+// preparation 35 us; largest and sums 250 (825 TFLOP/s); g 330 (625, and 537 MB written: one wavefront per SIMD, so that what
+// follows a tile's product is not hidden behind another's); g k and g' q 434 (950; the library's products 971 to 1,003); joining the parts 48.  Float32 rows of
+// 100 coordinates, 2,000 x 10,000, 228 us: six products for each, and g in three terms twice, 250 MB written by the second product (65 us)
+// and read by the third (93).  Small calls are seven launches that wait for each other (16-bit rows six): 100 x 1,100 x 32 50 to 54 us.
 #include <cmath>
 
 #include "contrast.h"
