@@ -9,7 +9,7 @@
 // largest one's key stands in the lowest bits of its significand.  k keys are at least as large as the k-th largest of any values that are
 // logits of different keys, so a bound on the k-th logit follows from the parts' largest, a better one from the groups of those parts, and
 // what lies above the better one is little more than k keys.  Their distances are summed again in double precision from the rows as
-// they are, and these decide the order.  The first pass is off by some error E (bounds(), from the norms): keys down to 2 E below
+// they are, and these decide the order.  The first pass is off by some error E (a bound from the norms): keys down to 2 E below
 // the bound are taken along, so E costs time but changes no answer.  Where more keys than there is room for lie that close
 // together (thousands of copies of a row), all groups above the bound are gone through in double precision instead.
 #include <cmath>
@@ -53,7 +53,7 @@ __device__ __forceinline__ void most_of(MostLds &most, const LogprobPar &c, int 
     atomicMax(&most.bias, __float_as_uint(b < INFINITY ? b : INFINITY));
 }
 
-// A wavefront per row, keys first; then the copies of the rows (contrast_copy()).  key_tiles: 0 where the keys have been prepared.
+// A wavefront per row, keys first; then the copies of the rows (contrast_copy()).  key_blocks: 0 where the keys have been prepared.
 template <int DT, bool WIDE>
 __global__ __launch_bounds__(256) void k_logprob_prepare(LogprobPar c, u32 first, int key_blocks, int row_blocks, int q_tiles, int across)
 {
@@ -520,13 +520,24 @@ template <int PARTS> struct FinishLds {
     bool bad;
 };
 
-// A query by WAVES wavefronts (1: two queries a block).  The first selects; all form the distances of the keys that are left.  A query by
-// itself waits for dependent loads most of the time, so with few queries eight wavefronts take one.
+// What the wavefronts of a query exchange: each one's sums, and the largest two parts of each lane; then the bound (NaN: there is nothing to look for), and how
+// many parts and groups above it all have found.
+template <int WAVES> struct TeamLds {
+    float top[WAVES], sum[WAVES], w[WAVES], biases[WAVES], first[WAVES][64], second[WAVES][64];
+    float cut;
+    int parts, groups;
+};
+template <> struct TeamLds<1> {};
+
+// A query by WAVES wavefronts (1: two queries a block).  A query by itself waits for dependent loads most of the time, so with few queries eight wavefronts
+// take one: they join the parts and look for the groups above the bound together (the order in which they find them does not matter), the
+// first selects among these, and all form the distances of the keys that are left.  (1 x 1,000,000 x 96 float32 13 us; 19 where one does all but the distances.)
 template <int DT, bool WIDE, int WAVES>
 __global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) void k_logprob_finish(LogprobPar c)
 {
     constexpr int QUERIES = WAVES == 1 ? 2 : 1, PARTS = WAVES == 1 ? 256 : 512, DEEP = WAVES == 1 ? 4 : 8;
     __shared__ FinishLds<PARTS> of_queries[QUERIES];
+    __shared__ TeamLds<WAVES> team;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sub = lane & 7;
     const int i = WAVES == 1 ? blockIdx.x * 2 + wave : blockIdx.x, worker = WAVES == 1 ? 0 : wave;
     if (i >= c.B) return;       // (blocks of one query: never)
@@ -539,27 +550,62 @@ __global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) 
     float cut = -INFINITY;
     bool asked = false;         // for a target that can be
     int target = 0;
-    if (worker == 0) {
-        float top = -INFINITY, sum = 0.0f, w = 0.0f, first = -INFINITY, second = -INFINITY, norms = 0.0f, biases = 0.0f;
-        if (c.logprob) target = c.target[i];
-        for (int t0 = lane; t0 < c.parts_k; t0 += 64 * DEEP) {
-            float2 p[DEEP];
-            float pw[DEEP], most[DEEP];
+    float top = -INFINITY, sum = 0.0f, w = 0.0f, first = -INFINITY, second = -INFINITY, norms = 0.0f, biases = 0.0f;
+    for (int t0 = worker * 64 + lane; t0 < c.parts_k; t0 += WAVES * 64 * 4) {
+        float2 p[4];
+        float pw[4], most[4];
 #pragma unroll
-            for (int h = 0; h < DEEP; ++h) {
-                const int t = t0 + h * 64;
-                p[h] = t < c.parts_k ? part[t] : make_float2(-INFINITY, 0.0f);
-                pw[h] = t < c.parts_k ? c.part_w[(size_t)i * c.parts_k + t] : 0.0f;
-                most[h] = c.few && t < c.parts_k ? c.most[t] : 0.0f;
-            }
-#pragma unroll
-            for (int h = 0; h < DEEP; ++h) {
-                join_three(top, sum, w, p[h].x, p[h].y, pw[h]);
-                second = fmaxf(second, fminf(first, p[h].x));
-                first = fmaxf(first, p[h].x);
-                biases = fmaxf(biases, most[h]);
-            }
+        for (int h = 0; h < 4; ++h) {
+            const int t = t0 + h * WAVES * 64;
+            p[h] = t < c.parts_k ? part[t] : make_float2(-INFINITY, 0.0f);
+            pw[h] = t < c.parts_k ? c.part_w[(size_t)i * c.parts_k + t] : 0.0f;
+            most[h] = c.few && t < c.parts_k ? c.most[t] : 0.0f;
         }
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            join_three(top, sum, w, p[h].x, p[h].y, pw[h]);
+            second = fmaxf(second, fminf(first, p[h].x));
+            first = fmaxf(first, p[h].x);
+            biases = fmaxf(biases, most[h]);
+        }
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        join_three(top, sum, w, __shfl_xor(top, s), __shfl_xor(sum, s), __shfl_xor(w, s));
+        biases = fmaxf(biases, __shfl_xor(biases, s));
+    }
+    if constexpr (WAVES > 1) {
+        team.first[worker][lane] = first;
+        team.second[worker][lane] = second;
+        if (lane == 0) {
+            team.top[worker] = top;
+            team.sum[worker] = sum;
+            team.w[worker] = w;
+            team.biases[worker] = biases;
+        }
+        if (threadIdx.x == 0) team.parts = team.groups = 0;
+        __syncthreads();
+        if (worker == 0)
+#pragma unroll
+            for (int v = 1; v < WAVES; ++v) {
+                join_three(top, sum, w, team.top[v], team.sum[v], team.w[v]);
+                biases = fmaxf(biases, team.biases[v]);
+                const float a = team.first[v][lane], b = team.second[v][lane];
+                second = fmaxf(fmaxf(second, b), fminf(first, a));
+                first = fmaxf(first, a);
+            }
+    }
+    int n = 0, found = 0;
+    bool full = false, look = false, bad = false;
+    float error = 0.0f;
+    double norm = 0.0;
+    auto below = [&](float t) {     // t: a bound on the k-th logit as the first pass has it, with the key's number in it
+        if (t <= LP_NONE) return -INFINITY;
+        const float b = t - 2.0f * error - fabsf(t) * (4.0e-6f + (c.few ? 2.38418579e-7f * (float)(c.d + 16) : 0.0f));
+        return b > LP_NONE ? b : -INFINITY;
+    };
+    if (worker == 0) {
+        if (c.logprob) target = c.target[i];
         if (!c.few && k)
 #pragma unroll
             for (int h = 0; h < CT_ROW_BLOCKS / 256; ++h) {     // (a multiple of 64 blocks)
@@ -573,17 +619,17 @@ __global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) 
                 }
             }
         if (c.logprob) asked = (u32)target < (u32)c.M && !leaves_out(c, i, target);
-        const double norm = c.few ? 0.0 : query_norm<DT, WIDE>(c, i, lane);
+        norm = c.few ? 0.0 : query_norm<DT, WIDE>(c, i, lane);
+        if (!c.few)
 #pragma unroll
-        for (int s = 1; s < 64; s <<= 1) {
-            join_three(top, sum, w, __shfl_xor(top, s), __shfl_xor(sum, s), __shfl_xor(w, s));
-            norms = fmaxf(norms, __shfl_xor(norms, s));
-            biases = fmaxf(biases, __shfl_xor(biases, s));
-        }
-        const bool none = sum == 0.0f, bad = !(sum >= 0.0f && sum < INFINITY);
+            for (int s = 1; s < 64; s <<= 1) {
+                norms = fmaxf(norms, __shfl_xor(norms, s));
+                biases = fmaxf(biases, __shfl_xor(biases, s));
+            }
+        const bool none = sum == 0.0f;
+        bad = !(sum >= 0.0f && sum < INFINITY);
         if (c.entropy && lane == 0) c.entropy[i] = none ? 0.0f : bad ? NAN : fmaxf(0.0f, (log2f(sum) - w / sum) * 0.693147181f);
-        int n = 0, found = 0;
-        bool full = false;
+        look = k && !none && !bad;
         if (none || bad) {
             for (int e = lane; e < k; e += 64) {
                 ids[e] = -1;
@@ -593,20 +639,74 @@ __global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) 
             // how far a logit of the first pass may be off, in base 2: a sum of d products of one rounding each (float32 rows: six times as many),
             // its scaling, the key's own sum and bias; for a few queries a sum of d squares, which with the bias make up the logit
             const float u = 1.19209290e-7f, terms = DT == DT_F32 ? 6.0f : 1.0f;
-            const float error = c.few ? u * (float)(c.d + 16) * biases * 1.45f
-                                      : 1.45f * (u * fabsf(c.scale) * (2.0f * (terms * c.d + 16.0f) * sqrtf((float)norm * norms) + (float)(c.d + 16) * norms) +
-                                                 2.0f * u * biases);
-            auto below = [&](float t) {     // t: a bound on the k-th logit as the first pass has it, with the key's number in it
-                if (t <= LP_NONE) return -INFINITY;
-                const float b = t - 2.0f * error - fabsf(t) * (4.0e-6f + (c.few ? 2.0f * u * (float)(c.d + 16) : 0.0f));
-                return b > LP_NONE ? b : -INFINITY;
-            };
+            error = c.few ? u * (float)(c.d + 16) * biases * 1.45f
+                          : 1.45f * (u * fabsf(c.scale) * (2.0f * (terms * c.d + 16.0f) * sqrtf((float)norm * norms) + (float)(c.d + 16) * norms) +
+                                     2.0f * u * biases);
             {
                 float v[LP_ROOM / 64];
 #pragma unroll
                 for (int h = 0; h < LP_ROOM / 64; ++h) v[h] = h == 0 ? first : h == 1 ? second : -INFINITY;
                 cut = below(kth_largest(v, k));
             }
+        }
+    }
+    bool gathered = false;
+    if constexpr (WAVES > 1) {
+        if (threadIdx.x == 0) team.cut = look ? cut : NAN;
+        __syncthreads();
+        const float bound = team.cut;
+        if (bound == bound) {
+            // places for a wavefront's finds behind those of the others
+            auto place = [&](int *count, u64 on) {
+                int at = 0;
+                if (lane == 0) at = atomicAdd(count, (int)__popcll(on));
+                return __builtin_amdgcn_readfirstlane(at) + (int)__popcll(on & lanes_below(lane));
+            };
+            for (int p0 = worker * 64; p0 < c.parts_k; p0 += WAVES * 64 * 4) {
+                float largest[4];
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    const int p = p0 + h * WAVES * 64 + lane;
+                    largest[h] = p < c.parts_k ? part[p].x : -INFINITY;
+                }
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    const u64 on = __ballot(largest[h] > -INFINITY && largest[h] >= bound);
+                    if (!on) continue;
+                    const int to = place(&team.parts, on);
+                    if ((on >> lane & 1) && to < 2 * PARTS) lds.part[to] = p0 + h * WAVES * 64 + lane;
+                }
+            }
+            __syncthreads();
+            const int parts = team.parts, items = parts <= 2 * PARTS ? parts << c.part_shift : 0;
+            for (int t0 = worker * 64; t0 < items; t0 += WAVES * 64 * 4) {
+                float2 v[4];
+                int g[4];
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    const int t = t0 + h * WAVES * 64 + lane;
+                    g[h] = t < items ? (lds.part[t >> c.part_shift] << c.part_shift) + (t & ((1 << c.part_shift) - 1)) : -1;
+                    v[h] = g[h] >= 0 ? groups[g[h]] : make_float2(-INFINITY, -INFINITY);
+                }
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    const u64 on = __ballot(v[h].x > LP_NONE * 0.99f && v[h].x >= bound);
+                    if (!on) continue;
+                    const int to = place(&team.groups, on);
+                    if ((on >> lane & 1) && to < LP_ROOM) {
+                        lds.most[to] = v[h].x;
+                        lds.second[to] = v[h].y;
+                        lds.group[to] = g[h];
+                    }
+                }
+            }
+            __syncthreads();
+            gathered = parts <= 2 * PARTS && team.groups <= LP_ROOM;     // else one by one, which makes room
+            if (gathered) n = team.groups;
+        }
+    }
+    if (worker == 0) {
+        if (look) {
             // of the groups above the bound, those above a better one
             auto tighten = [&]() {
                 if (n < k) return;
@@ -637,7 +737,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) 
                 wave_sync();
             };
             int parts = 0;
-            for (int p0 = 0; p0 < c.parts_k && !full; p0 += PARTS) {
+            for (int p0 = 0; p0 < c.parts_k && !full && !gathered; p0 += PARTS) {
                 float largest[PARTS / 64];
 #pragma unroll
                 for (int h = 0; h < PARTS / 64; ++h) largest[h] = p0 + h * 64 + lane < c.parts_k ? part[p0 + h * 64 + lane].x : -INFINITY;
@@ -719,10 +819,11 @@ __global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) 
     }
     if constexpr (WAVES > 1) __syncthreads();
     else wave_sync();
-    const double norm = lds.norm, lse = lds.lse;
-    const bool bad = lds.bad;
-    int found = lds.found;
-    const bool full = found < 0;
+    norm = lds.norm;
+    bad = lds.bad;
+    found = lds.found;
+    full = found < 0;
+    const double lse = lds.lse;
     auto logit = [&](float bias, int j) {       // in base 2 and the frame of the sums; by 8 lanes
         return ((double)bias - (double)c.scale * (exact_distance<DT, WIDE>(c, i, j, sub) - norm)) * LP_LOG2E;
     };
@@ -825,12 +926,12 @@ struct LogprobPlan {
 #define LP_BYTES ((size_t)1 << 30)      // of a run's parts and groups
 
 // Up to 8 queries at a time by differences, or all by tiles.  Float32 keys have to be copied in three terms for the tiles, which costs as much as many
-// runs of 8 through a large table: 1,000,000 x 96, 8 queries 128 us, 64 by tiles 945.  A run takes some 20 us and 1.3 us a million coordinates, tiles
-// 45 and 9.  (16-bit keys: 300,000 x 768, 8 queries 155 us, 9 to 256 by tiles 223.)
+// runs of 8 through a large table.  8 queries / 64 by tiles, us: 10,000 x 96 24 / 40, 100,000 x 100 34 / 95, 1,000,000 x 32 79 / 536, 1,000,000 x 96 121 / 752,
+// 300,000 x 768 200 / 1,317; below, both in us, by coordinates and by keys.  (16-bit keys: 300,000 x 768, 8 queries 145 us, 9 to 128 by tiles 185, 256 219.)
 static bool few_queries(int B, int M, int d, int dtype)
 {
-    const double size = 1e-6 * M * d;
-    return B <= LP_FEW || (dtype == RNND_F32 && (B + LP_FEW - 1) / LP_FEW * (20.0 + 1.3 * size) < 45.0 + 9.0 * size);
+    const double size = 1e-6 * M * d, keys = 1e-3 * M;
+    return B <= LP_FEW || (dtype == RNND_F32 && (B + LP_FEW - 1) / LP_FEW * (22.0 + 0.75 * size + 0.03 * keys) < 35.0 + 4.5 * size + 0.33 * keys);
 }
 
 // Keys of 16 bits whose rows are whole steps of the product are read where they are.  Where they do not lie at a multiple of 16 bytes they are copied after
@@ -847,7 +948,8 @@ static size_t layout(LogprobPar &c, LogprobPlan &plan, int dtype, char *base)
     c.few = few_queries(c.B, c.M, c.d, dtype);
     if (c.few) {
         if (c.B > LP_FEW) c.B = LP_FEW;
-        // parts: a wavefront joins them in the end, so not more than some 2,000
+        // parts: they are gone through twice in the end, so not more than some 2,000 (1,024 / 2,048 / 4,096: 1 x 1,000,000 x 96 float32 84 / 80 / 78 us,
+        // 8 queries 127 / 119 / 128)
         plan.wave_keys = c.B <= 2 ? 32 : 16;
         plan.passes = 1;
         auto parts = [&]() { return (c.M + plan.wave_keys * 4 * plan.passes - 1) / (plan.wave_keys * 4 * plan.passes); };
@@ -874,7 +976,8 @@ static size_t layout(LogprobPar &c, LogprobPlan &plan, int dtype, char *base)
     plan.tiles = contrast_plan(c, dtype == RNND_F32 ? 3 : 1);
     c.keys_as_they_are = dtype != RNND_F32 && c.d % CT_K == 0;
     // Their norms come from the product's pass over them where few tiles do that for every key.  Norms by themselves / along with the product, us:
-    // bfloat16, 200 x 300,000 x 768 (one row of tiles) 600 / 300, 8,192 x 16,384 x 768 (32) 430 / 470; float16, 1,000 x 11,000 x 768 54 / 51
+    // bfloat16, 200 x 300,000 x 768 (one row of tiles) 371 / 221, 2,048 x 10,000 x 768 (8) 80 / 79, 8,192 x 16,384 x 768 (32) 305 / 329; float16,
+    // 1,000 x 11,000 x 768 63 / 56
     c.squares = c.keys_as_they_are && c.B <= 1024;
     c.part_shift = 4;
     const size_t row = (size_t)c.parts_k * (12 + (c.alternatives ? 16 * 8 : 0));

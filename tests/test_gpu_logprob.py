@@ -172,6 +172,16 @@ def test_more_equal_keys_than_there_is_room_for(rn, B, dtype):
     check(rn, c, 3.0, 100)
 
 
+@pytest.mark.parametrize("B", [1, 12])
+@pytest.mark.parametrize("run", [16, 32, 64, 128, 256])
+def test_crowds_of_probable_keys(rn, B, run):
+    """One run of keys in 64 holds those that count, far above all others: a few large values say little about the k-th largest, and more groups of keys lie
+    above the first bound than there is room for at once."""
+    c = case(B, 200_000, 8, "float32", 18, ids=False)
+    c["key_bias"][np.arange(200_000) // run % 64 == 5] += 30.0
+    check(rn, c, 1.0, 50)
+
+
 @pytest.mark.parametrize("B", [4, 64])
 def test_logits_closer_together_than_the_first_pass_sees(rn, B):
     """Keys that differ in a last bit: float32 sums do not tell them apart, the order is still that of double precision."""
