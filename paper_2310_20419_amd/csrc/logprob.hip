@@ -202,16 +202,14 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_logprob_s
                     for (int n = 0; n < N; ++n) s[r][n] = odd[n] ? LP_NONE : s[r][n];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            if constexpr (TOPS) {       // (with the key's number in the lowest bits it does for the reference, too)
+            top[r] = s[r][0];       // (a number in the lowest bits would be more than the range of the exponential where a step is: from 2^28 on)
+#pragma unroll
+            for (int n = 1; n < N; ++n) top[r] = larger(top[r], s[r][n]);
+            if constexpr (TOPS) {
                 float most = LP_NONE, second = LP_NONE;
 #pragma unroll
                 for (int n = 0; n < N; ++n) into_group(most, second, s[r][n], n, N);
                 c.groups[((size_t)(at.row + m * 4 + r) * c.parts_k + at.half_c) * 16 + (threadIdx.x & 15)] = make_float2(most, second);
-                top[r] = most;
-            } else {
-                top[r] = s[r][0];
-#pragma unroll
-                for (int n = 1; n < N; ++n) top[r] = larger(top[r], s[r][n]);
             }
         }
         row16_larger(top);
