@@ -16,6 +16,7 @@ typedef unsigned short half_t;      // float16 or bfloat16, as the rows are
 #define CT_PAD 256          // rows are padded to the largest tile
 #define CT_K 64             // summed per step: 128 bytes of a row
 #define CT_NEVER (-2)       // an id that no key has
+#define CT_LOWEST (-2.0e38f)    // biases that are not above it leave a key out of the answers: in base 2 little is left of float32's range
 #define CT_ROW_BLOCKS 1024  // at most, for the norms and targets of the rows of a side
 
 __host__ __device__ constexpr int ct_up(int x, int m) { return (x + m - 1) / m * m; }
@@ -24,6 +25,7 @@ struct ContrastPar {
     const void *Q, *K;
     const int *target, *query_ids, *key_ids;
     const float *bias, *row_weight;
+    float left_out;                 // the largest bias that leaves a key out
     float scale, c1;                // c1 = 2 scale log2(e)
     int B, M, d;
     int dp, Bp, Mp, dr;             // padded to CT_K; dr: d padded to the tile of the gradient products
@@ -57,7 +59,7 @@ __device__ __forceinline__ int weight_exponent(u32 top) { return top >= 0x008000
 // ------------------------------------------------------------------------------------------------ preparation
 __device__ __forceinline__ bool key_gone(const ContrastPar &c, int j)
 {
-    return (c.key_ids && c.key_ids[j] < 0) || (c.bias && c.bias[j] == -INFINITY);
+    return (c.key_ids && c.key_ids[j] < 0) || (c.bias && c.bias[j] <= c.left_out);
 }
 __device__ __forceinline__ bool row_counts(const ContrastPar &c, int i)
 {

@@ -18,6 +18,7 @@
 
 #define LP_ROOM 256             // groups above the bound, and keys among them, that a wavefront has room for
 #define LP_NONE (-3.0e38f)      // stands for -infinity where bits are put into the significand
+#define LP_LIMIT (LP_NONE * 0.99f)      // logits that are not above it count as -infinity
 #define LP_LOG2E 1.4426950408889634
 #define LP_FEW 8                // queries at a time that are summed from differences
 #define LP_ALONE 512            // queries, for each of which there is room for a block of eight wavefronts
@@ -215,8 +216,8 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_logprob_s
         row16_larger(top);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const float ref = top[r] > LP_NONE * 0.99f ? top[r] : 0.0f;
-            top[r] = top[r] > LP_NONE * 0.99f ? top[r] : -INFINITY;
+            const float ref = top[r] > LP_LIMIT ? top[r] : 0.0f;
+            top[r] = top[r] > LP_LIMIT ? top[r] : -INFINITY;
             sum[r] = w[r] = 0.0f;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
@@ -375,7 +376,8 @@ __global__ __launch_bounds__(256) void k_logprob_few(LogprobPar c, int wave_keys
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             if (b >= c.B) break;
-            const float s = !on || (c.query_ids && name == c.query_ids[b]) ? -INFINITY : (bias - c.scale * far_of[b * 64 + lane]) * 1.44269504f;
+            float s = !on || (c.query_ids && name == c.query_ids[b]) ? -INFINITY : (bias - c.scale * far_of[b * 64 + lane]) * 1.44269504f;
+            s = s <= LP_LIMIT ? -INFINITY : s;      // (NaN stays)
             if (c.alternatives) {       // 8 lanes are a group
                 float x = __uint_as_float((__float_as_uint(fmaxf(s, LP_NONE)) & ~7u) | (u32)sub), y = LP_NONE;
                 auto with = [&](float ox, float oy) {
@@ -688,7 +690,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) 
                 }
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
-                    const u64 on = __ballot(v[h].x > LP_NONE * 0.99f && v[h].x >= bound);
+                    const u64 on = __ballot(v[h].x > LP_LIMIT && v[h].x >= bound);
                     if (!on) continue;
                     const int to = place(&team.groups, on);
                     if ((on >> lane & 1) && to < LP_ROOM) {
@@ -759,11 +761,11 @@ __global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) 
                     }
 #pragma unroll
                     for (int h = 0; h < DEEP; ++h) {
-                        u64 on = __ballot(v[h].x > LP_NONE * 0.99f && v[h].x >= cut);
+                        u64 on = __ballot(v[h].x > LP_LIMIT && v[h].x >= cut);
                         if (!on) continue;
                         if (n + (int)__popcll(on) > LP_ROOM && !full) {
                             tighten();
-                            on = __ballot(v[h].x > LP_NONE * 0.99f && v[h].x >= cut);
+                            on = __ballot(v[h].x > LP_LIMIT && v[h].x >= cut);
                             full = n + (int)__popcll(on) > LP_ROOM;
                         }
                         if (full) continue;
@@ -785,7 +787,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) 
             for (int e = 0; e < n && !full; e += 64) {
                 const bool in = e + lane < n && lds.most[e + lane] >= cut;
                 const int g = in ? lds.group[e + lane] : 0;
-                const int mine = !in ? 0 : lds.second[e + lane] >= cut && lds.second[e + lane] > LP_NONE * 0.99f ? size : 1;
+                const int mine = !in ? 0 : lds.second[e + lane] >= cut && lds.second[e + lane] > LP_LIMIT ? size : 1;
                 int upto = inclusive(mine, lane);
                 const int all = __builtin_amdgcn_readlane(upto, 63);
                 if (found + all > LP_ROOM) {
@@ -827,7 +829,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) 
     };
     auto log_of = [&](double s) {   // (a probability is not above 1)
         const double l = (s - lse) * 0.69314718055994531;
-        return bad ? NAN : (float)(l < 0.0 ? l : 0.0);
+        return bad ? NAN : s <= LP_LIMIT && lse > -INFINITY ? -INFINITY : (float)(l < 0.0 ? l : 0.0);
     };
     // the target behind the keys
     for (int e = worker * 8; e < (full ? 0 : found) + 1; e += WAVES * 8) {
@@ -848,7 +850,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) 
         for (int e = 0; e < found; e += 64) {
             const int j = e + lane < found ? lds.key[e + lane] : -1;
             const double s = j >= 0 ? lds.value[e + lane] : 0.0;
-            const bool on = j >= 0 && s > -INFINITY;
+            const bool on = j >= 0 && s > LP_LIMIT;
             int rank = 0;
 #pragma unroll 4
             for (int o = 0; o < found; ++o) {
@@ -874,11 +876,11 @@ __global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) 
     for (int g0 = 0; g0 < c.parts_k << c.part_shift; g0 += 64) {
         const int g = g0 + lane;
         const float largest = g < c.parts_k << c.part_shift ? groups[g].x : -INFINITY;
-        for (u64 on = __ballot(largest > LP_NONE * 0.99f && largest >= cut); on; on &= on - 1) {
+        for (u64 on = __ballot(largest > LP_LIMIT && largest >= cut); on; on &= on - 1) {
             const int key0 = (g0 + __builtin_ctzll(on)) << c.group_shift, j = key0 + (lane >> 3);
             bool in = lane >> 3 < size && j < c.M && !leaves_out(c, i, j);
             const double s = logit(in && c.bias ? c.bias[j] : 0.0f, in ? j : 0);
-            in &= s > -INFINITY;
+            in &= s > LP_LIMIT;
             for (int h = 0; h < size; ++h) {
                 if (!__builtin_amdgcn_readlane((int)in, h * 8)) continue;
                 const double x = __shfl(s, h * 8);
@@ -1118,6 +1120,7 @@ extern "C" int rnnd_logprob(const void *Q, int64_t B, const void *K, int64_t M, 
     c.query_ids = query_ids;
     c.key_ids = key_ids;
     c.bias = key_bias;
+    c.left_out = CT_LOWEST;
     c.scale = scale;
     c.c1 = (float)(2.0 * scale * LP_LOG2E);
     c.B = (int)B;
