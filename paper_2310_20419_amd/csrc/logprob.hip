@@ -19,6 +19,7 @@
 #define LP_ROOM 256             // groups above the bound, and keys among them, that a wavefront has room for
 #define LP_NONE (-3.0e38f)      // stands for -infinity where bits are put into the significand
 #define LP_LIMIT (LP_NONE * 0.99f)      // logits that are not above it count as -infinity
+#define LP_FAR (-1024.0f)        // 2^LP_FAR is 0 in float32, and times a sum it is still a number
 #define LP_LOG2E 1.4426950408889634
 #define LP_FEW 8                // queries at a time that are summed from differences
 #define LP_ALONE 512            // queries, for each of which there is room for a block of eight wavefronts
@@ -214,6 +215,12 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_logprob_s
             }
         }
         row16_larger(top);
+        const float largest = larger(larger(top[0], top[1]), larger(top[2], top[3]));
+        if (__any(largest > 1.0e37f))       // LP_NONE less that may be -infinity; what is below zero is nothing beside it
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int n = 0; n < N; ++n) s[r][n] = top[r] > 1.0e37f ? larger(s[r][n], 0.0f) : s[r][n];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const float ref = top[r] > LP_LIMIT ? top[r] : 0.0f;
@@ -248,7 +255,7 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_logprob_s
 __device__ __forceinline__ void join_three(float &top, float &sum, float &w, float ot, float os, float ow)
 {
     const float m = fmaxf(top, ot), ref = m == -INFINITY ? 0.0f : m;
-    const float da = fmaxf(top - ref, LP_NONE), db = fmaxf(ot - ref, LP_NONE), fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
+    const float da = fmaxf(top - ref, LP_FAR), db = fmaxf(ot - ref, LP_FAR), fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
     w = fa * fmaf(sum, da, w) + fb * fmaf(os, db, ow);
     sum = sum * fa + os * fb;
     top = m;
@@ -391,8 +398,8 @@ __global__ __launch_bounds__(256) void k_logprob_few(LogprobPar c, int wave_keys
                     c.groups[((size_t)b * gridDim.x + blockIdx.x) * (part_keys / 8) + (in_part + lane) / 8] = make_float2(x, y);
             }
             const float m = fmaxf(top[b], s), ref = m == -INFINITY ? 0.0f : m;      // a lane's own
-            const float da = fmaxf(top[b] - ref, LP_NONE), x = s - ref, fa = __builtin_amdgcn_exp2f(da), e = __builtin_amdgcn_exp2f(x);
-            w[b] = fmaf(e, fmaxf(x, LP_NONE), fa * fmaf(sum[b], da, w[b]));
+            const float da = fmaxf(top[b] - ref, LP_FAR), x = s - ref, fa = __builtin_amdgcn_exp2f(da), e = __builtin_amdgcn_exp2f(x);
+            w[b] = fmaf(e, fmaxf(x, LP_FAR), fa * fmaf(sum[b], da, w[b]));
             sum[b] = fmaf(sum[b], fa, e);
             top[b] = m;
         }
@@ -628,7 +635,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) 
             }
         const bool none = sum == 0.0f;
         bad = !(sum >= 0.0f && sum < INFINITY);
-        if (c.entropy && lane == 0) c.entropy[i] = none ? 0.0f : bad ? NAN : fmaxf(0.0f, (log2f(sum) - w / sum) * 0.693147181f);
+        if (c.entropy && lane == 0) {
+            const float h = (log2f(sum) - w / sum) * 0.693147181f;
+            c.entropy[i] = none ? 0.0f : bad ? NAN : h < 0.0f ? 0.0f : h;
+        }
         look = k && !none && !bad;
         if (none || bad) {
             for (int e = lane; e < k; e += 64) {

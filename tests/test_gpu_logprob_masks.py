@@ -1,14 +1,26 @@
-"""Masks in key_bias that are finite: the lowest float leaves a key out as -infinity does.  What such keys do not change are the answers about the others."""
+"""Masks in key_bias that are finite: the lowest float, which leaves a key out as -infinity does, and large ones that count.  What such keys do not change
+are the answers about the others."""
 import numpy as np
 import pytest
 
-from test_gpu_logprob import TYPES, call, case, rn       # noqa: F401
+from test_gpu_logprob import TYPES, call, case, check, rn       # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
 LOWEST = float(np.finfo(np.float32).min)
 # few queries, few and many by tiles (the keys' norms along with the product or by themselves; keys in place or copied)
 SIZES = [(3, 900, 40), (8, 900, 64), (40, 900, 64), (40, 900, 40), (1100, 900, 64)]
+
+
+class Biased:
+    """Calls with other biases than the case that the answers are compared with."""
+
+    def __init__(self, rn, bias):       # noqa: F811
+        self.rn, self.bias = rn, bias
+
+    def rnnd_logprob(self, *a, key_bias, **kw):
+        import torch
+        return self.rn.rnnd_logprob(*a, key_bias=torch.from_numpy(self.bias).cuda(), **kw)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -51,3 +63,36 @@ def test_distances_that_float32_does_not_hold(rn, B, M, d, dtype):       # noqa:
     near = torch.tensor([98, 99, 104, 105], dtype=torch.int32, device="cuda")
     assert torch.equal(ids[:, :4].sort(1)[0], near.expand(B, 4)) and (ids[:, 4:] == -1).all() and (tops[:, 4:] == -float("inf")).all()
     assert torch.isfinite(tops[:, :4]).all() and torch.isfinite(ent).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,M,d", SIZES)
+@pytest.mark.parametrize("mask", [-1e9, -1e30, -1e37, -1e38, -1.9e38])
+def test_masks_that_count(rn, B, M, d, mask, dtype):       # noqa: F811
+    """Probabilities of nothing, wherever they stand, whole parts of the keys among them."""
+    c = case(B, M, d, dtype, 23)
+    out = (np.arange(M) >= 300) | (np.arange(M) % 7 == 3)
+    ref = np.where(out, np.float32(-np.inf), c["key_bias"])
+    c["target"] = np.where(out[np.clip(c["target"], 0, M - 1)], 0, c["target"]).astype(np.int32)      # (that of a masked key is the mask)
+    for k in (0, 12):
+        check(Biased(rn, np.where(out & (c["key_bias"] > -np.inf), np.float32(mask), c["key_bias"])), dict(c, key_bias=ref), 3.0, k)
+
+
+@pytest.mark.parametrize("B,d", [(3, 40), (40, 64), (40, 40), (1100, 64)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_two_biases_above_all(rn, B, d, dtype):       # noqa: F811
+    """1e38 beside biases from 0 to -1.9e38: the two have the same logit (their distances are lost in a step of 1e31), so the entropy is log 2.  (A sum of
+    two ones, its logarithm and a quotient of zeros: a few steps.)  A log probability is a logit of double precision less the log of the sum, which
+    has the error of a float32 logit: bias times 1.44269504f, whose constant is off by less than U of itself and whose product is rounded, 2 U, and as much
+    again where the bias and the distance are two terms: 4 U 1e38, about 2.4e31.  It is not above 0."""
+    import torch
+    c = case(B, 900, d, dtype, 24, ids=False)
+    for other in (0.0, -1e30, -1.9e38, -np.inf):
+        c["key_bias"] = np.full(900, other, np.float32)
+        c["key_bias"][[100, 511]] = 1e38
+        c["target"][:] = 511
+        lp, ent, ids, tops = call(rn, c, 3.0, 2)
+        assert (ent.double() - np.log(2.0)).abs().max() <= 16 * 2.0 ** -24
+        for x in (lp, tops[:, 0], tops[:, 1]):
+            assert (x.double() + np.log(2.0)).abs().max() <= 4 * 2.0 ** -24 * 1e38 and (x <= 0).all()
+        assert torch.equal(ids.sort(1)[0], torch.tensor([[100, 511]], dtype=torch.int32, device="cuda").expand(B, 2))
