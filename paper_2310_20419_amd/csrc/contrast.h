@@ -184,7 +184,7 @@ __device__ __forceinline__ void key_sides(const ContrastPar &c, const int (&at)[
         if (lane != r || at[r] >= padded) continue;
         const int j = at[r];
         const bool gone = j >= c.M || key_gone(c, j);
-        const float bias = c.bias ? c.bias[j] : 0.0f;
+        const float bias = !gone && c.bias ? c.bias[j] : 0.0f;        // (there is none behind the last key)
         const float base = ONCE ? (float)(((double)bias - (double)c.scale * (double)sum[r]) * 1.4426950408889634) : (bias - c.scale * sum[r]) * 1.44269504f;
         c.key_base[j] = gone ? ALL && !(sum[r] < INFINITY) ? NAN : -INFINITY : base;
         c.key_id[j] = gone ? -1 : c.key_ids ? c.key_ids[j] : j;
