@@ -9,8 +9,9 @@
 // largest one's key stands in the lowest bits of its significand.  k keys are at least as large as the k-th largest of any values that are
 // logits of different keys, so a bound on the k-th logit follows from the parts' largest, a better one from the groups of those parts, and
 // what lies above the better one is little more than k keys.  Their distances are summed again in double precision from the rows as
-// they are, and these decide the order.  The first pass is off by some error E (a bound from the norms): keys down to 2 E below
-// the bound are taken along, so E costs time but changes no answer.  Where more keys than there is room for lie that close
+// they are, and these decide the order.  The first pass is off by some error E: keys down to 2 E below the bound are taken along, so E costs
+// time but changes no answer.  E is a bound from the rows' norms and the biases, of the keys that can be that probable: with scale > 0
+// a logit of at least t has scale |q - k|^2 <= (largest bias) - t, so a key a long way off, or with a bias far below zero, does not count for it.  Where more keys than there is room for lie that close
 // together (thousands of copies of a row), all groups above the bound are gone through in double precision instead.
 #include <cmath>
 
@@ -31,7 +32,7 @@ struct LogprobPar : ContrastPar {
     float *part_w;              // [B padded][parts_k] sum of 2^(s - top) (s - top), s in base 2
     float2 *groups;             // [B padded][parts_k][groups of a part] largest and second largest
     int group_shift, part_shift;    // keys of a group, groups of a part: powers of two
-    float *most;                // [2][CT_ROW_BLOCKS] largest |k|^2 and |bias| of a block of keys
+    float *most;                // [2][CT_ROW_BLOCKS] largest |k|^2 and bias_size() of a block of keys
     int most_blocks;
     bool squares;               // |k|^2 comes from the product's pass over the keys
     int few;                    // logits are from differences: the whole of s
@@ -45,14 +46,20 @@ __device__ __forceinline__ bool leaves_out(const LogprobPar &c, int i, int j)
 }
 
 // ------------------------------------------------------------------------------------------------ preparation
-// The largest |k|^2 and |bias| of a block's keys; what is not a number counts as infinite.
+// What of a bias counts for the error of the largest logits; what is not a number counts as infinite.  Biases below zero: logits that reach t have
+// biases of at least t, which counts for itself -- unless a negative scale makes them large again.
+__device__ __forceinline__ float bias_size(const LogprobPar &c, float b)
+{
+    const float x = c.scale < 0.0f ? fabsf(b) : b < 0.0f ? 0.0f : b;
+    return x < INFINITY ? x : INFINITY;
+}
+// The largest of a block's keys.
 struct MostLds { u32 norm, bias; };
 __device__ __forceinline__ void most_of(MostLds &most, const LogprobPar &c, int j, float norm)
 {
     if (j >= c.M || key_gone(c, j)) return;
-    const float b = c.bias ? fabsf(c.bias[j]) : 0.0f;
     atomicMax(&most.norm, __float_as_uint(norm < INFINITY ? norm : INFINITY));
-    atomicMax(&most.bias, __float_as_uint(b < INFINITY ? b : INFINITY));
+    atomicMax(&most.bias, __float_as_uint(c.bias ? bias_size(c, c.bias[j]) : 0.0f));
 }
 
 // A wavefront per row, keys first; then the copies of the rows (contrast_copy()).  key_blocks: 0 where the keys have been prepared.
@@ -172,8 +179,7 @@ __global__ __launch_bounds__(256, TILE == 256 || TERMS ? 1 : 2) void k_logprob_s
             for (int n = 0; n < N; ++n) {
                 if (id[n] < 0 || odd[n]) continue;
                 most = fmaxf(most, norm[n] < INFINITY ? norm[n] : INFINITY);
-                const float b = c.bias ? fabsf(side.base[at.in_col + n]) * 0.7f : 0.0f;
-                bias = fmaxf(bias, b < INFINITY ? b : INFINITY);
+                if (c.bias) bias = fmaxf(bias, bias_size(c, side.base[at.in_col + n] * 0.7f));
             }
 #pragma unroll
             for (int x = 8; x; x >>= 1) {
@@ -379,7 +385,7 @@ __global__ __launch_bounds__(256) void k_logprob_few(LogprobPar c, int wave_keys
             }
         }
         wave_sync();
-        if (on) biases = fmaxf(biases, fabsf(bias) < INFINITY ? fabsf(bias) : INFINITY);
+        if (on) biases = fmaxf(biases, bias_size(c, bias));
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             if (b >= c.B) break;
@@ -604,11 +610,31 @@ __global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) 
     }
     int n = 0, found = 0;
     bool full = false, look = false, bad = false;
-    float error = 0.0f;
     double norm = 0.0;
-    auto below = [&](float t) {     // t: a bound on the k-th logit as the first pass has it, with the key's number in it
+    // A bound on the logits to look at, from a bound t on the k-th one as the first pass has it (with the key's number in it).  k keys have t or more
+    // there, so with logits off by E the k-th is not below t - E, and what is not below that is not below t - 2 E in the first pass.  In base 2, u a step:
+    //   a few queries: a sum of d squares, which are bias - logit: E = u (d + 16) (largest bias + |t|)
+    //   tiles: a sum of d products of one rounding each (float32 rows: six times as many), its scaling, the key's own sum and bias:
+    //   E = u (2 a scale |q||k| + b scale |k|^2 + 2 |bias|), a and b from d.  For the largest |k| and |bias|; or, with scale > 0, for what keys with logits
+    //   down to t - E can have: scale (|k| - |q|)^2 <= R + E with R = largest bias + scale |q|^2 - t.  E takes (0.1 |q||k| + 0.01 |k|^2) scale at most
+    //   beside the biases (d = 65,536), so 0.9 |k| <= |q| + sqrt(R / scale) + sqrt(0.1 |q||k|), the last not above 0.32 |q| + 0.08 |k|.
+    float q = 0.0f;
+    auto below = [&](float t) {
         if (t <= LP_NONE) return -INFINITY;
-        const float b = t - 2.0f * error - fabsf(t) * (4.0e-6f + (c.few ? 2.38418579e-7f * (float)(c.d + 16) : 0.0f));
+        const float u = 1.19209290e-7f;
+        float error;
+        if (c.few) error = u * (float)(c.d + 16) * (1.45f * biases + fabsf(t));
+        else {
+            float size = biases, k = sqrtf(norms);
+            if (c.scale >= 0.0f) {
+                const float own = c.scale * q * q;
+                size = fmaxf(size, 0.7f * fabsf(t) + own);
+                const float room = fmaxf(biases + own - 0.693147181f * t, 0.0f) + 1.0e-5f * size;       // (and the roundings of its own)
+                k = c.scale > 0.0f ? fminf(k, 1.61f * q + 1.23f * sqrtf(room / c.scale)) : 0.0f;
+            }
+            error = 1.46f * u * (fabsf(c.scale) * (2.0f * ((DT == DT_F32 ? 6.0f : 1.0f) * c.d + 16.0f) * q * k + (float)(c.d + 16) * k * k) + 2.0f * size);
+        }
+        const float b = t - 2.0f * error - fabsf(t) * 4.0e-6f;
         return b > LP_NONE ? b : -INFINITY;
     };
     if (worker == 0) {
@@ -627,6 +653,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) 
             }
         if (c.logprob) asked = (u32)target < (u32)c.M && !leaves_out(c, i, target);
         norm = c.few ? 0.0 : query_norm<DT, WIDE>(c, i, lane);
+        q = sqrtf((float)norm);
         if (!c.few)
 #pragma unroll
             for (int s = 1; s < 64; s <<= 1) {
@@ -646,18 +673,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 128 : 64 * WAVES, WAVES == 1 ? 5 : 1) 
                 tops[e] = bad ? NAN : -INFINITY;
             }
         } else if (k) {
-            // how far a logit of the first pass may be off, in base 2: a sum of d products of one rounding each (float32 rows: six times as many),
-            // its scaling, the key's own sum and bias; for a few queries a sum of d squares, which with the bias make up the logit
-            const float u = 1.19209290e-7f, terms = DT == DT_F32 ? 6.0f : 1.0f;
-            error = c.few ? u * (float)(c.d + 16) * biases * 1.45f
-                          : 1.45f * (u * fabsf(c.scale) * (2.0f * (terms * c.d + 16.0f) * sqrtf((float)norm * norms) + (float)(c.d + 16) * norms) +
-                                     2.0f * u * biases);
-            {
-                float v[LP_ROOM / 64];
+            float v[LP_ROOM / 64];
 #pragma unroll
-                for (int h = 0; h < LP_ROOM / 64; ++h) v[h] = h == 0 ? first : h == 1 ? second : -INFINITY;
-                cut = below(kth_largest(v, k));
-            }
+            for (int h = 0; h < LP_ROOM / 64; ++h) v[h] = h == 0 ? first : h == 1 ? second : -INFINITY;
+            cut = below(kth_largest(v, k));
         }
     }
     bool gathered = false;

@@ -1,9 +1,9 @@
-"""Masks in key_bias that are finite: the lowest float, which leaves a key out as -infinity does, and large ones that count.  What such keys do not change
-are the answers about the others."""
+"""Masks in key_bias that are finite: the lowest float, which leaves a key out as -infinity does, large ones that count, and the usual -1e9; and rows
+far away from all others.  What such keys do not change are the answers about the others, nor (by much) the time that these take."""
 import numpy as np
 import pytest
 
-from test_gpu_logprob import TYPES, call, case, check, rn       # noqa: F401
+from test_gpu_logprob import TYPES, U, call, case, check, error_of_a_logit, rn       # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -96,3 +96,55 @@ def test_two_biases_above_all(rn, B, d, dtype):       # noqa: F811
         for x in (lp, tops[:, 0], tops[:, 1]):
             assert (x.double() + np.log(2.0)).abs().max() <= 4 * 2.0 ** -24 * 1e38 and (x <= 0).all()
         assert torch.equal(ids.sort(1)[0], torch.tensor([[100, 511]], dtype=torch.int32, device="cuda").expand(B, 2))
+
+
+def microseconds(run):
+    import torch
+    times = []
+    for i in range(8):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        run()
+        b.record()
+        torch.cuda.synchronize()
+        if i:
+            times.append(a.elapsed_time(b) * 1e3)
+    return min(times)
+
+
+@pytest.mark.parametrize("dtype,B,M,d", [("float32", 1, 200_000, 96), ("float32", 5, 100_000, 33), ("bfloat16", 2, 100_000, 64), ("float32", 300, 20_000, 40),
+                                         ("bfloat16", 64, 100_000, 64), ("float16", 1100, 20_000, 64), ("float16", 40, 50_000, 40)])
+@pytest.mark.parametrize("what", ["-1e9", "-1e30", "far", "farther", "infinite"])
+def test_keys_that_cannot_be_probable_cost_no_time(rn, dtype, B, M, d, what):       # noqa: F811
+    """One key in 100 masked, or one a long way off: the alternatives are those of double precision, and take no longer than without (1,000 times
+    as long where all keys are gone through; 4 times is far from either)."""
+    import torch
+    c = case(B, M, d, dtype, 25, ids=False, bias=False)
+    c["key_bias"] = np.zeros(M, np.float32)
+    x = {n: torch.from_numpy(v).cuda() if isinstance(v, np.ndarray) else v for n, v in c.items()}
+
+    def run():
+        return rn.rnnd_logprob(x["Q"], x["K"], 3.0, target=x["target"], alternatives=10, key_bias=x["key_bias"])
+    before = microseconds(run)
+    want = run()
+    keep = torch.ones(M, dtype=torch.bool, device="cuda")
+    if what[0] == "-":
+        x["key_bias"][7::100] = float(what)
+        keep[7::100] = False
+    else:
+        # (float16 has nothing beyond 65504, whose square times 64 is as far as it goes)
+        x["K"][M // 2] = 100.0 * x["K"][M // 2] if what == "far" else 6e4 if what == "farther" else 6e4 if dtype == "float16" else 1e25
+        keep[M // 2] = False
+    got = run()
+    assert microseconds(run) <= 4 * before
+    # what has gone was among the alternatives of some queries only: all others have theirs, in that order
+    same = keep[want[2].long()].all(1)
+    assert torch.equal(got[2][same], want[2][same]) and same.any()
+    # and as if these keys were left out (their probabilities are nothing: exp(-20,000) and less); two sums of logits that are each off by e,
+    # joined from at most M / 1000 + 40 parts with 4 u a time (float32 rows are taken from another point where a key that gives it has gone)
+    plain = dict(c, Q=x["Q"], K=torch.where(keep[:, None], x["K"], torch.zeros_like(x["K"])), key_bias=np.zeros(M, np.float32))
+    e = torch.from_numpy(error_of_a_logit(plain, 3.0, plain["key_bias"], np.zeros((B, M), bool))).cuda()
+    x["key_bias"] = torch.where(keep, 0.0, -float("inf"))
+    gone = run()
+    assert torch.equal(got[2], gone[2])
+    assert ((got[3].double() - gone[3].double()).abs() <= (2 * e + 2 * (260 + M / 250) * U)[:, None]).all()
