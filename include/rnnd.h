@@ -359,8 +359,9 @@ int rnnd_contrast(const void *Q, int64_t B, const void *K, int64_t M, int32_t d,
 int rnnd_contrast_workspace(int64_t B, int64_t M, int32_t d, int dtype, int want_grad, size_t *bytes);
 
 /* Distillation: the divergence of the softmax over squared distances from what another model (the teacher) said about each query's
- * most probable keys, with gradients.  Logits s_ij, the keys that are left out (key_ids[j] < 0, key_bias[j] = -infinity, for query i those with
- * key_ids[j] = query_ids[i]), biases, weights and errors as for rnnd_contrast; P_ij = exp(s_ij) / sum over the keys that are not left out.
+ * most probable keys, with gradients.  Logits s_ij, the keys that are left out (key_ids[j] < 0, for query i those with key_ids[j] = query_ids[i], key_bias[j]
+ * = -infinity; here any bias of -2e38 or less, the lowest float for instance), biases, weights and errors as for rnnd_contrast; P_ij = exp(s_ij) / sum over
+ * the keys that are not left out.
  * The list of query i is teacher_ids[i][0 .. entries), positions of keys, with teacher_logits beside them.  An entry is absent, and counts nowhere,
  * where its position is outside [0, M), its key is left out, its logit is -infinity, or an earlier entry that is not absent names the same key.
  *   tail = 0   p = softmax of the list's logits; loss[i] = sum_t p_t (log p_t - log P_t)
@@ -395,8 +396,8 @@ int rnnd_distill_workspace(int64_t B, int64_t M, int32_t d, int dtype, int32_t e
  * they are), whatever the error of the sums; it costs more where very many keys are within that error of each other.  The logits whose
  * log probabilities are given are from double precision too.  The sums over all keys are float32, with rnnd_contrast's errors of a logit; for up to
  * 8 queries (and more against a large table of float32 rows) the distances are summed from differences and have no error from far origins.
- * Where no key counts: logprob and entropy 0, no alternatives.  A bias of -2e38 or less (the lowest float, for instance) leaves its key out as
- * -infinity does, and logits below about -2e38 count as -infinity.  Where a logit that counts is NaN or +infinity: NaN, no alternatives (-1 and NaN).
+ * Where no key counts: logprob and entropy 0, no alternatives.  Logits below about -2e38 count as -infinity.  Where a logit that counts is NaN or
+ * +infinity: NaN, no alternatives (-1 and NaN).
  *   target       device int32 [B] or NULL with logprob NULL; entropy device float [B] or NULL
  *   alternatives 0 <= alternatives <= RNND_MAX_LISTED; top_ids device int32 [B x alternatives], top_logprob device float [B x alternatives] (NULL if 0)
  * 0 <= B <= RNND_MAX_CONTRAST, 1 <= M <= RNND_MAX_CONTRAST; many queries go through the keys in runs, so that the workspace stays at about a GB beside

@@ -650,7 +650,7 @@ extern "C" int rnnd_distill(const void *Q, int64_t B, const void *K, int64_t M, 
     c.query_ids = query_ids;
     c.key_ids = key_ids;
     c.bias = key_bias;
-    c.left_out = -INFINITY;
+    c.left_out = CT_LOWEST;
     c.row_weight = row_weight;
     c.scale = scale;
     c.c1 = (float)(2.0 * scale * 1.4426950408889634);
