@@ -183,11 +183,11 @@ __device__ __forceinline__ void distill_row(const DistillPar &c, int i, int lane
     double p[2];
 #pragma unroll
     for (int r = 0; r < 2; ++r) l[r] = on[r] ? c.logits[from + (k[r] & 0xFF)] : -INFINITY;
-    const float top = c.tail || !n ? 0.0f : wave_max_f32(fmaxf(l[0], l[1]));
+    const float most = n ? wave_max_f32(fmaxf(l[0], l[1])) : 0.0f, top = c.tail ? fmaxf(most, 0.0f) : most;      // (above 0 the sum is above 1)
 #pragma unroll
     for (int r = 0; r < 2; ++r) p[r] = on[r] ? exp((double)l[r] - (double)top) : 0.0;
     const double sum = wave_sum_f64(p[0] + p[1]);
-    const double rest = c.tail && sum < 1.0 ? 1.0 - sum : 0.0, mass = n ? sum + rest : 1.0;
+    const double rest = c.tail && top == 0.0f && sum < 1.0 ? 1.0 - sum : 0.0, mass = n ? sum + rest : 1.0;
 #pragma unroll
     for (int r = 0; r < 2; ++r)
         if (on[r]) {
