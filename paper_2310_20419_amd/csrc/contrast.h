@@ -41,7 +41,7 @@ struct ContrastPar {
     float *key_base;                // [M padded] (bias - scale |k|^2) log2(e), -inf where left out
     int *key_id;                    // [M padded]
     int2 *row_id;                   // [B padded] ids that a query leaves out: the target's, its own
-    float2 *row_g;                  // [B padded] lse in base 2 (infinite: the query does not count), its weight (float16: scaled)
+    float2 *row_g;                  // [B padded] lse in base 2 (infinite: the query does not count), its weight (float16: scaled); lists: distill.hip
     float *row_own;                 // [B] g at the target
     float *own_logit;               // [B]
     float2 *part;                   // [B padded][parts_k] largest and sum of a row's part

@@ -10,7 +10,7 @@
 // list, so that neither R nor what follows from it is a small difference of large numbers, and the logits of listed keys are written
 // out by the tile that they lie in.  The lists are sorted by key, with the place where every tile begins, so a tile marks its listed
 // keys in a bitmap in LDS while its first loads are under way; a key's place in the list is the number of marks before it in its row.
-// Off the list g is a factor of the row times 2^(s - reference), with w (R - r) and the log of the sum off the list: again no difference
+// Off the list g is a factor of the row times 2^(s - the largest logit there), w (R - r) over the sum there: again no difference
 // of large numbers where a key has little of both.  It is rounded to the type of the rows for the products (float32 rows: three terms).
 // Listed keys have the largest g, of both signs, and often rows that lie close together, so that rounded ones would leave an error of the
 // size of the gradient (float16, 300 queries, lists of 7: 3.5e-4 of its norm, where rounding the result costs 2.1e-4): theirs is float32, kept
@@ -321,9 +321,9 @@ __global__ __launch_bounds__(256) void k_distill_loss(DistillPar c, int row_bloc
     if (rest > 0.0f) {
         const double log_off = (double)top - (double)ref + log2((double)sum);
         loss = fma((double)rest, log2((double)rest) - (log_off - log_total), loss);
-        c.row_g[i] = make_float2(top + log2f(sum), up_w * (float)(off / total - (double)rest));
-    } else if (others)
-        c.row_g[i] = make_float2((float)((double)ref + log_total), up_w);
+    }
+    // (the sum off the list as a factor: its logarithm would be lost in the steps of logits of many millions)
+    if (others) c.row_g[i] = make_float2(top, (float)((double)up_w * (off / total - (double)rest) / (double)sum));
     c.loss[i] = (float)(loss * 0.69314718055994531);
 }
 

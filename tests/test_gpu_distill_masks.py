@@ -37,3 +37,29 @@ def test_more_than_a_probability_with_the_rest(rn, add, dtype):       # noqa: F8
         assert torch.isfinite(x.float()).all()
         # p is formed in double precision both times, from differences of about 10 (rounded to steps of 2^-4, so all but 1e30 hold them); float32 from there on
         assert (x.double() - y.double()).abs().max() <= 2.0 ** -20 * (1 + y.double().abs().max())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("mask", [-1e9, -1e30])
+def test_all_keys_off_the_lists_masked(rn, mask, dtype):       # noqa: F811
+    """What the teacher left has only masked keys to go to.  Their logits are as good as equal (a step of float32 is 64 or more there), and however it is
+    divided among them, g is R - r = -r in all; on the list it is P - p.  So a query's gradient is 2 scale w times differences that add up to 1 + 2 r
+    in weight, and the loss is r times the mask but for 4 steps and terms that do not grow with it."""
+    import torch
+    B, M, d, n = 50, 3000, 48, 6
+    c = case(B, M, d, n, dtype, 33, ids=False, mass=0.9)
+    c["teacher_ids"] = np.tile(np.arange(n) * 400, (B, 1)).astype(np.int32)
+    c["teacher_logits"] = np.log(np.tile(np.linspace(1, 2, n) / 10, (B, 1))).astype(np.float32)
+    r = 1 - np.exp(c["teacher_logits"].astype(np.float64)).sum(1)
+    c["key_bias"] = np.full(M, mask, np.float32)
+    c["key_bias"][c["teacher_ids"][0]] = 0.0
+    c["row_weight"] = np.ones(B, np.float32)
+    loss, dq, dk = call(rn, c, 3.0, True)
+    assert (abs(loss.double().cpu().numpy() + r * mask) <= 8 * 2.0 ** -24 * abs(mask) + 100).all()
+    q, k = c["Q"].double(), c["K"].double()
+    # (16-bit rows: a product's g is off by half a step of itself, 2^-9, and the result by as much)
+    assert (dq.double().abs() <= 2 * 3.0 * (1 + 2 * r.max()) * (k.abs().max() + q.abs().max()) * (1 + 2.0 ** -7)).all()
+    listed = torch.zeros(M, dtype=torch.bool, device="cuda")
+    listed[torch.from_numpy(c["teacher_ids"][0]).long().cuda()] = True
+    # the keys off the lists: -r of each query among them all
+    assert dk[~listed].double().abs().sum(0).max() <= 2 * 3.0 * r.sum() * (k.abs().max() + q.abs().max()) * (1 + 2.0 ** -7)
