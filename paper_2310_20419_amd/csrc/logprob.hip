@@ -50,7 +50,7 @@ __device__ __forceinline__ bool leaves_out(const LogprobPar &c, int i, int j)
 // biases of at least t, which counts for itself -- unless a negative scale makes them large again.
 __device__ __forceinline__ float bias_size(const LogprobPar &c, float b)
 {
-    const float x = c.scale < 0.0f ? fabsf(b) : b < 0.0f ? 0.0f : b;
+    const float x = c.scale < 0.0f ? fabsf(b) : b <= 0.0f ? 0.0f : b;       // (without a sign: their bits are compared)
     return x < INFINITY ? x : INFINITY;
 }
 // The largest of a block's keys.

@@ -148,3 +148,21 @@ def test_keys_that_cannot_be_probable_cost_no_time(rn, dtype, B, M, d, what):   
     gone = run()
     assert torch.equal(got[2], gone[2])
     assert ((got[3].double() - gone[3].double()).abs() <= (2 * e + 2 * (260 + M / 250) * U)[:, None]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,d", [(8, 64), (64, 64), (64, 40), (1100, 64)])
+def test_biases_that_make_up_for_distances(rn, B, d, dtype):       # noqa: F811
+    """Long keys with biases as large as their squares, so that logits are small differences, beside biases of zero with a sign: the first pass's error is
+    that of the long keys, and the order that of double precision."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(26)
+    M, scale, k = 20_000, 1.0, 10
+    K = (30.0 * torch.randn(M, d, device="cuda", generator=g)).to(getattr(torch, dtype))
+    Q = (0.003 * torch.randn(B, d, device="cuda", generator=g)).to(K.dtype)
+    K[::8] = 0
+    bias = K.double().square().sum(1).float()
+    bias[::8] = -0.0
+    ids = rn.rnnd_logprob(Q, K, scale, alternatives=k, key_bias=bias)[2]
+    s = torch.stack([bias.double() - (K.double() - q.double()).square().sum(1) for q in Q])
+    assert torch.equal(ids.long(), s.sort(dim=1, descending=True, stable=True)[1][:, :k])
