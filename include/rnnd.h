@@ -387,14 +387,16 @@ int rnnd_distill_workspace(int64_t B, int64_t M, int32_t d, int dtype, int32_t e
 
 /* Log probabilities under the softmax over squared distances: of a given key, the entropy, and the most probable keys.  Logits s_ij and
  * the keys that are left out as for rnnd_distill; lse_i = log(sum_j exp s_ij), log P_ij = s_ij - lse_i.
- *   logprob[i]      log P of key target[i]; 0 where target[i] is outside [0, M) or names a key that is left out (also the query's own)
+ *   logprob[i]      log P of key target[i] (-infinity where its logit counts as that); 0 where target[i] is outside [0, M) or names a key that is left out
+ *                   (also the query's own)
  *   entropy[i]      -sum_j P_ij log P_ij
  *   top_ids[i]      the `alternatives` most probable keys (positions), most probable first, the lowest position first where their logits are equal;
  *                   -1 where there are fewer
  *   top_logprob[i]  their log P; -infinity where there are fewer
  * The order of the alternatives is that of the logits in double precision (each distance summed in double precision from the rows as
- * they are), whatever the error of the sums; it costs more where very many keys are within that error of each other.  The logits whose
- * log probabilities are given are from double precision too.  The sums over all keys are float32, with rnnd_contrast's errors of a logit; for up to
+ * they are), whatever the error of the sums; it costs more, by far in large tables, where hundreds of keys or more are within that error of the
+ * least probable alternative (copies of a row; keys with a mask like -1e9 where fewer than `alternatives` are without: -infinity leaves them out).  The logits
+ * whose log probabilities are given are from double precision too.  The sums over all keys are float32, with rnnd_contrast's errors of a logit; for up to
  * 8 queries (and more against a large table of float32 rows) the distances are summed from differences and have no error from far origins.
  * Where no key counts: logprob and entropy 0, no alternatives.  Logits below about -2e38 count as -infinity.  Where a logit that counts is NaN or
  * +infinity: NaN, no alternatives (-1 and NaN).

@@ -955,8 +955,8 @@ struct LogprobPlan {
 #define LP_BYTES ((size_t)1 << 30)      // of a run's parts and groups
 
 // Up to 8 queries at a time by differences, or all by tiles.  Float32 keys have to be copied in three terms for the tiles, which costs as much as many
-// runs of 8 through a large table.  8 queries / 64 by tiles, us: 10,000 x 96 24 / 40, 100,000 x 100 34 / 95, 1,000,000 x 32 79 / 536, 1,000,000 x 96 121 / 752,
-// 300,000 x 768 200 / 1,317; below, both in us, by coordinates and by keys.  (16-bit keys: 300,000 x 768, 8 queries 145 us, 9 to 128 by tiles 185, 256 219.)
+// runs of 8 through a large table.  8 queries / 64 by tiles, us: 10,000 x 96 24 / 40, 100,000 x 100 34 / 98, 1,000,000 x 32 80 / 543, 1,000,000 x 96 121 / 759,
+// 300,000 x 768 201 / 1,319; below, both in us, by coordinates and by keys.  (16-bit keys: 300,000 x 768, 8 queries 144 us, 9 to 128 by tiles 186, 256 225.)
 static bool few_queries(int B, int M, int d, int dtype)
 {
     const double size = 1e-6 * M * d, keys = 1e-3 * M;
@@ -996,16 +996,16 @@ static size_t layout(LogprobPar &c, LogprobPlan &plan, int dtype, char *base)
         return off;
     }
     // Tiles: as contrast_plan(), but that there is one product.  16-bit rows, tiles of 128 / 256, us: up to 128 queries, where half of one of 256 would be padding,
-    // 100 x 300,000, d = 128 99 / 108, 256 105 / 125, 768 195 / 224; more of them read the keys once instead of twice, 200 x 300,000, d = 64 103 / 100, 128 107 / 111,
-    // 192 135 / 121, 256 153 / 130, 768 254 / 224, 400 x 300,000 x 256 255 / 238; 8,192 x 16,384, d = 128 146 / 157, 256 179 / 180, 384 211 / 209, 768 311 / 289.
-    // Float32 rows, two workgroups / terms together: 3,000 x 12,000, d = 100 97 / 124, 768 361 / 386, 1,536 693 / 712; 700 x 4,000 x 300 57 / 54.
+    // 100 x 300,000, d = 128 90 / 110, 256 97 / 124, 768 188 / 222; more of them read the keys once instead of twice, 200 x 300,000, d = 64 92 / 100, 128 102 / 111,
+    // 192 131 / 120, 256 148 / 131, 768 256 / 226, 400 x 300,000 x 256 250 / 241; 8,192 x 16,384, d = 128 160 / 171, 256 199 / 198, 384 232 / 231, 768 338 / 321.
+    // Float32 rows, two workgroups / terms together: 3,000 x 12,000, d = 100 102 / 128, 768 368 / 399, 1,536 693 / 717; 700 x 4,000 x 300 59 / 56.
     const bool large = (c.B + 255LL) / 256 * ((c.M + 255LL) / 256) >= 512 && c.B > 128 && c.d > (c.B <= 1024 ? 160 : 320);
     c.tile = dtype != RNND_F32 && large ? 256 : 128;
     c.terms_from = 1536;
     plan.tiles = contrast_plan(c, dtype == RNND_F32 ? 3 : 1);
     c.keys_as_they_are = dtype != RNND_F32 && c.d % CT_K == 0;
     // Their norms come from the product's pass over them where few tiles do that for every key.  Norms by themselves / along with the product, us:
-    // bfloat16, 200 x 300,000 x 768 (one row of tiles) 371 / 221, 2,048 x 10,000 x 768 (8) 80 / 79, 8,192 x 16,384 x 768 (32) 305 / 329; float16,
+    // bfloat16, 200 x 300,000 x 768 (one row of tiles) 373 / 226, 2,048 x 10,000 x 768 (8) 81 / 79, 8,192 x 16,384 x 768 (32) 303 / 328; float16,
     // 1,000 x 11,000 x 768 63 / 56
     c.squares = c.keys_as_they_are && c.B <= 1024;
     c.part_shift = 4;
